@@ -179,7 +179,7 @@ def _run_own(s):
     if op == "embed":
         return {"out": ops.embed(s["table"], s["tokens"], s["scale"])}
     if op == "embed_grad":
-        return {"grad": ops.embed_grad(s["tokens"], s["d_out"], c["vocab"], s["scale"], dtype=DTYPES[c["grad"]])}
+        return {"grad": ops.embed_grad(s["tokens"], s["d_out"], c["vocab"], s["scale"], dtype=DTYPES[c["grad"]], workers=c["m"])}
     if op == "logprob":
         r = ops.token_logprobs(s["logits"], s["targets"], top=c["top"])
         return _named(r, c["top"])
