@@ -402,6 +402,71 @@ OLS_API const char* ols_kernel_name(int kind);
 OLS_API int64_t ols_trace_count(ols_handle h);
 OLS_API int ols_trace_get(ols_handle h, int64_t idx, ols_trace_entry* out);
 
+/* ---- operators of token models ----------------------------------------------------------------
+ *
+ * What a model over tokens needs between the ids and a row of g (and to answer with): lookup, gated feed-forward block,
+ * log probabilities, clipping.  They take no handle: sizes, device pointers, strides and a stream.  Conventions:
+ *   - The call only enqueues kernels on `stream` (hipStream_t; NULL: the default stream), so it can be captured into a HIP
+ *     graph.  Nothing is kept between calls.  Tensors and workspace have to live until that work has run.
+ *   - `groups` workers go in one call; worker i's tensors are i * (its stride) elements behind worker 0's, so that weights
+ *     and gradients can lie in the rows of x and g (stride ld).  A stride of 0 shares an input among the workers.
+ *   - A row's elements are contiguous; rows lie `..._row` elements apart.  Tensors are fp32 or bf16 and need the alignment
+ *     of their type only, unless stated otherwise.  Sums are fp32 or wider; results are rounded once, to nearest even.
+ *   - Workspace: 256-byte aligned, not cleared, at least what ols_..._workspace_bytes says (which returns a negative error
+ *     code for sizes that the operator refuses); NULL where that is 0.
+ *   - Results do not depend on timing: every sum has one order. */
+enum { OLS_F32 = 0, OLS_BF16 = 1 };
+#define OLS_MAX_TOP 32
+
+/* Embedding lookup with scaling: out[n] = scale * table[ids[n]].  An id outside [0, vocab) is no token (padding): its row is
+ * zero.  groups <= 4096, tokens <= 2^24, vocab <= 2^24, width <= 2^20. */
+OLS_API int ols_embed(int groups, int64_t tokens, int64_t vocab, int64_t width, const int32_t* ids_dev, int64_t ids_group,
+                      const void* table_dev, int dtype, int64_t table_row, int64_t table_group, float scale, void* out_dev, int out_dtype,
+                      int64_t out_row, int64_t out_group, void* stream);
+
+/* Its gradient: grad[v] = scale * sum of d_out[n] over ids[n] == v, in ascending n; rows of ids that do not occur are zero.
+ * accumulate != 0 adds to what grad holds and leaves those rows alone (a table that other operators use as well). */
+OLS_API int ols_embed_grad(int groups, int64_t tokens, int64_t vocab, int64_t width, const int32_t* ids_dev, int64_t ids_group,
+                           const void* d_out_dev, int dtype, int64_t d_out_row, int64_t d_out_group, float scale, void* grad_dev, int grad_dtype,
+                           int64_t grad_row, int64_t grad_group, int accumulate, void* ws_dev, int64_t ws_bytes, void* stream);
+OLS_API int64_t ols_embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t vocab, int64_t width);
+
+/* Log probabilities: per row of logits z
+ *     logsumexp = log sum e^z,   logprob = z[target] - logsumexp,   entropy = -sum p log p,   p = e^(z - logsumexp),
+ * and the `top` tokens of the largest logits, best first, ties to the lower index: their log probabilities and indices
+ * (top_... are [rows][top], top <= min(OLS_MAX_TOP, vocab); NULL with top == 0).
+ *   - A logit of -inf cannot occur: probability 0, gradient 0, never an alternative (index -1, log probability -inf where
+ *     fewer than `top` tokens can).  A row of nothing else: logsumexp and logprob -inf, entropy 0, gradient 0.
+ *   - A NaN or +inf in a row makes its results and its gradient NaN and its alternatives' indices -1.
+ *   - A target outside [0, vocab) (or targets == NULL) is none: logprob 0 and no part of the gradient.
+ * stats ([rows][2]: the largest logit m and the sum of e^(z - m)) is what the gradient alone needs later: unlike the logsumexp
+ * it keeps the probabilities' precision whatever the size of the logits.
+ * With d_logits the same call computes the gradient for upstream gradients d_logprob and d_entropy (each [rows]; NULL:
+ * zeros), which a training loss knows beforehand:
+ *     d_logits_j = d_logprob ([j == target] - p_j) - d_entropy p_j (log p_j + entropy);
+ * the logits are then read once where a workgroup's registers hold a row (131072 bf16 or 65536 fp32 logits).  It may lie on
+ * the logits (same pointer and row stride).  vocab <= 2^24. */
+OLS_API int ols_token_logprobs(int64_t rows, int64_t vocab, const void* logits_dev, int dtype, int64_t row_stride, const int32_t* targets_dev,
+                               float* logprob_dev, float* entropy_dev, float* logsumexp_dev, float* stats_dev, int top,
+                               float* top_logprob_dev, int32_t* top_index_dev, const float* d_logprob_dev, const float* d_entropy_dev, void* d_logits_dev,
+                               int64_t d_stride, void* ws_dev, int64_t ws_bytes, void* stream);
+OLS_API int64_t ols_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int top);
+/* The gradient alone, from the stats and entropy of an earlier call (entropy may be NULL with d_entropy NULL). */
+OLS_API int ols_token_logprobs_grad(int64_t rows, int64_t vocab, const void* logits_dev, int dtype, int64_t row_stride,
+                                    const int32_t* targets_dev, const float* stats_dev, const float* entropy_dev, const float* d_logprob_dev,
+                                    const float* d_entropy_dev, void* d_logits_dev, int64_t d_stride, void* stream);
+
+/* Global gradient norm and clipping over n contiguous tensors: per group
+ *     norm = sqrt(sum of squares of all its tensors' elements),   out = in * min(1, max_norm / norm).
+ * in_dev, out_dev, numel and group are HOST arrays of n entries, read before the call returns; group is non-decreasing
+ * (NULL: one group).  norms_dev: [groups] fp32 on the device; 0 for a group without elements.  out_dev[i] may equal
+ * in_dev[i]; out_dev == NULL computes the norms only.  Squares are summed in fp64: no gradient of finite elements overflows.
+ * A NaN in a group makes its norm and all its outputs NaN; an infinity makes the norm infinite, the infinite elements NaN and
+ * the others 0: look at the norm before the step. */
+OLS_API int ols_clip_gradients(int n, const void* const* in_dev, void* const* out_dev, const int64_t* numel, const int32_t* group, int groups,
+                               int dtype, float max_norm, float* norms_dev, void* ws_dev, int64_t ws_bytes, void* stream);
+OLS_API int64_t ols_clip_workspace_bytes(int n, const int64_t* numel, const int32_t* group, int groups);
+
 OLS_API const char* ols_last_error(void);
 OLS_API const char* ols_version(void);
 

@@ -10,6 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("OLS_LIBRARY", os.path.join(HERE, "libols.so"))   # override: an alternative build
 
 OLS_OK, OLS_EINVAL, OLS_ESTATE, OLS_EHIP, OLS_ENOMEM = 0, -1, -2, -3, -4
+OLS_F32, OLS_BF16 = 0, 1
+OLS_MAX_TOP = 32
 (OLS_OPT_NESTEROV, OLS_OPT_FUSE_PULL, OLS_OPT_SERIALIZE, OLS_OPT_DRY_RUN, OLS_OPT_KERNEL_TIMING, OLS_OPT_TRACE,
  OLS_OPT_MEAN_SPLIT, OLS_OPT_FUSE_MEAN, OLS_OPT_TUNING) = range(1, 10)
 (OLS_OPT_GEMM_SPLITK, OLS_OPT_FUSE_GEMM_UPDATE, OLS_OPT_GEMM_FORCE_GENERAL, OLS_OPT_ANCHOR_DELAY_US,
@@ -34,6 +36,7 @@ class OlsError(RuntimeError):
 
 _H = C.c_void_p
 _P = C.c_void_p
+_I = C.c_int64
 _SIGNATURES = {
     "ols_create": (_H, [C.c_int, C.c_int64, C.c_int, C.c_float, C.c_float, C.c_float]),
     "ols_destroy": (C.c_int, [_H]),
@@ -69,6 +72,14 @@ _SIGNATURES = {
     "ols_kernel_name": (C.c_char_p, [C.c_int]),
     "ols_trace_count": (C.c_int64, [_H]),
     "ols_trace_get": (C.c_int, [_H, C.c_int64, C.POINTER(ols_trace_entry)]),
+    "ols_embed": (C.c_int, [C.c_int, _I, _I, _I, _P, _I, _P, C.c_int, _I, _I, C.c_float, _P, C.c_int, _I, _I, _P]),
+    "ols_embed_grad": (C.c_int, [C.c_int, _I, _I, _I, _P, _I, _P, C.c_int, _I, _I, C.c_float, _P, C.c_int, _I, _I, C.c_int, _P, _I, _P]),
+    "ols_embed_grad_workspace_bytes": (_I, [C.c_int, _I, _I, _I]),
+    "ols_token_logprobs": (C.c_int, [_I, _I, _P, C.c_int, _I, _P, _P, _P, _P, _P, C.c_int, _P, _P, _P, _P, _P, _I, _P, _I, _P]),
+    "ols_token_logprobs_workspace_bytes": (_I, [_I, _I, C.c_int, C.c_int]),
+    "ols_token_logprobs_grad": (C.c_int, [_I, _I, _P, C.c_int, _I, _P, _P, _P, _P, _P, _P, _I, _P]),
+    "ols_clip_gradients": (C.c_int, [C.c_int, _P, _P, _P, _P, C.c_int, C.c_int, C.c_float, _P, _P, _I, _P]),
+    "ols_clip_workspace_bytes": (_I, [C.c_int, _P, _P, C.c_int]),
     "ols_last_error": (C.c_char_p, []),
     "ols_version": (C.c_char_p, []),
 }
@@ -239,6 +250,46 @@ def ols_kernel_stats(h, kind):
     n, ms = C.c_int64(0), C.c_double(0.0)
     _check(load().ols_kernel_stats(h, kind, C.byref(n), C.byref(ms)))
     return n.value, ms.value
+
+
+# ---- operators of token models: no handle, every pointer and stride explicit -------------------------------------
+def ols_embed(*args):
+    _check(load().ols_embed(*args))
+
+
+def ols_embed_grad(*args):
+    _check(load().ols_embed_grad(*args))
+
+
+def ols_token_logprobs(*args):
+    _check(load().ols_token_logprobs(*args))
+
+
+def ols_token_logprobs_grad(*args):
+    _check(load().ols_token_logprobs_grad(*args))
+
+
+def ols_clip_gradients(n, inputs, outputs, numel, group, groups, dtype, max_norm, norms, ws, ws_bytes, stream):
+    """inputs, outputs, numel, group: ctypes arrays of n entries (outputs, group: or None)."""
+    _check(load().ols_clip_gradients(n, inputs, outputs, numel, group, groups, dtype, max_norm, norms, ws, ws_bytes, stream))
+
+
+def _bytes(n):
+    if n < 0:
+        raise OlsError(int(n), last_error())
+    return n
+
+
+def ols_embed_grad_workspace_bytes(groups, tokens, vocab, width):
+    return _bytes(load().ols_embed_grad_workspace_bytes(groups, tokens, vocab, width))
+
+
+def ols_token_logprobs_workspace_bytes(rows, vocab, dtype, top):
+    return _bytes(load().ols_token_logprobs_workspace_bytes(rows, vocab, dtype, top))
+
+
+def ols_clip_workspace_bytes(n, numel, group, groups):
+    return _bytes(load().ols_clip_workspace_bytes(n, numel, group, groups))
 
 
 def ols_trace(h):

@@ -30,6 +30,10 @@ SOURCES = [
     "kernels_bn.hip",
     "kernels_conv_bf16.hip",
     "kernels_conv_bf16_slices.hip",
+    "ols_operators.hip",
+    "kernels_embed.hip",
+    "kernels_logprob.hip",
+    "kernels_clip.hip",
 ]
 
 # packed-fp32 VALU forms stay disabled for every device translation unit

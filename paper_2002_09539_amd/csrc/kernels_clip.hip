@@ -1,0 +1,124 @@
+// The norm of the gradients of a model over all its tensors, per group (one model, or each worker's), and clipping:
+//
+//   norm_g = sqrt(sum over the tensors of group g of x^2)        out = x min(1, max_norm / norm_g)
+//
+// Squares and their sums are in fp64: an fp32 of any size has a square that neither overflows nor vanishes there, and the
+// matrix-free fp64 rate (two operations for four bytes read) is far from what bounds a stream.  Sums have one order: a
+// workgroup's over its chunk, then the chunks of a group in turn.
+//
+// Two launches: the sums of squares of chunks, then the scaled copy, whose every workgroup adds up its group's sums itself
+// (a few thousand numbers from the L2) instead of waiting for a launch between.  The gradients are read twice.  The groups
+// are taken in batches small enough that the second reading finds them in the 256 MiB memory-side cache, and a batch that
+// is a single larger group is scaled in the reverse order, so that what was read last is found there.
+#include "element_io.h"
+#include "ols_internal.h"
+
+namespace ols {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ int find_tensor(const ClipTable& t, int chunk) {   // the last entry whose first chunk is at most `chunk`
+    int lo = 0, hi = t.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (t.first_chunk[mid] <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ double block_sum(double v) {   // the result is in every lane
+    __shared__ double part[kThreads / 64];
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < kThreads / 64; ++w) s += part[w];
+    return s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void clip_squares_kernel(ClipTable t, int64_t chunk_elems, double* partial) {
+    const int k = find_tensor(t, blockIdx.x);
+    const int64_t from = (int64_t)(blockIdx.x - t.first_chunk[k]) * chunk_elems, to = min(from + chunk_elems, t.numel[k]);
+    const T* x = (const T*)t.in[k];
+    double sum[4] = {0, 0, 0, 0};
+    for (int64_t i = from + threadIdx.x * 8; i < to; i += 4 * kThreads * 8) {
+        float v[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t at = i + (int64_t)u * kThreads * 8;
+            load_upto8(x + at, (int)max((int64_t)0, min((int64_t)8, to - at)), 0.0f, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[u] = fma((double)v[u][e], (double)v[u][e], sum[u]);
+    }
+    const double s = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    if (threadIdx.x == 0) partial[t.chunk_base + blockIdx.x] = s;
+}
+
+// the sum of a group's chunks: lane i adds up chunks i, i + 256, .. and the workgroup joins the lanes
+__device__ __forceinline__ double group_norm(const double* partial, int64_t first, int64_t count) {
+    double s = 0.0;
+    for (int64_t i = threadIdx.x; i < count; i += kThreads) s += partial[first + i];
+    return sqrt(block_sum(s));
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipTable t, int64_t chunk_elems, const double* partial, float max_norm, float* norms) {
+    const int chunk = t.reverse ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    const int k = find_tensor(t, chunk);
+    const double norm = group_norm(partial, t.group_first[k], t.group_chunks[k]);
+    if (threadIdx.x == 0 && t.chunk_base + chunk == t.group_first[k]) norms[t.group[k]] = (float)norm;
+    const T* x = (const T*)t.in[k];
+    T* out = (T*)t.out[k];
+    const bool clip = !(norm <= (double)max_norm);      // a NaN clips: it reaches every element
+    if (!clip && x == out) return;
+    const float scale = clip ? (float)((double)max_norm / norm) : 1.0f;
+    const int64_t from = (int64_t)(chunk - t.first_chunk[k]) * chunk_elems, to = min(from + chunk_elems, t.numel[k]);
+    for (int64_t i = from + threadIdx.x * 8; i < to; i += 4 * kThreads * 8) {
+        float v[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t at = i + (int64_t)u * kThreads * 8;
+            load_upto8(x + at, (int)max((int64_t)0, min((int64_t)8, to - at)), 0.0f, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t at = i + (int64_t)u * kThreads * 8;
+            if (at >= to) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u][e] *= scale;
+            store_upto8(out + at, (int)min((int64_t)8, to - at), v[u]);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void clip_norms_kernel(ClipGroups g, const double* partial, float* norms) {
+    const double norm = group_norm(partial, g.first[blockIdx.x], g.count[blockIdx.x]);
+    if (threadIdx.x == 0) norms[g.group[blockIdx.x]] = (float)norm;
+}
+
+}  // namespace
+
+hipError_t launch_clip_squares(const ClipTable& t, int dtype, int64_t chunk_elems, int blocks, double* partial, hipStream_t stream) {
+    if (dtype == OLS_F32) clip_squares_kernel<float><<<blocks, kThreads, 0, stream>>>(t, chunk_elems, partial);
+    else clip_squares_kernel<uint16_t><<<blocks, kThreads, 0, stream>>>(t, chunk_elems, partial);
+    return hipGetLastError();
+}
+hipError_t launch_clip_scale(const ClipTable& t, int dtype, int64_t chunk_elems, int blocks, const double* partial, float max_norm, float* norms,
+                             hipStream_t stream) {
+    if (dtype == OLS_F32) clip_scale_kernel<float><<<blocks, kThreads, 0, stream>>>(t, chunk_elems, partial, max_norm, norms);
+    else clip_scale_kernel<uint16_t><<<blocks, kThreads, 0, stream>>>(t, chunk_elems, partial, max_norm, norms);
+    return hipGetLastError();
+}
+hipError_t launch_clip_norms(const ClipGroups& g, int groups, const double* partial, float* norms, hipStream_t stream) {
+    clip_norms_kernel<<<groups, kThreads, 0, stream>>>(g, partial, norms);
+    return hipGetLastError();
+}
+
+}  // namespace ols

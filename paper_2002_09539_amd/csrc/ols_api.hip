@@ -53,6 +53,8 @@ struct TimedLaunch {
 
 }  // namespace
 
+int ols::report(int code, const char* message) { return fail(code, "%s", message); }
+
 struct ols_ctx {
     // problem
     int m = 0, tau = 1;

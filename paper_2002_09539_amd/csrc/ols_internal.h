@@ -447,4 +447,79 @@ int64_t bn_partial_floats(int groups, int P, int C);
 hipError_t ensure_dynamic_lds(const void* kernel, size_t bytes);
 inline int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 
+// ---------------------------------------------------------------------------------------------
+// Operators of token models (kernels_embed.hip, kernels_logprob.hip, kernels_clip.hip); the entry points that check their
+// arguments are in ols_operators.hip.  Strides in elements.
+// ---------------------------------------------------------------------------------------------
+int report(int code, const char* message);   // sets ols_last_error of this thread, returns code
+
+struct EmbedParams {
+    int groups, dtype, out_dtype;
+    int64_t tokens, vocab, width;
+    const void* table;
+    int64_t table_row, table_group;
+    const int32_t* ids;
+    int64_t ids_group;
+    float scale;
+    void* out;
+    int64_t out_row, out_group;
+};
+hipError_t launch_embed(const EmbedParams& p, hipStream_t stream);
+
+struct EmbedGradParams {
+    int groups, dtype, grad_dtype, accumulate;
+    int64_t tokens, vocab, width;
+    const int32_t* ids;
+    int64_t ids_group;
+    const void* dout;
+    int64_t dout_row, dout_group;
+    float scale;
+    void* grad;
+    int64_t grad_row, grad_group;
+};
+int64_t embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t width);
+hipError_t launch_embed_grad(const EmbedGradParams& p, void* ws, hipStream_t stream);
+
+struct LogprobParams {
+    int dtype, top;
+    int64_t rows, vocab;
+    const void* logits;
+    int64_t row_stride;
+    const int32_t* targets;
+    float *logprob, *entropy, *lse, *stats, *top_logprob;   // stats: [rows][2], maximum and sum of e^(z - maximum)
+    int32_t* top_index;
+    const float *g_logprob, *g_entropy;
+    void* d_logits;
+    int64_t d_stride;
+    // set by the launcher
+    int parts;
+    int64_t part;
+    float *part_stats, *part_val;
+    int32_t* part_idx;
+};
+int64_t logprob_workspace_bytes(int dtype, int64_t rows, int64_t vocab, int top);
+hipError_t launch_logprob(LogprobParams p, void* ws, hipStream_t stream);        // with d_logits: the gradient as well
+hipError_t launch_logprob_grad(const LogprobParams& p, hipStream_t stream);      // from p.stats and p.entropy
+
+// Tensors of one launch, by value in the kernel arguments (4 KiB): no table to upload, nothing to keep alive.
+constexpr int kClipTensors = 88;
+struct ClipTable {
+    int n, reverse;
+    int64_t chunk_base;                    // of the launch's first chunk among the partial sums
+    const void* in[kClipTensors];
+    void* out[kClipTensors];
+    int64_t numel[kClipTensors], group_first[kClipTensors];   // group_first: the group's first partial sum
+    int group_chunks[kClipTensors], group[kClipTensors], first_chunk[kClipTensors];
+};
+static_assert(sizeof(ClipTable) <= 4000, "kernel arguments");
+constexpr int kClipGroups = 160;
+struct ClipGroups {
+    int64_t first[kClipGroups];
+    int count[kClipGroups], group[kClipGroups];
+};
+hipError_t launch_clip_squares(const ClipTable& t, int dtype, int64_t chunk_elems, int blocks, double* partial, hipStream_t stream);
+hipError_t launch_clip_scale(const ClipTable& t, int dtype, int64_t chunk_elems, int blocks, const double* partial, float max_norm, float* norms,
+                             hipStream_t stream);
+hipError_t launch_clip_norms(const ClipGroups& g, int groups, const double* partial, float* norms, hipStream_t stream);
+
 }  // namespace ols

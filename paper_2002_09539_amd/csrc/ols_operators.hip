@@ -1,0 +1,326 @@
+// Entry points of the operators of token models: argument checks, workspace sizes, launches on the caller's stream.
+//
+// Nothing is kept between calls.  Every check is on the host, before anything is launched; a call that fails has launched
+// nothing (an error of the HIP runtime aside).
+#include <stdarg.h>
+#include <stdio.h>
+
+#include <algorithm>
+
+#include "ols_internal.h"
+
+using namespace ols;
+
+namespace {
+
+int bad(const char* fmt, ...) {
+    char text[400];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(text, sizeof(text), fmt, ap);
+    va_end(ap);
+    return report(OLS_EINVAL, text);
+}
+int done(hipError_t e, const char* what) {
+    if (e == hipSuccess) return OLS_OK;
+    char text[400];
+    snprintf(text, sizeof(text), "%s: %s", what, hipGetErrorString(e));
+    return report(OLS_EHIP, text);
+}
+
+bool is_dtype(int t) { return t == OLS_F32 || t == OLS_BF16; }
+int64_t size_of(int t) { return t == OLS_F32 ? 4 : 2; }
+bool element_aligned(const void* p, int t) { return ((uintptr_t)p & (uintptr_t)(size_of(t) - 1)) == 0; }
+bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+constexpr int kMaxGroups = 4096;
+constexpr int64_t kMaxTokens = 1 << 24, kMaxVocab = 1 << 24, kMaxWidth = 1 << 20, kMaxStride = (int64_t)1 << 40;
+
+bool stride_ok(int64_t row, int64_t width) { return row >= width && row <= kMaxStride; }
+bool group_ok(int64_t g) { return g >= 0 && g <= kMaxStride; }
+
+// Bytes that a workspace needs, checked against what the caller brought.
+int check_ws(const char* who, const void* ws, int64_t have, int64_t need) {
+    if (need == 0) return OLS_OK;
+    if (!ws || have < need) {
+        char text[200];
+        snprintf(text, sizeof(text), "%s: workspace of %lld bytes, %lld are needed", who, (long long)(ws ? have : 0), (long long)need);
+        return report(OLS_ENOMEM, text);
+    }
+    if (!aligned(ws, 256)) return bad("%s: the workspace must be 256-byte aligned", who);
+    return OLS_OK;
+}
+
+int check_embed(const char* who, int groups, int64_t tokens, int64_t vocab, int64_t width) {
+    if (groups < 1 || groups > kMaxGroups) return bad("%s: groups must be in [1, %d], got %d", who, kMaxGroups, groups);
+    if (tokens < 0 || tokens > kMaxTokens) return bad("%s: tokens must be in [0, 2^24], got %lld", who, (long long)tokens);
+    if (vocab < 1 || vocab > kMaxVocab) return bad("%s: vocab must be in [1, 2^24], got %lld", who, (long long)vocab);
+    if (width < 1 || width > kMaxWidth) return bad("%s: width must be in [1, 2^20], got %lld", who, (long long)width);
+    return OLS_OK;
+}
+
+int check_logprob(const char* who, int dtype, int64_t rows, int64_t vocab, const void* logits, int64_t stride, const int32_t* targets) {
+    if (!is_dtype(dtype)) return bad("%s: unknown type %d", who, dtype);
+    if (rows < 0 || rows > 0x7fffffff) return bad("%s: rows must be in [0, 2^31), got %lld", who, (long long)rows);
+    if (vocab < 1 || vocab > kMaxVocab) return bad("%s: vocab must be in [1, 2^24], got %lld", who, (long long)vocab);
+    if (rows == 0) return OLS_OK;
+    if (!logits || !element_aligned(logits, dtype)) return bad("%s: logits are null or not aligned to their type", who);
+    if (!stride_ok(stride, vocab)) return bad("%s: rows of %lld logits cannot be %lld elements apart", who, (long long)vocab, (long long)stride);
+    if (!aligned(targets, 4)) return bad("%s: targets are not aligned to their type", who);
+    return OLS_OK;
+}
+
+// ---- clipping -----------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kChunk = 16384;             // elements of a workgroup's chunk, doubled until no group has more than kMostChunks
+constexpr int64_t kMostChunks = 2048;
+constexpr int64_t kBatchBytes = 96ll << 20;   // groups whose second reading is to find them in the memory-side cache
+
+int check_clip(const char* who, int n, const int64_t* numel, const int32_t* group, int groups) {
+    if (n < 0 || n > (1 << 20)) return bad("%s: number of tensors must be in [0, 2^20], got %d", who, n);
+    if (groups < 1 || groups > kMaxGroups) return bad("%s: groups must be in [1, %d], got %d", who, kMaxGroups, groups);
+    if (n > 0 && !numel) return bad("%s: null sizes", who);
+    if (groups > 1 && n > 0 && !group) return bad("%s: several groups need the tensors' group numbers", who);
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (numel[i] < 0 || numel[i] > kMaxStride) return bad("%s: tensor %d has %lld elements", who, i, (long long)numel[i]);
+        total += numel[i];
+        if (total > kMaxStride) return bad("%s: more than 2^40 elements in all", who);
+        if (!group) continue;
+        if (group[i] < 0 || group[i] >= groups) return bad("%s: tensor %d is of group %d of %d", who, i, (int)group[i], groups);
+        if (i && group[i] < group[i - 1]) return bad("%s: the tensors must be in the order of their groups (tensor %d)", who, i);
+    }
+    return OLS_OK;
+}
+
+int group_of(const int32_t* group, int i) { return group ? group[i] : 0; }
+
+int64_t clip_chunk(int n, const int64_t* numel, const int32_t* group) {
+    int64_t most = 0, sum = 0;
+    for (int i = 0; i < n; ++i) {
+        if (i && group_of(group, i) != group_of(group, i - 1)) sum = 0;
+        sum += numel[i];
+        most = std::max(most, sum);
+    }
+    int64_t chunk = kChunk;
+    while (most / chunk > kMostChunks) chunk *= 2;
+    return chunk;
+}
+
+int64_t chunks_of(int64_t numel, int64_t chunk) { return (numel + chunk - 1) / chunk; }
+
+// Walks the tensors [i, end) in tables of at most kClipTensors, skipping empty ones, and hands each table to `go`.
+template <typename F>
+int clip_tables(int i, int end, const void* const* in, void* const* out, const int64_t* numel, const int32_t* group, int64_t chunk, int64_t base, F && go) {
+    while (i < end) {
+        ClipTable t = {};
+        int blocks = 0;
+        t.chunk_base = base;
+        for (; i < end && t.n < kClipTensors; ++i) {
+            const int64_t c = chunks_of(numel[i], chunk);
+            if (c == 0) continue;
+            if (blocks + c > 0x3fffffff) break;
+            const int k = t.n++;
+            t.in[k] = in[i], t.out[k] = out ? out[i] : nullptr, t.numel[k] = numel[i], t.group[k] = group_of(group, i);
+            t.first_chunk[k] = blocks;
+            blocks += (int)c;
+        }
+        if (blocks) {
+            const int rc = go(t, blocks);
+            if (rc != OLS_OK) return rc;
+        }
+        base += blocks;
+    }
+    return OLS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ols_embed(int groups, int64_t tokens, int64_t vocab, int64_t width, const int32_t* ids_dev, int64_t ids_group, const void* table_dev, int dtype,
+              int64_t table_row, int64_t table_group, float scale, void* out_dev, int out_dtype, int64_t out_row, int64_t out_group, void* stream) {
+    const char* who = "ols_embed";
+    if (const int rc = check_embed(who, groups, tokens, vocab, width)) return rc;
+    if (!is_dtype(dtype) || !is_dtype(out_dtype)) return bad("%s: unknown type", who);
+    if (tokens == 0) return OLS_OK;
+    if (!ids_dev || !table_dev || !out_dev) return bad("%s: null pointer", who);
+    if (!aligned(ids_dev, 4) || !element_aligned(table_dev, dtype) || !element_aligned(out_dev, out_dtype))
+        return bad("%s: a pointer is not aligned to its type", who);
+    if (!stride_ok(table_row, width) || !stride_ok(out_row, width)) return bad("%s: rows of %lld elements overlap at the given strides", who, (long long)width);
+    if (!group_ok(ids_group) || !group_ok(table_group) || !group_ok(out_group)) return bad("%s: a worker's stride is out of range", who);
+    if (groups > 1 && out_group < (tokens - 1) * out_row + width) return bad("%s: the workers' outputs overlap", who);
+    EmbedParams p;
+    p.groups = groups, p.dtype = dtype, p.out_dtype = out_dtype, p.tokens = tokens, p.vocab = vocab, p.width = width;
+    p.table = table_dev, p.table_row = table_row, p.table_group = table_group, p.ids = ids_dev, p.ids_group = ids_group, p.scale = scale;
+    p.out = out_dev, p.out_row = out_row, p.out_group = out_group;
+    return done(launch_embed(p, (hipStream_t)stream), who);
+}
+
+int64_t ols_embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t vocab, int64_t width) {
+    if (const int rc = check_embed("ols_embed_grad_workspace_bytes", groups, tokens, vocab, width)) return rc;
+    return embed_grad_workspace_bytes(groups, tokens, width);
+}
+
+int ols_embed_grad(int groups, int64_t tokens, int64_t vocab, int64_t width, const int32_t* ids_dev, int64_t ids_group, const void* d_out_dev, int dtype,
+                   int64_t d_out_row, int64_t d_out_group, float scale, void* grad_dev, int grad_dtype, int64_t grad_row, int64_t grad_group, int accumulate,
+                   void* ws_dev, int64_t ws_bytes, void* stream) {
+    const char* who = "ols_embed_grad";
+    if (const int rc = check_embed(who, groups, tokens, vocab, width)) return rc;
+    if (!is_dtype(dtype) || !is_dtype(grad_dtype)) return bad("%s: unknown type", who);
+    if (tokens > 0 && (!ids_dev || !d_out_dev)) return bad("%s: null pointer", who);
+    if (!grad_dev) return bad("%s: null gradient", who);
+    if (!aligned(ids_dev, 4) || !element_aligned(d_out_dev, dtype) || !element_aligned(grad_dev, grad_dtype))
+        return bad("%s: a pointer is not aligned to its type", who);
+    if (!stride_ok(d_out_row, width) || !stride_ok(grad_row, width)) return bad("%s: rows of %lld elements overlap at the given strides", who, (long long)width);
+    if (!group_ok(ids_group) || !group_ok(d_out_group) || !group_ok(grad_group)) return bad("%s: a worker's stride is out of range", who);
+    if (groups > 1 && grad_group < (vocab - 1) * grad_row + width) return bad("%s: the workers' gradients overlap", who);
+    if (const int rc = check_ws(who, ws_dev, ws_bytes, embed_grad_workspace_bytes(groups, tokens, width))) return rc;
+    EmbedGradParams p;
+    p.groups = groups, p.dtype = dtype, p.grad_dtype = grad_dtype, p.accumulate = accumulate != 0, p.tokens = tokens, p.vocab = vocab, p.width = width;
+    p.ids = ids_dev, p.ids_group = ids_group, p.dout = d_out_dev, p.dout_row = d_out_row, p.dout_group = d_out_group, p.scale = scale;
+    p.grad = grad_dev, p.grad_row = grad_row, p.grad_group = grad_group;
+    return done(launch_embed_grad(p, ws_dev, (hipStream_t)stream), who);
+}
+
+int64_t ols_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int top) {
+    const char* who = "ols_token_logprobs_workspace_bytes";
+    if (const int rc = check_logprob(who, dtype, 0, vocab, nullptr, vocab, nullptr)) return rc;
+    if (rows < 0 || rows > 0x7fffffff) return bad("%s: rows must be in [0, 2^31), got %lld", who, (long long)rows);
+    if (top < 0 || top > OLS_MAX_TOP || top > vocab) return bad("%s: top must be in [0, min(%d, vocab)], got %d", who, OLS_MAX_TOP, top);
+    return logprob_workspace_bytes(dtype, rows, vocab, top);
+}
+
+int ols_token_logprobs(int64_t rows, int64_t vocab, const void* logits_dev, int dtype, int64_t row_stride, const int32_t* targets_dev, float* logprob_dev,
+                       float* entropy_dev, float* logsumexp_dev, float* stats_dev, int top, float* top_logprob_dev, int32_t* top_index_dev, const float* d_logprob_dev,
+                       const float* d_entropy_dev, void* d_logits_dev, int64_t d_stride, void* ws_dev, int64_t ws_bytes, void* stream) {
+    const char* who = "ols_token_logprobs";
+    if (const int rc = check_logprob(who, dtype, rows, vocab, logits_dev, row_stride, targets_dev)) return rc;
+    if (top < 0 || top > OLS_MAX_TOP || top > vocab) return bad("%s: top must be in [0, min(%d, vocab)], got %d", who, OLS_MAX_TOP, top);
+    if (rows == 0) return OLS_OK;
+    if (!logprob_dev || !entropy_dev || !logsumexp_dev || !stats_dev) return bad("%s: null result", who);
+    if (top > 0 && (!top_logprob_dev || !top_index_dev)) return bad("%s: null results for the alternatives", who);
+    if (!aligned(logprob_dev, 4) || !aligned(entropy_dev, 4) || !aligned(logsumexp_dev, 4) || !aligned(stats_dev, 4) || !aligned(top_logprob_dev, 4) || !aligned(top_index_dev, 4) ||
+        !aligned(d_logprob_dev, 4) || !aligned(d_entropy_dev, 4))
+        return bad("%s: a pointer is not aligned to its type", who);
+    if (d_logits_dev) {
+        if (!element_aligned(d_logits_dev, dtype)) return bad("%s: the gradient is not aligned to its type", who);
+        if (!stride_ok(d_stride, vocab)) return bad("%s: rows of %lld gradients cannot be %lld elements apart", who, (long long)vocab, (long long)d_stride);
+        if (d_logits_dev == logits_dev && d_stride != row_stride) return bad("%s: a gradient in place needs the logits' row stride", who);
+    }
+    if (const int rc = check_ws(who, ws_dev, ws_bytes, logprob_workspace_bytes(dtype, rows, vocab, top))) return rc;
+    LogprobParams p = {};
+    p.dtype = dtype, p.top = top, p.rows = rows, p.vocab = vocab, p.logits = logits_dev, p.row_stride = row_stride, p.targets = targets_dev;
+    p.logprob = logprob_dev, p.entropy = entropy_dev, p.lse = logsumexp_dev, p.stats = stats_dev, p.top_logprob = top_logprob_dev, p.top_index = top_index_dev;
+    p.g_logprob = d_logprob_dev, p.g_entropy = d_entropy_dev, p.d_logits = d_logits_dev, p.d_stride = d_stride;
+    return done(launch_logprob(p, ws_dev, (hipStream_t)stream), who);
+}
+
+int ols_token_logprobs_grad(int64_t rows, int64_t vocab, const void* logits_dev, int dtype, int64_t row_stride, const int32_t* targets_dev,
+                            const float* stats_dev, const float* entropy_dev, const float* d_logprob_dev, const float* d_entropy_dev, void* d_logits_dev,
+                            int64_t d_stride, void* stream) {
+    const char* who = "ols_token_logprobs_grad";
+    if (const int rc = check_logprob(who, dtype, rows, vocab, logits_dev, row_stride, targets_dev)) return rc;
+    if (rows == 0) return OLS_OK;
+    if (!stats_dev || !d_logits_dev) return bad("%s: null pointer", who);
+    if (d_entropy_dev && !entropy_dev) return bad("%s: the entropy's gradient needs the entropy", who);
+    if (!aligned(stats_dev, 4) || !aligned(entropy_dev, 4) || !aligned(d_logprob_dev, 4) || !aligned(d_entropy_dev, 4) || !element_aligned(d_logits_dev, dtype))
+        return bad("%s: a pointer is not aligned to its type", who);
+    if (!stride_ok(d_stride, vocab)) return bad("%s: rows of %lld gradients cannot be %lld elements apart", who, (long long)vocab, (long long)d_stride);
+    if (d_logits_dev == logits_dev && d_stride != row_stride) return bad("%s: a gradient in place needs the logits' row stride", who);
+    LogprobParams p = {};
+    p.dtype = dtype, p.rows = rows, p.vocab = vocab, p.logits = logits_dev, p.row_stride = row_stride, p.targets = targets_dev;
+    p.stats = const_cast<float*>(stats_dev), p.entropy = const_cast<float*>(entropy_dev), p.g_logprob = d_logprob_dev, p.g_entropy = d_entropy_dev;
+    p.d_logits = d_logits_dev, p.d_stride = d_stride;
+    return done(launch_logprob_grad(p, (hipStream_t)stream), who);
+}
+
+int64_t ols_clip_workspace_bytes(int n, const int64_t* numel, const int32_t* group, int groups) {
+    if (const int rc = check_clip("ols_clip_workspace_bytes", n, numel, group, groups)) return rc;
+    const int64_t chunk = clip_chunk(n, numel, group);
+    int64_t chunks = 0;
+    for (int i = 0; i < n; ++i) chunks += chunks_of(numel[i], chunk);
+    return 8 * chunks;
+}
+
+int ols_clip_gradients(int n, const void* const* in_dev, void* const* out_dev, const int64_t* numel, const int32_t* group, int groups, int dtype,
+                       float max_norm, float* norms_dev, void* ws_dev, int64_t ws_bytes, void* stream) {
+    const char* who = "ols_clip_gradients";
+    if (const int rc = check_clip(who, n, numel, group, groups)) return rc;
+    if (!is_dtype(dtype)) return bad("%s: unknown type %d", who, dtype);
+    if (!norms_dev || !aligned(norms_dev, 4)) return bad("%s: norms are null or not aligned to their type", who);
+    if (n > 0 && !in_dev) return bad("%s: null pointers", who);
+    if (out_dev && !(max_norm >= 0.0f)) return bad("%s: max_norm must not be negative", who);
+    for (int i = 0; i < n; ++i) {
+        if (numel[i] == 0) continue;
+        if (!in_dev[i] || !element_aligned(in_dev[i], dtype)) return bad("%s: tensor %d is null or not aligned to its type", who, i);
+        if (out_dev && (!out_dev[i] || !element_aligned(out_dev[i], dtype))) return bad("%s: output %d is null or not aligned to its type", who, i);
+    }
+    const int64_t chunk = clip_chunk(n, numel, group);
+    int64_t need = 0;
+    for (int i = 0; i < n; ++i) need += 8 * chunks_of(numel[i], chunk);
+    if (const int rc = check_ws(who, ws_dev, ws_bytes, need)) return rc;
+    double* partial = (double*)ws_dev;
+    const hipStream_t s = (hipStream_t)stream;
+
+    ClipGroups left = {};      // groups whose norm no scaling launch writes
+    int left_n = 0;
+    auto flush = [&]() {
+        const int k = left_n;
+        left_n = 0;
+        return k ? done(launch_clip_norms(left, k, partial, norms_dev, s), who) : OLS_OK;
+    };
+    int64_t base = 0;
+    int i = 0, g = 0;
+    while (g < groups) {
+        // a batch: whole groups [g, to_g), tensors [i, to)
+        const int first = i;
+        int to_g = g;
+        int64_t elems = 0, chunks = 0;
+        while (to_g < groups) {
+            int j = i;
+            int64_t e = 0, c = 0;
+            for (; j < n && group_of(group, j) == to_g; ++j) e += numel[j], c += chunks_of(numel[j], chunk);
+            if (to_g > g && out_dev && (elems + e) * size_of(dtype) > kBatchBytes) break;
+            if (!out_dev || c == 0) {
+                left.first[left_n] = base + chunks, left.count[left_n] = (int)c, left.group[left_n] = to_g;
+                ++left_n;
+            }
+            elems += e, chunks += c, i = j, ++to_g;
+            if (left_n == kClipGroups) break;
+        }
+        int rc = clip_tables(first, i, in_dev, out_dev, numel, group, chunk, base,
+                             [&](const ClipTable& t, int blocks) { return done(launch_clip_squares(t, dtype, chunk, blocks, partial, s), who); });
+        if (rc != OLS_OK) return rc;
+        if (out_dev && chunks) {
+            // where each tensor's group begins among the partial sums, followed along the tables
+            int64_t at = base, group_first = base, group_count = 0;
+            int seen = first;
+            int current = -1;
+            rc = clip_tables(first, i, in_dev, out_dev, numel, group, chunk, base, [&](ClipTable& t, int blocks) {
+                for (int k = 0; k < t.n; ++k) {
+                    if (t.group[k] != current) {
+                        current = t.group[k];
+                        group_first = at, group_count = 0;
+                        while (seen < i && group_of(group, seen) < current) ++seen;
+                        for (; seen < i && group_of(group, seen) == current; ++seen) group_count += chunks_of(numel[seen], chunk);
+                    }
+                    t.group_first[k] = group_first, t.group_chunks[k] = (int)group_count;
+                    at += chunks_of(t.numel[k], chunk);
+                }
+                t.reverse = elems * size_of(dtype) > kBatchBytes;
+                return done(launch_clip_scale(t, dtype, chunk, blocks, partial, max_norm, norms_dev, s), who);
+            });
+            if (rc != OLS_OK) return rc;
+        }
+        if (!out_dev || left_n == kClipGroups) {
+            rc = flush();
+            if (rc != OLS_OK) return rc;
+        }
+        base += chunks;
+        g = to_g;
+    }
+    return flush();
+}
+
+}  // extern "C"
