@@ -431,6 +431,41 @@ OLS_API int ols_embed_grad(int groups, int64_t tokens, int64_t vocab, int64_t wi
                            int64_t grad_row, int64_t grad_group, int accumulate, void* ws_dev, int64_t ws_bytes, void* stream);
 OLS_API int64_t ols_embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t vocab, int64_t width);
 
+/* Gated feed-forward block:
+ *     a = x w_gate,   b = x w_up,   h = act(a) b,   y = h w_down
+ * with x [rows][width], w_gate and w_up [width][hidden], w_down [hidden][out], y [rows][out]; no biases.
+ *   - dtype: the type of x, y, dy and dx.  OLS_F32: products of fp32 accuracy (every operand as three bf16 terms that add up to
+ *     it exactly; weights and their gradients are fp32 too).  OLS_BF16: products of bf16 operands with fp32 sums; h and the
+ *     gradients at a and b are rounded to bf16 where they become operands.  The weights are bf16, or fp32 master weights that
+ *     are rounded to bf16 on the way (weight_dtype); their gradients are either (grad_dtype).
+ *   - ols_gated_ffn reads x and the weights and writes y.  For a later backward pass give it `saved` (ols_gated_ffn_saved_bytes,
+ *     256-byte aligned), where it leaves a, b and h; NULL otherwise.  Up to 8 rows without `saved` are read by kernels made for
+ *     single tokens.
+ *   - ols_gated_ffn_grad reads dy, x, the weights and `saved` and writes dx, g_gate, g_up and g_down (of the weights' shapes);
+ *     one whose dev is NULL is not computed.  Gradients are written, not added to.
+ *   - Limits: groups <= 4096; width, hidden and out <= 2^20; rows <= 2^24; row strides of dx, y and the gradients must not make
+ *     rows or workers overlap. */
+enum { OLS_ACT_SILU = 0, OLS_ACT_GELU = 1 /* x Phi(x), by the error function */, OLS_ACT_RELU = 2 };
+typedef struct ols_matrix {
+    void* dev;
+    int64_t row, group;         /* elements between rows, and between workers */
+} ols_matrix;
+typedef struct ols_ffn {
+    int32_t groups, act, dtype, weight_dtype, grad_dtype, reserved;
+    int64_t rows, width, hidden, out;
+    ols_matrix x, w_gate, w_up, w_down, y;
+    ols_matrix dy, dx, g_gate, g_up, g_down;
+    void* saved;
+    int64_t saved_bytes;
+    void* ws;
+    int64_t ws_bytes;
+} ols_ffn;
+OLS_API int ols_gated_ffn(const ols_ffn* f, void* stream);
+OLS_API int ols_gated_ffn_grad(const ols_ffn* f, void* stream);
+OLS_API int64_t ols_gated_ffn_saved_bytes(const ols_ffn* f);
+/* Of either call, for the tensors that f holds (operands that lie well are read in place); grad: 0 forward, 1 backward. */
+OLS_API int64_t ols_gated_ffn_workspace_bytes(const ols_ffn* f, int grad);
+
 /* Log probabilities: per row of logits z
  *     logsumexp = log sum e^z,   logprob = z[target] - logsumexp,   entropy = -sum p log p,   p = e^(z - logsumexp),
  * and the `top` tokens of the largest logits, best first, ties to the lower index: their log probabilities and indices

@@ -12,6 +12,7 @@ LIB_PATH = os.environ.get("OLS_LIBRARY", os.path.join(HERE, "libols.so"))   # ov
 OLS_OK, OLS_EINVAL, OLS_ESTATE, OLS_EHIP, OLS_ENOMEM = 0, -1, -2, -3, -4
 OLS_F32, OLS_BF16 = 0, 1
 OLS_MAX_TOP = 32
+OLS_ACT_SILU, OLS_ACT_GELU, OLS_ACT_RELU = range(3)
 (OLS_OPT_NESTEROV, OLS_OPT_FUSE_PULL, OLS_OPT_SERIALIZE, OLS_OPT_DRY_RUN, OLS_OPT_KERNEL_TIMING, OLS_OPT_TRACE,
  OLS_OPT_MEAN_SPLIT, OLS_OPT_FUSE_MEAN, OLS_OPT_TUNING) = range(1, 10)
 (OLS_OPT_GEMM_SPLITK, OLS_OPT_FUSE_GEMM_UPDATE, OLS_OPT_GEMM_FORCE_GENERAL, OLS_OPT_ANCHOR_DELAY_US,
@@ -26,6 +27,17 @@ TUNE_FWD, TUNE_DW, TUNE_DA = 0, 256, 512    # OLS_OPT_TUNING value = one of thes
 class ols_trace_entry(C.Structure):
     _fields_ = [("kind", C.c_int32), ("stream", C.c_int32), ("src_buf", C.c_int32), ("dst_buf", C.c_int32),
                 ("waited", C.c_int32), ("k", C.c_int32)]
+
+
+class ols_matrix(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("row", C.c_int64), ("group", C.c_int64)]
+
+
+class ols_ffn(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("groups", "act", "dtype", "weight_dtype", "grad_dtype", "reserved")]
+                + [(n, C.c_int64) for n in ("rows", "width", "hidden", "out")]
+                + [(n, ols_matrix) for n in ("x", "w_gate", "w_up", "w_down", "y", "dy", "dx", "g_gate", "g_up", "g_down")]
+                + [("saved", C.c_void_p), ("saved_bytes", C.c_int64), ("ws", C.c_void_p), ("ws_bytes", C.c_int64)])
 
 
 class OlsError(RuntimeError):
@@ -75,6 +87,10 @@ _SIGNATURES = {
     "ols_embed": (C.c_int, [C.c_int, _I, _I, _I, _P, _I, _P, C.c_int, _I, _I, C.c_float, _P, C.c_int, _I, _I, _P]),
     "ols_embed_grad": (C.c_int, [C.c_int, _I, _I, _I, _P, _I, _P, C.c_int, _I, _I, C.c_float, _P, C.c_int, _I, _I, C.c_int, _P, _I, _P]),
     "ols_embed_grad_workspace_bytes": (_I, [C.c_int, _I, _I, _I]),
+    "ols_gated_ffn": (C.c_int, [_P, _P]),
+    "ols_gated_ffn_grad": (C.c_int, [_P, _P]),
+    "ols_gated_ffn_saved_bytes": (_I, [_P]),
+    "ols_gated_ffn_workspace_bytes": (_I, [_P, C.c_int]),
     "ols_token_logprobs": (C.c_int, [_I, _I, _P, C.c_int, _I, _P, _P, _P, _P, _P, C.c_int, _P, _P, _P, _P, _P, _I, _P, _I, _P]),
     "ols_token_logprobs_workspace_bytes": (_I, [_I, _I, C.c_int, C.c_int]),
     "ols_token_logprobs_grad": (C.c_int, [_I, _I, _P, C.c_int, _I, _P, _P, _P, _P, _P, _P, _I, _P]),
@@ -261,6 +277,14 @@ def ols_embed_grad(*args):
     _check(load().ols_embed_grad(*args))
 
 
+def ols_gated_ffn(f, stream):
+    _check(load().ols_gated_ffn(C.byref(f), stream))
+
+
+def ols_gated_ffn_grad(f, stream):
+    _check(load().ols_gated_ffn_grad(C.byref(f), stream))
+
+
 def ols_token_logprobs(*args):
     _check(load().ols_token_logprobs(*args))
 
@@ -282,6 +306,14 @@ def _bytes(n):
 
 def ols_embed_grad_workspace_bytes(groups, tokens, vocab, width):
     return _bytes(load().ols_embed_grad_workspace_bytes(groups, tokens, vocab, width))
+
+
+def ols_gated_ffn_saved_bytes(f):
+    return _bytes(load().ols_gated_ffn_saved_bytes(C.byref(f)))
+
+
+def ols_gated_ffn_workspace_bytes(f, grad):
+    return _bytes(load().ols_gated_ffn_workspace_bytes(C.byref(f), grad))
 
 
 def ols_token_logprobs_workspace_bytes(rows, vocab, dtype, top):

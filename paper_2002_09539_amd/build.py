@@ -32,6 +32,7 @@ SOURCES = [
     "kernels_conv_bf16_slices.hip",
     "ols_operators.hip",
     "kernels_embed.hip",
+    "kernels_ffn.hip",
     "kernels_logprob.hip",
     "kernels_clip.hip",
 ]

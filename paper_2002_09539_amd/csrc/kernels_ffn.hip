@@ -1,0 +1,464 @@
+// Gated feed-forward block, forward and backward, per worker:
+//
+//   a = x Wg,   b = x Wu,   h = act(a) b,   y = h Wd
+//   dh = dy Wd^T,   da = dh b act'(a),   db = dh act(a),   dx = da Wg^T + db Wu^T
+//   dWg = x^T da,   dWu = x^T db,   dWd = h^T dy
+//
+// Both first projections, the activation and the product are one kernel: a tile holds the same columns of a and of b in the
+// registers of the same lanes.  Likewise dh never exists in memory: its tiles become da and db.  The products are those of
+// ffn_gemm.h; storage type fp32 takes them through three bf16 planes per operand.  An operand whose rows are 16-byte aligned
+// bf16 is read where it lies; others are laid out in the workspace first (rounded to bf16 where the weights are fp32 master
+// weights of a bf16 block), by a streaming pass.
+//
+// Few rows (answering token by token) leave nothing to multiply but every weight to read once: there a lane owns eight
+// columns, 32 lanes share the contraction, and several workgroups share it further so that the whole device reads.
+#include <algorithm>
+
+#include "ffn_gemm.h"
+
+namespace ols {
+
+namespace ffn {
+
+constexpr int kFewRows = 8;          // at most: weights are read by the vector unit
+constexpr int kFewThreads = 256;
+constexpr int kFewCols = 64;         // columns of a workgroup: a line of 128 bytes of bf16 weights
+constexpr int kFewSlab = 1024;       // contraction indices whose inputs lie in LDS at a time
+
+struct PackParams {
+    const void* src;
+    int64_t row, group, rows, cols, cols8;
+    uint16_t* dst;                   // [group][plane][rows][cols8]
+};
+
+template <typename T, bool SPLIT>
+__global__ __launch_bounds__(256) void pack_kernel(PackParams p) {
+    const int64_t units = p.cols8 / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= p.rows * units) return;
+    const int64_t r = i / units, c = i % units * 8, g = blockIdx.y;
+    float v[8];
+    load_upto8((const T*)p.src + g * p.group + r * p.row + c, (int)min((int64_t)8, p.cols - c), 0.0f, v);
+    constexpr int P = SPLIT ? 3 : 1;
+    uint16_t* out = p.dst + (g * P * p.rows + r) * p.cols8 + c;
+    if constexpr (SPLIT) {
+        const Split8 s = split8(f4{v[0], v[1], v[2], v[3]}, f4{v[4], v[5], v[6], v[7]});
+        *(u4*)out = s.hi;
+        *(u4*)(out + p.rows * p.cols8) = s.mid;
+        *(u4*)(out + 2 * p.rows * p.cols8) = s.lo;
+    } else {
+        store8(out, v);
+    }
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------------------------
+
+struct FewParams {
+    int64_t rows, K, N, n8;
+    const void *w, *w2;              // w2: the second projection
+    int64_t w_row, w2_row, w_group, w2_group;
+    const void* x;                   // first stage: [rows][K]
+    int64_t x_row, x_group;
+    const float* in;                 // second stage: the first one's partial sums [range][group][rows][2 n8_in]
+    int in_ranges, act;
+    int64_t in8;
+    int ranges;
+    float* partial;                  // [range][group][rows][panels n8]
+};
+
+// R rows at once.  FIRST: x from memory and two weight matrices; otherwise h = act(a) b from the partial sums of a and b.
+template <typename TX, typename TW, int R, bool FIRST>
+__global__ __launch_bounds__(kFewThreads) void few_kernel(FewParams p) {
+    constexpr int PANELS = FIRST ? 2 : 1;
+    __shared__ __align__(16) float xs[kFewSlab][R];
+    __shared__ float red[kFewThreads / 64][PANELS][R][kFewCols];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, cl = lane % 8, kl = threadIdx.x / 8;
+    const int64_t col = (int64_t)blockIdx.x * kFewCols + cl * 8, group = blockIdx.z;
+    const int range = blockIdx.y;
+    const int64_t from = p.K * range / p.ranges, to = p.K * (range + 1) / p.ranges;
+    const int left = (int)max((int64_t)0, min((int64_t)8, p.N - col));
+    const TW* w = (const TW*)p.w + group * p.w_group + col;
+    const TW* w2 = FIRST ? (const TW*)p.w2 + group * p.w2_group + col : nullptr;
+    float acc[PANELS][R][8] = {};
+    for (int64_t k0 = from; k0 < to; k0 += kFewSlab) {
+        const int n = (int)min((int64_t)kFewSlab, to - k0);
+        __syncthreads();
+        for (int r = 0; r < R; ++r)
+            for (int i = threadIdx.x; i < n; i += kFewThreads) {
+                float v = 0.0f;
+                if (r < p.rows) {
+                    if constexpr (FIRST) {
+                        v = load1((const TX*)p.x + group * p.x_group + r * p.x_row + k0 + i);
+                    } else {
+                        float a = 0.0f, b = 0.0f;
+                        for (int s = 0; s < p.in_ranges; ++s) {
+                            const float* in = p.in + (((int64_t)s * gridDim.z + group) * p.rows + r) * 2 * p.in8 + k0 + i;
+                            a += in[0], b += in[p.in8];
+                        }
+                        v = act_value(p.act, a) * b;
+                    }
+                }
+                xs[i][r] = v;
+            }
+        __syncthreads();
+        for (int i = kl; i < n; i += 4 * 32) {
+            float u[4][PANELS][8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t k = k0 + i + 32 * j;
+                const int have = i + 32 * j < n ? left : 0;
+                load_upto8(w + k * p.w_row, have, 0.0f, u[j][0]);
+                if constexpr (FIRST) load_upto8(w2 + k * p.w2_row, have, 0.0f, u[j][1]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (i + 32 * j >= n) continue;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float x = xs[i + 32 * j][r];
+#pragma unroll
+                    for (int t = 0; t < PANELS; ++t)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) acc[t][r][e] = fmaf(x, u[j][t][e], acc[t][r][e]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < PANELS; ++t)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float v = acc[t][r][e];
+                for (int o = 8; o < 64; o <<= 1) v += __shfl_xor(v, o);
+                if (lane < 8) red[wave][t][r][cl * 8 + e] = v;
+            }
+    __syncthreads();
+    for (int i = threadIdx.x; i < PANELS * R * kFewCols; i += kFewThreads) {
+        const int c = i % kFewCols, r = i / kFewCols % R, t = i / (kFewCols * R);
+        const int64_t n = (int64_t)blockIdx.x * kFewCols + c;
+        if (r >= p.rows || n >= p.n8) continue;
+        float v = 0.0f;
+        for (int k = 0; k < kFewThreads / 64; ++k) v += red[k][t][r][c];
+        p.partial[(((int64_t)range * gridDim.z + group) * p.rows + r) * PANELS * p.n8 + t * p.n8 + n] = v;
+    }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+
+int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
+int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+
+struct Arena {
+    char* base;
+    int64_t at = 0;
+    void* take(int64_t bytes) {
+        void* p = base + at;
+        at = up256(at + bytes);
+        return p;
+    }
+};
+
+// An operand as the products read it: [group][plane][outer][inner8], or the caller's tensor itself.
+struct View {
+    const uint16_t* p = nullptr;
+    int64_t pitch = 0, group = 0, plane = 0, inner8 = 0;
+};
+
+bool lies_well(const ols_matrix& m, int dtype, int64_t inner) {
+    return dtype == OLS_BF16 && inner % 8 == 0 && m.row % 8 == 0 && m.row <= (1 << 22) && m.group % 8 == 0 && ((uintptr_t)m.dev & 15) == 0;
+}
+
+struct Maker {                         // lays operands out; without a stream it only measures
+    const ols_ffn& f;
+    Arena& ws;
+    hipStream_t stream;
+    bool go;
+    hipError_t err = hipSuccess;
+    bool split() const { return f.dtype == OLS_F32; }
+    int planes() const { return split() ? 3 : 1; }
+
+    View operand(const ols_matrix& m, int dtype, int64_t outer, int64_t inner, bool may_lie) {
+        View v;
+        v.inner8 = up8(inner);
+        if (may_lie && !split() && lies_well(m, dtype, inner)) {
+            v.p = (const uint16_t*)m.dev, v.pitch = m.row, v.group = m.group;
+            return v;
+        }
+        const int64_t per = outer * v.inner8;
+        const int groups = m.group == 0 ? 1 : f.groups;      // shared by the workers: laid out once
+        uint16_t* dst = (uint16_t*)ws.take(2 * per * planes() * groups);
+        v.p = dst, v.pitch = v.inner8, v.plane = per, v.group = groups == 1 ? 0 : per * planes();
+        if (go && err == hipSuccess) {
+            const PackParams p{m.dev, m.row, m.group, outer, inner, v.inner8, dst};
+            const dim3 grid((unsigned)((outer * (v.inner8 / 8) + 255) / 256), groups);
+            if (split()) pack_kernel<float, true><<<grid, 256, 0, stream>>>(p);
+            else if (dtype == OLS_F32) pack_kernel<float, false><<<grid, 256, 0, stream>>>(p);
+            else pack_kernel<uint16_t, false><<<grid, 256, 0, stream>>>(p);
+            err = hipGetLastError();
+        }
+        return v;
+    }
+    // gate and up are read with one pitch: where theirs differ, both are laid out
+    bool pair_lies() const {
+        return lies_well(f.w_gate, f.weight_dtype, f.hidden) && lies_well(f.w_up, f.weight_dtype, f.hidden) && f.w_gate.row == f.w_up.row;
+    }
+    View internal(int64_t rows, int64_t inner, void* at) const {
+        View v;
+        v.inner8 = v.pitch = up8(inner), v.plane = rows * v.inner8, v.group = planes() * v.plane, v.p = (const uint16_t*)at;
+        return v;
+    }
+    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * planes() * f.groups * rows * up8(inner); }
+};
+
+// the planes' products, largest first
+constexpr int kPlanePairs[6][2] = {{0, 0}, {0, 1}, {1, 0}, {1, 1}, {0, 2}, {2, 0}};
+
+void set_segments(Job& j, const View& a, const View& b, const View* a2, const View* b2, bool split) {
+    j.segments = 0, j.seg_second = 0;
+    const int tensors = a2 ? 2 : 1, pairs = split ? 6 : 1;
+    for (int k = 0; k < pairs; ++k)
+        for (int t = 0; t < tensors; ++t) {
+            const int s = j.segments++;
+            j.seg_a[s] = kPlanePairs[k][0] * a.plane + (t ? a2->p - a.p : 0);
+            j.seg_b[s] = kPlanePairs[k][1] * b.plane;
+            if (t) j.seg_second |= 1u << s;
+        }
+    j.big = tensors;
+    j.a = a.p, j.a_group = a.group, j.a_pitch = a.pitch, j.a_inner8 = a.inner8;
+    j.b = b.p, j.b_group = b.group, j.b_pitch = b.pitch, j.b_inner8 = b.inner8;
+    if (b2) j.b2 = b2->p, j.b2_group = b2->group;
+}
+
+struct Shape {
+    int bm;                 // 256 or 128 rows and columns of a tile (columns: of both panels together)
+    int splits;
+};
+
+// Large tiles where they fill the device; otherwise small ones, whose contraction is cut into ranges until about two
+// workgroups a compute unit run or a range is down to four slices.
+Shape choose(const Job* jobs, int n, int groups, int panels, bool split) {
+    int64_t big = 0, small = 0, slices = 1 << 30;
+    for (int i = 0; i < n; ++i) {
+        big += groups * tiles_of(jobs[i].M, 256) * tiles_of(jobs[i].N, 256 / panels);
+        small += groups * tiles_of(jobs[i].M, 128) * tiles_of(jobs[i].N, 128 / panels);
+        slices = std::min(slices, tiles_of(jobs[i].K, kBK));
+    }
+    if (big >= 160 && !split) return {256, 1};
+    const int64_t splits = std::max((int64_t)1, std::min(std::min((int64_t)16, 512 / std::max(small, (int64_t)1)), slices / 4));
+    return {128, (int)splits};
+}
+
+template <bool A_RC, bool B_RC, Epi EPI>
+hipError_t product(Job* jobs, int n, int groups, bool split, Arena& ws, bool go, hipStream_t stream) {
+    constexpr int PANELS = EPI == kUp ? 2 : 1;
+    if (n == 0) return hipSuccess;
+    const Shape shape = choose(jobs, n, groups, PANELS, split);
+    GemmArgs p = {};
+    p.jobs = n, p.groups = groups, p.splits = shape.splits;
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        Job& j = p.job[i];
+        j = jobs[i];
+        j.tiles_m = (int)tiles_of(j.M, shape.bm), j.tiles_n = (int)tiles_of(j.N, shape.bm / PANELS);
+        p.first[i] = (int)total;
+        total += (int64_t)j.tiles_m * j.tiles_n * groups * shape.splits;
+        if (shape.splits > 1) j.partial = (float*)ws.take(4 * shape.splits * groups * j.M * PANELS * j.epi.n8);
+    }
+    if (!go) return hipSuccess;
+    if (total > 0x3fffffff) return hipErrorInvalidValue;
+    p.total = (int)total, p.chunk = (int)((total + kXcds - 1) / kXcds);
+    const int blocks = p.chunk * kXcds;
+    if (split) gemm_kernel<A_RC, B_RC, EPI, true, 128, 128, 256><<<blocks, 256, 0, stream>>>(p);
+    else if (shape.bm == 256) gemm_kernel<A_RC, B_RC, EPI, false, 256, 256, 512><<<blocks, 512, 0, stream>>>(p);
+    else gemm_kernel<A_RC, B_RC, EPI, false, 128, 128, 256><<<blocks, 256, 0, stream>>>(p);
+    hipError_t e = hipGetLastError();
+    for (int i = 0; i < n && shape.splits > 1 && e == hipSuccess; ++i) {
+        const Job& j = p.job[i];
+        const unsigned joins = (unsigned)((groups * j.M * (j.epi.n8 / 4) + 255) / 256);
+        if (split) join_kernel<EPI, true><<<joins, 256, 0, stream>>>(j.epi, j.partial, j.M, groups, shape.splits);
+        else join_kernel<EPI, false><<<joins, 256, 0, stream>>>(j.epi, j.partial, j.M, groups, shape.splits);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+Epilogue store_to(const ols_matrix& m, int64_t n, int dtype) {
+    Epilogue e = {};
+    e.n = n, e.n8 = up8(n), e.c = m.dev, e.c_row = m.row, e.c_group = m.group, e.c_f32 = dtype == OLS_F32;
+    return e;
+}
+
+// what a forward call leaves for the backward one
+struct Saved {
+    int64_t off_a, off_b, off_h, bytes;
+};
+Saved saved_layout(const ols_ffn& f) {
+    const int64_t elems = f.groups * f.rows * up8(f.hidden);
+    Saved s;
+    s.off_a = 0;
+    s.off_b = up256(elems * (f.dtype == OLS_F32 ? 4 : 2));
+    s.off_h = 2 * s.off_b;
+    s.bytes = up256(s.off_h + elems * 2 * (f.dtype == OLS_F32 ? 3 : 1));
+    return s;
+}
+
+template <typename TX, typename TW, bool FIRST>
+void few(const FewParams& p, int groups, hipStream_t stream) {
+    const dim3 grid((unsigned)tiles_of(p.n8, kFewCols), p.ranges, groups);
+    if (p.rows == 1) few_kernel<TX, TW, 1, FIRST><<<grid, kFewThreads, 0, stream>>>(p);
+    else if (p.rows == 2) few_kernel<TX, TW, 2, FIRST><<<grid, kFewThreads, 0, stream>>>(p);
+    else if (p.rows <= 4) few_kernel<TX, TW, 4, FIRST><<<grid, kFewThreads, 0, stream>>>(p);
+    else few_kernel<TX, TW, 8, FIRST><<<grid, kFewThreads, 0, stream>>>(p);
+}
+template <bool FIRST>
+void few(const FewParams& p, const ols_ffn& f, hipStream_t stream) {
+    if (f.dtype == OLS_F32) few<float, float, FIRST>(p, f.groups, stream);
+    else if (f.weight_dtype == OLS_F32) few<uint16_t, float, FIRST>(p, f.groups, stream);
+    else few<uint16_t, uint16_t, FIRST>(p, f.groups, stream);
+}
+
+int few_ranges(int64_t K, int64_t cols, int groups) {
+    const int64_t blocks = tiles_of(cols, kFewCols) * groups;
+    return (int)std::max((int64_t)1, std::min(512 / blocks, K / 128));
+}
+
+// Forward; with go false only the workspace is measured.
+hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
+    if (f.rows == 0) return hipSuccess;
+    const int64_t h8 = up8(f.hidden);
+    if (f.rows <= kFewRows && !f.saved) {
+        FewParams p = {};
+        p.rows = f.rows, p.K = f.width, p.N = f.hidden, p.n8 = h8, p.act = f.act;
+        p.w = f.w_gate.dev, p.w_row = f.w_gate.row, p.w_group = f.w_gate.group;
+        p.w2 = f.w_up.dev, p.w2_row = f.w_up.row, p.w2_group = f.w_up.group;
+        p.x = f.x.dev, p.x_row = f.x.row, p.x_group = f.x.group;
+        p.ranges = few_ranges(f.width, h8, f.groups);
+        p.partial = (float*)ws.take(4 * p.ranges * f.groups * f.rows * 2 * h8);
+        FewParams d = {};
+        d.rows = f.rows, d.K = f.hidden, d.N = f.out, d.n8 = up8(f.out), d.act = f.act;
+        d.w = f.w_down.dev, d.w_row = f.w_down.row, d.w_group = f.w_down.group;
+        d.in = p.partial, d.in_ranges = p.ranges, d.in8 = h8;
+        d.ranges = few_ranges(f.hidden, d.n8, f.groups);
+        d.partial = (float*)ws.take(4 * d.ranges * f.groups * f.rows * d.n8);
+        if (!go) return hipSuccess;
+        few<true>(p, f, stream);
+        few<false>(d, f, stream);
+        const Epilogue e = store_to(f.y, f.out, f.dtype);
+        join_kernel<kStore, false><<<(unsigned)((f.groups * f.rows * (d.n8 / 4) + 255) / 256), 256, 0, stream>>>(e, d.partial, f.rows, f.groups, d.ranges);
+        return hipGetLastError();
+    }
+    Maker mk{f, ws, stream, go};
+    const View x = mk.operand(f.x, f.dtype, f.rows, f.width, true);
+    const View wg = mk.operand(f.w_gate, f.weight_dtype, f.width, f.hidden, mk.pair_lies());
+    const View wu = mk.operand(f.w_up, f.weight_dtype, f.width, f.hidden, mk.pair_lies());
+    const View wd = mk.operand(f.w_down, f.weight_dtype, f.hidden, f.out, true);
+    if (mk.err != hipSuccess) return mk.err;
+    const Saved s = saved_layout(f);
+    char* saved = (char*)f.saved;
+    void* hp = saved ? (void*)(saved + s.off_h) : ws.take(mk.internal_bytes(f.rows, f.hidden));
+    const View h = mk.internal(f.rows, f.hidden, hp);
+
+    Job up = {};
+    up.M = f.rows, up.N = f.hidden, up.K = f.width;
+    set_segments(up, x, wg, nullptr, &wu, mk.split());
+    up.epi.n = f.hidden, up.epi.n8 = h8, up.epi.m = f.rows, up.epi.act = f.act;
+    up.epi.a = saved ? saved + s.off_a : nullptr, up.epi.b = saved ? saved + s.off_b : nullptr, up.epi.h = (uint16_t*)hp;
+    hipError_t e = product<false, true, kUp>(&up, 1, f.groups, mk.split(), ws, go, stream);
+    if (e != hipSuccess) return e;
+    Job down = {};
+    down.M = f.rows, down.N = f.out, down.K = f.hidden;
+    set_segments(down, h, wd, nullptr, nullptr, mk.split());
+    down.epi = store_to(f.y, f.out, f.dtype);
+    return product<false, true, kStore>(&down, 1, f.groups, mk.split(), ws, go, stream);
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(char* p, int64_t row_bytes, int64_t pitch, int64_t rows, int64_t group, int unit) {
+    const int64_t per = row_bytes / unit, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * per) return;
+    char* at = p + blockIdx.y * group + i / per * pitch + i % per * unit;
+    if (unit == 4) *(float*)at = 0.0f;
+    else *(uint16_t*)at = 0;
+}
+
+hipError_t zero(const ols_matrix& m, int64_t rows, int64_t cols, int dtype, int groups, hipStream_t stream) {
+    const int unit = dtype == OLS_F32 ? 4 : 2;
+    zero_kernel<<<dim3((unsigned)((rows * cols + 255) / 256), groups), 256, 0, stream>>>((char*)m.dev, cols * unit, m.row * unit, rows, m.group * unit, unit);
+    return hipGetLastError();
+}
+
+hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
+    const ols_matrix* grads[3] = {&f.g_gate, &f.g_up, &f.g_down};
+    if (f.rows == 0) {                       // sums over no rows
+        for (int i = 0; i < 3 && go; ++i)
+            if (grads[i]->dev) {
+                const hipError_t e = zero(*grads[i], i < 2 ? f.width : f.hidden, i < 2 ? f.hidden : f.out, f.grad_dtype, f.groups, stream);
+                if (e != hipSuccess) return e;
+            }
+        return hipSuccess;
+    }
+    Maker mk{f, ws, stream, go};
+    const bool to_up = f.dx.dev || f.g_gate.dev || f.g_up.dev, weights_up = f.g_gate.dev || f.g_up.dev;
+    const int64_t h8 = up8(f.hidden);
+    const Saved s = saved_layout(f);
+    char* saved = (char*)f.saved;
+    const View h = mk.internal(f.rows, f.hidden, saved + s.off_h);
+    const View dy = mk.operand(f.dy, f.dtype, f.rows, f.out, true);
+    View x, wg, wu, wd;
+    if (weights_up) x = mk.operand(f.x, f.dtype, f.rows, f.width, true);
+    if (to_up) wd = mk.operand(f.w_down, f.weight_dtype, f.hidden, f.out, true);
+    if (f.dx.dev) {
+        wg = mk.operand(f.w_gate, f.weight_dtype, f.width, f.hidden, mk.pair_lies());
+        wu = mk.operand(f.w_up, f.weight_dtype, f.width, f.hidden, mk.pair_lies());
+    }
+    if (mk.err != hipSuccess) return mk.err;
+    View da, db;
+    hipError_t e = hipSuccess;
+    if (to_up) {
+        void* pa = ws.take(mk.internal_bytes(f.rows, f.hidden));
+        void* pb = ws.take(mk.internal_bytes(f.rows, f.hidden));
+        da = mk.internal(f.rows, f.hidden, pa), db = mk.internal(f.rows, f.hidden, pb);
+        Job dh = {};
+        dh.M = f.rows, dh.N = f.hidden, dh.K = f.out;
+        set_segments(dh, dy, wd, nullptr, nullptr, mk.split());
+        dh.epi.n = f.hidden, dh.epi.n8 = h8, dh.epi.m = f.rows, dh.epi.act = f.act;
+        dh.epi.a = saved + s.off_a, dh.epi.b = saved + s.off_b, dh.epi.h = (uint16_t*)pa, dh.epi.h2 = (uint16_t*)pb;
+        e = product<false, false, kGateGrad>(&dh, 1, f.groups, mk.split(), ws, go, stream);
+        if (e != hipSuccess) return e;
+    }
+    if (f.dx.dev) {
+        Job dx = {};
+        dx.M = f.rows, dx.N = f.width, dx.K = f.hidden;
+        set_segments(dx, da, wg, &db, &wu, mk.split());
+        dx.epi = store_to(f.dx, f.width, f.dtype);
+        e = product<false, false, kStore>(&dx, 1, f.groups, mk.split(), ws, go, stream);
+        if (e != hipSuccess) return e;
+    }
+    Job dw[kMaxJobs] = {};
+    int n = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (!grads[i]->dev) continue;
+        Job& j = dw[n++];
+        j.M = i < 2 ? f.width : f.hidden, j.N = i < 2 ? f.hidden : f.out, j.K = f.rows;
+        set_segments(j, i < 2 ? x : h, i == 0 ? da : i == 1 ? db : dy, nullptr, nullptr, mk.split());
+        j.epi = store_to(*grads[i], j.N, f.grad_dtype);
+    }
+    return product<true, true, kStore>(dw, n, f.groups, mk.split(), ws, go, stream);
+}
+
+}  // namespace ffn
+
+int64_t ffn_saved_bytes(const ols_ffn& f) { return f.rows == 0 ? 0 : ffn::saved_layout(f).bytes; }
+int64_t ffn_workspace_bytes(const ols_ffn& f, bool grad) {
+    ffn::Arena ws{nullptr};
+    if (grad) (void)ffn::backward(f, ws, false, nullptr);
+    else (void)ffn::forward(f, ws, false, nullptr);
+    return ws.at;
+}
+hipError_t launch_ffn(const ols_ffn& f, bool grad, hipStream_t stream) {
+    ffn::Arena ws{(char*)f.ws};
+    return grad ? ffn::backward(f, ws, true, stream) : ffn::forward(f, ws, true, stream);
+}
+
+}  // namespace ols

@@ -448,7 +448,7 @@ hipError_t ensure_dynamic_lds(const void* kernel, size_t bytes);
 inline int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 
 // ---------------------------------------------------------------------------------------------
-// Operators of token models (kernels_embed.hip, kernels_logprob.hip, kernels_clip.hip); the entry points that check their
+// Operators of token models (kernels_embed.hip, kernels_ffn.hip, kernels_logprob.hip, kernels_clip.hip); the entry points that check their
 // arguments are in ols_operators.hip.  Strides in elements.
 // ---------------------------------------------------------------------------------------------
 int report(int code, const char* message);   // sets ols_last_error of this thread, returns code
@@ -500,6 +500,10 @@ struct LogprobParams {
 int64_t logprob_workspace_bytes(int dtype, int64_t rows, int64_t vocab, int top);
 hipError_t launch_logprob(LogprobParams p, void* ws, hipStream_t stream);        // with d_logits: the gradient as well
 hipError_t launch_logprob_grad(const LogprobParams& p, hipStream_t stream);      // from p.stats and p.entropy
+
+int64_t ffn_saved_bytes(const ols_ffn& f);
+int64_t ffn_workspace_bytes(const ols_ffn& f, bool grad);
+hipError_t launch_ffn(const ols_ffn& f, bool grad, hipStream_t stream);
 
 // Tensors of one launch, by value in the kernel arguments (4 KiB): no table to upload, nothing to keep alive.
 constexpr int kClipTensors = 88;

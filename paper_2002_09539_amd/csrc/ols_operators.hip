@@ -70,6 +70,37 @@ int check_logprob(const char* who, int dtype, int64_t rows, int64_t vocab, const
     return OLS_OK;
 }
 
+// ---- gated feed-forward block ---------------------------------------------------------------------------------------------
+
+int check_ffn(const char* who, const ols_ffn* f) {
+    if (!f) return bad("%s: null descriptor", who);
+    if (f->groups < 1 || f->groups > kMaxGroups) return bad("%s: groups must be in [1, %d], got %d", who, kMaxGroups, (int)f->groups);
+    if (f->act < OLS_ACT_SILU || f->act > OLS_ACT_RELU) return bad("%s: unknown activation %d", who, (int)f->act);
+    if (!is_dtype(f->dtype) || !is_dtype(f->weight_dtype) || !is_dtype(f->grad_dtype)) return bad("%s: unknown type", who);
+    if (f->dtype == OLS_F32 && (f->weight_dtype != OLS_F32 || f->grad_dtype != OLS_F32)) return bad("%s: an fp32 block has fp32 weights and gradients", who);
+    if (f->rows < 0 || f->rows > kMaxTokens) return bad("%s: rows must be in [0, 2^24], got %lld", who, (long long)f->rows);
+    const int64_t sizes[3] = {f->width, f->hidden, f->out};
+    for (int i = 0; i < 3; ++i)
+        if (sizes[i] < 1 || sizes[i] > kMaxWidth)
+            return bad("%s: width, hidden and out must be in [1, 2^20], got %lld, %lld, %lld", who, (long long)f->width, (long long)f->hidden, (long long)f->out);
+    return OLS_OK;
+}
+
+int check_matrix(const char* who, const char* name, const ols_matrix& m, int64_t rows, int64_t cols, int dtype, int groups, bool written) {
+    if (!m.dev || !element_aligned(m.dev, dtype)) return bad("%s: %s is null or not aligned to its type", who, name);
+    if (!stride_ok(m.row, cols)) return bad("%s: rows of %s, of %lld elements, cannot be %lld apart", who, name, (long long)cols, (long long)m.row);
+    if (!group_ok(m.group)) return bad("%s: the workers' stride of %s is out of range", who, name);
+    if (written && groups > 1 && m.group < (rows - 1) * m.row + cols) return bad("%s: the workers' %s overlap", who, name);
+    return OLS_OK;
+}
+
+int check_ffn_operands(const char* who, const ols_ffn& f) {
+    if (const int rc = check_matrix(who, "x", f.x, f.rows, f.width, f.dtype, f.groups, false)) return rc;
+    if (const int rc = check_matrix(who, "w_gate", f.w_gate, f.width, f.hidden, f.weight_dtype, f.groups, false)) return rc;
+    if (const int rc = check_matrix(who, "w_up", f.w_up, f.width, f.hidden, f.weight_dtype, f.groups, false)) return rc;
+    return check_matrix(who, "w_down", f.w_down, f.hidden, f.out, f.weight_dtype, f.groups, false);
+}
+
 // ---- clipping -----------------------------------------------------------------------------------------------------------
 
 constexpr int64_t kChunk = 16384;             // elements of a workgroup's chunk, doubled until no group has more than kMostChunks
@@ -181,6 +212,51 @@ int ols_embed_grad(int groups, int64_t tokens, int64_t vocab, int64_t width, con
     p.ids = ids_dev, p.ids_group = ids_group, p.dout = d_out_dev, p.dout_row = d_out_row, p.dout_group = d_out_group, p.scale = scale;
     p.grad = grad_dev, p.grad_row = grad_row, p.grad_group = grad_group;
     return done(launch_embed_grad(p, ws_dev, (hipStream_t)stream), who);
+}
+
+int64_t ols_gated_ffn_saved_bytes(const ols_ffn* f) {
+    if (const int rc = check_ffn("ols_gated_ffn_saved_bytes", f)) return rc;
+    return ffn_saved_bytes(*f);
+}
+
+int64_t ols_gated_ffn_workspace_bytes(const ols_ffn* f, int grad) {
+    if (const int rc = check_ffn("ols_gated_ffn_workspace_bytes", f)) return rc;
+    return ffn_workspace_bytes(*f, grad != 0);
+}
+
+int ols_gated_ffn(const ols_ffn* f, void* stream) {
+    const char* who = "ols_gated_ffn";
+    if (const int rc = check_ffn(who, f)) return rc;
+    if (f->rows == 0) return OLS_OK;
+    if (const int rc = check_ffn_operands(who, *f)) return rc;
+    if (const int rc = check_matrix(who, "y", f->y, f->rows, f->out, f->dtype, f->groups, true)) return rc;
+    if (f->saved) {
+        if (f->saved_bytes < ffn_saved_bytes(*f)) return bad("%s: `saved` of %lld bytes, %lld are needed", who, (long long)f->saved_bytes, (long long)ffn_saved_bytes(*f));
+        if (!aligned(f->saved, 256)) return bad("%s: `saved` must be 256-byte aligned", who);
+    }
+    if (const int rc = check_ws(who, f->ws, f->ws_bytes, ffn_workspace_bytes(*f, false))) return rc;
+    return done(launch_ffn(*f, false, (hipStream_t)stream), who);
+}
+
+int ols_gated_ffn_grad(const ols_ffn* f, void* stream) {
+    const char* who = "ols_gated_ffn_grad";
+    if (const int rc = check_ffn(who, f)) return rc;
+    const ols_matrix* g[3] = {&f->g_gate, &f->g_up, &f->g_down};
+    const char* names[3] = {"g_gate", "g_up", "g_down"};
+    for (int i = 0; i < 3; ++i)
+        if (g[i]->dev)
+            if (const int rc = check_matrix(who, names[i], *g[i], i < 2 ? f->width : f->hidden, i < 2 ? f->hidden : f->out, f->grad_dtype, f->groups, true)) return rc;
+    if (f->rows > 0) {
+        if (const int rc = check_ffn_operands(who, *f)) return rc;
+        if (const int rc = check_matrix(who, "dy", f->dy, f->rows, f->out, f->dtype, f->groups, false)) return rc;
+        if (f->dx.dev)
+            if (const int rc = check_matrix(who, "dx", f->dx, f->rows, f->width, f->dtype, f->groups, true)) return rc;
+        if (!f->saved || f->saved_bytes < ffn_saved_bytes(*f))
+            return bad("%s: `saved` of %lld bytes, %lld are needed", who, (long long)(f->saved ? f->saved_bytes : 0), (long long)ffn_saved_bytes(*f));
+        if (!aligned(f->saved, 256)) return bad("%s: `saved` must be 256-byte aligned", who);
+        if (const int rc = check_ws(who, f->ws, f->ws_bytes, ffn_workspace_bytes(*f, true))) return rc;
+    }
+    return done(launch_ffn(*f, true, (hipStream_t)stream), who);
 }
 
 int64_t ols_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int top) {

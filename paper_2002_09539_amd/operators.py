@@ -128,6 +128,111 @@ def embed_grad(tokens, d_out, vocab, scale=1.0, out=None, dtype=torch.float32, a
     return out
 
 
+# ---- gated feed-forward block -------------------------------------------------------------------------------------
+FfnGrads = namedtuple("FfnGrads", "x w_gate w_up w_down")
+
+_ACT = {"silu": B.OLS_ACT_SILU, "gelu": B.OLS_ACT_GELU, "relu": B.OLS_ACT_RELU}
+
+
+def _matrix(t, m, shape, name):
+    """A tensor as the C boundary takes it: [m][rows][cols], without the worker axis [rows][cols] shared by the workers."""
+    if tuple(t.shape) not in ((m, *shape), shape) or (t.dim() == 2 and name not in _SHARED and m > 1):
+        _refuse("%s must be of shape %s, got %s", name, (m, *shape), tuple(t.shape))
+    group, row = _rows(t if t.dim() == 3 else t.unsqueeze(0), name)
+    return B.ols_matrix(t.data_ptr(), row, group)
+
+
+_SHARED = ("x", "w_gate", "w_up", "w_down", "dy")    # inputs that may come without a worker axis
+
+
+def _ffn(x, w_gate, w_up, w_down, act, others):
+    device = _on_gpu(x, w_gate, w_up, w_down, *others)
+    if act not in _ACT:
+        _refuse("unknown activation %r: one of %s", act, ", ".join(_ACT))
+    if x.dim() not in (2, 3) or w_gate.dim() not in (2, 3):
+        _refuse("x is [rows, width] or [m, rows, width], weights [width, hidden] or [m, width, hidden]")
+    workers = x.dim() == 3 or w_gate.dim() == 3
+    m = x.shape[0] if x.dim() == 3 else w_gate.shape[0] if workers else 1
+    rows, width, hidden, out = x.shape[-2], x.shape[-1], w_gate.shape[-1], w_down.shape[-1]
+    if w_gate.dtype != w_up.dtype or w_gate.dtype != w_down.dtype:
+        _refuse("the weights must share one type")
+    f = B.ols_ffn()
+    f.groups, f.act, f.dtype, f.weight_dtype = m, _ACT[act], _dtype(x, "x"), _dtype(w_gate, "the weights")
+    f.grad_dtype = f.weight_dtype
+    f.rows, f.width, f.hidden, f.out = rows, width, hidden, out
+    f.x = _matrix(x, m, (rows, width), "x")
+    f.w_gate = _matrix(w_gate, m, (width, hidden), "w_gate")
+    f.w_up = _matrix(w_up, m, (width, hidden), "w_up")
+    f.w_down = _matrix(w_down, m, (hidden, out), "w_down")
+    return f, device, ((m,) if workers else ())
+
+
+def gated_ffn(x, w_gate, w_up, w_down, act="silu", save=False, out=None):
+    """y = (act(x w_gate) * (x w_up)) w_down; act: "silu", "gelu" (by the error function) or "relu".
+
+    x: [rows, width] or [m, rows, width]; weights: [width, hidden], [width, hidden], [hidden, out], with or without the
+    workers' axis in front (without: shared).  x bf16: products of bf16 operands, weights bf16 or fp32 (rounded on the way);
+    x fp32: products of fp32 accuracy, fp32 weights.  save=True returns (y, saved) for gated_ffn_grad."""
+    f, device, lead = _ffn(x, w_gate, w_up, w_down, act, (out,))
+    shape = (*lead, f.rows, f.out)
+    with torch.cuda.device(device):
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=device)
+        elif tuple(out.shape) != shape or out.dtype != x.dtype:
+            _refuse("out must be of shape %s and x's type", shape)
+        f.y = _matrix(out, f.groups, (f.rows, f.out), "out")
+        saved = None
+        if save:
+            f.saved_bytes = B.ols_gated_ffn_saved_bytes(f)
+            saved = torch.empty(f.saved_bytes, dtype=torch.uint8, device=device)
+            f.saved = saved.data_ptr() if f.saved_bytes else None
+        f.ws_bytes = B.ols_gated_ffn_workspace_bytes(f, 0)
+        ws = _workspace(f.ws_bytes, device)
+        f.ws = _ptr(ws)
+        B.ols_gated_ffn(f, _stream(device))
+    return (out, saved) if save else out
+
+
+def gated_ffn_grad(dy, x, w_gate, w_up, w_down, saved, act="silu", out=None, grad_dtype=None, need_x=True):
+    """Gradients of sum(dy * y): FfnGrads(x, w_gate, w_up, w_down), from what gated_ffn(..., save=True) left.
+
+    The weights' gradients are of grad_dtype (the weights' type by default) and have a worker axis if anything has one: a
+    shared weight's gradient is each worker's.  out: a FfnGrads of tensors to write to (views of gradient rows, say; None
+    entries are allocated); need_x=False leaves out the gradient at x."""
+    f, device, lead = _ffn(x, w_gate, w_up, w_down, act, (dy, saved, *(out or ())))
+    if dy.dtype != x.dtype:
+        _refuse("dy must be of x's type")
+    f.dy = _matrix(dy, f.groups, (f.rows, f.out), "dy")
+    shapes = ((f.rows, f.width), (f.width, f.hidden), (f.width, f.hidden), (f.hidden, f.out))
+    if out is not None:
+        types = {t.dtype for t in out[1:] if t is not None}
+        if len(types) > 1 or (grad_dtype and types - {grad_dtype}):
+            _refuse("the weights' gradients must share one type")
+        grad_dtype = grad_dtype or (types.pop() if types else None)
+    grad_dtype = grad_dtype or w_gate.dtype
+    f.grad_dtype = _dtype(grad_dtype, "grad_dtype")
+    with torch.cuda.device(device):
+        made = []
+        for i, (name, shape) in enumerate(zip(("dx", "g_gate", "g_up", "g_down"), shapes)):
+            t = out[i] if out is not None else None
+            if i == 0 and not need_x:
+                made.append(None)
+                continue
+            dtype = x.dtype if i == 0 else grad_dtype
+            if t is None:
+                t = torch.empty(*lead, *shape, dtype=dtype, device=device)
+            elif tuple(t.shape) != (*lead, *shape) or t.dtype != dtype:
+                _refuse("out.%s must be %s of shape %s", FfnGrads._fields[i], dtype, (*lead, *shape))
+            setattr(f, name, _matrix(t, f.groups, shape, name))
+            made.append(t)
+        f.saved, f.saved_bytes = (saved.data_ptr() if saved.numel() else None), saved.numel()
+        f.ws_bytes = B.ols_gated_ffn_workspace_bytes(f, 1)
+        ws = _workspace(f.ws_bytes, device)
+        f.ws = _ptr(ws)
+        B.ols_gated_ffn_grad(f, _stream(device))
+    return FfnGrads(*made)
+
+
 # ---- log probabilities --------------------------------------------------------------------------------------------
 def _logit_rows(t, name):
     if t.dim() < 1 or t.shape[-1] < 1:
