@@ -8,14 +8,22 @@
 // largest of the nine products of planes are six segments of one longer contraction (split_bf16.h says why six are enough).
 // The gradient at the block's input, da Wg^T + db Wu^T, is two segments as well.
 //
-// A tile's slices of 64 contraction indices go from memory straight into LDS (16 bytes a lane, no registers in between),
-// into one of two buffers while the other is multiplied; one barrier a slice.  The direct copy writes a wavefront's lanes
-// side by side, so rows cannot be padded against bank conflicts: instead every lane fetches another chunk of its row
-// than its place says (place = chunk XOR a function of the row), and the fragment reads look there.  Buffer descriptors end at
-// the operand's last element, so rows and columns that a tile hangs over read as zeros.
+// A tile's slices of 32 contraction indices go from memory straight into LDS (16 bytes a lane, no registers in between),
+// into a ring of four buffers: three slices are under way while one is multiplied.  The direct copy writes a wavefront's
+// lanes side by side, so rows cannot be padded against bank conflicts: instead every lane fetches another chunk of its row
+// than its place says (place = chunk XOR a function of the row), and the fragment reads look there.  Buffer descriptors end
+// at the operand's last element, so rows and columns that a tile hangs over read as zeros.
 //
-// The products are formed with the operands swapped (MFMA rows = columns of C): a lane then holds four consecutive
-// columns of one row of C, which the epilogues read and write as vectors.
+// Each of a slice's two steps first requests the next step's fragments, the second one those of the next slice, in front of
+// which stands the only barrier of a slice.
+//
+// What bounds it, measured on 8192 x 2048 x 11264 (K contiguous in both): without the copies, on what lies in LDS, 1300 to
+// 1440 TFLOP/s; without the products 1200 with tiles of 256 x 128 and two thirds of the bytes with 256 x 256; together 1137.
+// Tiles of 256 x 128, two workgroups a compute unit: 974.  Two buffers of 64 indices: 1107 to 1123.  Four wavefronts of
+// 128 x 128, one a SIMD: 750.  A library's product of this size runs at 1100 to 1370.
+//
+// Results pass through LDS on their way out: what a lane holds after the MFMAs are four columns of a row, and memory wants
+// whole lines (with 8-byte pieces, the product with the gradients' epilogue ran at 410 TFLOP/s instead of 540).
 #pragma once
 #include <type_traits>
 
@@ -25,7 +33,8 @@
 namespace ols {
 namespace ffn {
 
-constexpr int kBK = 64;              // contraction indices of a slice
+constexpr int kBK = 32;              // contraction indices of a slice
+constexpr int kRing = 4;             // buffers
 constexpr int kXcds = 8;
 constexpr int kMaxSegments = 12;
 
@@ -34,55 +43,54 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 // Addresses in LDS are an array plus ONE integer offset: the compiler tells the two buffers apart (and so does not make a
 // fragment read wait for the copies into the other one) only where it finds the array within a few steps of the access.
 
-// What a tile copies of one operand.
-struct Operand {
-    const uint16_t* base;            // of the group and segment
-    int64_t pitch;                   // elements between outer indices (rows of KC, contraction indices of RC)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }   // the same in every lane: kept as a scalar
+
+// Where the next slice of a tile lies: its first element and the bytes from there to the operand's last one.
+struct Cursor {
+    const char* at;
+    int64_t left;
+    int64_t step;                        // bytes from slice to slice
+    __device__ rsrc_t window() const { return make_rsrc(at, (unsigned)min(max(left, (int64_t)0), (int64_t)0x7ffffff0)); }
+    __device__ void advance() { at += step, left -= step; }
 };
 
-// bytes from (outer o, inner i) to the end of the operand's last line, at most 2^31
-__device__ __forceinline__ unsigned bytes_left(int64_t outer, int64_t inner8, int64_t pitch, int64_t o, int64_t i) {
-    const int64_t left = o < outer ? 2 * ((outer - 1 - o) * pitch + inner8 - i) : 0;
-    return (unsigned)min(max(left, (int64_t)0), (int64_t)0x7ffffff0);
-}
-
-// KC tile: LDS [ROWS][64], chunk c (8 elements) of row r at place c ^ (r & 7).
+// KC tile: LDS [ROWS][32], chunk c (8 elements) of row r at place c ^ (r / 4 & 3): sixteen rows' chunks lie on different banks.
 template <int ROWS, int THREADS>
 struct TileKC {
     static constexpr int kBytes = ROWS * kBK * 2;
     static constexpr int kCopies = kBytes / 1024 / (THREADS / 64);      // per wavefront
-    static_assert(kBytes % (1024 * (THREADS / 64)) == 0, "whole copies");
-    static constexpr int64_t kUnit = 1;
-    unsigned lane_off;
-    int chunk;                       // the lane's chunk within the slice
+    static_assert(kBytes % (1024 * (THREADS / 64)) == 0 && kBK == 32, "whole copies of sixteen rows");
+    unsigned lane_off, step;
+    int chunk;                           // the lane's chunk within the slice
     __device__ TileKC(int64_t pitch) {
-        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-        chunk = (lane % 8) ^ (lane / 8);
-        lane_off = (unsigned)((wave * 8 + lane / 8) * pitch * 2 + chunk * 16);
+        const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
+        chunk = (lane % 4) ^ (lane / 16);
+        lane_off = (unsigned)((wave * 16 + lane / 4) * pitch * 2 + chunk * 16);
+        step = (unsigned)(THREADS / 64 * 16 * pitch * 2);
     }
-    // rows [row0, row0 + ROWS), contraction indices [k0, k0 + 64) of [rows][k8]
-    __device__ void copy(char* lds, int at, const Operand& m, int64_t rows, int64_t k8, int64_t row0, int64_t k0) const {
-        const int wave = threadIdx.x / 64;
-        const rsrc_t rs = make_rsrc(m.base + row0 * m.pitch + k0, bytes_left(rows, k8, m.pitch, row0, k0));
-        const unsigned off = chunk * 8 < k8 - k0 ? lane_off : 0x7ffffff0u;     // past the row's end: zeros
-        const unsigned step = (unsigned)(THREADS / 64 * 8 * m.pitch * 2);
+    // rows [row0, row0 + ROWS), contraction indices from k0 of [rows][k8]
+    __device__ static Cursor cursor(const uint16_t* base, int64_t pitch, int64_t rows, int64_t k8, int64_t row0, int64_t k0) {
+        return {(const char*)(base + row0 * pitch + k0), 2 * ((rows - 1 - row0) * pitch + k8 - k0), 2 * kBK};
+    }
+    __device__ void copy(char* lds, int at, const Cursor& c, int64_t k_left) const {
+        const int wave = uniform(threadIdx.x / 64);
+        const rsrc_t rs = c.window();
+        const unsigned off = chunk * 8 < k_left ? lane_off : 0x40000000u;      // past the row's end: beyond the window, zeros
 #pragma unroll
         for (int t = 0; t < kCopies; ++t)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(lds + (at + (t * (THREADS / 64) + wave) * 1024)), 16,
-                                                     (int)(off >= 0x7ffffff0u ? off : off + t * step), 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(lds + (at + (t * (THREADS / 64) + wave) * 1024)), 16, (int)(off + t * step), 0, 0, 0);
     }
     // 32 rows from r0 of the tile at `at`, 16 contraction indices 16 s ..: the lane holds k = 16 s + 8 (lane / 32) + 0..7 of row
     // r0 + lane % 32
     __device__ static int lane_part(int at, int r0, int lane) {
         const int r = r0 + lane % 32;
-        return at + r * (kBK * 2) + (((lane / 32) ^ (r & 7)) << 4);
+        return at + r * (kBK * 2) + (((lane / 32) ^ ((r >> 2) & 3)) << 4);
     }
-    __device__ static bf16x8 frag(const char* lds, int part, int s) { return __builtin_bit_cast(bf16x8, *(const u4*)(lds + (part ^ (s << 5))));
-    }
+    __device__ static bf16x8 frag(const char* lds, int part, int s) { return __builtin_bit_cast(bf16x8, *(const u4*)(lds + (part ^ (s << 5)))); }
 };
 
-// RC tile: LDS [64][COLS], chunk q of line k at place q ^ swizzle(k): the four lines that a transposing read takes together
-// fall on different banks.
+// RC tile: LDS [32][COLS], chunk q of line k at place q ^ swizzle(k): the four lines that a transposing read takes together
+// lie on different banks.
 template <int COLS, int THREADS>
 struct TileRC {
     static constexpr int kBytes = COLS * kBK * 2;
@@ -91,19 +99,21 @@ struct TileRC {
     static_assert(kBytes % (1024 * (THREADS / 64)) == 0 && 64 % kChunks == 0, "whole copies");
     static constexpr int kShift = COLS >= 128 ? 2 : 1;
     __device__ static int swizzle(int k) { return (k & 3) << kShift; }
-    unsigned lane_off;
-    int line;
+    unsigned lane_off, step;
     __device__ TileRC(int64_t pitch) {
-        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-        line = wave * kLines + lane / kChunks;                          // the copies of a lane are a multiple of 4 lines apart
+        const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
+        const int line = wave * kLines + lane / kChunks;                // the copies of a lane are a multiple of 4 lines apart
         static_assert((THREADS / 64) * kLines % 4 == 0, "one swizzle per lane");
         lane_off = (unsigned)(line * pitch * 2 + ((lane % kChunks) ^ swizzle(line)) * 16);
+        step = (unsigned)(THREADS / 64 * kLines * pitch * 2);
     }
-    // columns [col0, ..), contraction indices [k0, ..) of [K][cols8]
-    __device__ void copy(char* lds, int at, const Operand& m, int64_t cols8, int64_t K, int64_t col0, int64_t k0) const {
-        const int wave = threadIdx.x / 64;
-        const rsrc_t rs = make_rsrc(m.base + k0 * m.pitch + col0, bytes_left(K, cols8, m.pitch, k0, col0));
-        const unsigned step = (unsigned)(THREADS / 64 * kLines * m.pitch * 2);
+    // columns [col0, ..), contraction indices from k0 of [K][cols8]
+    __device__ static Cursor cursor(const uint16_t* base, int64_t pitch, int64_t cols8, int64_t K, int64_t col0, int64_t k0) {
+        return {(const char*)(base + k0 * pitch + col0), 2 * ((K - 1 - k0) * pitch + cols8 - col0), 2 * kBK * pitch};
+    }
+    __device__ void copy(char* lds, int at, const Cursor& c, int64_t) const {
+        const int wave = uniform(threadIdx.x / 64);
+        const rsrc_t rs = c.window();
 #pragma unroll
         for (int t = 0; t < kCopies; ++t)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(lds + (at + (t * (THREADS / 64) + wave) * 1024)), 16, (int)(lane_off + t * step), 0, 0, 0);
@@ -123,7 +133,6 @@ struct TileRC {
     }
 };
 
-
 // ---- what is done with a product ------------------------------------------------------------------------------------------
 
 enum Epi { kUp, kStore, kGateGrad };
@@ -135,10 +144,12 @@ struct Epilogue {
     int64_t c_row, c_group;
     int c_f32;
     // kUp: a and b (where they are kept) and h are written; kGateGrad: a and b are read, da and db are written.  Internal
-    // tensors have rows of n8 elements; those of planes have [plane][m][n8] per group.
+    // tensors have rows of n8 elements, pitch apart; those of planes have [plane][m][pitch] per group.
     int act;
-    int64_t m, n8;
-    void *a, *b;                        // storage type of the call: fp32 with three planes, bf16 with one
+    int64_t m, n8, pitch;
+    // a and b stay fp32 in a bf16 block as well: rounded to bf16 they would put the weights' gradients at 1.8 times the error of
+    // their own rounding (3.1e-3 against 64 bits where da's and the result's roundings alone make 2.3e-3).
+    float *a, *b;
     uint16_t *h, *h2;                   // kUp: h.  kGateGrad: da, db
 };
 
@@ -159,84 +170,49 @@ __device__ __forceinline__ void act_both(int act, float a, float& value, float& 
     }
 }
 
-typedef unsigned int u2any __attribute__((ext_vector_type(2), aligned(2)));
-typedef unsigned int u4any4 __attribute__((ext_vector_type(4), aligned(4)));
-
-__device__ __forceinline__ void store4(uint16_t* p, const float (&v)[4], int left) {
-    if (left >= 4) {
-        *(u2any*)p = u2any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = bf16_of(v[e]);
-    }
-}
-__device__ __forceinline__ void store4(float* p, const float (&v)[4], int left) {
-    if (left >= 4) {
-        *(u4any4*)p = u4any4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = v[e];
-    }
-}
-__device__ __forceinline__ void load4(const uint16_t* p, float (&v)[4]) {    // 8-byte aligned
-    const u2 w = *(const u2*)p;
-    v[0] = bf16_lo(w[0]), v[1] = bf16_hi(w[0]), v[2] = bf16_lo(w[1]), v[3] = bf16_hi(w[1]);
-}
-__device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
-    const f4 w = *(const f4*)p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = w[e];
-}
-
-// four elements of an internal tensor: one bf16 plane, or the three that add up to the fp32 values
+// eight elements of an internal tensor: one bf16 plane, or the three that add up to the fp32 values
 template <bool SPLIT>
-__device__ __forceinline__ void store_planes(uint16_t* p, int64_t plane, const float (&v)[4]) {
+__device__ __forceinline__ void store_planes(uint16_t* p, int64_t plane, const float (&v)[8]) {
     if constexpr (!SPLIT) {
-        *(u2*)p = u2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        *(u4*)p = u4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     } else {
-        const Split8 s = split8(f4{v[0], v[1], v[2], v[3]}, f4{0, 0, 0, 0});
-        *(u2*)p = u2{s.hi[0], s.hi[1]};
-        *(u2*)(p + plane) = u2{s.mid[0], s.mid[1]};
-        *(u2*)(p + 2 * plane) = u2{s.lo[0], s.lo[1]};
+        const Split8 s = split8(f4{v[0], v[1], v[2], v[3]}, f4{v[4], v[5], v[6], v[7]});
+        *(u4*)p = s.hi;
+        *(u4*)(p + plane) = s.mid;
+        *(u4*)(p + 2 * plane) = s.lo;
     }
 }
 
-// Columns n .. n + 3 (n a multiple of 4) of row m; `second`: the product with the other panel.
+// Columns n .. n + 7 (n a multiple of 8) of row m; `second`: the product with the other panel.
 template <Epi EPI, bool SPLIT>
-__device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m, int64_t n, const float (&v)[4], const float (&second)[4]) {
-    using T = typename std::conditional<SPLIT, float, uint16_t>::type;
+__device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m, int64_t n, const float (&v)[8], const float (&second)[8]) {
     constexpr int P = SPLIT ? 3 : 1;
+    if (n >= e.n8) return;
     if constexpr (EPI == kStore) {
-        const int64_t left = e.n - n;
-        if (left <= 0) return;
+        const int left = (int)min((int64_t)8, e.n - n);
         const int64_t at = group * e.c_group + m * e.c_row + n;
-        if (e.c_f32) store4((float*)e.c + at, v, (int)min(left, (int64_t)4));
-        else store4((uint16_t*)e.c + at, v, (int)min(left, (int64_t)4));
+        if (e.c_f32) store_upto8((float*)e.c + at, left, v);
+        else store_upto8((uint16_t*)e.c + at, left, v);
     } else {
-        if (n >= e.n8) return;
-        const int64_t at = (group * e.m + m) * e.n8 + n, plane = e.m * e.n8, at_planes = (group * P * e.m + m) * e.n8 + n;
-        float x[4], y[4];
+        const int64_t at = (group * e.m + m) * e.pitch + n, plane = e.m * e.pitch, at_planes = (group * P * e.m + m) * e.pitch + n;
+        float a[8], b[8], x[8], y[8];
         if constexpr (EPI == kUp) {
-            float a[4], b[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 const bool real = n + i < e.n;           // the padding of internal rows is zero whatever the operands hold
                 a[i] = real ? v[i] : 0.0f, b[i] = real ? second[i] : 0.0f;
                 x[i] = real ? act_value(e.act, a[i]) * b[i] : 0.0f;
             }
             if (e.a) {
-                store4((T*)e.a + at, a, 4);
-                store4((T*)e.b + at, b, 4);
+                store8(e.a + at, a);
+                store8(e.b + at, b);
             }
             store_planes<SPLIT>(e.h + at_planes, plane, x);
         } else {
-            float a[4], b[4];
-            load4((const T*)e.a + at, a);
-            load4((const T*)e.b + at, b);
+            load8(e.a + at, a);
+            load8(e.b + at, b);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 const bool real = n + i < e.n;
                 float value, slope;
                 act_both(e.act, a[i], value, slope);
@@ -259,48 +235,77 @@ struct Job {
     unsigned seg_second;                 // bit s: segment s takes b2
     int segments, big;                   // the first `big` segments hold the large products
     int tiles_m, tiles_n;
-    float* partial;                      // splits > 1: [split][group][M][columns of all panels]
     Epilogue epi;
 };
 constexpr int kMaxJobs = 3;
 struct GemmArgs {
     Job job[kMaxJobs];
-    int jobs, groups, splits, total, chunk;      // total: tiles of all jobs, groups and ranges of K; chunk: of one XCD
-    int first[kMaxJobs];                         // each job's first tile
+    int jobs, groups;
+    int first[kMaxJobs];                 // each job's first tile
+    // Tiles [0, whole) are computed by a workgroup each.  The `rest` behind them would leave most of the device idle in a round of
+    // their own: their contractions are cut into `ranges`, whose sums go to `partial` ([range][tile][rows][columns]) and are
+    // joined by another launch.
+    int whole, rest, ranges;
+    float* partial;
 };
 
-template <bool A_RC, bool B_RC, Epi EPI, bool SPLIT, int BM, int BN, int THREADS>
-__global__ __launch_bounds__(THREADS, 2) void gemm_kernel(GemmArgs p) {
-    constexpr int WAVES = THREADS / 64, WN = BN / 64, WM = WAVES / WN, TM = BM / WM / 32, TN = 2;
-    constexpr int PANELS = EPI == kUp ? 2 : 1;
-    using TA = typename std::conditional<A_RC, TileRC<BM, THREADS>, TileKC<BM, THREADS>>::type;
-    using TB = typename std::conditional<B_RC, TileRC<BN / PANELS, THREADS>, TileKC<BN / PANELS, THREADS>>::type;
-    constexpr int kBytes = TA::kBytes + PANELS * TB::kBytes;
-    __shared__ __align__(1024) char buf0[kBytes];
-    __shared__ __align__(1024) char buf1[kBytes];
-
-    // the hardware deals workgroup b to XCD b % 8: each XCD takes a contiguous range of tiles, whose operands its L2 keeps
-    int tile = (int)(blockIdx.x % kXcds) * p.chunk + (int)(blockIdx.x / kXcds);
-    if ((int)(blockIdx.x / kXcds) >= p.chunk || tile >= p.total) return;
+struct TilePlace {
+    int job;
+    int64_t group, m0, n0;
+};
+__device__ __forceinline__ TilePlace place_of(const GemmArgs& p, int tile, int bm, int bn) {
     int j = 0;
     while (j + 1 < p.jobs && tile >= p.first[j + 1]) ++j;
     const Job& q = p.job[j];
     tile -= p.first[j];
     const int per_group = q.tiles_m * q.tiles_n;
-    const int range = tile / (per_group * p.groups);
-    const int64_t group = tile / per_group % p.groups;
+    TilePlace t;
+    t.job = j, t.group = tile / per_group;
     tile %= per_group;
-    constexpr int kBand = 8;                                  // tiles in bands of eight rows of tiles, down each column of the band
-    const int band = tile / (kBand * q.tiles_n), rows_here = min(kBand, q.tiles_m - band * kBand);
-    const int in_band = tile - band * kBand * q.tiles_n;
-    const int64_t m0 = (int64_t)(band * kBand + in_band % rows_here) * BM;
-    const int64_t n0 = (int64_t)(in_band / rows_here) * (BN / PANELS);
+    constexpr int kBand = 8;             // bands of eight rows of tiles, down each column of the band: what runs together shares operands
+    const int band = tile / (kBand * q.tiles_n), rows = min(kBand, q.tiles_m - band * kBand), in_band = tile - band * kBand * q.tiles_n;
+    t.m0 = (int64_t)(band * kBand + in_band % rows) * bm, t.n0 = (int64_t)(in_band / rows) * bn;
+    return t;
+}
 
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave / WN, wn = wave % WN;
+// T x T tiles: 256 with eight wavefronts of 64 x 128, 128 with four of 64 x 64.
+template <int T>
+constexpr int gemm_threads() { return T == 256 ? 512 : 256; }
+
+template <bool A_RC, bool B_RC, Epi EPI, bool SPLIT, int T>
+__global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) {
+    constexpr int THREADS = gemm_threads<T>(), TM = 2, TN = T / 64;
+    constexpr int PANELS = EPI == kUp ? 2 : 1;
+    using TA = typename std::conditional<A_RC, TileRC<T, THREADS>, TileKC<T, THREADS>>::type;
+    using TB = typename std::conditional<B_RC, TileRC<T / PANELS, THREADS>, TileKC<T / PANELS, THREADS>>::type;
+    constexpr int kBytes = TA::kBytes + PANELS * TB::kBytes;
+    static_assert(kBytes * kRing >= THREADS / 64 * 32 * TN * 32 * 4, "the results of 32 rows of every wavefront are staged in the buffers");
+    __shared__ __align__(1024) char buf0[kBytes];
+    __shared__ __align__(1024) char buf1[kBytes];
+    __shared__ __align__(1024) char buf2[kBytes];
+    __shared__ __align__(1024) char buf3[kBytes];
+
+    // the hardware deals workgroup b to XCD b % 8: each XCD takes a contiguous range of tiles, whose operands its L2 keeps
+    int tile, range = -1;
+    if ((int)blockIdx.x < p.whole) {
+        const int per = (p.whole + kXcds - 1) / kXcds, full = p.whole % kXcds == 0 ? kXcds : p.whole % kXcds, xcd = blockIdx.x % kXcds;
+        tile = xcd * per - max(0, xcd - full) + blockIdx.x / kXcds;        // the first `full` XCDs take one tile more where it does not divide
+    } else {
+        const int u = blockIdx.x - p.whole;
+        range = u / p.rest, tile = p.whole + u % p.rest;
+    }
+    const TilePlace at = place_of(p, tile, T, T / PANELS);
+    const Job& q = p.job[at.job];
+
+    const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), wm = wave / 2, wn = wave % 2;
     const TA ta(q.a_pitch);
     const TB tb(q.b_pitch);
     const int slices = (int)((q.K + kBK - 1) / kBK);
-    const int from = (int)((int64_t)slices * range / p.splits), here = (int)((int64_t)slices * (range + 1) / p.splits) - from;
+    const int from = range < 0 ? 0 : (int)((int64_t)slices * range / p.ranges);
+    const int here = (range < 0 ? slices : (int)((int64_t)slices * (range + 1) / p.ranges)) - from;
+    const uint16_t* base_a = q.a + at.group * q.a_group;
+    const uint16_t* base_b = q.b + at.group * q.b_group;
+    const uint16_t* base_b2 = q.b2 + at.group * q.b2_group;
 
     f16v acc[TM][TN];
 #pragma unroll
@@ -310,49 +315,61 @@ __global__ __launch_bounds__(THREADS, 2) void gemm_kernel(GemmArgs p) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][t][r] = 0.0f;
 
-    auto copy = [&](char* lds, int it) {
-        const int seg = it / here;
-        const int64_t k0 = (int64_t)(from + it - seg * here) * kBK;
-        const Operand a{q.a + group * q.a_group + q.seg_a[seg], q.a_pitch};
-        const bool second = (q.seg_second >> seg) & 1u;
-        const Operand b{(second ? q.b2 + group * q.b2_group : q.b + group * q.b_group) + q.seg_b[seg], q.b_pitch};
-        if constexpr (A_RC) ta.copy(lds, 0, a, q.a_inner8, q.K, m0, k0);
-        else ta.copy(lds, 0, a, q.M, q.a_inner8, m0, k0);
-        if constexpr (B_RC) tb.copy(lds, TA::kBytes, b, q.b_inner8, q.K, n0, k0);
-        else tb.copy(lds, TA::kBytes, b, q.N, q.b_inner8, n0, k0);
-        if constexpr (PANELS == 2) {
-            const Operand b2{q.b2 + group * q.b2_group + q.seg_b[seg], q.b_pitch};
-            tb.copy(lds, TA::kBytes + TB::kBytes, b2, q.b_inner8, q.K, n0, k0);
+    int seg = 0, left_slices = here;                      // of the next copy
+    int64_t k_left;
+    Cursor cur_a, cur_b, cur_b2;
+    auto enter = [&]() {                                  // the segment's first slice of this range
+        const int64_t k0 = (int64_t)from * kBK;
+        const uint16_t* a = base_a + q.seg_a[seg];
+        const uint16_t* b = (PANELS == 1 && ((q.seg_second >> seg) & 1u) ? base_b2 : base_b) + q.seg_b[seg];
+        cur_a = A_RC ? TA::cursor(a, q.a_pitch, q.a_inner8, q.K, at.m0, k0) : TA::cursor(a, q.a_pitch, q.M, q.a_inner8, at.m0, k0);
+        cur_b = B_RC ? TB::cursor(b, q.b_pitch, q.b_inner8, q.K, at.n0, k0) : TB::cursor(b, q.b_pitch, q.N, q.b_inner8, at.n0, k0);
+        if constexpr (PANELS == 2) cur_b2 = TB::cursor(base_b2 + q.seg_b[seg], q.b_pitch, q.b_inner8, q.K, at.n0, k0);
+        k_left = (A_RC ? q.K : q.a_inner8) - k0;
+    };
+    enter();
+    auto copy = [&](char* lds) {
+        ta.copy(lds, 0, cur_a, k_left);
+        tb.copy(lds, TA::kBytes, cur_b, k_left);
+        if constexpr (PANELS == 2) tb.copy(lds, TA::kBytes + TB::kBytes, cur_b2, k_left);
+        cur_a.advance(), cur_b.advance();
+        if constexpr (PANELS == 2) cur_b2.advance();
+        k_left -= kBK;
+        if (--left_slices == 0) {
+            if (++seg < q.segments) left_slices = here, enter();
+            else cur_a.left = cur_b.left = cur_b2.left = 0, cur_a.step = cur_b.step = cur_b2.step = 0;   // from here on nothing is read
         }
     };
     int part_a[TM], part_b[TN];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) part_a[i] = TA::lane_part(0, wm * (BM / WM) + 32 * i, lane);
+    for (int i = 0; i < TM; ++i) part_a[i] = TA::lane_part(0, wm * (32 * TM) + 32 * i, lane);
 #pragma unroll
-    for (int t = 0; t < TN; ++t) part_b[t] = TB::lane_part(TA::kBytes + (PANELS == 2 ? t * TB::kBytes : 0), PANELS == 2 ? wn * 32 : wn * 64 + 32 * t, lane);
-    // opaque from here on: addresses stay an array plus one offset (see the top of the file)
+    for (int t = 0; t < TN; ++t) {
+        constexpr int kPer = TN / PANELS;                 // fragments of a panel
+        part_b[t] = TB::lane_part(TA::kBytes + t / kPer * TB::kBytes, wn * (T / 2 / PANELS) + 32 * (t % kPer), lane);
+    }
+    bf16x8 fa[2][TM], fb[2][TN];
+    auto fetch = [&](const char* lds, int s) {            // step s of a slice, 0 or 1
+        // opaque: addresses stay an array plus one offset (see the top of the file), and are formed here instead of being kept
+        // for every step and buffer
 #pragma unroll
-    for (int i = 0; i < TM; ++i) asm("" : "+v"(part_a[i]));
-#pragma unroll
-    for (int t = 0; t < TN; ++t) asm("" : "+v"(part_b[t]));
-    auto multiply = [&](const char* lds) {
-        bf16x8 fa[2][TM], fb[2][TN];
-        auto fetch = [&](int s, bf16x8 (&x)[TM], bf16x8 (&y)[TN]) {
-#pragma unroll
-            for (int t = 0; t < TN; ++t) y[t] = TB::frag(lds, part_b[t], s);
-#pragma unroll
-            for (int i = 0; i < TM; ++i) x[i] = TA::frag(lds, part_a[i], s);
-        };
-        fetch(0, fa[0], fb[0]);
-#pragma unroll
-        for (int s = 0; s < kBK / 16; ++s) {
-            if (s + 1 < kBK / 16) fetch(s + 1, fa[(s + 1) & 1], fb[(s + 1) & 1]);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int t = 0; t < TN; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][t], fa[s & 1][i], acc[i][t], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);     // fragments of two steps at a time, not of the whole slice: registers
+        for (int t = 0; t < TN; ++t) {
+            int part = part_b[t];
+            asm volatile("" : "+v"(part));
+            fb[s & 1][t] = TB::frag(lds, part, s);
         }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            int part = part_a[i];
+            asm volatile("" : "+v"(part));
+            fa[s & 1][i] = TA::frag(lds, part, s);
+        }
+    };
+    auto multiply = [&](int s) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int t = 0; t < TN; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][t], fa[s & 1][i], acc[i][t], 0, 0, 0);
     };
     // fp32: the large products come first.  Where their sum is infinite the small ones, products of an infinity with a remainder
     // of zero among them, have nothing to add: such sums are kept as they are (a bit each for +inf and -inf; a NaN stays one).
@@ -369,23 +386,42 @@ __global__ __launch_bounds__(THREADS, 2) void gemm_kernel(GemmArgs p) {
                     neg[i][t] |= acc[i][t][r] == -INFINITY ? 1u << r : 0u;
                 }
     };
-    // The slice has landed, and everyone is done with the buffer that the next copy overwrites.
-    auto turn = [&]() {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // this wavefront's copies; the others' are behind the barrier
-        __syncthreads();
+    // In front of slice it + 1: this wavefront's copies of it have landed (those of the two slices behind it may be under way)
+    // and its fragments of slice `it` are in registers; behind the barrier that holds for all wavefronts, so slice it + 1 can
+    // be read and the buffer of slice `it` overwritten.  Copies past the end (windows of no bytes) keep the count the same.
+    constexpr int kPerSlice = TA::kCopies + PANELS * TB::kCopies;
+    static_assert(kPerSlice == 4 && kRing == 4, "the counts below are of four copies a slice");
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
-    if (end > 0) copy(buf0, 0);
-    for (int it = 0; it < end; it += 2) {
-        turn();
-        if (it + 1 < end) copy(buf1, it + 1);
+    auto slice = [&](char* lds, char* next, int it) {
         if (SPLIT && it == small_from) mark();
-        multiply(buf0);
-        if (it + 1 >= end) break;
-        turn();
-        if (it + 2 < end) copy(buf0, it + 2);
-        if (SPLIT && it + 1 == small_from) mark();
-        multiply(buf1);
+        fetch(lds, 1);
+        multiply(0);
+        __builtin_amdgcn_sched_barrier(0);                // fragments of two steps at a time: registers
+        __builtin_amdgcn_s_waitcnt(0x0078);               // vmcnt(8) lgkmcnt(0)
+        barrier();
+        fetch(next, 0);
+        copy(lds);
+        multiply(1);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    copy(buf0);
+    copy(buf1);
+    copy(buf2);
+    copy(buf3);
+    __builtin_amdgcn_s_waitcnt(0x0f7c);                   // vmcnt(12)
+    barrier();
+    fetch(buf0, 0);
+    for (int it = 0; it < end; it += kRing) {
+        slice(buf0, buf1, it);
+        if (it + 1 < end) slice(buf1, buf2, it + 1);
+        if (it + 2 < end) slice(buf2, buf3, it + 2);
+        if (it + 3 < end) slice(buf3, buf0, it + 3);
     }
+    __builtin_amdgcn_s_waitcnt(0x0070);                   // the copies past the end write zeros into LDS
     if constexpr (SPLIT) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -395,54 +431,71 @@ __global__ __launch_bounds__(THREADS, 2) void gemm_kernel(GemmArgs p) {
                 for (int r = 0; r < 16; ++r) acc[i][t][r] = (pos[i][t] >> r) & 1u ? INFINITY : (neg[i][t] >> r) & 1u ? -INFINITY : acc[i][t][r];
     }
 
+    // 32 rows at a time: LDS [32][TN * 32] of this wavefront, chunks of 16 bytes at place chunk ^ (row & 15)
+    __syncthreads();                                      // everyone is done with the operands
+    constexpr int kCols = TN * 32, kUnits = kCols / 8 / PANELS, kRows = 64 / kUnits;
+    const int lane_row = lane % 32, out_row = lane / kUnits, unit = lane % kUnits;
+    constexpr int kPart = THREADS / 64 / kRing;           // wavefronts that stage in one buffer
+    char* bufs[kRing] = {buf0, buf1, buf2, buf3};
+    float* stage = (float*)bufs[0] + wave % kPart * 32 * kCols;
+#pragma unroll
+    for (int i = 1; i < kRing; ++i) stage = wave / kPart == i ? (float*)bufs[i] + wave % kPart * 32 * kCols : stage;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + wm * (BM / WM) + 32 * i + lane % 32;
-        if (m >= q.M) continue;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            float v[2][4];
+        for (int t = 0; t < TN; ++t)
 #pragma unroll
-            for (int t = 0; t < TN; ++t)
+            for (int g = 0; g < 4; ++g) {
+                const int chunk = 8 * t + 2 * g + lane / 32;
+                *(f4*)(stage + lane_row * kCols + 4 * (chunk ^ (lane_row & 15))) = f4{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
+            }
+        __builtin_amdgcn_wave_barrier();                  // written and read by one wavefront: LDS keeps its order
+#pragma unroll 1
+        for (int r0 = 0; r0 < 32; r0 += kRows) {
+            const int r = r0 + out_row;
+            float v[PANELS][8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[t][e] = acc[i][t][4 * g + e];
-            const int in = 8 * g + 4 * (lane / 32);
-            if (p.splits > 1) {
-                const int64_t width = PANELS * q.epi.n8;
-                float* row = q.partial + ((range * (int64_t)p.groups + group) * q.M + m) * width;
+            for (int q2 = 0; q2 < PANELS; ++q2)
 #pragma unroll
-                for (int t = 0; t < TN; ++t) {
-                    const int64_t n = PANELS == 2 ? n0 + wn * 32 + in : n0 + wn * 64 + 32 * t + in;
-                    if (n < q.epi.n8) store4(row + (PANELS == 2 ? t * q.epi.n8 : 0) + n, v[t], 4);
+                for (int h = 0; h < 2; ++h) {
+                    const int chunk = q2 * (kCols / 4 / PANELS) + 2 * unit + h;
+                    const f4 w = *(const f4*)(stage + r * kCols + 4 * (chunk ^ (r & 15)));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[q2][4 * h + e] = w[e];
                 }
-            } else if constexpr (PANELS == 2) {
-                emit<EPI, SPLIT>(q.epi, group, m, n0 + wn * 32 + in, v[0], v[1]);
-            } else {
+            const int row = wm * (32 * TM) + 32 * i + r, col = wn * (T / 2 / PANELS) + 8 * unit;
+            if (range >= 0) {
+                float* out = p.partial + ((int64_t)range * p.rest + (tile - p.whole)) * (T * T) + (int64_t)row * T + col;
 #pragma unroll
-                for (int t = 0; t < TN; ++t) emit<EPI, SPLIT>(q.epi, group, m, n0 + wn * 64 + 32 * t + in, v[t], v[t]);
+                for (int q2 = 0; q2 < PANELS; ++q2) store8(out + q2 * (T / PANELS), v[q2]);
+            } else if (at.m0 + row < q.M) {
+                emit<EPI, SPLIT>(q.epi, at.group, at.m0 + row, at.n0 + col, v[0], v[PANELS - 1]);
             }
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
-// Adds up the ranges of K, in order, and does the epilogue's work.
-template <Epi EPI, bool SPLIT>
-__global__ __launch_bounds__(256) void join_kernel(Epilogue e, const float* partial, int64_t rows, int groups, int splits) {
-    constexpr int PANELS = EPI == kUp ? 2 : 1;
-    const int64_t quads = e.n8 / 4, width = PANELS * e.n8, stride = (int64_t)groups * rows * width;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= groups * rows * quads) return;
-    const int64_t n = i % quads * 4, row = i / quads;
-    float v[2][4] = {};
-    for (int s = 0; s < splits; ++s)
+// Adds up the ranges of the tiles whose contraction was cut, in order, and does the epilogue's work.
+template <Epi EPI, bool SPLIT, int T>
+__global__ __launch_bounds__(256) void join_kernel(GemmArgs p) {
+    constexpr int PANELS = EPI == kUp ? 2 : 1, kUnits = T / PANELS / 8;
+    const TilePlace at = place_of(p, p.whole + blockIdx.x, T, T / PANELS);
+    const Job& q = p.job[at.job];
+    const int i = blockIdx.y * 256 + threadIdx.x, row = i / kUnits, col = i % kUnits * 8;
+    if (at.m0 + row >= q.M || at.n0 + col >= q.epi.n8) return;
+    float v[PANELS][8] = {};
+    const float* in = p.partial + (int64_t)blockIdx.x * (T * T) + (int64_t)row * T + col;
+#pragma unroll 4
+    for (int s = 0; s < p.ranges; ++s)
 #pragma unroll
-        for (int t = 0; t < PANELS; ++t) {
-            float x[4];
-            load4(partial + s * stride + row * width + t * e.n8 + n, x);
+        for (int q2 = 0; q2 < PANELS; ++q2) {
+            float x[8];
+            load8(in + (int64_t)s * p.rest * (T * T) + q2 * (T / PANELS), x);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[t][k] += x[k];
+            for (int e = 0; e < 8; ++e) v[q2][e] += x[e];
         }
-    emit<EPI, SPLIT>(e, row / rows, row % rows, n, v[0], v[PANELS - 1]);
+    emit<EPI, SPLIT>(q.epi, at.group, at.m0 + row, at.n0 + col, v[0], v[PANELS - 1]);
 }
 
 }  // namespace ffn

@@ -27,8 +27,8 @@ constexpr int kFewSlab = 1024;       // contraction indices whose inputs lie in 
 
 struct PackParams {
     const void* src;
-    int64_t row, group, rows, cols, cols8;
-    uint16_t* dst;                   // [group][plane][rows][cols8]
+    int64_t row, group, rows, cols, cols8, pitch;
+    uint16_t* dst;                   // [group][plane][rows][pitch]
 };
 
 template <typename T, bool SPLIT>
@@ -39,12 +39,12 @@ __global__ __launch_bounds__(256) void pack_kernel(PackParams p) {
     float v[8];
     load_upto8((const T*)p.src + g * p.group + r * p.row + c, (int)min((int64_t)8, p.cols - c), 0.0f, v);
     constexpr int P = SPLIT ? 3 : 1;
-    uint16_t* out = p.dst + (g * P * p.rows + r) * p.cols8 + c;
+    uint16_t* out = p.dst + (g * P * p.rows + r) * p.pitch + c;
     if constexpr (SPLIT) {
         const Split8 s = split8(f4{v[0], v[1], v[2], v[3]}, f4{v[4], v[5], v[6], v[7]});
         *(u4*)out = s.hi;
-        *(u4*)(out + p.rows * p.cols8) = s.mid;
-        *(u4*)(out + 2 * p.rows * p.cols8) = s.lo;
+        *(u4*)(out + p.rows * p.pitch) = s.mid;
+        *(u4*)(out + 2 * p.rows * p.pitch) = s.lo;
     } else {
         store8(out, v);
     }
@@ -150,6 +150,11 @@ int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
+// Elements between the rows of internal tensors.  Rows of 5632 elements side by side put what the tiles read at one time on a
+// few channels of the L2 (the product for dx, 8192 x 2048 over twice 5632: 909 TFLOP/s; with 64 / 192 elements between the rows
+// 1079 / 1137, with 128 to 1024 about the latter).
+int64_t internal_pitch(int64_t n) { return n < 1024 ? up8(n) : (n + 63) / 64 * 64 + 192; }
+
 struct Arena {
     char* base;
     int64_t at = 0;
@@ -181,17 +186,17 @@ struct Maker {                         // lays operands out; without a stream it
 
     View operand(const ols_matrix& m, int dtype, int64_t outer, int64_t inner, bool may_lie) {
         View v;
-        v.inner8 = up8(inner);
+        v.inner8 = up8(inner), v.pitch = internal_pitch(inner);
         if (may_lie && !split() && lies_well(m, dtype, inner)) {
             v.p = (const uint16_t*)m.dev, v.pitch = m.row, v.group = m.group;
             return v;
         }
-        const int64_t per = outer * v.inner8;
+        const int64_t per = outer * v.pitch;
         const int groups = m.group == 0 ? 1 : f.groups;      // shared by the workers: laid out once
         uint16_t* dst = (uint16_t*)ws.take(2 * per * planes() * groups);
-        v.p = dst, v.pitch = v.inner8, v.plane = per, v.group = groups == 1 ? 0 : per * planes();
+        v.p = dst, v.plane = per, v.group = groups == 1 ? 0 : per * planes();
         if (go && err == hipSuccess) {
-            const PackParams p{m.dev, m.row, m.group, outer, inner, v.inner8, dst};
+            const PackParams p{m.dev, m.row, m.group, outer, inner, v.inner8, v.pitch, dst};
             const dim3 grid((unsigned)((outer * (v.inner8 / 8) + 255) / 256), groups);
             if (split()) pack_kernel<float, true><<<grid, 256, 0, stream>>>(p);
             else if (dtype == OLS_F32) pack_kernel<float, false><<<grid, 256, 0, stream>>>(p);
@@ -206,10 +211,10 @@ struct Maker {                         // lays operands out; without a stream it
     }
     View internal(int64_t rows, int64_t inner, void* at) const {
         View v;
-        v.inner8 = v.pitch = up8(inner), v.plane = rows * v.inner8, v.group = planes() * v.plane, v.p = (const uint16_t*)at;
+        v.inner8 = up8(inner), v.pitch = internal_pitch(inner), v.plane = rows * v.pitch, v.group = planes() * v.plane, v.p = (const uint16_t*)at;
         return v;
     }
-    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * planes() * f.groups * rows * up8(inner); }
+    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * planes() * f.groups * rows * internal_pitch(inner); }
 };
 
 // the planes' products, largest first
@@ -231,23 +236,37 @@ void set_segments(Job& j, const View& a, const View& b, const View* a2, const Vi
     if (b2) j.b2 = b2->p, j.b2_group = b2->group;
 }
 
+constexpr int kCus = 256;
+
 struct Shape {
-    int bm;                 // 256 or 128 rows and columns of a tile (columns: of both panels together)
-    int splits;
+    int t;                             // rows and columns of a tile (columns: of both panels together)
+    int whole, rest, ranges;
 };
 
-// Large tiles where they fill the device; otherwise small ones, whose contraction is cut into ranges until about two
-// workgroups a compute unit run or a range is down to four slices.
+int64_t count_tiles(const Job* jobs, int n, int groups, int panels, int t) {
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) tiles += groups * tiles_of(jobs[i].M, t) * tiles_of(jobs[i].N, t / panels);
+    return tiles;
+}
+
+// Tiles that fill whole rounds of the device are computed whole; the contractions of the rest are cut until they fill one
+// more round (or a range is down to four slices).
+Shape rounds(int t, int64_t tiles, int64_t slices) {
+    const int64_t slots = t == 256 ? kCus : 2 * kCus;     // workgroups that run together: a small one takes half the LDS
+    Shape s{t, (int)(tiles / slots * slots), 0, 1};
+    s.rest = (int)(tiles - s.whole);
+    if (s.rest) s.ranges = (int)std::max((int64_t)1, std::min(slots / s.rest, slices / 8));
+    if (s.ranges == 1) s.whole += s.rest, s.rest = 0;
+    return s;
+}
+
 Shape choose(const Job* jobs, int n, int groups, int panels, bool split) {
-    int64_t big = 0, small = 0, slices = 1 << 30;
-    for (int i = 0; i < n; ++i) {
-        big += groups * tiles_of(jobs[i].M, 256) * tiles_of(jobs[i].N, 256 / panels);
-        small += groups * tiles_of(jobs[i].M, 128) * tiles_of(jobs[i].N, 128 / panels);
-        slices = std::min(slices, tiles_of(jobs[i].K, kBK));
-    }
-    if (big >= 160 && !split) return {256, 1};
-    const int64_t splits = std::max((int64_t)1, std::min(std::min((int64_t)16, 512 / std::max(small, (int64_t)1)), slices / 4));
-    return {128, (int)splits};
+    int64_t slices = (int64_t)1 << 40;             // of a segment, which is what is cut
+    for (int i = 0; i < n; ++i) slices = std::min(slices, tiles_of(jobs[i].K, kBK));
+    const int64_t big = count_tiles(jobs, n, groups, panels, 256), small = count_tiles(jobs, n, groups, panels, 128);
+    const Shape s = rounds(256, big, slices);
+    if (!split && s.whole + (int64_t)s.rest * s.ranges >= 160) return s;
+    return rounds(128, small, slices);
 }
 
 template <bool A_RC, bool B_RC, Epi EPI>
@@ -255,33 +274,50 @@ hipError_t product(Job* jobs, int n, int groups, bool split, Arena& ws, bool go,
     constexpr int PANELS = EPI == kUp ? 2 : 1;
     if (n == 0) return hipSuccess;
     const Shape shape = choose(jobs, n, groups, PANELS, split);
+    const int t = shape.t;
+    if (count_tiles(jobs, n, groups, PANELS, t) > 0x0fffffff) return hipErrorInvalidValue;
     GemmArgs p = {};
-    p.jobs = n, p.groups = groups, p.splits = shape.splits;
-    int64_t total = 0;
+    p.jobs = n, p.groups = groups, p.whole = shape.whole, p.rest = shape.rest, p.ranges = shape.ranges;
+    int first = 0;
     for (int i = 0; i < n; ++i) {
         Job& j = p.job[i];
         j = jobs[i];
-        j.tiles_m = (int)tiles_of(j.M, shape.bm), j.tiles_n = (int)tiles_of(j.N, shape.bm / PANELS);
-        p.first[i] = (int)total;
-        total += (int64_t)j.tiles_m * j.tiles_n * groups * shape.splits;
-        if (shape.splits > 1) j.partial = (float*)ws.take(4 * shape.splits * groups * j.M * PANELS * j.epi.n8);
+        j.tiles_m = (int)tiles_of(j.M, t), j.tiles_n = (int)tiles_of(j.N, t / PANELS);
+        p.first[i] = first;
+        first += j.tiles_m * j.tiles_n * groups;
     }
+    const bool joins = shape.rest > 0;
+    if (joins) p.partial = (float*)ws.take((int64_t)4 * shape.rest * shape.ranges * t * t);
     if (!go) return hipSuccess;
-    if (total > 0x3fffffff) return hipErrorInvalidValue;
-    p.total = (int)total, p.chunk = (int)((total + kXcds - 1) / kXcds);
-    const int blocks = p.chunk * kXcds;
-    if (split) gemm_kernel<A_RC, B_RC, EPI, true, 128, 128, 256><<<blocks, 256, 0, stream>>>(p);
-    else if (shape.bm == 256) gemm_kernel<A_RC, B_RC, EPI, false, 256, 256, 512><<<blocks, 512, 0, stream>>>(p);
-    else gemm_kernel<A_RC, B_RC, EPI, false, 128, 128, 256><<<blocks, 256, 0, stream>>>(p);
-    hipError_t e = hipGetLastError();
-    for (int i = 0; i < n && shape.splits > 1 && e == hipSuccess; ++i) {
-        const Job& j = p.job[i];
-        const unsigned joins = (unsigned)((groups * j.M * (j.epi.n8 / 4) + 255) / 256);
-        if (split) join_kernel<EPI, true><<<joins, 256, 0, stream>>>(j.epi, j.partial, j.M, groups, shape.splits);
-        else join_kernel<EPI, false><<<joins, 256, 0, stream>>>(j.epi, j.partial, j.M, groups, shape.splits);
-        e = hipGetLastError();
+    const unsigned blocks = shape.whole + shape.rest * shape.ranges;
+    const dim3 join_grid(shape.rest, (unsigned)(t * (t / PANELS / 8) / 256));
+    if (split) {
+        gemm_kernel<A_RC, B_RC, EPI, true, 128><<<blocks, 256, 0, stream>>>(p);
+        if (joins) join_kernel<EPI, true, 128><<<join_grid, 256, 0, stream>>>(p);
+    } else if (t == 256) {
+        gemm_kernel<A_RC, B_RC, EPI, false, 256><<<blocks, 512, 0, stream>>>(p);
+        if (joins) join_kernel<EPI, false, 256><<<join_grid, 256, 0, stream>>>(p);
+    } else {
+        gemm_kernel<A_RC, B_RC, EPI, false, 128><<<blocks, 256, 0, stream>>>(p);
+        if (joins) join_kernel<EPI, false, 128><<<join_grid, 256, 0, stream>>>(p);
     }
-    return e;
+    return hipGetLastError();
+}
+
+// Adds up the ranges of the kernels for few rows.
+__global__ __launch_bounds__(256) void few_join_kernel(Epilogue e, const float* partial, int64_t rows, int groups, int ranges) {
+    const int64_t units = e.n8 / 8, stride = (int64_t)groups * rows * e.n8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= groups * rows * units) return;
+    const int64_t n = i % units * 8, row = i / units;
+    float v[8] = {};
+#pragma unroll 4
+    for (int s = 0; s < ranges; ++s) {
+        float x[8];
+        load8(partial + s * stride + row * e.n8 + n, x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += x[k];
+    }
+    emit<kStore, false>(e, row / rows, row % rows, n, v, v);
 }
 
 Epilogue store_to(const ols_matrix& m, int64_t n, int dtype) {
@@ -295,10 +331,10 @@ struct Saved {
     int64_t off_a, off_b, off_h, bytes;
 };
 Saved saved_layout(const ols_ffn& f) {
-    const int64_t elems = f.groups * f.rows * up8(f.hidden);
+    const int64_t elems = f.groups * f.rows * internal_pitch(f.hidden);
     Saved s;
     s.off_a = 0;
-    s.off_b = up256(elems * (f.dtype == OLS_F32 ? 4 : 2));
+    s.off_b = up256(elems * 4);
     s.off_h = 2 * s.off_b;
     s.bytes = up256(s.off_h + elems * 2 * (f.dtype == OLS_F32 ? 3 : 1));
     return s;
@@ -346,7 +382,7 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         few<true>(p, f, stream);
         few<false>(d, f, stream);
         const Epilogue e = store_to(f.y, f.out, f.dtype);
-        join_kernel<kStore, false><<<(unsigned)((f.groups * f.rows * (d.n8 / 4) + 255) / 256), 256, 0, stream>>>(e, d.partial, f.rows, f.groups, d.ranges);
+        few_join_kernel<<<(unsigned)((f.groups * f.rows * (d.n8 / 8) + 255) / 256), 256, 0, stream>>>(e, d.partial, f.rows, f.groups, d.ranges);
         return hipGetLastError();
     }
     Maker mk{f, ws, stream, go};
@@ -363,8 +399,8 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
     Job up = {};
     up.M = f.rows, up.N = f.hidden, up.K = f.width;
     set_segments(up, x, wg, nullptr, &wu, mk.split());
-    up.epi.n = f.hidden, up.epi.n8 = h8, up.epi.m = f.rows, up.epi.act = f.act;
-    up.epi.a = saved ? saved + s.off_a : nullptr, up.epi.b = saved ? saved + s.off_b : nullptr, up.epi.h = (uint16_t*)hp;
+    up.epi.n = f.hidden, up.epi.n8 = h8, up.epi.pitch = internal_pitch(f.hidden), up.epi.m = f.rows, up.epi.act = f.act;
+    up.epi.a = saved ? (float*)(saved + s.off_a) : nullptr, up.epi.b = saved ? (float*)(saved + s.off_b) : nullptr, up.epi.h = (uint16_t*)hp;
     hipError_t e = product<false, true, kUp>(&up, 1, f.groups, mk.split(), ws, go, stream);
     if (e != hipSuccess) return e;
     Job down = {};
@@ -422,8 +458,8 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         Job dh = {};
         dh.M = f.rows, dh.N = f.hidden, dh.K = f.out;
         set_segments(dh, dy, wd, nullptr, nullptr, mk.split());
-        dh.epi.n = f.hidden, dh.epi.n8 = h8, dh.epi.m = f.rows, dh.epi.act = f.act;
-        dh.epi.a = saved + s.off_a, dh.epi.b = saved + s.off_b, dh.epi.h = (uint16_t*)pa, dh.epi.h2 = (uint16_t*)pb;
+        dh.epi.n = f.hidden, dh.epi.n8 = h8, dh.epi.pitch = internal_pitch(f.hidden), dh.epi.m = f.rows, dh.epi.act = f.act;
+        dh.epi.a = (float*)(saved + s.off_a), dh.epi.b = (float*)(saved + s.off_b), dh.epi.h = (uint16_t*)pa, dh.epi.h2 = (uint16_t*)pb;
         e = product<false, false, kGateGrad>(&dh, 1, f.groups, mk.split(), ws, go, stream);
         if (e != hipSuccess) return e;
     }
