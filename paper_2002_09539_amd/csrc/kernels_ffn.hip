@@ -239,8 +239,8 @@ void set_segments(Job& j, const View& a, const View& b, const View* a2, const Vi
 constexpr int kCus = 256;
 
 struct Shape {
-    int t;                             // rows and columns of a tile (columns: of both panels together)
-    int whole, rest, ranges;
+    int t = 0;                         // rows and columns of a tile (columns: of both panels together)
+    int whole = 0, rest = 0, ranges = 1;
 };
 
 int64_t count_tiles(const Job* jobs, int n, int groups, int panels, int t) {
@@ -249,24 +249,50 @@ int64_t count_tiles(const Job* jobs, int n, int groups, int panels, int t) {
     return tiles;
 }
 
-// Tiles that fill whole rounds of the device are computed whole; the contractions of the rest are cut until they fill one
-// more round (or a range is down to four slices).
-Shape rounds(int t, int64_t tiles, int64_t slices) {
-    const int64_t slots = t == 256 ? kCus : 2 * kCus;     // workgroups that run together: a small one takes half the LDS
-    Shape s{t, (int)(tiles / slots * slots), 0, 1};
-    s.rest = (int)(tiles - s.whole);
-    if (s.rest) s.ranges = (int)std::max((int64_t)1, std::min(slots / s.rest, slices / 8));
-    if (s.ranges == 1) s.whole += s.rest, s.rest = 0;
-    return s;
+// What a product takes, in microseconds, by tile, and by how the tiles of the last round are cut.  Fitted to products of 32 to 8192
+// rows and 256 to 5632 columns over 300 to 8192 indices (within 15 % of most).  A slice of 32 indices takes a workgroup 0.3 us where
+// few run, 0.4 with one on every compute unit and 0.6 with two (tiles of 128); 0.75 to 0.95 with one tile of 256.  Examples,
+// 2048 x 1024 over 2816: tiles of 128 whole 40.4 us, cut in 2 / 4 / 8: 31.7 / 32.3 / 45.3; of 256, 74.6 whole, cut in 4 / 8: 38.6 / 40.2.
+// 2048 x 5632 over 1024: tiles of 128 39.0, of 256 36.2.  64 x 1024 over 4096: tiles of 128 whole 41.4, cut in 16: 12.8.
+double estimate(const Shape& s, int64_t slices) {
+    const int64_t slots = s.t == 256 ? kCus : 2 * kCus;
+    auto slice_us = [&](double blocks) {
+        const double one = std::min(1.0, blocks / kCus), two = std::min(1.0, std::max(0.0, blocks / kCus - 1.0));
+        return s.t == 256 ? 0.75 + 0.2 * one : 0.3 + 0.1 * one + 0.2 * two;
+    };
+    const double ends = s.t == 256 ? 8.0 : 4.0;
+    double us = 0.0;
+    if (s.whole) us += (double)((s.whole + slots - 1) / slots) * (slices * slice_us((double)std::min((int64_t)s.whole, slots)) + ends);
+    if (s.rest) {
+        const double blocks = (double)s.rest * s.ranges;
+        us += ((double)slices / s.ranges + 0.5) * slice_us(blocks) + ends + 5.0 + blocks * s.t * s.t * 4.0 / 8e6;
+    }
+    return us;
 }
 
+// The tile, and whether the contractions of the tiles that fill no whole round are cut.
 Shape choose(const Job* jobs, int n, int groups, int panels, bool split) {
-    int64_t slices = (int64_t)1 << 40;             // of a segment, which is what is cut
-    for (int i = 0; i < n; ++i) slices = std::min(slices, tiles_of(jobs[i].K, kBK));
-    const int64_t big = count_tiles(jobs, n, groups, panels, 256), small = count_tiles(jobs, n, groups, panels, 128);
-    const Shape s = rounds(256, big, slices);
-    if (!split && s.whole + (int64_t)s.rest * s.ranges >= 160) return s;
-    return rounds(128, small, slices);
+    int64_t slices = (int64_t)1 << 40, work = 1;
+    for (int i = 0; i < n; ++i) {
+        slices = std::min(slices, tiles_of(jobs[i].K, kBK));
+        work = std::max(work, tiles_of(jobs[i].K, kBK) * jobs[i].segments);
+    }
+    Shape best{};
+    double best_us = 1e300;
+    for (int t = 128; t <= (split ? 128 : 256); t += 128) {          // three planes of every operand leave no registers for large tiles
+        const int64_t slots = t == 256 ? kCus : 2 * kCus, tiles = count_tiles(jobs, n, groups, panels, t);
+        if (tiles > 0x0fffffff) continue;
+        for (int ranges : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            Shape s{t, (int)tiles, 0, 1};
+            if (ranges > 1) {
+                s.whole = (int)(tiles / slots * slots), s.rest = (int)(tiles - s.whole), s.ranges = ranges;
+                if (s.rest == 0 || slices / ranges < 4 || (int64_t)s.rest * ranges > slots) continue;
+            }
+            const double us = estimate(s, work);
+            if (us < best_us) best = s, best_us = us;
+        }
+    }
+    return best;
 }
 
 template <bool A_RC, bool B_RC, Epi EPI>
@@ -275,7 +301,7 @@ hipError_t product(Job* jobs, int n, int groups, bool split, Arena& ws, bool go,
     if (n == 0) return hipSuccess;
     const Shape shape = choose(jobs, n, groups, PANELS, split);
     const int t = shape.t;
-    if (count_tiles(jobs, n, groups, PANELS, t) > 0x0fffffff) return hipErrorInvalidValue;
+    if (t == 0) return hipErrorInvalidValue;              // more tiles than a launch numbers
     GemmArgs p = {};
     p.jobs = n, p.groups = groups, p.whole = shape.whole, p.rest = shape.rest, p.ranges = shape.ranges;
     int first = 0;
