@@ -12,11 +12,12 @@
 //   1. radix sort of (id, position), 9 bits a pass: per-workgroup digit counts, then a stable scatter in which every
 //      wavefront ranks 64 ids at a time by matching ballots.  Up to kSortItems ids per worker take one workgroup and
 //      one launch for all passes.
-//   2. the sorted list is cut into runs of kRun positions; a run that lies inside ONE id is added up by a wavefront of its
-//      own into a partial row (an id that makes up 6 % of 32 768 tokens is a sum of 2 000 rows, which one wavefront alone
-//      would take 100 us to follow).
-//   3. a wavefront per table row finds its segment by bisection and writes scale * (rows before the first whole run, the
-//      whole runs' partials, rows after the last), or zeros.  Every row of the table is written once, so no fill precedes.
+//   2. the sorted list is cut into runs of kRun positions, a wavefront each, so that the work does not depend on how often
+//      an id occurs.  A sum that lies inside a run is a row of the gradient; one that reaches over its end goes to a partial
+//      row.  (With a wavefront per table row, the row of an id that makes up 6 % of 32 768 tokens took longer than all
+//      the others together: 288 us instead of 60.)
+//   3. a wavefront per table row adds up the partial rows of an id that several runs hold, and writes zeros for an id that
+//      does not occur.  Every row of the table is written once.
 #include "element_io.h"
 #include "ols_internal.h"
 
@@ -30,8 +31,9 @@ constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortItems = 4096;            // ids of one workgroup of the sort
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr int kRun = 64;                    // sorted positions of a partial row
-constexpr int kRowsPerBlock = 16;           // table rows of a workgroup of the last stage: four per wavefront
+constexpr int kPerWave = kSortItems / kSortWaves, kPerLane = kPerWave / 64;
+constexpr int kRun = 32;                    // sorted positions of a run
+constexpr int kRowsPerBlock = 32;           // table rows of a workgroup of the last stage: eight per wavefront
 
 template <typename TI, typename TO>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedParams p, int lanes) {
@@ -64,10 +66,20 @@ struct SortParams {
     int32_t* keys_out;
     int32_t* pos_out;
     int32_t* counts;             // [group][block][kDigits]
+    int32_t* bounds;             // [group][2][vocab]: cleared by the first launch, see RowsParams
     int64_t n;                   // ids per group
     int blocks, shift;
     int64_t vocab;
 };
+
+// Workgroups behind those of the sort clear the table of bounds.
+constexpr int kClearInts = 16384;           // of one workgroup
+__device__ __forceinline__ bool cleared(const SortParams& p, int group, int block) {
+    if (block < 0) return false;
+    const int64_t n = 2 * p.vocab, from = (int64_t)block * kClearInts, to = min(n, from + kClearInts);
+    for (int64_t i = from + threadIdx.x; i < to; i += kSortThreads) p.bounds[group * n + i] = 0;
+    return true;
+}
 
 __device__ __forceinline__ int key_at(const SortParams& p, int group, int64_t i, bool first) {
     if (!first) return p.keys_in[(int64_t)group * p.n + i];
@@ -87,20 +99,39 @@ __device__ __forceinline__ unsigned long long same_digit(int digit, bool valid) 
     return m;
 }
 
+// The items of a lane: kPerLane of its wavefront's, 64 apart, loaded together.
+struct Items {
+    int key[kPerLane], pos[kPerLane];
+    bool valid[kPerLane];
+};
+__device__ __forceinline__ Items load_items(const SortParams& p, int group, int block, bool first, bool with_pos) {
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const int64_t base = (int64_t)block * kSortItems + wave * kPerWave + lane;
+    Items t;
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+        const int64_t i = base + 64 * k;
+        t.valid[k] = i < p.n;
+        t.key[k] = t.valid[k] ? key_at(p, group, i, first) : 0;
+        t.pos[k] = with_pos && t.valid[k] ? (first ? (int)i : p.pos_in[(int64_t)group * p.n + i]) : 0;
+    }
+    return t;
+}
+
 // One stable pass over the items of one workgroup: item i goes behind every item of a smaller digit and every earlier
 // item of its own.  `before[d]`: how many items of all workgroups precede this workgroup's first one of digit d.
-__device__ void scatter_block(const SortParams& p, int group, int block, bool first, int (*cnt)[kDigits], const int* before) {
+__device__ void scatter_block(const SortParams& p, int group, const Items& t, int (*cnt)[kDigits], const int* before) {
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    constexpr int kPerWave = kSortItems / kSortWaves;
-    const int64_t base = (int64_t)block * kSortItems + wave * kPerWave;
+    unsigned long long same[kPerLane];
+    int digit[kPerLane];
     for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) (&cnt[0][0])[i] = 0;
     __syncthreads();
-    for (int k = 0; k < kPerWave; k += 64) {
-        const int64_t i = base + k + lane;
-        const bool valid = i < p.n;
-        const int digit = valid ? (key_at(p, group, i, first) >> p.shift) & (kDigits - 1) : 0;
-        const unsigned long long same = same_digit(digit, valid);
-        if (valid && (same & ((1ull << lane) - 1)) == 0) cnt[wave][digit] += __popcll(same);
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+        digit[k] = (t.key[k] >> p.shift) & (kDigits - 1);
+        same[k] = same_digit(digit[k], t.valid[k]);
+        if (t.valid[k] && (same[k] & ((1ull << lane) - 1)) == 0) cnt[wave][digit[k]] += __popcll(same[k]);
+        __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
     for (int d = threadIdx.x; d < kDigits; d += kSortThreads) {
@@ -112,21 +143,17 @@ __device__ void scatter_block(const SortParams& p, int group, int block, bool fi
         }
     }
     __syncthreads();
-    for (int k = 0; k < kPerWave; k += 64) {
-        const int64_t i = base + k + lane;
-        const bool valid = i < p.n;
-        const int key = valid ? key_at(p, group, i, first) : 0;
-        const int digit = (key >> p.shift) & (kDigits - 1);
-        const unsigned long long same = same_digit(digit, valid);
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        if (valid) {
-            const int64_t at = (int64_t)group * p.n + cnt[wave][digit] + rank;
-            p.keys_out[at] = key;
-            p.pos_out[at] = first ? (int)i : p.pos_in[(int64_t)group * p.n + i];
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+        const int rank = __popcll(same[k] & ((1ull << lane) - 1));
+        if (t.valid[k]) {
+            const int64_t at = (int64_t)group * p.n + cnt[wave][digit[k]] + rank;
+            p.keys_out[at] = t.key[k];
+            p.pos_out[at] = t.pos[k];
         }
         // every lane has read the counter before the first of its digit moves it on (one wavefront, in step)
         __builtin_amdgcn_wave_barrier();
-        if (valid && rank == 0) cnt[wave][digit] += __popcll(same);
+        if (t.valid[k] && rank == 0) cnt[wave][digit[k]] += __popcll(same[k]);
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
@@ -154,13 +181,12 @@ __device__ void scan_digits(int* total) {
     __syncthreads();
 }
 
-__device__ void count_block(const SortParams& p, int group, int block, bool first, int* hist) {
+__device__ void count_block(const SortParams& p, const Items& t, int* hist) {
     for (int d = threadIdx.x; d < kDigits; d += kSortThreads) hist[d] = 0;
     __syncthreads();
-    for (int k = threadIdx.x; k < kSortItems; k += kSortThreads) {
-        const int64_t i = (int64_t)block * kSortItems + k;
-        if (i < p.n) atomicAdd(&hist[(key_at(p, group, i, first) >> p.shift) & (kDigits - 1)], 1);
-    }
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k)
+        if (t.valid[k]) atomicAdd(&hist[(t.key[k] >> p.shift) & (kDigits - 1)], 1);
     __syncthreads();
 }
 
@@ -169,6 +195,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_one_block_kernel(SortParams
                                                                       int32_t* pos_b, int passes) {
     __shared__ int cnt[kSortWaves][kDigits];
     __shared__ int before[kDigits];
+    if (cleared(p, blockIdx.y, (int)blockIdx.x - 1)) return;
     for (int pass = 0; pass < passes; ++pass) {
         const bool to_a = (passes - 1 - pass) % 2 == 0;   // the last pass ends in a
         p.keys_out = to_a ? keys_a : keys_b;
@@ -176,9 +203,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_one_block_kernel(SortParams
         p.keys_in = to_a ? keys_b : keys_a;
         p.pos_in = to_a ? pos_b : pos_a;
         p.shift = pass * kDigitBits;
-        count_block(p, blockIdx.x, 0, pass == 0, before);
+        const Items t = load_items(p, blockIdx.y, 0, pass == 0, true);
+        count_block(p, t, before);
         scan_digits(before);
-        scatter_block(p, blockIdx.x, 0, pass == 0, cnt, before);
+        scatter_block(p, blockIdx.y, t, cnt, before);
         __threadfence_block();
         __syncthreads();
     }
@@ -186,7 +214,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_one_block_kernel(SortParams
 
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortParams p, int first) {
     __shared__ int hist[kDigits];
-    count_block(p, blockIdx.y, blockIdx.x, first, hist);
+    if (cleared(p, blockIdx.y, (int)blockIdx.x - p.blocks)) return;
+    count_block(p, load_items(p, blockIdx.y, blockIdx.x, first, false), hist);
     int32_t* out = p.counts + ((int64_t)blockIdx.y * p.blocks + blockIdx.x) * kDigits;
     for (int d = threadIdx.x; d < kDigits; d += kSortThreads) out[d] = hist[d];
 }
@@ -199,9 +228,11 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortParams p
     static_assert(kSortThreads == 2 * kDigits, "two lanes add up a digit's counts");
     const int32_t* counts = p.counts + (int64_t)blockIdx.y * p.blocks * kDigits;
     const int d = threadIdx.x % kDigits, half = threadIdx.x / kDigits, me = blockIdx.x;
+    const Items t = load_items(p, blockIdx.y, blockIdx.x, first, true);
     if (half == 0) before[d] = 0, total[d] = 0;
     __syncthreads();
     int less = 0, all = 0;
+#pragma unroll 4
     for (int b = half; b < p.blocks; b += 2) {
         const int c = counts[(int64_t)b * kDigits + d];
         all += c;
@@ -213,7 +244,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortParams p
     scan_digits(total);
     if (half == 0) before[d] += total[d];
     __syncthreads();
-    scatter_block(p, blockIdx.y, blockIdx.x, first, cnt, before);
+    scatter_block(p, blockIdx.y, t, cnt, before);
 }
 
 // ---- sums over sorted positions -----------------------------------------------------------------------------------------
@@ -222,149 +253,191 @@ struct RowsParams {
     EmbedGradParams g;
     const int32_t* keys;
     const int32_t* pos;
-    float* partial;      // [group][runs][width]
+    int32_t* bounds;     // [group][2][vocab]: an id's first sorted position and one behind its last; 0, 0 where there is none
+    float* partial;      // [group][run][2][width]: the sum that the run begins in the middle of, and the one that it ends in the middle of
     int64_t runs;
 };
 
-// Adds rows pos[from .. to) of dout, columns c + 512 t + 8 lane .., in that order.  The positions are loaded 64 at a time
-// and handed round; four rows' loads are in flight together.
-template <typename TI, int NV>
-__device__ __forceinline__ void add_rows(const RowsParams& q, int64_t group, int64_t from, int64_t to, int64_t c, int lane, float (&sum)[NV][8]) {
-    const int32_t* pos = q.pos + group * q.g.tokens;
-    const TI* base = (const TI*)q.g.dout + group * q.g.dout_group;
-    for (int64_t i0 = from; i0 < to; i0 += 64) {
-        const int have = (int)min((int64_t)64, to - i0);
-        const int mine = lane < have ? pos[i0 + lane] : 0;
-        for (int k = 0; k < have; k += 4) {
-            float v[4][NV][8];
+// Eight elements as they lie in memory, so that several rows' loads can be in flight in few registers.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<uint16_t> {
+    static constexpr int kBatch = 8;
+    u4 a;
+    __device__ void load(const uint16_t* p, int left) {
+        if (left >= 8) {
+            a = *(const u4any*)p;
+        } else {
+            float v[8];
+            load_upto8(p, left, 0.0f, v);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t row = __shfl(mine, min(k + r, have - 1));
-#pragma unroll
-                for (int t = 0; t < NV; ++t) {
-                    const int64_t at = c + 512 * t + 8 * lane;
-                    load_upto8(base + row * q.g.dout_row + at, k + r < have ? (int)max((int64_t)0, min((int64_t)8, q.g.width - at)) : 0, 0.0f, v[r][t]);
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (k + r < have) {
-#pragma unroll
-                    for (int t = 0; t < NV; ++t)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sum[t][e] += v[r][t][e];
-                }
+            for (int e = 0; e < 4; ++e) a[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
         }
     }
-}
+    __device__ float get(int e) const { return e % 2 ? bf16_hi(a[e / 2]) : bf16_lo(a[e / 2]); }
+};
+template <>
+struct Raw8<float> {
+    static constexpr int kBatch = 4;
+    float v[8];
+    __device__ void load(const float* p, int left) { load_upto8(p, left, 0.0f, v); }
+    __device__ float get(int e) const { return v[e]; }
+};
 
-template <typename TI, int NV>
-__global__ __launch_bounds__(kThreads) void embed_runs_kernel(RowsParams q) {
-    const int lane = threadIdx.x % 64;
-    const int64_t run = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64, group = blockIdx.y;
-    const int64_t from = run * kRun, to = from + kRun;
-    if (run >= q.runs || to > q.g.tokens) return;
-    const int32_t* keys = q.keys + group * q.g.tokens;
-    const int id = keys[from];
-    if (id != keys[to - 1] || id >= q.g.vocab) return;
-    const int64_t c = (int64_t)blockIdx.z * 512 * NV;
-    float sum[NV][8] = {};
-    add_rows<TI, NV>(q, group, from, to, c, lane, sum);
-    float* out = q.partial + (group * q.runs + run) * q.g.width;
+// Columns c + 512 t + 8 lane .. of a row of the gradient.
+template <typename TO, int NV>
+__device__ __forceinline__ void write_row(const RowsParams& q, int64_t group, int64_t v, int64_t c, int lane, const float (&sum)[NV][8]) {
+    TO* out = (TO*)q.g.grad + group * q.g.grad_group + v * q.g.grad_row;
 #pragma unroll
     for (int t = 0; t < NV; ++t) {
         const int64_t at = c + 512 * t + 8 * lane;
-        if (at < q.g.width) store_upto8(out + at, (int)min((int64_t)8, q.g.width - at), sum[t]);
+        if (at >= q.g.width) continue;
+        const int left = (int)min((int64_t)8, q.g.width - at);
+        float o[8];
+        if (q.g.accumulate) {
+            load_upto8(out + at, left, 0.0f, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(q.g.scale, sum[t][e], o[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = q.g.scale * sum[t][e];
+        }
+        store_upto8(out + at, left, o);
     }
 }
 
 template <typename TI, typename TO, int NV>
-__global__ __launch_bounds__(kThreads) void embed_rows_kernel(RowsParams q) {
-    __shared__ int64_t start[kRowsPerBlock + 1];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t v0 = (int64_t)blockIdx.x * kRowsPerBlock, group = blockIdx.y;
-    const int32_t* keys = q.keys + group * q.g.tokens;
-    if (threadIdx.x <= kRowsPerBlock) {   // the first position whose id is at least v0 + threadIdx.x
-        const int64_t v = v0 + threadIdx.x;
-        int64_t lo = 0, hi = q.g.tokens;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) / 2;
-            if (keys[mid] < v) lo = mid + 1;
-            else hi = mid;
-        }
-        start[threadIdx.x] = lo;
+__global__ __launch_bounds__(kThreads) void embed_runs_kernel(RowsParams q) {
+    constexpr int B = Raw8<TI>::kBatch;
+    static_assert(kRun % B == 0 && kRun < 64, "whole batches, and a lane per position");
+    const int lane = threadIdx.x % 64;
+    const int64_t run = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = blockIdx.y;
+    if (run >= q.runs) return;
+    const int64_t n = q.g.tokens, from = run * kRun;
+    const int have = (int)min((int64_t)kRun, n - from);
+    const int32_t* keys = q.keys + group * n + from;
+    // lane i holds position i's id and row; lane `have` the next run's first id, `before` is the previous run's last
+    const int key = lane < have || (lane == have && from + have < n) ? keys[lane] : -1;
+    const int row = lane < have ? q.pos[group * n + from + lane] : 0;
+    const int before = from > 0 ? keys[-1] : -1;
+    const int up = __shfl_up(key, 1), down = __shfl_down(key, 1);
+    const int64_t vocab = q.g.vocab;
+    if (blockIdx.z == 0 && lane < have && key < vocab) {
+        int32_t* b = q.bounds + group * 2 * vocab;
+        if ((lane ? up : before) != key) b[key] = (int)(from + lane);
+        if (down != key) b[vocab + key] = (int)(from + lane + 1);
     }
-    __syncthreads();
     const int64_t c = (int64_t)blockIdx.z * 512 * NV;
-    for (int r = wave; r < kRowsPerBlock; r += kThreads / 64) {
-        const int64_t v = v0 + r;
-        if (v >= q.g.vocab) break;
-        const int64_t from = start[r], to = start[r + 1];
-        if (from == to && q.g.accumulate) continue;
-        float sum[NV][8] = {};
-        if (from < to) {
-            const int64_t first = (from + kRun - 1) / kRun, last = to / kRun;   // whole runs [first, last)
-            if (first >= last) {
-                add_rows<TI, NV>(q, group, from, to, c, lane, sum);
+    const TI* base = (const TI*)q.g.dout + group * q.g.dout_group + c;
+    float sum[NV][8] = {};
+    bool open = __builtin_amdgcn_readlane(key, 0) == before;    // the sum began in an earlier run
+    for (int k = 0; k < have; k += B) {
+        Raw8<TI> v[B][NV];
+#pragma unroll
+        for (int r = 0; r < B; ++r) {
+            const TI* src = base + __builtin_amdgcn_readlane(row, k + r) * q.g.dout_row;     // positions past the end: row 0
+#pragma unroll
+            for (int t = 0; t < NV; ++t) {
+                const int64_t at = 512 * t + 8 * lane;
+                v[r][t].load(src + at, (int)max((int64_t)0, min((int64_t)8, q.g.width - c - at)));
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < B; ++r) {
+            const int i = k + r, id = __builtin_amdgcn_readlane(key, i);
+            if (i >= have || id >= vocab) return;               // sorted: what is no token comes last
+#pragma unroll
+            for (int t = 0; t < NV; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[t][e] += v[r][t].get(e);
+            const bool ends = __builtin_amdgcn_readlane(key, i + 1) != id;
+            if (!ends && i + 1 < have) continue;
+            if (ends && !open) {
+                write_row<TO, NV>(q, group, id, c, lane, sum);
             } else {
-                add_rows<TI, NV>(q, group, from, first * kRun, c, lane, sum);
-                const float* part = q.partial + (group * q.runs + first) * q.g.width;
-                for (int64_t k = 0; k < last - first; k += 4) {
-                    float p[4][NV][8];
+                float* out = q.partial + ((group * q.runs + run) * 2 + (open ? 0 : 1)) * q.g.width + c;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int t = 0; t < NV; ++t) {
-                            const int64_t at = c + 512 * t + 8 * lane;
-                            const bool there = k + j < last - first && at < q.g.width;
-                            load_upto8(part + (k + j) * q.g.width + at, there ? (int)min((int64_t)8, q.g.width - at) : 0, 0.0f, p[j][t]);
-                        }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int t = 0; t < NV; ++t)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) sum[t][e] += p[j][t][e];
+                for (int t = 0; t < NV; ++t) {
+                    const int64_t at = 512 * t + 8 * lane;
+                    if (c + at < q.g.width) store_upto8(out + at, (int)min((int64_t)8, q.g.width - c - at), sum[t]);
                 }
-                add_rows<TI, NV>(q, group, last * kRun, to, c, lane, sum);
             }
+            open = false;
+#pragma unroll
+            for (int t = 0; t < NV; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[t][e] = 0.0f;
         }
-        TO* out = (TO*)q.g.grad + group * q.g.grad_group + v * q.g.grad_row;
-#pragma unroll
-        for (int t = 0; t < NV; ++t) {
-            const int64_t at = c + 512 * t + 8 * lane;
-            if (at >= q.g.width) continue;
-            const int left = (int)min((int64_t)8, q.g.width - at);
-            float o[8];
-            if (q.g.accumulate) {
-                load_upto8(out + at, left, 0.0f, o);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = fmaf(q.g.scale, sum[t][e], o[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = q.g.scale * sum[t][e];
+    }
+}
+
+template <typename TO, int NV>
+__global__ __launch_bounds__(kThreads) void embed_rows_kernel(RowsParams q) {
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t v0 = (int64_t)blockIdx.x * kRowsPerBlock + wave * (kRowsPerBlock / 4), group = blockIdx.y, vocab = q.g.vocab;
+    const int32_t* b = q.bounds + group * 2 * vocab;
+    const bool mine = lane < kRowsPerBlock / 4 && v0 + lane < vocab;
+    const int first = mine ? b[v0 + lane] : 0, last = mine ? b[vocab + v0 + lane] : 0;
+    const int64_t c = (int64_t)blockIdx.z * 512 * NV;
+    for (int r = 0; r < kRowsPerBlock / 4 && v0 + r < vocab; ++r) {
+        const int from = __builtin_amdgcn_readlane(first, r), to = __builtin_amdgcn_readlane(last, r);
+        if (to == 0) {
+            if (q.g.accumulate) continue;
+            TO* out = (TO*)q.g.grad + group * q.g.grad_group + (v0 + r) * q.g.grad_row;
+            const int64_t end = min(q.g.width, c + 512 * NV);
+            constexpr int kVec = 16 / sizeof(TO);
+            for (int64_t at = c + lane * kVec; at < end; at += 64 * kVec) {
+                if (at + kVec <= end) {
+                    *(u4any*)(out + at) = u4any{0u, 0u, 0u, 0u};
+                } else {
+                    for (int e = 0; e < end - at; ++e) store1(out + at + e, 0.0f);
+                }
             }
-            store_upto8(out + at, left, o);
+            continue;
         }
+        const int64_t run0 = from / kRun, run1 = (to - 1) / kRun;
+        if (run0 == run1) continue;                            // its run has written it
+        float sum[NV][8] = {};
+        for (int64_t k = run0; k <= run1; k += 4) {
+            float p[4][NV][8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float* part = q.partial + ((group * q.runs + k + j) * 2 + (k + j == run0 ? 1 : 0)) * q.g.width + c;
+#pragma unroll
+                for (int t = 0; t < NV; ++t) {
+                    const int64_t at = 512 * t + 8 * lane;
+                    load_upto8(part + at, k + j <= run1 ? (int)max((int64_t)0, min((int64_t)8, q.g.width - c - at)) : 0, 0.0f, p[j][t]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int t = 0; t < NV; ++t)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[t][e] += p[j][t][e];
+        }
+        write_row<TO, NV>(q, group, v0 + r, c, lane, sum);
     }
 }
 
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
 struct GradPlan {
-    int64_t blocks, runs, off_keys[2], off_pos[2], off_counts, off_partial, bytes;
+    int64_t blocks, runs, off_keys[2], off_pos[2], off_counts, off_bounds, off_partial, bytes;
 };
-GradPlan grad_plan(int groups, int64_t tokens, int64_t width) {
+GradPlan grad_plan(int groups, int64_t tokens, int64_t vocab, int64_t width) {
     GradPlan p;
     p.blocks = (tokens + kSortItems - 1) / kSortItems;
-    p.runs = tokens / kRun;
+    p.runs = (tokens + kRun - 1) / kRun;
     int64_t at = 0;
     for (int i = 0; i < 2; ++i) {
         p.off_keys[i] = at, at = up256(at + groups * tokens * 4);
         p.off_pos[i] = at, at = up256(at + groups * tokens * 4);
     }
     p.off_counts = at, at = up256(at + (p.blocks > 1 ? groups * p.blocks * kDigits * 4 : 0));
-    p.off_partial = at, at = up256(at + groups * p.runs * width * 4);
+    p.off_bounds = at, at = up256(at + groups * 2 * vocab * 4);
+    p.off_partial = at, at = up256(at + groups * p.runs * 2 * width * 4);
     p.bytes = at;
     return p;
 }
@@ -373,8 +446,8 @@ template <typename TI, typename TO, int NV>
 void launch_sums(const RowsParams& q, hipStream_t stream) {
     const int tiles = (int)((q.g.width + 512 * NV - 1) / (512 * NV));
     if (q.runs)
-        embed_runs_kernel<TI, NV><<<dim3((unsigned)((q.runs + 3) / 4), q.g.groups, tiles), kThreads, 0, stream>>>(q);
-    embed_rows_kernel<TI, TO, NV><<<dim3((unsigned)((q.g.vocab + kRowsPerBlock - 1) / kRowsPerBlock), q.g.groups, tiles), kThreads, 0, stream>>>(q);
+        embed_runs_kernel<TI, TO, NV><<<dim3((unsigned)((q.runs + 3) / 4), q.g.groups, tiles), kThreads, 0, stream>>>(q);
+    embed_rows_kernel<TO, NV><<<dim3((unsigned)((q.g.vocab + kRowsPerBlock - 1) / kRowsPerBlock), q.g.groups, tiles), kThreads, 0, stream>>>(q);
 }
 
 template <typename TI, typename TO>
@@ -399,44 +472,39 @@ hipError_t launch_embed(const EmbedParams& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-int64_t embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t width) { return grad_plan(groups, tokens, width).bytes; }
+int64_t embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t vocab, int64_t width) { return grad_plan(groups, tokens, vocab, width).bytes; }
 
 hipError_t launch_embed_grad(const EmbedGradParams& g, void* ws, hipStream_t stream) {
     if (g.groups == 0 || g.width == 0) return hipSuccess;
-    const GradPlan plan = grad_plan(g.groups, g.tokens, g.width);
+    const GradPlan plan = grad_plan(g.groups, g.tokens, g.vocab, g.width);
     char* w = (char*)ws;
     int32_t* keys[2] = {(int32_t*)(w + plan.off_keys[0]), (int32_t*)(w + plan.off_keys[1])};
     int32_t* pos[2] = {(int32_t*)(w + plan.off_pos[0]), (int32_t*)(w + plan.off_pos[1])};
     int bits = 1;
     while (bits < 31 && (g.vocab >> bits) != 0) ++bits;   // the key `vocab` stands for "no token"
     const int passes = (bits + kDigitBits - 1) / kDigitBits;
-    if (g.tokens > 0) {
-        SortParams s;
-        s.ids = g.ids, s.ids_group = g.ids_group, s.n = g.tokens, s.vocab = g.vocab;
-        s.counts = (int32_t*)(w + plan.off_counts);
-        s.blocks = (int)plan.blocks;
-        s.keys_in = s.pos_in = nullptr, s.keys_out = s.pos_out = nullptr, s.shift = 0;
-        if (plan.blocks == 1) {
-            sort_one_block_kernel<<<g.groups, kSortThreads, 0, stream>>>(s, keys[0], pos[0], keys[1], pos[1], passes);
-        } else {
-            for (int pass = 0; pass < passes; ++pass) {
-                const int to = (passes - 1 - pass) % 2;   // the last pass ends in list 0
-                s.keys_in = keys[1 - to], s.pos_in = pos[1 - to], s.keys_out = keys[to], s.pos_out = pos[to];
-                s.shift = pass * kDigitBits;
-                const dim3 grid((unsigned)plan.blocks, g.groups);
-                sort_count_kernel<<<grid, kSortThreads, 0, stream>>>(s, pass == 0);
-                sort_scatter_kernel<<<grid, kSortThreads, 0, stream>>>(s, pass == 0);
-            }
+    SortParams s = {};
+    s.ids = g.ids, s.ids_group = g.ids_group, s.n = g.tokens, s.vocab = g.vocab;
+    s.counts = (int32_t*)(w + plan.off_counts), s.bounds = (int32_t*)(w + plan.off_bounds);
+    s.blocks = (int)plan.blocks;
+    const unsigned clear = (unsigned)((2 * g.vocab + kClearInts - 1) / kClearInts);
+    if (plan.blocks <= 1) {          // without ids the passes find none
+        sort_one_block_kernel<<<dim3(1 + clear, g.groups), kSortThreads, 0, stream>>>(s, keys[0], pos[0], keys[1], pos[1], g.tokens > 0 ? passes : 0);
+    } else {
+        for (int pass = 0; pass < passes; ++pass) {
+            const int to = (passes - 1 - pass) % 2;   // the last pass ends in list 0
+            s.keys_in = keys[1 - to], s.pos_in = pos[1 - to], s.keys_out = keys[to], s.pos_out = pos[to];
+            s.shift = pass * kDigitBits;
+            sort_count_kernel<<<dim3((unsigned)plan.blocks + (pass == 0 ? clear : 0), g.groups), kSortThreads, 0, stream>>>(s, pass == 0);
+            sort_scatter_kernel<<<dim3((unsigned)plan.blocks, g.groups), kSortThreads, 0, stream>>>(s, pass == 0);
         }
     }
     RowsParams q;
-    q.g = g, q.keys = keys[0], q.pos = pos[0], q.partial = (float*)(w + plan.off_partial), q.runs = plan.runs;
-    if (g.vocab > 0) {
-        if (g.dtype == OLS_F32 && g.grad_dtype == OLS_F32) launch_sums<float, float>(q, stream);
-        else if (g.dtype == OLS_F32) launch_sums<float, uint16_t>(q, stream);
-        else if (g.grad_dtype == OLS_F32) launch_sums<uint16_t, float>(q, stream);
-        else launch_sums<uint16_t, uint16_t>(q, stream);
-    }
+    q.g = g, q.keys = keys[0], q.pos = pos[0], q.partial = (float*)(w + plan.off_partial), q.runs = plan.runs, q.bounds = s.bounds;
+    if (g.dtype == OLS_F32 && g.grad_dtype == OLS_F32) launch_sums<float, float>(q, stream);
+    else if (g.dtype == OLS_F32) launch_sums<float, uint16_t>(q, stream);
+    else if (g.grad_dtype == OLS_F32) launch_sums<uint16_t, float>(q, stream);
+    else launch_sums<uint16_t, uint16_t>(q, stream);
     return hipGetLastError();
 }
 

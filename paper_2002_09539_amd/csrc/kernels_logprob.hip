@@ -85,13 +85,30 @@ __device__ __forceinline__ void store_vec(T* row, int64_t i, int64_t end, const 
     }
 }
 
+// Reductions of a wavefront in the vector unit's own data path (a shuffle through LDS costs ten times an operation): lanes of
+// a row of 16 by shifts, then the rows' last lanes are handed on.  Lane 63 ends with the result, which all read.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float v, float other) {      // lanes that receive nothing see `other`
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 __device__ __forceinline__ float wave_max(float v) {
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
+    v = fmaxf(v, moved<0x111, 0xf>(v, -INFINITY));
+    v = fmaxf(v, moved<0x112, 0xf>(v, -INFINITY));
+    v = fmaxf(v, moved<0x114, 0xf>(v, -INFINITY));
+    v = fmaxf(v, moved<0x118, 0xf>(v, -INFINITY));
+    v = fmaxf(v, moved<0x142, 0xa>(v, -INFINITY));
+    v = fmaxf(v, moved<0x143, 0xc>(v, -INFINITY));
+    return lane_of(v, 63);
 }
 __device__ __forceinline__ float wave_sum(float v) {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    v += moved<0x111, 0xf>(v, 0.0f);
+    v += moved<0x112, 0xf>(v, 0.0f);
+    v += moved<0x114, 0xf>(v, 0.0f);
+    v += moved<0x118, 0xf>(v, 0.0f);
+    v += moved<0x142, 0xa>(v, 0.0f);
+    v += moved<0x143, 0xc>(v, 0.0f);
+    return lane_of(v, 63);
 }
 
 struct RowResult {
@@ -129,29 +146,38 @@ __device__ __forceinline__ float logit_grad(const GradRow& r, float z, int64_t j
 // places among the listed: value descending, index ascending
 __device__ __forceinline__ bool beats(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
 
+// Writes the best k of `count` listed logits in their order.  Up to 64 are compared by the first wavefront in registers.
 template <int THREADS>
 __device__ __forceinline__ void write_best(const float* val, const int* idx, int count, int k, float* out_val, int* out_idx) {
     for (int i = threadIdx.x; i < k; i += THREADS)
         if (i >= count) out_val[i] = -INFINITY, out_idx[i] = -1;
+    if (count <= 64) {
+        if (threadIdx.x >= 64) return;
+        const int i = threadIdx.x;
+        const float v = i < count ? val[i] : -INFINITY;
+        const int at = i < count ? idx[i] : 0x7fffffff;
+        int place = 0;
+        for (int j = 0; j < count; ++j) place += beats(lane_of(v, j), __builtin_amdgcn_readlane(at, j), v, at) ? 1 : 0;
+        if (i < count && place < k) out_val[place] = v, out_idx[place] = at;
+        return;
+    }
     for (int i = threadIdx.x; i < count; i += THREADS) {
         const float v = val[i];
         const int at = idx[i];
         int place = 0;
+#pragma unroll 8
         for (int j = 0; j < count; ++j) place += beats(val[j], idx[j], v, at) ? 1 : 0;
         if (place < k) out_val[place] = v, out_idx[place] = at;
     }
 }
 
-// The best k of what the workgroup holds, as (value, index) pairs in LDS, best first; -1 and -inf where there are fewer.
-template <typename T, int THREADS, int NV>
-__device__ void best_of_part(const u4 (&v)[NV], float lane_max, int64_t start, int k, float* lds_val, int* lds_idx, float* best_val, int* best_idx) {
-    constexpr int N = Vec<T>::kN, WAVES = THREADS / 64;
-    __shared__ float tops[WAVES * kMaxTop];
-    __shared__ int listed, equal;
-    __shared__ float bound;
+// The k-th largest of all lanes' values (k <= 32; -inf where fewer lanes hold more).  Every wavefront puts its k largest into
+// `tops`, largest first, and then merges the lists by itself: lane w holds the head of list w.
+template <int THREADS>
+__device__ __forceinline__ float kth_of_lanes(float mine, int k, float* tops) {
+    constexpr int WAVES = THREADS / 64;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    if (threadIdx.x == 0) listed = 0, bound = -INFINITY;
-    float left = lane_max;
+    float left = mine;
     for (int i = 0; i < k; ++i) {
         const float top = wave_max(left);
         if (lane == 0) tops[wave * k + i] = top;
@@ -159,18 +185,33 @@ __device__ void best_of_part(const u4 (&v)[NV], float lane_max, int64_t start, i
         if (at && lane == __ffsll(at) - 1) left = -INFINITY;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < WAVES * k; i += THREADS) {   // the k-th largest lane maximum
-        const float mine = tops[i];
-        int before = 0;
-        for (int j = 0; j < WAVES * k; ++j) before += tops[j] > mine || (tops[j] == mine && j < i) ? 1 : 0;
-        if (before == k - 1) bound = mine;
+    int used = 0;
+    float head = lane < WAVES ? tops[lane * k] : -INFINITY, bound = -INFINITY;
+    for (int i = 0; i < k; ++i) {
+        bound = wave_max(head);
+        const unsigned long long at = __ballot(head == bound);
+        if (at && lane == __ffsll(at) - 1) head = lane < WAVES && ++used < k ? tops[lane * k + used] : -INFINITY;
     }
-    __syncthreads();
-    const float limit = bound;
-    int same = 0;               // logits equal to the bound that this wavefront has listed
+    return bound;
+}
+
+// The best k of what the workgroup holds, as (value, index) pairs in LDS, best first; -1 and -inf where there are fewer.
+template <typename T, int THREADS, int NV>
+__device__ void best_of_part(const u4 (&v)[NV], float lane_max, int64_t start, int k, float* lds_val, int* lds_idx, float* best_val, int* best_idx) {
+    constexpr int N = Vec<T>::kN, WAVES = THREADS / 64;
+    __shared__ float tops[WAVES * kMaxTop];
+    __shared__ int listed;
+    const int lane = threadIdx.x % 64;
+    if (threadIdx.x == 0) listed = 0;
+    const float limit = kth_of_lanes<THREADS>(lane_max, k, tops);
+    int same = 0;               // logits equal to the limit that this wavefront has listed
     if (__ballot(lane_max >= limit && lane_max > -INFINITY)) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            float top = Vec<T>::get(v[j], 0);
+#pragma unroll
+            for (int e = 1; e < N; ++e) top = fmaxf(top, Vec<T>::get(v[j], e));
+            if (!__ballot(top >= limit && top > -INFINITY)) continue;
             unsigned above = 0, at = 0;
 #pragma unroll
             for (int e = 0; e < N; ++e) {
@@ -178,21 +219,25 @@ __device__ void best_of_part(const u4 (&v)[NV], float lane_max, int64_t start, i
                 above |= x > limit ? 1u << e : 0u;
                 at |= x == limit && x > -INFINITY ? 1u << e : 0u;
             }
-            if (!__ballot(above | at)) continue;
             const int64_t first = start + ((int64_t)j * THREADS + threadIdx.x) * N;
             int rank = __popc(at);                       // equal ones of earlier lanes
-            for (int o = 1; o < 64; o <<= 1) {
-                const int u = __shfl_up(rank, o);
-                if (lane >= o) rank += u;
+            if (__ballot(at)) {
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int u = __shfl_up(rank, o);
+                    if (lane >= o) rank += u;
+                }
             }
             const int in_vec = __shfl(rank, 63);
             rank += same - __popc(at);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
+            for (unsigned todo = above | at; todo; todo &= todo - 1) {
+                const int e = __ffs(todo) - 1;
                 const bool eq = (at >> e) & 1u;
-                if (((above >> e) & 1u) || (eq && rank < k)) {
+                if (!eq || rank < k) {
                     const int to = atomicAdd(&listed, 1);
-                    lds_val[to] = Vec<T>::get(v[j], e);
+                    float x = Vec<T>::get(v[j], 0);
+#pragma unroll
+                    for (int c = 1; c < N; ++c) x = c == e ? Vec<T>::get(v[j], c) : x;
+                    lds_val[to] = x;
                     lds_idx[to] = (int)(first + e);
                 }
                 rank += eq ? 1 : 0;
@@ -209,6 +254,14 @@ __device__ void best_of_part(const u4 (&v)[NV], float lane_max, int64_t start, i
 // at most k equal to it.
 template <typename T, int THREADS, int NV>
 constexpr int list_entries(int k) { return k * NV * Vec<T>::kN + THREADS / 64 * k; }
+
+// Every pass unpacks the logits anew: without this, the compiler keeps them as fp32 from pass to pass, which is twice the
+// registers and spills.
+template <int NV>
+__device__ __forceinline__ void keep_packed(u4 (&v)[NV]) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) asm("" : "+v"(v[j]));
+}
 
 template <typename T, int THREADS, int NV, bool GRAD>
 __global__ __launch_bounds__(THREADS, 4) void logprob_kernel(LogprobParams p) {
@@ -234,6 +287,7 @@ __global__ __launch_bounds__(THREADS, 4) void logprob_kernel(LogprobParams p) {
 #pragma unroll
         for (int e = 0; e < N; ++e) m = fmaxf(m, Vec<T>::get(v[j], e));
     const float lane_max = m;
+    keep_packed(v);
     m = wave_max(m);
     if (lane == 0) red_m[wave] = m;
     __syncthreads();
@@ -259,6 +313,7 @@ __global__ __launch_bounds__(THREADS, 4) void logprob_kernel(LogprobParams p) {
     s = t = 0.0f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) s += red_s[w], t += red_t[w];
+    keep_packed(v);
     const Stats all{m, s, t};
     if (p.top > 0) {
         float* list_val = (float*)dyn;
@@ -309,6 +364,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobParams p) {
     __shared__ float red[3][4];
     __shared__ float best_val[kMaxTop];
     __shared__ int best_idx[kMaxTop];
+    __shared__ float tops[4 * kMaxTop];
     __shared__ int count;
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -337,14 +393,18 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobParams p) {
         p.stats[2 * row] = r.m, p.stats[2 * row + 1] = r.s;
     }
     if (p.top == 0) return;
+    // the k-th best of the parts' best ones is a limit for the row's k-th best
     const int n = p.parts * p.top;
     float* val = (float*)dyn;
     int* idx = (int*)(val + n);
+    const float* in_val = p.part_val + row * n;
+    const float limit = kth_of_lanes<256>((int)threadIdx.x < p.parts ? in_val[threadIdx.x * p.top] : -INFINITY, p.top, tops);
     for (int i = threadIdx.x; i < n; i += 256) {
+        const float v = in_val[i];
         const int at = p.part_idx[row * n + i];
-        if (at < 0) continue;
+        if (at < 0 || v < limit) continue;
         const int to = atomicAdd(&count, 1);
-        val[to] = p.part_val[row * n + i], idx[to] = at;
+        val[to] = v, idx[to] = at;
     }
     __syncthreads();
     write_best<256>(val, idx, count, p.top, best_val, best_idx);
@@ -419,8 +479,14 @@ RowPlan row_plan(int dtype, int64_t rows, int64_t vocab) {
     const int64_t vecs = (r.part + unit - 1) / unit;    // per lane of 256
     r.threads = vecs <= 16 ? 256 : vecs <= 32 ? 512 : 1024;
     const int64_t per = (r.part + r.threads * n - 1) / (r.threads * n);
-    r.nv = per <= 2 ? 2 : per <= 4 ? 4 : per <= 8 ? 8 : 16;
+    r.nv = per <= 2 ? 2 : per <= 4 ? 4 : per <= 8 ? 8 : per <= 10 ? 10 : per <= 13 ? 13 : 16;
     return r;
+}
+
+template <typename T, int NV>
+hipError_t launch_long(const LogprobParams& p, const RowPlan& r, hipStream_t stream) {
+    if (r.threads == 256) return launch_rows<T, 256, NV>(p, stream);
+    return r.threads == 512 ? launch_rows<T, 512, NV>(p, stream) : launch_rows<T, 1024, NV>(p, stream);
 }
 
 template <typename T>
@@ -429,9 +495,9 @@ hipError_t launch_typed(const LogprobParams& p, const RowPlan& r, hipStream_t st
         if (r.nv == 2) return launch_rows<T, 256, 2>(p, stream);
         if (r.nv == 4) return launch_rows<T, 256, 4>(p, stream);
         if (r.nv == 8) return launch_rows<T, 256, 8>(p, stream);
-        return launch_rows<T, 256, 16>(p, stream);
     }
-    return r.threads == 512 ? launch_rows<T, 512, 16>(p, stream) : launch_rows<T, 1024, 16>(p, stream);
+    // registers that hold nothing are still gone through: 50 001 logits in 13 vectors a lane instead of 16
+    return r.nv <= 10 ? launch_long<T, 10>(p, r, stream) : r.nv == 13 ? launch_long<T, 13>(p, r, stream) : launch_long<T, 16>(p, r, stream);
 }
 
 template <typename T>

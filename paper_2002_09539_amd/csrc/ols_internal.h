@@ -477,7 +477,7 @@ struct EmbedGradParams {
     void* grad;
     int64_t grad_row, grad_group;
 };
-int64_t embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t width);
+int64_t embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t vocab, int64_t width);
 hipError_t launch_embed_grad(const EmbedGradParams& p, void* ws, hipStream_t stream);
 
 struct LogprobParams {

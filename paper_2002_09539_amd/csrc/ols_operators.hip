@@ -190,7 +190,7 @@ int ols_embed(int groups, int64_t tokens, int64_t vocab, int64_t width, const in
 
 int64_t ols_embed_grad_workspace_bytes(int groups, int64_t tokens, int64_t vocab, int64_t width) {
     if (const int rc = check_embed("ols_embed_grad_workspace_bytes", groups, tokens, vocab, width)) return rc;
-    return embed_grad_workspace_bytes(groups, tokens, width);
+    return embed_grad_workspace_bytes(groups, tokens, vocab, width);
 }
 
 int ols_embed_grad(int groups, int64_t tokens, int64_t vocab, int64_t width, const int32_t* ids_dev, int64_t ids_group, const void* d_out_dev, int dtype,
@@ -206,7 +206,7 @@ int ols_embed_grad(int groups, int64_t tokens, int64_t vocab, int64_t width, con
     if (!stride_ok(d_out_row, width) || !stride_ok(grad_row, width)) return bad("%s: rows of %lld elements overlap at the given strides", who, (long long)width);
     if (!group_ok(ids_group) || !group_ok(d_out_group) || !group_ok(grad_group)) return bad("%s: a worker's stride is out of range", who);
     if (groups > 1 && grad_group < (vocab - 1) * grad_row + width) return bad("%s: the workers' gradients overlap", who);
-    if (const int rc = check_ws(who, ws_dev, ws_bytes, embed_grad_workspace_bytes(groups, tokens, width))) return rc;
+    if (const int rc = check_ws(who, ws_dev, ws_bytes, embed_grad_workspace_bytes(groups, tokens, vocab, width))) return rc;
     EmbedGradParams p;
     p.groups = groups, p.dtype = dtype, p.grad_dtype = grad_dtype, p.accumulate = accumulate != 0, p.tokens = tokens, p.vocab = vocab, p.width = width;
     p.ids = ids_dev, p.ids_group = ids_group, p.dout = d_out_dev, p.dout_row = d_out_row, p.dout_group = d_out_group, p.scale = scale;
