@@ -69,4 +69,29 @@ __device__ __forceinline__ void store_upto8(T* p, int left, const float (&v)[8])
     }
 }
 
+// Eight elements as they lie in memory, for loads in flight: bf16 takes half the registers until it is used.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<uint16_t> {
+    u4 a;
+    __device__ void load(const uint16_t* p, int left) {
+        if (left >= 8) {
+            a = *(const u4any*)p;
+        } else {
+            float v[8];
+            load_upto8(p, left, 0.0f, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+        }
+    }
+    __device__ float get(int e) const { return e % 2 ? bf16_hi(a[e / 2]) : bf16_lo(a[e / 2]); }
+};
+template <>
+struct Raw8<float> {
+    float v[8];
+    __device__ void load(const float* p, int left) { load_upto8(p, left, 0.0f, v); }
+    __device__ float get(int e) const { return v[e]; }
+};
+
 }  // namespace ols

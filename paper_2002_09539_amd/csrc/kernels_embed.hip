@@ -258,32 +258,9 @@ struct RowsParams {
     int64_t runs;
 };
 
-// Eight elements as they lie in memory, so that several rows' loads can be in flight in few registers.
+// Rows whose loads are in flight together.
 template <typename T>
-struct Raw8;
-template <>
-struct Raw8<uint16_t> {
-    static constexpr int kBatch = 8;
-    u4 a;
-    __device__ void load(const uint16_t* p, int left) {
-        if (left >= 8) {
-            a = *(const u4any*)p;
-        } else {
-            float v[8];
-            load_upto8(p, left, 0.0f, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-        }
-    }
-    __device__ float get(int e) const { return e % 2 ? bf16_hi(a[e / 2]) : bf16_lo(a[e / 2]); }
-};
-template <>
-struct Raw8<float> {
-    static constexpr int kBatch = 4;
-    float v[8];
-    __device__ void load(const float* p, int left) { load_upto8(p, left, 0.0f, v); }
-    __device__ float get(int e) const { return v[e]; }
-};
+constexpr int row_batch() { return sizeof(T) == 2 ? 8 : 4; }
 
 // Columns c + 512 t + 8 lane .. of a row of the gradient.
 template <typename TO, int NV>
@@ -309,7 +286,7 @@ __device__ __forceinline__ void write_row(const RowsParams& q, int64_t group, in
 
 template <typename TI, typename TO, int NV>
 __global__ __launch_bounds__(kThreads) void embed_runs_kernel(RowsParams q) {
-    constexpr int B = Raw8<TI>::kBatch;
+    constexpr int B = row_batch<TI>();
     static_assert(kRun % B == 0 && kRun < 64, "whole batches, and a lane per position");
     const int lane = threadIdx.x % 64;
     const int64_t run = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = blockIdx.y;

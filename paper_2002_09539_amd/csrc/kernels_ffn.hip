@@ -11,7 +11,8 @@
 // weights of a bf16 block), by a streaming pass.
 //
 // Few rows (answering token by token) leave nothing to multiply but every weight to read once: there a lane owns eight
-// columns, 32 lanes share the contraction, and several workgroups share it further so that the whole device reads.
+// columns, 32 lanes share the contraction, and several workgroups share it further, so that nearly all weights are under way
+// at once.
 #include <algorithm>
 
 #include "ffn_gemm.h"
@@ -78,9 +79,21 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewParams p) {
     const int left = (int)max((int64_t)0, min((int64_t)8, p.N - col));
     const TW* w = (const TW*)p.w + group * p.w_group + col;
     const TW* w2 = FIRST ? (const TW*)p.w2 + group * p.w2_group + col : nullptr;
+    constexpr int B = sizeof(TW) == 2 ? 8 : 4;                  // indices whose weights are in flight together
+    Raw8<TW> u[B][PANELS];
+    auto request = [&](int64_t k0, int i, int n) {
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const int64_t k = k0 + i + 32 * j;
+            const int have = i + 32 * j < n ? left : 0;
+            u[j][0].load(w + k * p.w_row, have);
+            if constexpr (FIRST) u[j][1].load(w2 + k * p.w2_row, have);
+        }
+    };
     float acc[PANELS][R][8] = {};
     for (int64_t k0 = from; k0 < to; k0 += kFewSlab) {
         const int n = (int)min((int64_t)kFewSlab, to - k0);
+        request(k0, kl, n);                                     // before the inputs are waited for
         __syncthreads();
         for (int r = 0; r < R; ++r)
             for (int i = threadIdx.x; i < n; i += kFewThreads) {
@@ -90,27 +103,20 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewParams p) {
                         v = load1((const TX*)p.x + group * p.x_group + r * p.x_row + k0 + i);
                     } else {
                         float a = 0.0f, b = 0.0f;
-                        for (int s = 0; s < p.in_ranges; ++s) {
-                            const float* in = p.in + (((int64_t)s * gridDim.z + group) * p.rows + r) * 2 * p.in8 + k0 + i;
-                            a += in[0], b += in[p.in8];
-                        }
+                        const float* in = p.in + (group * p.rows + r) * 2 * p.in8 + k0 + i;
+                        const int64_t step = (int64_t)gridDim.z * p.rows * 2 * p.in8;
+#pragma unroll 4
+                        for (int s = 0; s < p.in_ranges; ++s) a += in[s * step], b += in[s * step + p.in8];
                         v = act_value(p.act, a) * b;
                     }
                 }
                 xs[i][r] = v;
             }
         __syncthreads();
-        for (int i = kl; i < n; i += 4 * 32) {
-            float u[4][PANELS][8];
+        for (int i = kl; i < n; i += 32 * B) {
+            if (i > kl) request(k0, i, n);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t k = k0 + i + 32 * j;
-                const int have = i + 32 * j < n ? left : 0;
-                load_upto8(w + k * p.w_row, have, 0.0f, u[j][0]);
-                if constexpr (FIRST) load_upto8(w2 + k * p.w2_row, have, 0.0f, u[j][1]);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < B; ++j) {
                 if (i + 32 * j >= n) continue;
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
@@ -118,7 +124,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewParams p) {
 #pragma unroll
                     for (int t = 0; t < PANELS; ++t)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) acc[t][r][e] = fmaf(x, u[j][t][e], acc[t][r][e]);
+                        for (int e = 0; e < 8; ++e) acc[t][r][e] = fmaf(x, u[j][t].get(e), acc[t][r][e]);
                 }
             }
         }
@@ -383,7 +389,7 @@ void few(const FewParams& p, const ols_ffn& f, hipStream_t stream) {
 
 int few_ranges(int64_t K, int64_t cols, int groups) {
     const int64_t blocks = tiles_of(cols, kFewCols) * groups;
-    return (int)std::max((int64_t)1, std::min(512 / blocks, K / 128));
+    return (int)std::max((int64_t)1, std::min(1024 / blocks, K / 256));
 }
 
 // Forward; with go false only the workspace is measured.

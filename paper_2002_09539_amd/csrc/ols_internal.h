@@ -506,24 +506,22 @@ int64_t ffn_workspace_bytes(const ols_ffn& f, bool grad);
 hipError_t launch_ffn(const ols_ffn& f, bool grad, hipStream_t stream);
 
 // Tensors of one launch, by value in the kernel arguments (4 KiB): no table to upload, nothing to keep alive.
-constexpr int kClipTensors = 88;
+constexpr int kClipTensors = 76;
 struct ClipTable {
-    int n, reverse;
-    int64_t chunk_base;                    // of the launch's first chunk among the partial sums
+    int n;
     const void* in[kClipTensors];
     void* out[kClipTensors];
-    int64_t numel[kClipTensors], group_first[kClipTensors];   // group_first: the group's first partial sum
-    int group_chunks[kClipTensors], group[kClipTensors], first_chunk[kClipTensors];
+    int64_t numel[kClipTensors], first_sum[kClipTensors], group_first[kClipTensors];   // first partial sum of the tensor, and of its group
+    int group_chunks[kClipTensors], group[kClipTensors], first_chunk[kClipTensors];    // first_chunk: the tensor's first workgroup
 };
-static_assert(sizeof(ClipTable) <= 4000, "kernel arguments");
+static_assert(sizeof(ClipTable) <= 4040, "kernel arguments");
 constexpr int kClipGroups = 160;
 struct ClipGroups {
     int64_t first[kClipGroups];
     int count[kClipGroups], group[kClipGroups];
 };
-hipError_t launch_clip_squares(const ClipTable& t, int dtype, int64_t chunk_elems, int blocks, double* partial, hipStream_t stream);
-hipError_t launch_clip_scale(const ClipTable& t, int dtype, int64_t chunk_elems, int blocks, const double* partial, float max_norm, float* norms,
-                             hipStream_t stream);
+hipError_t launch_clip(const ClipTable& t, int dtype, int64_t chunk_elems, int blocks, bool copy, double* partial, float max_norm, float* norms,
+                       hipStream_t stream);     // the sums of squares, or the scaled copy
 hipError_t launch_clip_norms(const ClipGroups& g, int groups, const double* partial, float* norms, hipStream_t stream);
 
 }  // namespace ols

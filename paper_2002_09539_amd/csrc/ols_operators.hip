@@ -105,8 +105,6 @@ int check_ffn_operands(const char* who, const ols_ffn& f) {
 
 constexpr int64_t kChunk = 16384;             // elements of a workgroup's chunk, doubled until no group has more than kMostChunks
 constexpr int64_t kMostChunks = 2048;
-constexpr int64_t kBatchBytes = 96ll << 20;   // groups whose second reading is to find them in the memory-side cache
-
 int check_clip(const char* who, int n, const int64_t* numel, const int32_t* group, int groups) {
     if (n < 0 || n > (1 << 20)) return bad("%s: number of tensors must be in [0, 2^20], got %d", who, n);
     if (groups < 1 || groups > kMaxGroups) return bad("%s: groups must be in [1, %d], got %d", who, kMaxGroups, groups);
@@ -140,29 +138,44 @@ int64_t clip_chunk(int n, const int64_t* numel, const int32_t* group) {
 
 int64_t chunks_of(int64_t numel, int64_t chunk) { return (numel + chunk - 1) / chunk; }
 
-// Walks the tensors [i, end) in tables of at most kClipTensors, skipping empty ones, and hands each table to `go`.
-template <typename F>
-int clip_tables(int i, int end, const void* const* in, void* const* out, const int64_t* numel, const int32_t* group, int64_t chunk, int64_t base, F && go) {
-    while (i < end) {
-        ClipTable t = {};
-        int blocks = 0;
-        t.chunk_base = base;
-        for (; i < end && t.n < kClipTensors; ++i) {
-            const int64_t c = chunks_of(numel[i], chunk);
-            if (c == 0) continue;
-            if (blocks + c > 0x3fffffff) break;
-            const int k = t.n++;
-            t.in[k] = in[i], t.out[k] = out ? out[i] : nullptr, t.numel[k] = numel[i], t.group[k] = group_of(group, i);
-            t.first_chunk[k] = blocks;
-            blocks += (int)c;
+struct ClipCall {
+    int n;
+    const void* const* in;
+    void* const* out;
+    const int64_t* numel;
+    const int32_t* group;
+    int64_t chunk;
+    int dtype;
+    float max_norm;
+    float* norms;
+    double* partial;
+    hipStream_t stream;
+};
+
+// One stage of a call, in as many launches as its tensors fill tables.
+hipError_t clip_stage(const ClipCall& c, bool copy) {
+    ClipTable t = {};
+    int blocks = 0, seen = -1;
+    int64_t at = 0, group_first = 0, group_chunks = 0;
+    for (int i = 0; i < c.n; ++i) {
+        if (group_of(c.group, i) != seen) {
+            seen = group_of(c.group, i);
+            group_first = at, group_chunks = 0;
+            for (int j = i; copy && j < c.n && group_of(c.group, j) == seen; ++j) group_chunks += chunks_of(c.numel[j], c.chunk);
         }
-        if (blocks) {
-            const int rc = go(t, blocks);
-            if (rc != OLS_OK) return rc;
+        const int64_t chunks = chunks_of(c.numel[i], c.chunk);
+        if (chunks == 0) continue;
+        if (t.n == kClipTensors || blocks + chunks > 0x3fffffff) {
+            const hipError_t e = launch_clip(t, c.dtype, c.chunk, blocks, copy, c.partial, c.max_norm, c.norms, c.stream);
+            if (e != hipSuccess) return e;
+            t.n = 0, blocks = 0;
         }
-        base += blocks;
+        const int k = t.n++;
+        t.in[k] = c.in[i], t.out[k] = copy ? c.out[i] : nullptr, t.numel[k] = c.numel[i], t.first_sum[k] = at;
+        t.group_first[k] = group_first, t.group_chunks[k] = (int)group_chunks, t.group[k] = seen, t.first_chunk[k] = blocks;
+        blocks += (int)chunks, at += chunks;
     }
-    return OLS_OK;
+    return launch_clip(t, c.dtype, c.chunk, blocks, copy, c.partial, c.max_norm, c.norms, c.stream);
 }
 
 }  // namespace
@@ -336,67 +349,20 @@ int ols_clip_gradients(int n, const void* const* in_dev, void* const* out_dev, c
     int64_t need = 0;
     for (int i = 0; i < n; ++i) need += 8 * chunks_of(numel[i], chunk);
     if (const int rc = check_ws(who, ws_dev, ws_bytes, need)) return rc;
-    double* partial = (double*)ws_dev;
-    const hipStream_t s = (hipStream_t)stream;
-
-    ClipGroups left = {};      // groups whose norm no scaling launch writes
-    int left_n = 0;
-    auto flush = [&]() {
-        const int k = left_n;
-        left_n = 0;
-        return k ? done(launch_clip_norms(left, k, partial, norms_dev, s), who) : OLS_OK;
-    };
-    int64_t base = 0;
-    int i = 0, g = 0;
-    while (g < groups) {
-        // a batch: whole groups [g, to_g), tensors [i, to)
-        const int first = i;
-        int to_g = g;
-        int64_t elems = 0, chunks = 0;
-        while (to_g < groups) {
-            int j = i;
-            int64_t e = 0, c = 0;
-            for (; j < n && group_of(group, j) == to_g; ++j) e += numel[j], c += chunks_of(numel[j], chunk);
-            if (to_g > g && out_dev && (elems + e) * size_of(dtype) > kBatchBytes) break;
-            if (!out_dev || c == 0) {
-                left.first[left_n] = base + chunks, left.count[left_n] = (int)c, left.group[left_n] = to_g;
-                ++left_n;
-            }
-            elems += e, chunks += c, i = j, ++to_g;
-            if (left_n == kClipGroups) break;
-        }
-        int rc = clip_tables(first, i, in_dev, out_dev, numel, group, chunk, base,
-                             [&](const ClipTable& t, int blocks) { return done(launch_clip_squares(t, dtype, chunk, blocks, partial, s), who); });
-        if (rc != OLS_OK) return rc;
-        if (out_dev && chunks) {
-            // where each tensor's group begins among the partial sums, followed along the tables
-            int64_t at = base, group_first = base, group_count = 0;
-            int seen = first;
-            int current = -1;
-            rc = clip_tables(first, i, in_dev, out_dev, numel, group, chunk, base, [&](ClipTable& t, int blocks) {
-                for (int k = 0; k < t.n; ++k) {
-                    if (t.group[k] != current) {
-                        current = t.group[k];
-                        group_first = at, group_count = 0;
-                        while (seen < i && group_of(group, seen) < current) ++seen;
-                        for (; seen < i && group_of(group, seen) == current; ++seen) group_count += chunks_of(numel[seen], chunk);
-                    }
-                    t.group_first[k] = group_first, t.group_chunks[k] = (int)group_count;
-                    at += chunks_of(t.numel[k], chunk);
-                }
-                t.reverse = elems * size_of(dtype) > kBatchBytes;
-                return done(launch_clip_scale(t, dtype, chunk, blocks, partial, max_norm, norms_dev, s), who);
-            });
-            if (rc != OLS_OK) return rc;
-        }
-        if (!out_dev || left_n == kClipGroups) {
-            rc = flush();
-            if (rc != OLS_OK) return rc;
-        }
-        base += chunks;
-        g = to_g;
+    const ClipCall c{n, in_dev, out_dev, numel, group, chunk, dtype, max_norm, norms_dev, (double*)ws_dev, (hipStream_t)stream};
+    hipError_t e = clip_stage(c, false);
+    if (e == hipSuccess && out_dev) e = clip_stage(c, true);
+    // the groups whose norm no copy has written: all without outputs, otherwise those without elements
+    ClipGroups left;
+    int left_n = 0, i = 0;
+    int64_t at = 0;
+    for (int g = 0; g < groups && e == hipSuccess; ++g) {
+        const int64_t first = at;
+        for (; i < n && group_of(group, i) == g; ++i) at += chunks_of(numel[i], chunk);
+        if (!out_dev || at == first) left.first[left_n] = first, left.count[left_n] = (int)(at - first), left.group[left_n] = g, ++left_n;
+        if (left_n == kClipGroups || (g + 1 == groups && left_n)) e = launch_clip_norms(left, left_n, c.partial, norms_dev, c.stream), left_n = 0;
     }
-    return flush();
+    return done(e, who);
 }
 
 }  // extern "C"

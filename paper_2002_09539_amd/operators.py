@@ -6,7 +6,9 @@ kept.  Tensors are fp32 or bf16, ids int32.  A leading axis of m workers can sta
 weights and gradients can be views of the rows of a Session's x and g; rows may be strided, elements of a row may not.
 Tensors that were made on another stream are the caller's to order and to record, as with any torch operation.
 """
+import contextlib
 import ctypes as C
+import operator
 from collections import namedtuple
 
 import torch
@@ -37,6 +39,15 @@ def _on_gpu(first, *others):
         if t is not None and t.device != first.device:
             _refuse("tensors are on %s and %s", first.device, t.device)
     return first.device
+
+
+_SAME = contextlib.nullcontext()
+
+
+def _on(device):
+    """The tensors' device as the current one, which it mostly is."""
+    index = device if isinstance(device, int) else device.index
+    return _SAME if index == torch.cuda.current_device() else torch.cuda.device(index)
 
 
 def _stream(device):
@@ -89,7 +100,7 @@ def embed(table, tokens, scale=1.0, out=None, dtype=None):
     elif tuple(out.shape) != (*tokens.shape, width) or not out.is_contiguous() or (dtype and out.dtype != dtype):
         _refuse("out must be a contiguous %s of the result's type", (*tokens.shape, width))
     tg, tr = _rows(t3, "table")
-    with torch.cuda.device(device):
+    with _on(device):
         B.ols_embed(m, n, vocab, width, ids.data_ptr(), ids_group, t3.data_ptr(), _dtype(table, "table"), tr, tg, float(scale), out.data_ptr(),
                     _dtype(out, "out"), width, n * width, _stream(device))
     return out
@@ -121,7 +132,7 @@ def embed_grad(tokens, d_out, vocab, scale=1.0, out=None, dtype=torch.float32, a
     dg, dr = _rows(d3, "d_out")
     og, orow = _rows(o3, "out")
     nbytes = B.ols_embed_grad_workspace_bytes(m, n, vocab, width)
-    with torch.cuda.device(device):
+    with _on(device):
         ws = _workspace(nbytes, device)
         B.ols_embed_grad(m, n, vocab, width, ids.data_ptr(), ids_group, d3.data_ptr(), _dtype(d_out, "d_out"), dr, dg, float(scale), out.data_ptr(),
                          _dtype(out, "out"), orow, og, int(accumulate), _ptr(ws), nbytes, _stream(device))
@@ -175,7 +186,7 @@ def gated_ffn(x, w_gate, w_up, w_down, act="silu", save=False, out=None):
     x fp32: products of fp32 accuracy, fp32 weights.  save=True returns (y, saved) for gated_ffn_grad."""
     f, device, lead = _ffn(x, w_gate, w_up, w_down, act, (out,))
     shape = (*lead, f.rows, f.out)
-    with torch.cuda.device(device):
+    with _on(device):
         if out is None:
             out = torch.empty(shape, dtype=x.dtype, device=device)
         elif tuple(out.shape) != shape or out.dtype != x.dtype:
@@ -211,7 +222,7 @@ def gated_ffn_grad(dy, x, w_gate, w_up, w_down, saved, act="silu", out=None, gra
         grad_dtype = grad_dtype or (types.pop() if types else None)
     grad_dtype = grad_dtype or w_gate.dtype
     f.grad_dtype = _dtype(grad_dtype, "grad_dtype")
-    with torch.cuda.device(device):
+    with _on(device):
         made = []
         for i, (name, shape) in enumerate(zip(("dx", "g_gate", "g_up", "g_down"), shapes)):
             t = out[i] if out is not None else None
@@ -268,7 +279,7 @@ def _logprobs(logits, targets, top, d_logprob, d_entropy, d_logits):
         d_stride = _logit_rows(d_logits, "out")[2]
     top = int(top)
     nbytes = B.ols_token_logprobs_workspace_bytes(rows, vocab, code, top)
-    with torch.cuda.device(device):
+    with _on(device):
         ws = _workspace(nbytes, device)
         results = torch.empty(3, *shape, dtype=torch.float32, device=device)
         stats = torch.empty(*shape, 2, dtype=torch.float32, device=device)
@@ -313,7 +324,7 @@ def token_logprobs_grad(logits, targets, result, d_logprob, d_entropy=None, out=
     d_entropy = _per_row(d_entropy, shape, torch.float32, "d_entropy")
     stats = _per_row(result.stats, (*shape, 2), torch.float32, "stats")
     entropy = _per_row(result.entropy, shape, torch.float32, "entropy")
-    with torch.cuda.device(device):
+    with _on(device):
         B.ols_token_logprobs_grad(rows, vocab, z.data_ptr(), _dtype(logits, "logits"), stride, _ptr(targets), stats.data_ptr(), entropy.data_ptr(),
                                   _ptr(d_logprob), _ptr(d_entropy), out.data_ptr(), _logit_rows(out, "out")[2], _stream(device))
     return out
@@ -330,24 +341,32 @@ def _clip(grads, max_norm, groups, out):
     out = grads if out is None else list(out)
     if len(out) != n:
         _refuse("%d outputs for %d tensors", len(out), n)
-    for t, o in zip(grads, out):
-        if t.dtype != dtype or o.dtype != dtype or t.device != device or o.device != device:
-            _refuse("the tensors must share one type and one device")
-        if not t.is_contiguous() or not o.is_contiguous() or t.shape != o.shape:
-            _refuse("the tensors must be contiguous, and outputs of their inputs' shapes")
-    order, group_array, count = range(n), None, 1
+    every = grads if out is grads else grads + out
+    place = first.get_device()
+    if any(t.dtype != dtype or t.get_device() != place for t in every):
+        _refuse("the tensors must share one type and one device")
+    if not all([t.is_contiguous() for t in every]):
+        _refuse("the tensors must be contiguous")
+    sizes = [t.numel() for t in grads]
+    if out is not grads and [t.numel() for t in out] != sizes:
+        _refuse("outputs must have their inputs' sizes")
+    order, group_array, count = None, None, 1
     if groups is not None:
-        groups = [int(g) for g in groups]
+        groups = list(map(int, groups))
         if len(groups) != n or min(groups) < 0:
             _refuse("every tensor needs the number of its group")
         count = max(groups) + 1
-        order = sorted(range(n), key=groups.__getitem__)      # stable: a group's tensors keep their order
-        group_array = (C.c_int32 * n)(*[groups[i] for i in order])
-    inputs = (C.c_void_p * n)(*[grads[i].data_ptr() for i in order])
-    numel = (C.c_int64 * n)(*[grads[i].numel() for i in order])
-    outputs = None if max_norm is None else inputs if out is grads else (C.c_void_p * n)(*[out[i].data_ptr() for i in order])
+        if any(map(operator.gt, groups, groups[1:])):
+            order = sorted(range(n), key=groups.__getitem__)      # stable: a group's tensors keep their order
+            groups, sizes = [groups[i] for i in order], [sizes[i] for i in order]
+            grads, out = [grads[i] for i in order], (None if out is grads else [out[i] for i in order])
+            out = grads if out is None else out
+        group_array = (C.c_int32 * n)(*groups)
+    inputs = (C.c_void_p * n)(*[t.data_ptr() for t in grads])
+    numel = (C.c_int64 * n)(*sizes)
+    outputs = None if max_norm is None else inputs if out is grads else (C.c_void_p * n)(*[t.data_ptr() for t in out])
     nbytes = B.ols_clip_workspace_bytes(n, numel, group_array, count)
-    with torch.cuda.device(device):
+    with _on(place):
         norms = torch.empty(count, dtype=torch.float32, device=device)
         ws = _workspace(nbytes, device)
         B.ols_clip_gradients(n, inputs, outputs, numel, group_array, count, code, 0.0 if max_norm is None else float(max_norm), norms.data_ptr(),
