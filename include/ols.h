@@ -390,6 +390,10 @@ OLS_API int ols_set_option(ols_handle h, int key, int64_t value);
 /* Local iterations completed so far (k). */
 OLS_API int64_t ols_iteration(ols_handle h);
 
+/* Which replica buffer holds the models for work enqueued on the main stream from now on: 0 x_dev, 1 x_alt_dev (the two take
+ * turns, see ols_bind), for callers that compute gradients themselves.  OLS_ESTATE while a deferred step awaits ols_sync_pull. */
+OLS_API int ols_params_buffer(ols_handle h);
+
 /* ---- instrumentation ------------------------------------------------------------------------- */
 
 /* Accumulated HIP-event timing of one kernel kind since OLS_OPT_KERNEL_TIMING was enabled.

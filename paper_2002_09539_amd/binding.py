@@ -80,6 +80,7 @@ _SIGNATURES = {
     "ols_sync": (C.c_int, [_H]),
     "ols_set_option": (C.c_int, [_H, C.c_int, C.c_int64]),
     "ols_iteration": (C.c_int64, [_H]),
+    "ols_params_buffer": (C.c_int, [_H]),
     "ols_kernel_stats": (C.c_int, [_H, C.c_int, C.POINTER(C.c_int64), C.POINTER(C.c_double)]),
     "ols_kernel_name": (C.c_char_p, [C.c_int]),
     "ols_trace_count": (C.c_int64, [_H]),
@@ -262,6 +263,10 @@ def ols_iteration(h):
     return load().ols_iteration(h)
 
 
+def ols_params_buffer(h):
+    return _bytes(load().ols_params_buffer(h))
+
+
 def ols_kernel_stats(h, kind):
     n, ms = C.c_int64(0), C.c_double(0.0)
     _check(load().ols_kernel_stats(h, kind, C.byref(n), C.byref(ms)))
@@ -298,7 +303,7 @@ def ols_clip_gradients(n, inputs, outputs, numel, group, groups, dtype, max_norm
     _check(load().ols_clip_gradients(n, inputs, outputs, numel, group, groups, dtype, max_norm, norms, ws, ws_bytes, stream))
 
 
-def _bytes(n):
+def _bytes(n):     # a size or an index, or a negative error code
     if n < 0:
         raise OlsError(int(n), last_error())
     return n

@@ -13,6 +13,12 @@
 
 namespace ols {
 
+// Orders what the lanes of one wavefront write and read in LDS, which the hardware does in the order of its instructions.
+__device__ __forceinline__ void in_wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 typedef unsigned int u4any __attribute__((ext_vector_type(4), aligned(2)));   // sixteen bytes at any element's address
 
 __device__ __forceinline__ uint16_t bf16_of(float v) { return (uint16_t)pack_bf16(v, 0.0f); }   // to nearest even

@@ -75,10 +75,11 @@ struct TileKC {
     __device__ void copy(char* lds, int at, const Cursor& c, int64_t k_left) const {
         const int wave = uniform(threadIdx.x / 64);
         const rsrc_t rs = c.window();
-        const unsigned off = chunk * 8 < k_left ? lane_off : 0x40000000u;      // past the row's end: beyond the window, zeros
+        const bool inside = chunk * 8 < k_left;               // past the row's end: beyond any window, zeros
 #pragma unroll
         for (int t = 0; t < kCopies; ++t)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(lds + (at + (t * (THREADS / 64) + wave) * 1024)), 16, (int)(off + t * step), 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(lds + (at + (t * (THREADS / 64) + wave) * 1024)), 16,
+                                                     (int)(inside ? lane_off + t * step : 0x7ffffff0u), 0, 0, 0);
     }
     // 32 rows from r0 of the tile at `at`, 16 contraction indices 16 s ..: the lane holds k = 16 s + 8 (lane / 32) + 0..7 of row
     // r0 + lane % 32
@@ -153,18 +154,24 @@ struct Epilogue {
     uint16_t *h, *h2;                   // kUp: h.  kGateGrad: da, db
 };
 
+// By the hardware's exponential and reciprocal, each good to a unit in the last place; the argument's rounding adds 2^-24 |a| to
+// the exponential's relative error where it is small against one or the activation against its slope's tail.  (With expf and a
+// correctly rounded division the epilogues were bound by the vector unit: 517 and 317 us of the two products that have one.)
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+__device__ __forceinline__ float sigmoid(float a) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-a)); }
+
 __device__ __forceinline__ float act_value(int act, float a) {
-    if (act == OLS_ACT_SILU) return a / (1.0f + expf(-a));
+    if (act == OLS_ACT_SILU) return a * sigmoid(a);
     if (act == OLS_ACT_GELU) return 0.5f * a * (1.0f + erff(a * 0.70710678118654752440f));
     return a <= 0.0f ? 0.0f : a;
 }
 __device__ __forceinline__ void act_both(int act, float a, float& value, float& slope) {
     if (act == OLS_ACT_SILU) {
-        const float g = 1.0f / (1.0f + expf(-a));
+        const float g = sigmoid(a);
         value = a * g, slope = g * (1.0f + a * (1.0f - g));
     } else if (act == OLS_ACT_GELU) {
         const float cdf = 0.5f * (1.0f + erff(a * 0.70710678118654752440f));
-        value = a * cdf, slope = cdf + a * expf(-0.5f * a * a) * 0.39894228040143267794f;
+        value = a * cdf, slope = cdf + a * exp_of(-0.5f * a * a) * 0.39894228040143267794f;
     } else {
         value = a <= 0.0f ? 0.0f : a, slope = a > 0.0f ? 1.0f : 0.0f;
     }
@@ -195,13 +202,15 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
         else store_upto8((uint16_t*)e.c + at, left, v);
     } else {
         const int64_t at = (group * e.m + m) * e.pitch + n, plane = e.m * e.pitch, at_planes = (group * P * e.m + m) * e.pitch + n;
+        const int real = (int)min((int64_t)8, e.n - n);
         float a[8], b[8], x[8], y[8];
         if constexpr (EPI == kUp) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool real = n + i < e.n;           // the padding of internal rows is zero whatever the operands hold
-                a[i] = real ? v[i] : 0.0f, b[i] = real ? second[i] : 0.0f;
-                x[i] = real ? act_value(e.act, a[i]) * b[i] : 0.0f;
+            for (int i = 0; i < 8; ++i) a[i] = v[i], b[i] = second[i], x[i] = act_value(e.act, v[i]) * second[i];
+            if (real < 8) {                              // the padding of internal rows is zero whatever the operands hold
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i >= real) a[i] = b[i] = x[i] = 0.0f;
             }
             if (e.a) {
                 store8(e.a + at, a);
@@ -213,11 +222,14 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
             load8(e.b + at, b);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool real = n + i < e.n;
                 float value, slope;
                 act_both(e.act, a[i], value, slope);
-                x[i] = real ? v[i] * b[i] * slope : 0.0f;
-                y[i] = real ? v[i] * value : 0.0f;
+                x[i] = v[i] * b[i] * slope, y[i] = v[i] * value;
+            }
+            if (real < 8) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i >= real) x[i] = y[i] = 0.0f;
             }
             store_planes<SPLIT>(e.h + at_planes, plane, x);
             store_planes<SPLIT>(e.h2 + at_planes, plane, y);
@@ -449,7 +461,7 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
                 const int chunk = 8 * t + 2 * g + lane / 32;
                 *(f4*)(stage + lane_row * kCols + 4 * (chunk ^ (lane_row & 15))) = f4{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
             }
-        __builtin_amdgcn_wave_barrier();                  // written and read by one wavefront: LDS keeps its order
+        in_wave_order();                                  // written and read by one wavefront: LDS keeps its order
 #pragma unroll 1
         for (int r0 = 0; r0 < 32; r0 += kRows) {
             const int r = r0 + out_row;
@@ -472,7 +484,7 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
                 emit<EPI, SPLIT>(q.epi, at.group, at.m0 + row, at.n0 + col, v[0], v[PANELS - 1]);
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        in_wave_order();
     }
 }
 

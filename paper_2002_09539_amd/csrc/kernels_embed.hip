@@ -131,7 +131,7 @@ __device__ void scatter_block(const SortParams& p, int group, const Items& t, in
         digit[k] = (t.key[k] >> p.shift) & (kDigits - 1);
         same[k] = same_digit(digit[k], t.valid[k]);
         if (t.valid[k] && (same[k] & ((1ull << lane) - 1)) == 0) cnt[wave][digit[k]] += __popcll(same[k]);
-        __builtin_amdgcn_wave_barrier();
+        in_wave_order();
     }
     __syncthreads();
     for (int d = threadIdx.x; d < kDigits; d += kSortThreads) {
@@ -152,9 +152,9 @@ __device__ void scatter_block(const SortParams& p, int group, const Items& t, in
             p.pos_out[at] = t.pos[k];
         }
         // every lane has read the counter before the first of its digit moves it on (one wavefront, in step)
-        __builtin_amdgcn_wave_barrier();
+        in_wave_order();
         if (t.valid[k] && rank == 0) cnt[wave][digit[k]] += __popcll(same[k]);
-        __builtin_amdgcn_wave_barrier();
+        in_wave_order();
     }
     __syncthreads();
 }

@@ -1943,6 +1943,13 @@ int ols_set_option(ols_handle c, int key, int64_t value) {
 
 int64_t ols_iteration(ols_handle c) { return c ? c->k : -1; }
 
+int ols_params_buffer(ols_handle c) {
+    if (int rc = need(c)) return rc;
+    if (!c->bound || !c->inited) return fail(OLS_ESTATE, "ols_bind and ols_init_params must precede ols_params_buffer");
+    if (c->pending_update) return fail(OLS_ESTATE, "a deferred local step has not been applied: ols_sync_pull is due");
+    return c->cur;
+}
+
 int ols_kernel_stats(ols_handle c, int kind, int64_t* launches, double* total_ms) {
     if (int rc = need(c)) return rc;
     if (kind < 0 || kind >= OLS_K_COUNT) return fail(OLS_EINVAL, "bad kernel kind");

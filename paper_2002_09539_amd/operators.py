@@ -33,10 +33,11 @@ def _dtype(t, name):
 
 def _on_gpu(first, *others):
     """The device that all tensors are on."""
-    if not first.is_cuda:
+    place = first.get_device()
+    if place < 0:
         _refuse("tensors must be on the GPU: there is no CPU path")
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != place:
             _refuse("tensors are on %s and %s", first.device, t.device)
     return first.device
 
@@ -51,17 +52,19 @@ def _on(device):
 
 
 def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+    """The handle of torch's current stream (torch.cuda.current_stream(device).cuda_stream without the object)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _rows(t, name):
     """(worker stride, row stride) of a [m][rows][width] tensor whose rows are contiguous."""
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    m, rows, width = t.shape
+    group, row, step = t.stride()
+    if step != 1 and width > 1:
         _refuse("%s: the elements of a row must be contiguous", name)
-    if t.numel() == 0:
-        return 0, max(1, t.shape[2])
-    row = t.stride(1) if t.shape[1] > 1 else max(t.shape[2], t.stride(1))
-    return (t.stride(0) if t.shape[0] > 1 else 0), row
+    if m * rows * width == 0:
+        return 0, max(1, width)
+    return (group if m > 1 else 0), (row if rows > 1 else max(width, row))
 
 
 def _workspace(nbytes, device):
@@ -147,9 +150,12 @@ _ACT = {"silu": B.OLS_ACT_SILU, "gelu": B.OLS_ACT_GELU, "relu": B.OLS_ACT_RELU}
 
 def _matrix(t, m, shape, name):
     """A tensor as the C boundary takes it: [m][rows][cols], without the worker axis [rows][cols] shared by the workers."""
-    if tuple(t.shape) not in ((m, *shape), shape) or (t.dim() == 2 and name not in _SHARED and m > 1):
-        _refuse("%s must be of shape %s, got %s", name, (m, *shape), tuple(t.shape))
-    group, row = _rows(t if t.dim() == 3 else t.unsqueeze(0), name)
+    have = tuple(t.shape)
+    if have == shape and (m == 1 or name in _SHARED):
+        t = t.unsqueeze(0)
+    elif have != (m, *shape):
+        _refuse("%s must be of shape %s, got %s", name, (m, *shape), have)
+    group, row = _rows(t, name)
     return B.ols_matrix(t.data_ptr(), row, group)
 
 

@@ -8,6 +8,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from . import operators
 
 
 def _ptr(t):
@@ -125,6 +126,16 @@ class Session:
     def set_gradient(self, g):
         assert g.is_contiguous() and tuple(g.shape) == (self.m, self.ld) and g.dtype == torch.float32
         B.ols_set_gradient(self.h, _ptr(g))
+
+    def models(self):
+        """[m][ld]: the replica buffer that holds the models now (for gradients computed outside the library)."""
+        return self.x_alt if B.ols_params_buffer(self.h) else self.x
+
+    def clip_gradients(self, max_norm):
+        """Scales every worker's gradient row to a norm of at most max_norm, on the main stream, before local_step; returns
+        the m norms before that (a device tensor)."""
+        with torch.cuda.stream(self.main):
+            return operators.clip_grad_norm([row[: self.d] for row in self.g], max_norm, groups=range(self.m))
 
     def local_step(self):
         B.ols_local_step(self.h)
