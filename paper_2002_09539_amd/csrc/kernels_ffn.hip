@@ -26,17 +26,19 @@ constexpr int kFewThreads = 256;
 constexpr int kFewCols = 64;         // columns of a workgroup: a line of 128 bytes of bf16 weights
 constexpr int kFewSlab = 1024;       // contraction indices whose inputs lie in LDS at a time
 
-struct PackParams {
+struct PackJob {
     const void* src;
     int64_t row, group, rows, cols, cols8, pitch;
     uint16_t* dst;                   // [group][plane][rows][pitch]
+    int dtype, groups;
+};
+constexpr int kMaxPacks = 5;
+struct PackParams {                  // all operands of a call in one launch
+    PackJob job[kMaxPacks];
 };
 
 template <typename T, bool SPLIT>
-__global__ __launch_bounds__(256) void pack_kernel(PackParams p) {
-    const int64_t units = p.cols8 / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= p.rows * units) return;
-    const int64_t r = i / units, c = i % units * 8, g = blockIdx.y;
+__device__ __forceinline__ void pack_unit(const PackJob& p, int64_t g, int64_t r, int64_t c) {
     float v[8];
     load_upto8((const T*)p.src + g * p.group + r * p.row + c, (int)min((int64_t)8, p.cols - c), 0.0f, v);
     constexpr int P = SPLIT ? 3 : 1;
@@ -49,6 +51,16 @@ __global__ __launch_bounds__(256) void pack_kernel(PackParams p) {
     } else {
         store8(out, v);
     }
+}
+
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void pack_kernel(PackParams all) {
+    const PackJob& p = all.job[blockIdx.z];
+    const int64_t units = p.cols8 / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
+    if (i >= p.rows * units || g >= p.groups) return;
+    const int64_t r = i / units, c = i % units * 8;
+    if (SPLIT || p.dtype == OLS_F32) pack_unit<float, SPLIT>(p, g, r, c);
+    else pack_unit<uint16_t, SPLIT>(p, g, r, c);
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------------
@@ -186,7 +198,8 @@ struct Maker {                         // lays operands out; without a stream it
     Arena& ws;
     hipStream_t stream;
     bool go;
-    hipError_t err = hipSuccess;
+    PackParams packs = {};
+    int n_packs = 0;
     bool split() const { return f.dtype == OLS_F32; }
     int planes() const { return split() ? 3 : 1; }
 
@@ -201,15 +214,21 @@ struct Maker {                         // lays operands out; without a stream it
         const int groups = m.group == 0 ? 1 : f.groups;      // shared by the workers: laid out once
         uint16_t* dst = (uint16_t*)ws.take(2 * per * planes() * groups);
         v.p = dst, v.plane = per, v.group = groups == 1 ? 0 : per * planes();
-        if (go && err == hipSuccess) {
-            const PackParams p{m.dev, m.row, m.group, outer, inner, v.inner8, v.pitch, dst};
-            const dim3 grid((unsigned)((outer * (v.inner8 / 8) + 255) / 256), groups);
-            if (split()) pack_kernel<float, true><<<grid, 256, 0, stream>>>(p);
-            else if (dtype == OLS_F32) pack_kernel<float, false><<<grid, 256, 0, stream>>>(p);
-            else pack_kernel<uint16_t, false><<<grid, 256, 0, stream>>>(p);
-            err = hipGetLastError();
-        }
+        packs.job[n_packs++] = PackJob{m.dev, m.row, m.group, outer, inner, v.inner8, v.pitch, dst, dtype, groups};
         return v;
+    }
+    hipError_t lay_out() const {       // the operands asked for
+        if (!go || n_packs == 0) return hipSuccess;
+        int64_t units = 0;
+        int groups = 1;
+        for (int i = 0; i < n_packs; ++i) {
+            units = std::max(units, packs.job[i].rows * (packs.job[i].cols8 / 8));
+            groups = std::max(groups, packs.job[i].groups);
+        }
+        const dim3 grid((unsigned)((units + 255) / 256), groups, n_packs);
+        if (split()) pack_kernel<true><<<grid, 256, 0, stream>>>(packs);
+        else pack_kernel<false><<<grid, 256, 0, stream>>>(packs);
+        return hipGetLastError();
     }
     // gate and up are read with one pitch: where theirs differ, both are laid out
     bool pair_lies() const {
@@ -260,24 +279,26 @@ int64_t count_tiles(const Job* jobs, int n, int groups, int panels, int t) {
 // few run, 0.4 with one on every compute unit and 0.6 with two (tiles of 128); 0.75 to 0.95 with one tile of 256.  Examples,
 // 2048 x 1024 over 2816: tiles of 128 whole 40.4 us, cut in 2 / 4 / 8: 31.7 / 32.3 / 45.3; of 256, 74.6 whole, cut in 4 / 8: 38.6 / 40.2.
 // 2048 x 5632 over 1024: tiles of 128 39.0, of 256 36.2.  64 x 1024 over 4096: tiles of 128 whole 41.4, cut in 16: 12.8.
-double estimate(const Shape& s, int64_t slices) {
+// An epilogue with an activation takes a tile 10 to 25 us more, and less where it is done by the launch that joins ranges
+// (three ragged fp32 workers, 201 x 517 over 131, Gaussian: 39.7 us whole).
+double estimate(const Shape& s, int64_t slices, bool activation) {
     const int64_t slots = s.t == 256 ? kCus : 2 * kCus;
     auto slice_us = [&](double blocks) {
         const double one = std::min(1.0, blocks / kCus), two = std::min(1.0, std::max(0.0, blocks / kCus - 1.0));
         return s.t == 256 ? 0.75 + 0.2 * one : 0.3 + 0.1 * one + 0.2 * two;
     };
-    const double ends = s.t == 256 ? 8.0 : 4.0;
+    const double ends = s.t == 256 ? 8.0 : 4.0, act = activation ? 12.0 : 0.0;
     double us = 0.0;
-    if (s.whole) us += (double)((s.whole + slots - 1) / slots) * (slices * slice_us((double)std::min((int64_t)s.whole, slots)) + ends);
+    if (s.whole) us += (double)((s.whole + slots - 1) / slots) * (slices * slice_us((double)std::min((int64_t)s.whole, slots)) + ends + act);
     if (s.rest) {
         const double blocks = (double)s.rest * s.ranges;
-        us += ((double)slices / s.ranges + 0.5) * slice_us(blocks) + ends + 5.0 + blocks * s.t * s.t * 4.0 / 8e6;
+        us += ((double)slices / s.ranges + 0.5) * slice_us(blocks) + ends + 5.0 + act / 4 + blocks * s.t * s.t * 4.0 / 8e6;
     }
     return us;
 }
 
 // The tile, and whether the contractions of the tiles that fill no whole round are cut.
-Shape choose(const Job* jobs, int n, int groups, int panels, bool split) {
+Shape choose(const Job* jobs, int n, int groups, int panels, bool split, bool activation) {
     int64_t slices = (int64_t)1 << 40, work = 1;
     for (int i = 0; i < n; ++i) {
         slices = std::min(slices, tiles_of(jobs[i].K, kBK));
@@ -292,9 +313,9 @@ Shape choose(const Job* jobs, int n, int groups, int panels, bool split) {
             Shape s{t, (int)tiles, 0, 1};
             if (ranges > 1) {
                 s.whole = (int)(tiles / slots * slots), s.rest = (int)(tiles - s.whole), s.ranges = ranges;
-                if (s.rest == 0 || slices / ranges < 4 || (int64_t)s.rest * ranges > slots) continue;
+                if (s.rest == 0 || slices < ranges || work / ranges < 4 || (int64_t)s.rest * ranges > slots) continue;
             }
-            const double us = estimate(s, work);
+            const double us = estimate(s, work, activation);
             if (us < best_us) best = s, best_us = us;
         }
     }
@@ -305,7 +326,7 @@ template <bool A_RC, bool B_RC, Epi EPI>
 hipError_t product(Job* jobs, int n, int groups, bool split, Arena& ws, bool go, hipStream_t stream) {
     constexpr int PANELS = EPI == kUp ? 2 : 1;
     if (n == 0) return hipSuccess;
-    const Shape shape = choose(jobs, n, groups, PANELS, split);
+    const Shape shape = choose(jobs, n, groups, PANELS, split, EPI != kStore);
     const int t = shape.t;
     if (t == 0) return hipErrorInvalidValue;              // more tiles than a launch numbers
     GemmArgs p = {};
@@ -422,7 +443,8 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
     const View wg = mk.operand(f.w_gate, f.weight_dtype, f.width, f.hidden, mk.pair_lies());
     const View wu = mk.operand(f.w_up, f.weight_dtype, f.width, f.hidden, mk.pair_lies());
     const View wd = mk.operand(f.w_down, f.weight_dtype, f.hidden, f.out, true);
-    if (mk.err != hipSuccess) return mk.err;
+    hipError_t e = mk.lay_out();
+    if (e != hipSuccess) return e;
     const Saved s = saved_layout(f);
     char* saved = (char*)f.saved;
     void* hp = saved ? (void*)(saved + s.off_h) : ws.take(mk.internal_bytes(f.rows, f.hidden));
@@ -433,7 +455,7 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
     set_segments(up, x, wg, nullptr, &wu, mk.split());
     up.epi.n = f.hidden, up.epi.n8 = h8, up.epi.pitch = internal_pitch(f.hidden), up.epi.m = f.rows, up.epi.act = f.act;
     up.epi.a = saved ? (float*)(saved + s.off_a) : nullptr, up.epi.b = saved ? (float*)(saved + s.off_b) : nullptr, up.epi.h = (uint16_t*)hp;
-    hipError_t e = product<false, true, kUp>(&up, 1, f.groups, mk.split(), ws, go, stream);
+    e = product<false, true, kUp>(&up, 1, f.groups, mk.split(), ws, go, stream);
     if (e != hipSuccess) return e;
     Job down = {};
     down.M = f.rows, down.N = f.out, down.K = f.hidden;
@@ -480,9 +502,9 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         wg = mk.operand(f.w_gate, f.weight_dtype, f.width, f.hidden, mk.pair_lies());
         wu = mk.operand(f.w_up, f.weight_dtype, f.width, f.hidden, mk.pair_lies());
     }
-    if (mk.err != hipSuccess) return mk.err;
+    hipError_t e = mk.lay_out();
+    if (e != hipSuccess) return e;
     View da, db;
-    hipError_t e = hipSuccess;
     if (to_up) {
         void* pa = ws.take(mk.internal_bytes(f.rows, f.hidden));
         void* pb = ws.take(mk.internal_bytes(f.rows, f.hidden));
