@@ -299,7 +299,7 @@ def ols_token_logprobs_grad(*args):
 
 
 def ols_clip_gradients(n, inputs, outputs, numel, group, groups, dtype, max_norm, norms, ws, ws_bytes, stream):
-    """inputs, outputs, numel, group: ctypes arrays of n entries (outputs, group: or None)."""
+    """inputs, outputs, numel, group: addresses of host arrays of n entries (outputs, group: or None)."""
     _check(load().ols_clip_gradients(n, inputs, outputs, numel, group, groups, dtype, max_norm, norms, ws, ws_bytes, stream))
 
 

@@ -32,8 +32,8 @@ constexpr int kSortItems = 4096;            // ids of one workgroup of the sort
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kPerWave = kSortItems / kSortWaves, kPerLane = kPerWave / 64;
-constexpr int kRun = 32;                    // sorted positions of a run
-constexpr int kRowsPerBlock = 32;           // table rows of a workgroup of the last stage: eight per wavefront
+constexpr int kRun = 16;                    // sorted positions of a run
+constexpr int kRowsPerWave = 8;             // table rows of a wavefront of the last stage
 
 template <typename TI, typename TO>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedParams p, int lanes) {
@@ -259,8 +259,8 @@ struct RowsParams {
 };
 
 // Rows whose loads are in flight together.
-template <typename T>
-constexpr int row_batch() { return sizeof(T) == 2 ? 8 : 4; }
+template <typename T, int NV>
+constexpr int row_batch() { return sizeof(T) * NV <= 4 ? 8 : 4; }
 
 // Columns c + 512 t + 8 lane .. of a row of the gradient.
 template <typename TO, int NV>
@@ -286,7 +286,7 @@ __device__ __forceinline__ void write_row(const RowsParams& q, int64_t group, in
 
 template <typename TI, typename TO, int NV>
 __global__ __launch_bounds__(kThreads) void embed_runs_kernel(RowsParams q) {
-    constexpr int B = row_batch<TI>();
+    constexpr int B = row_batch<TI, NV>();
     static_assert(kRun % B == 0 && kRun < 64, "whole batches, and a lane per position");
     const int lane = threadIdx.x % 64;
     const int64_t run = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = blockIdx.y;
@@ -351,17 +351,21 @@ __global__ __launch_bounds__(kThreads) void embed_runs_kernel(RowsParams q) {
 
 template <typename TO, int NV>
 __global__ __launch_bounds__(kThreads) void embed_rows_kernel(RowsParams q) {
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int64_t v0 = (int64_t)blockIdx.x * kRowsPerBlock + wave * (kRowsPerBlock / 4), group = blockIdx.y, vocab = q.g.vocab;
+    // a wavefront's rows lie far apart: the frequent ids, whose sums take longest, are mostly neighbours
+    const int lane = threadIdx.x % 64;
+    const int64_t waves = (int64_t)gridDim.x * (kThreads / 64), v0 = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t group = blockIdx.y, vocab = q.g.vocab;
     const int32_t* b = q.bounds + group * 2 * vocab;
-    const bool mine = lane < kRowsPerBlock / 4 && v0 + lane < vocab;
-    const int first = mine ? b[v0 + lane] : 0, last = mine ? b[vocab + v0 + lane] : 0;
+    const bool mine = lane < kRowsPerWave && v0 + lane * waves < vocab;
+    const int first = mine ? b[v0 + lane * waves] : 0, last = mine ? b[vocab + v0 + lane * waves] : 0;
     const int64_t c = (int64_t)blockIdx.z * 512 * NV;
-    for (int r = 0; r < kRowsPerBlock / 4 && v0 + r < vocab; ++r) {
+    for (int r = 0; r < kRowsPerWave; ++r) {
+        const int64_t v = v0 + r * waves;
+        if (v >= vocab) break;
         const int from = __builtin_amdgcn_readlane(first, r), to = __builtin_amdgcn_readlane(last, r);
         if (to == 0) {
             if (q.g.accumulate) continue;
-            TO* out = (TO*)q.g.grad + group * q.g.grad_group + (v0 + r) * q.g.grad_row;
+            TO* out = (TO*)q.g.grad + group * q.g.grad_group + v * q.g.grad_row;
             const int64_t end = min(q.g.width, c + 512 * NV);
             constexpr int kVec = 16 / sizeof(TO);
             for (int64_t at = c + lane * kVec; at < end; at += 64 * kVec) {
@@ -394,7 +398,7 @@ __global__ __launch_bounds__(kThreads) void embed_rows_kernel(RowsParams q) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum[t][e] += p[j][t][e];
         }
-        write_row<TO, NV>(q, group, v0 + r, c, lane, sum);
+        write_row<TO, NV>(q, group, v, c, lane, sum);
     }
 }
 
@@ -424,7 +428,7 @@ void launch_sums(const RowsParams& q, hipStream_t stream) {
     const int tiles = (int)((q.g.width + 512 * NV - 1) / (512 * NV));
     if (q.runs)
         embed_runs_kernel<TI, TO, NV><<<dim3((unsigned)((q.runs + 3) / 4), q.g.groups, tiles), kThreads, 0, stream>>>(q);
-    embed_rows_kernel<TO, NV><<<dim3((unsigned)((q.g.vocab + kRowsPerBlock - 1) / kRowsPerBlock), q.g.groups, tiles), kThreads, 0, stream>>>(q);
+    embed_rows_kernel<TO, NV><<<dim3((unsigned)((q.g.vocab + 4 * kRowsPerWave - 1) / (4 * kRowsPerWave)), q.g.groups, tiles), kThreads, 0, stream>>>(q);
 }
 
 template <typename TI, typename TO>

@@ -7,8 +7,7 @@ weights and gradients can be views of the rows of a Session's x and g; rows may 
 Tensors that were made on another stream are the caller's to order and to record, as with any torch operation.
 """
 import contextlib
-import ctypes as C
-import operator
+from array import array
 from collections import namedtuple
 
 import torch
@@ -349,7 +348,7 @@ def _clip(grads, max_norm, groups, out):
         _refuse("%d outputs for %d tensors", len(out), n)
     every = grads if out is grads else grads + out
     place = first.get_device()
-    if any(t.dtype != dtype or t.get_device() != place for t in every):
+    if {t.dtype for t in every} != {dtype} or {t.get_device() for t in every} != {place}:
         _refuse("the tensors must share one type and one device")
     if not all([t.is_contiguous() for t in every]):
         _refuse("the tensors must be contiguous")
@@ -358,24 +357,24 @@ def _clip(grads, max_norm, groups, out):
         _refuse("outputs must have their inputs' sizes")
     order, group_array, count = None, None, 1
     if groups is not None:
-        groups = list(map(int, groups))
+        groups = list(groups)
         if len(groups) != n or min(groups) < 0:
             _refuse("every tensor needs the number of its group")
         count = max(groups) + 1
-        if any(map(operator.gt, groups, groups[1:])):
+        if sorted(groups) != groups:
             order = sorted(range(n), key=groups.__getitem__)      # stable: a group's tensors keep their order
             groups, sizes = [groups[i] for i in order], [sizes[i] for i in order]
             grads, out = [grads[i] for i in order], (None if out is grads else [out[i] for i in order])
             out = grads if out is None else out
-        group_array = (C.c_int32 * n)(*groups)
-    inputs = (C.c_void_p * n)(*[t.data_ptr() for t in grads])
-    numel = (C.c_int64 * n)(*sizes)
-    outputs = None if max_norm is None else inputs if out is grads else (C.c_void_p * n)(*[t.data_ptr() for t in out])
-    nbytes = B.ols_clip_workspace_bytes(n, numel, group_array, count)
+        group_array = array("i", groups)
+    inputs, numel = array("Q", [t.data_ptr() for t in grads]), array("q", sizes)
+    outputs = None if max_norm is None else inputs if out is grads else array("Q", [t.data_ptr() for t in out])
+    at = lambda a: None if a is None else a.buffer_info()[0]  # noqa: E731
+    nbytes = B.ols_clip_workspace_bytes(n, at(numel), at(group_array), count)
     with _on(place):
         norms = torch.empty(count, dtype=torch.float32, device=device)
         ws = _workspace(nbytes, device)
-        B.ols_clip_gradients(n, inputs, outputs, numel, group_array, count, code, 0.0 if max_norm is None else float(max_norm), norms.data_ptr(),
+        B.ols_clip_gradients(n, at(inputs), at(outputs), at(numel), at(group_array), count, code, 0.0 if max_norm is None else float(max_norm), norms.data_ptr(),
                              _ptr(ws), nbytes, _stream(device))
     return norms
 
