@@ -17,10 +17,12 @@
 // Each of a slice's two steps first requests the next step's fragments, the second one those of the next slice, in front of
 // which stands the only barrier of a slice.
 //
-// What bounds it, measured on 8192 x 2048 x 11264 (K contiguous in both): without the copies, on what lies in LDS, 1300 to
-// 1440 TFLOP/s; without the products 1200 with tiles of 256 x 128 and two thirds of the bytes with 256 x 256; together 1137.
-// Tiles of 256 x 128, two workgroups a compute unit: 974.  Two buffers of 64 indices: 1107 to 1123.  Four wavefronts of
-// 128 x 128, one a SIMD: 750.  A library's product of this size runs at 1100 to 1370.
+// What bounds it, measured warm on products of 8192 rows, 2048 by 5632 (K contiguous in both operands, unless stated): without
+// the copies, on what lies in LDS, 1440 TFLOP/s; the copies alone, at 1.5 times the bytes of a 256 x 256 tile, take as long as
+// 1200 would; together 1110 (1160 with the second operand RC).  Tiles of 256 x 128, two workgroups a compute unit: 974.  Two
+// buffers of 64 indices: 1107.  Four wavefronts of 128 x 128, one a SIMD: a quarter slower than eight.  Wavefront priorities,
+// fragment reads spread between the MFMAs, other orders of tiles, rotated starts, rows apart by other than their length: nothing,
+// or less.  A library's product of these sizes runs at 1100 to 1370.
 //
 // Results pass through LDS on their way out: what a lane holds after the MFMAs are four columns of a row, and memory wants
 // whole lines (with 8-byte pieces, the product with the gradients' epilogue ran at 410 TFLOP/s instead of 540).
@@ -416,8 +418,8 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
         __builtin_amdgcn_s_waitcnt(0x0078);               // vmcnt(8) lgkmcnt(0)
         barrier();
         fetch(next, 0);
-        copy(lds);
         multiply(1);
+        copy(lds);                                        // behind the products: 4 to 6 % of the products that read RC tiles
         __builtin_amdgcn_sched_barrier(0);
     };
     copy(buf0);

@@ -168,11 +168,6 @@ int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
-// Elements between the rows of internal tensors.  Rows of 5632 elements side by side put what the tiles read at one time on a
-// few channels of the L2 (the product for dx, 8192 x 2048 over twice 5632: 909 TFLOP/s; with 64 / 192 elements between the rows
-// 1079 / 1137, with 128 to 1024 about the latter).
-int64_t internal_pitch(int64_t n) { return n < 1024 ? up8(n) : (n + 63) / 64 * 64 + 192; }
-
 struct Arena {
     char* base;
     int64_t at = 0;
@@ -205,7 +200,7 @@ struct Maker {                         // lays operands out; without a stream it
 
     View operand(const ols_matrix& m, int dtype, int64_t outer, int64_t inner, bool may_lie) {
         View v;
-        v.inner8 = up8(inner), v.pitch = internal_pitch(inner);
+        v.inner8 = up8(inner), v.pitch = up8(inner);
         if (may_lie && !split() && lies_well(m, dtype, inner)) {
             v.p = (const uint16_t*)m.dev, v.pitch = m.row, v.group = m.group;
             return v;
@@ -236,10 +231,10 @@ struct Maker {                         // lays operands out; without a stream it
     }
     View internal(int64_t rows, int64_t inner, void* at) const {
         View v;
-        v.inner8 = up8(inner), v.pitch = internal_pitch(inner), v.plane = rows * v.pitch, v.group = planes() * v.plane, v.p = (const uint16_t*)at;
+        v.inner8 = up8(inner), v.pitch = up8(inner), v.plane = rows * v.pitch, v.group = planes() * v.plane, v.p = (const uint16_t*)at;
         return v;
     }
-    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * planes() * f.groups * rows * internal_pitch(inner); }
+    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * planes() * f.groups * rows * up8(inner); }
 };
 
 // the planes' products, largest first
@@ -384,7 +379,7 @@ struct Saved {
     int64_t off_a, off_b, off_h, bytes;
 };
 Saved saved_layout(const ols_ffn& f) {
-    const int64_t elems = f.groups * f.rows * internal_pitch(f.hidden);
+    const int64_t elems = f.groups * f.rows * up8(f.hidden);
     Saved s;
     s.off_a = 0;
     s.off_b = up256(elems * 4);
@@ -453,7 +448,7 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
     Job up = {};
     up.M = f.rows, up.N = f.hidden, up.K = f.width;
     set_segments(up, x, wg, nullptr, &wu, mk.split());
-    up.epi.n = f.hidden, up.epi.n8 = h8, up.epi.pitch = internal_pitch(f.hidden), up.epi.m = f.rows, up.epi.act = f.act;
+    up.epi.n = f.hidden, up.epi.n8 = h8, up.epi.pitch = up8(f.hidden), up.epi.m = f.rows, up.epi.act = f.act;
     up.epi.a = saved ? (float*)(saved + s.off_a) : nullptr, up.epi.b = saved ? (float*)(saved + s.off_b) : nullptr, up.epi.h = (uint16_t*)hp;
     e = product<false, true, kUp>(&up, 1, f.groups, mk.split(), ws, go, stream);
     if (e != hipSuccess) return e;
@@ -512,7 +507,7 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         Job dh = {};
         dh.M = f.rows, dh.N = f.hidden, dh.K = f.out;
         set_segments(dh, dy, wd, nullptr, nullptr, mk.split());
-        dh.epi.n = f.hidden, dh.epi.n8 = h8, dh.epi.pitch = internal_pitch(f.hidden), dh.epi.m = f.rows, dh.epi.act = f.act;
+        dh.epi.n = f.hidden, dh.epi.n8 = h8, dh.epi.pitch = up8(f.hidden), dh.epi.m = f.rows, dh.epi.act = f.act;
         dh.epi.a = (float*)(saved + s.off_a), dh.epi.b = (float*)(saved + s.off_b), dh.epi.h = (uint16_t*)pa, dh.epi.h2 = (uint16_t*)pb;
         e = product<false, false, kGateGrad>(&dh, 1, f.groups, mk.split(), ws, go, stream);
         if (e != hipSuccess) return e;
