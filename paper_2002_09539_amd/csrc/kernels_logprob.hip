@@ -15,6 +15,11 @@
 // followed by its gradient.  Rows that no workgroup holds, and rows too few to fill the device, are cut into parts whose
 // statistics and best k a second launch joins.
 //
+// The logits stay packed as they were read and are unpacked anew by each pass (kept as fp32 from pass to pass they spill: 1.25 ms
+// instead of 0.43 below).  8192 rows of 50 001 bf16 logits, loss and gradient: 430 us (3.8 TB/s; 396 with rows of 50 000, which
+// start on whole vectors, and 4.85 TB/s with 32 000).  1531 rows of 32 003 bf16 with five alternatives: 34 us, 26 without.  Four
+// rows of 128 000 fp32 with eight: 8 us in 252 parts, 7 to join them.
+//
 // Best k: the k-th largest of the lanes' maxima is a bound that at least k logits reach and that few others do: fewer
 // than k lanes hold anything above it.  Those above it go to a list in LDS; of those equal to it a wavefront needs only
 // its first k in index order.  Every listed logit then counts the listed ones that beat it (larger, or equal and
