@@ -4,9 +4,8 @@
 // that the block needs.  An operand is a matrix of 16-byte aligned rows; it is read either
 //   * "KC": the contraction index is the contiguous one (memory [rows][K]), or
 //   * "RC": the operand's own index is (memory [K][rows]), transposed by the LDS read.
-// Segments make fp32 products out of bf16 ones: an fp32 operand is three bf16 planes that add up to it exactly, and the six
-// largest of the nine products of planes are six segments of one longer contraction (split_bf16.h says why six are enough).
-// The gradient at the block's input, da Wg^T + db Wu^T, is two segments as well.
+// The gradient at the block's input, da Wg^T + db Wu^T, is two segments of one contraction.  Products of fp32 operands are
+// in ffn_gemm_f32.h, on the same tiles, jobs and epilogues.
 //
 // A tile's slices of 32 contraction indices go from memory straight into LDS (16 bytes a lane, no registers in between),
 // into a ring of four buffers: three slices are under way while one is multiplied.  The direct copy writes a wavefront's
@@ -38,7 +37,6 @@ namespace ffn {
 constexpr int kBK = 32;              // contraction indices of a slice
 constexpr int kRing = 4;             // buffers
 constexpr int kXcds = 8;
-constexpr int kMaxSegments = 12;
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
@@ -147,7 +145,7 @@ struct Epilogue {
     int64_t c_row, c_group;
     int c_f32;
     // kUp: a and b (where they are kept) and h are written; kGateGrad: a and b are read, da and db are written.  Internal
-    // tensors have rows of n8 elements, pitch apart; those of planes have [plane][m][pitch] per group.
+    // tensors have rows of n8 elements, pitch apart, h and its gradients three times that where they are kept as terms.
     int act;
     int64_t m, n8, pitch;
     // a and b stay fp32 in a bf16 block as well: rounded to bf16 they would put the weights' gradients at 1.8 times the error of
@@ -179,16 +177,16 @@ __device__ __forceinline__ void act_both(int act, float a, float& value, float& 
     }
 }
 
-// eight elements of an internal tensor: one bf16 plane, or the three that add up to the fp32 values
+// eight elements of an internal tensor: bf16, or the three terms that add up to the fp32 values, side by side
 template <bool SPLIT>
-__device__ __forceinline__ void store_planes(uint16_t* p, int64_t plane, const float (&v)[8]) {
+__device__ __forceinline__ void store_terms(uint16_t* p, const float (&v)[8]) {
     if constexpr (!SPLIT) {
         *(u4*)p = u4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     } else {
         const Split8 s = split8(f4{v[0], v[1], v[2], v[3]}, f4{v[4], v[5], v[6], v[7]});
         *(u4*)p = s.hi;
-        *(u4*)(p + plane) = s.mid;
-        *(u4*)(p + 2 * plane) = s.lo;
+        *(u4*)(p + 8) = s.mid;
+        *(u4*)(p + 16) = s.lo;
     }
 }
 
@@ -203,7 +201,7 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
         if (e.c_f32) store_upto8((float*)e.c + at, left, v);
         else store_upto8((uint16_t*)e.c + at, left, v);
     } else {
-        const int64_t at = (group * e.m + m) * e.pitch + n, plane = e.m * e.pitch, at_planes = (group * P * e.m + m) * e.pitch + n;
+        const int64_t at = (group * e.m + m) * e.pitch + n;
         const int real = (int)min((int64_t)8, e.n - n);
         float a[8], b[8], x[8], y[8];
         if constexpr (EPI == kUp) {
@@ -218,7 +216,7 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
                 store8(e.a + at, a);
                 store8(e.b + at, b);
             }
-            store_planes<SPLIT>(e.h + at_planes, plane, x);
+            store_terms<SPLIT>(e.h + P * at, x);
         } else {
             load8(e.a + at, a);
             load8(e.b + at, b);
@@ -233,8 +231,8 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
                 for (int i = 0; i < 8; ++i)
                     if (i >= real) x[i] = y[i] = 0.0f;
             }
-            store_planes<SPLIT>(e.h + at_planes, plane, x);
-            store_planes<SPLIT>(e.h2 + at_planes, plane, y);
+            store_terms<SPLIT>(e.h + P * at, x);
+            store_terms<SPLIT>(e.h2 + P * at, y);
         }
     }
 }
@@ -245,9 +243,8 @@ struct Job {
     const uint16_t *a, *b, *b2;          // b2: kUp's second panel, or the second tensor of segments that say so
     int64_t a_group, b_group, b2_group, a_pitch, b_pitch;
     int64_t M, N, K, a_inner8, b_inner8; // inner extents of the operands as stored, up to 8 elements
-    int64_t seg_a[kMaxSegments], seg_b[kMaxSegments];
-    unsigned seg_second;                 // bit s: segment s takes b2
-    int segments, big;                   // the first `big` segments hold the large products
+    int64_t second_a;                    // from a to the second segment's operand
+    int segments;                        // 1, or 2: the second one takes b2
     int tiles_m, tiles_n;
     Epilogue epi;
 };
@@ -282,11 +279,69 @@ __device__ __forceinline__ TilePlace place_of(const GemmArgs& p, int tile, int b
     return t;
 }
 
+// The tile of a workgroup, and the range of its contraction (-1: all of it).  The hardware deals workgroup b to XCD b % 8: each XCD
+// takes a contiguous range of tiles, whose operands its L2 keeps.
+__device__ __forceinline__ int tile_of_block(const GemmArgs& p, int& range) {
+    range = -1;
+    if ((int)blockIdx.x < p.whole) {
+        const int per = (p.whole + kXcds - 1) / kXcds, full = p.whole % kXcds == 0 ? kXcds : p.whole % kXcds, xcd = blockIdx.x % kXcds;
+        return xcd * per - max(0, xcd - full) + blockIdx.x / kXcds;        // the first `full` XCDs take one tile more where it does not divide
+    }
+    const int u = blockIdx.x - p.whole;
+    range = u / p.rest;
+    return p.whole + u % p.rest;
+}
+
+// A wavefront's part of a tile on its way out, through its own piece of LDS: 32 rows at a time as [32][TN * 32], chunks of 16 bytes
+// at place chunk ^ (row & 15).
+template <Epi EPI, bool SPLIT, int T, int TM, int TN>
+__device__ __forceinline__ void write_tile(const f16v (&acc)[TM][TN], float* stage, const GemmArgs& p, const TilePlace& at, int tile, int range) {
+    constexpr int PANELS = EPI == kUp ? 2 : 1;
+    constexpr int kCols = TN * 32, kUnits = kCols / 8 / PANELS, kRows = 64 / kUnits;
+    const Job& q = p.job[at.job];
+    const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), wm = wave / 2, wn = wave % 2;
+    const int lane_row = lane % 32, out_row = lane / kUnits, unit = lane % kUnits;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int chunk = 8 * t + 2 * g + lane / 32;
+                *(f4*)(stage + lane_row * kCols + 4 * (chunk ^ (lane_row & 15))) = f4{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
+            }
+        in_wave_order();                                  // written and read by one wavefront: LDS keeps its order
+#pragma unroll 1
+        for (int r0 = 0; r0 < 32; r0 += kRows) {
+            const int r = r0 + out_row;
+            float v[PANELS][8];
+#pragma unroll
+            for (int q2 = 0; q2 < PANELS; ++q2)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int chunk = q2 * (kCols / 4 / PANELS) + 2 * unit + h;
+                    const f4 w = *(const f4*)(stage + r * kCols + 4 * (chunk ^ (r & 15)));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[q2][4 * h + e] = w[e];
+                }
+            const int row = wm * (32 * TM) + 32 * i + r, col = wn * (T / 2 / PANELS) + 8 * unit;
+            if (range >= 0) {
+                float* out = p.partial + ((int64_t)range * p.rest + (tile - p.whole)) * (T * T) + (int64_t)row * T + col;
+#pragma unroll
+                for (int q2 = 0; q2 < PANELS; ++q2) store8(out + q2 * (T / PANELS), v[q2]);
+            } else if (at.m0 + row < q.M) {
+                emit<EPI, SPLIT>(q.epi, at.group, at.m0 + row, at.n0 + col, v[0], v[PANELS - 1]);
+            }
+        }
+        in_wave_order();
+    }
+}
+
 // T x T tiles: 256 with eight wavefronts of 64 x 128, 128 with four of 64 x 64.
 template <int T>
 constexpr int gemm_threads() { return T == 256 ? 512 : 256; }
 
-template <bool A_RC, bool B_RC, Epi EPI, bool SPLIT, int T>
+template <bool A_RC, bool B_RC, Epi EPI, int T>
 __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) {
     constexpr int THREADS = gemm_threads<T>(), TM = 2, TN = T / 64;
     constexpr int PANELS = EPI == kUp ? 2 : 1;
@@ -299,15 +354,8 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
     __shared__ __align__(1024) char buf2[kBytes];
     __shared__ __align__(1024) char buf3[kBytes];
 
-    // the hardware deals workgroup b to XCD b % 8: each XCD takes a contiguous range of tiles, whose operands its L2 keeps
-    int tile, range = -1;
-    if ((int)blockIdx.x < p.whole) {
-        const int per = (p.whole + kXcds - 1) / kXcds, full = p.whole % kXcds == 0 ? kXcds : p.whole % kXcds, xcd = blockIdx.x % kXcds;
-        tile = xcd * per - max(0, xcd - full) + blockIdx.x / kXcds;        // the first `full` XCDs take one tile more where it does not divide
-    } else {
-        const int u = blockIdx.x - p.whole;
-        range = u / p.rest, tile = p.whole + u % p.rest;
-    }
+    int range;
+    const int tile = tile_of_block(p, range);
     const TilePlace at = place_of(p, tile, T, T / PANELS);
     const Job& q = p.job[at.job];
 
@@ -334,11 +382,11 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
     Cursor cur_a, cur_b, cur_b2;
     auto enter = [&]() {                                  // the segment's first slice of this range
         const int64_t k0 = (int64_t)from * kBK;
-        const uint16_t* a = base_a + q.seg_a[seg];
-        const uint16_t* b = (PANELS == 1 && ((q.seg_second >> seg) & 1u) ? base_b2 : base_b) + q.seg_b[seg];
+        const uint16_t* a = seg ? base_a + q.second_a : base_a;
+        const uint16_t* b = PANELS == 1 && seg ? base_b2 : base_b;
         cur_a = A_RC ? TA::cursor(a, q.a_pitch, q.a_inner8, q.K, at.m0, k0) : TA::cursor(a, q.a_pitch, q.M, q.a_inner8, at.m0, k0);
         cur_b = B_RC ? TB::cursor(b, q.b_pitch, q.b_inner8, q.K, at.n0, k0) : TB::cursor(b, q.b_pitch, q.N, q.b_inner8, at.n0, k0);
-        if constexpr (PANELS == 2) cur_b2 = TB::cursor(base_b2 + q.seg_b[seg], q.b_pitch, q.b_inner8, q.K, at.n0, k0);
+        if constexpr (PANELS == 2) cur_b2 = TB::cursor(base_b2, q.b_pitch, q.b_inner8, q.K, at.n0, k0);
         k_left = (A_RC ? q.K : q.a_inner8) - k0;
     };
     enter();
@@ -385,21 +433,7 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
 #pragma unroll
             for (int t = 0; t < TN; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][t], fa[s & 1][i], acc[i][t], 0, 0, 0);
     };
-    // fp32: the large products come first.  Where their sum is infinite the small ones, products of an infinity with a remainder
-    // of zero among them, have nothing to add: such sums are kept as they are (a bit each for +inf and -inf; a NaN stays one).
-    const int small_from = SPLIT ? here * q.big : -1, end = here * q.segments;
-    unsigned pos[TM][TN] = {}, neg[TM][TN] = {};
-    auto mark = [&]() {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int t = 0; t < TN; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    pos[i][t] |= acc[i][t][r] == INFINITY ? 1u << r : 0u;
-                    neg[i][t] |= acc[i][t][r] == -INFINITY ? 1u << r : 0u;
-                }
-    };
+    const int end = here * q.segments;
     // In front of slice it + 1: this wavefront's copies of it have landed (those of the two slices behind it may be under way)
     // and its fragments of slice `it` are in registers; behind the barrier that holds for all wavefronts, so slice it + 1 can
     // be read and the buffer of slice `it` overwritten.  Copies past the end (windows of no bytes) keep the count the same.
@@ -410,8 +444,7 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    auto slice = [&](char* lds, char* next, int it) {
-        if (SPLIT && it == small_from) mark();
+    auto slice = [&](char* lds, char* next) {
         fetch(lds, 1);
         multiply(0);
         __builtin_amdgcn_sched_barrier(0);                // fragments of two steps at a time: registers
@@ -430,64 +463,20 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
     barrier();
     fetch(buf0, 0);
     for (int it = 0; it < end; it += kRing) {
-        slice(buf0, buf1, it);
-        if (it + 1 < end) slice(buf1, buf2, it + 1);
-        if (it + 2 < end) slice(buf2, buf3, it + 2);
-        if (it + 3 < end) slice(buf3, buf0, it + 3);
+        slice(buf0, buf1);
+        if (it + 1 < end) slice(buf1, buf2);
+        if (it + 2 < end) slice(buf2, buf3);
+        if (it + 3 < end) slice(buf3, buf0);
     }
     __builtin_amdgcn_s_waitcnt(0x0070);                   // the copies past the end write zeros into LDS
-    if constexpr (SPLIT) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int t = 0; t < TN; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][t][r] = (pos[i][t] >> r) & 1u ? INFINITY : (neg[i][t] >> r) & 1u ? -INFINITY : acc[i][t][r];
-    }
 
-    // 32 rows at a time: LDS [32][TN * 32] of this wavefront, chunks of 16 bytes at place chunk ^ (row & 15)
     __syncthreads();                                      // everyone is done with the operands
-    constexpr int kCols = TN * 32, kUnits = kCols / 8 / PANELS, kRows = 64 / kUnits;
-    const int lane_row = lane % 32, out_row = lane / kUnits, unit = lane % kUnits;
-    constexpr int kPart = THREADS / 64 / kRing;           // wavefronts that stage in one buffer
+    constexpr int kPart = THREADS / 64 / kRing, kFloats = 32 * TN * 32;   // wavefronts that stage in one buffer
     char* bufs[kRing] = {buf0, buf1, buf2, buf3};
-    float* stage = (float*)bufs[0] + wave % kPart * 32 * kCols;
+    float* stage = (float*)bufs[0] + wave % kPart * kFloats;
 #pragma unroll
-    for (int i = 1; i < kRing; ++i) stage = wave / kPart == i ? (float*)bufs[i] + wave % kPart * 32 * kCols : stage;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-#pragma unroll
-        for (int t = 0; t < TN; ++t)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int chunk = 8 * t + 2 * g + lane / 32;
-                *(f4*)(stage + lane_row * kCols + 4 * (chunk ^ (lane_row & 15))) = f4{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
-            }
-        in_wave_order();                                  // written and read by one wavefront: LDS keeps its order
-#pragma unroll 1
-        for (int r0 = 0; r0 < 32; r0 += kRows) {
-            const int r = r0 + out_row;
-            float v[PANELS][8];
-#pragma unroll
-            for (int q2 = 0; q2 < PANELS; ++q2)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int chunk = q2 * (kCols / 4 / PANELS) + 2 * unit + h;
-                    const f4 w = *(const f4*)(stage + r * kCols + 4 * (chunk ^ (r & 15)));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[q2][4 * h + e] = w[e];
-                }
-            const int row = wm * (32 * TM) + 32 * i + r, col = wn * (T / 2 / PANELS) + 8 * unit;
-            if (range >= 0) {
-                float* out = p.partial + ((int64_t)range * p.rest + (tile - p.whole)) * (T * T) + (int64_t)row * T + col;
-#pragma unroll
-                for (int q2 = 0; q2 < PANELS; ++q2) store8(out + q2 * (T / PANELS), v[q2]);
-            } else if (at.m0 + row < q.M) {
-                emit<EPI, SPLIT>(q.epi, at.group, at.m0 + row, at.n0 + col, v[0], v[PANELS - 1]);
-            }
-        }
-        in_wave_order();
-    }
+    for (int i = 1; i < kRing; ++i) stage = wave / kPart == i ? (float*)bufs[i] + wave % kPart * kFloats : stage;
+    write_tile<EPI, false, T>(acc, stage, p, at, tile, range);
 }
 
 // Adds up the ranges of the tiles whose contraction was cut, in order, and does the epilogue's work.

@@ -6,7 +6,7 @@
 //
 // Both first projections, the activation and the product are one kernel: a tile holds the same columns of a and of b in the
 // registers of the same lanes.  Likewise dh never exists in memory: its tiles become da and db.  The products are those of
-// ffn_gemm.h; storage type fp32 takes them through three bf16 planes per operand.  An operand whose rows are 16-byte aligned
+// ffn_gemm.h; storage type fp32 takes them through three bf16 terms per operand (ffn_gemm_f32.h).  An operand whose rows are 16-byte aligned
 // bf16 is read where it lies; others are laid out in the workspace first (rounded to bf16 where the weights are fp32 master
 // weights of a bf16 block), by a streaming pass.
 //
@@ -15,12 +15,13 @@
 // at once.  One row through 2048 - 5632 - 2048 in bf16: 25 us in three launches (12.5, 8 and 4: the first reads 46 MB at 3.7
 // TB/s; with half the workgroups and half the loads in flight 17.5, 11.5 and 3.5).
 //
-// 8192 rows through 2048 - 5632 - 2048, forward and backward, bf16: 1.81 ms, 940 TFLOP/s; ffn_gemm.h says what bounds the products.
+// 8192 rows through 2048 - 5632 - 2048, forward and backward, bf16: 1.79 ms, 950 TFLOP/s; ffn_gemm.h says what bounds the products.
 // The two with an epilogue of their own add the time of its memory traffic, since the tiles of a round end together: 461 MB
 // written behind a, b and h, 553 MB read and written behind da and db.
 #include <algorithm>
 
 #include "ffn_gemm.h"
+#include "ffn_gemm_f32.h"
 
 namespace ols {
 
@@ -33,8 +34,8 @@ constexpr int kFewSlab = 1024;       // contraction indices whose inputs lie in 
 
 struct PackJob {
     const void* src;
-    int64_t row, group, rows, cols, cols8, pitch;
-    uint16_t* dst;                   // [group][plane][rows][pitch]
+    int64_t row, group, rows, cols, cols8;
+    uint16_t* dst;                   // [group][rows][cols8]
     int dtype, groups;
 };
 constexpr int kMaxPacks = 5;
@@ -42,30 +43,38 @@ struct PackParams {                  // all operands of a call in one launch
     PackJob job[kMaxPacks];
 };
 
-template <typename T, bool SPLIT>
-__device__ __forceinline__ void pack_unit(const PackJob& p, int64_t g, int64_t r, int64_t c) {
-    float v[8];
+template <typename T>
+__device__ __forceinline__ void read_unit(const PackJob& p, int64_t g, int64_t i, float (&v)[8]) {
+    const int64_t units = p.cols8 / 8, r = i / units, c = i % units * 8;
     load_upto8((const T*)p.src + g * p.group + r * p.row + c, (int)min((int64_t)8, p.cols - c), 0.0f, v);
-    constexpr int P = SPLIT ? 3 : 1;
-    uint16_t* out = p.dst + (g * P * p.rows + r) * p.pitch + c;
-    if constexpr (SPLIT) {
-        const Split8 s = split8(f4{v[0], v[1], v[2], v[3]}, f4{v[4], v[5], v[6], v[7]});
-        *(u4*)out = s.hi;
-        *(u4*)(out + p.rows * p.pitch) = s.mid;
-        *(u4*)(out + 2 * p.rows * p.pitch) = s.lo;
-    } else {
-        store8(out, v);
-    }
 }
 
+// Rows follow one another without gaps, so unit i of eight elements (48 bytes as terms) lies behind unit i - 1.  A wavefront's terms
+// pass through LDS and are written as whole lines.
 template <bool SPLIT>
 __global__ __launch_bounds__(256) void pack_kernel(PackParams all) {
     const PackJob& p = all.job[blockIdx.z];
-    const int64_t units = p.cols8 / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
-    if (i >= p.rows * units || g >= p.groups) return;
-    const int64_t r = i / units, c = i % units * 8;
-    if (SPLIT || p.dtype == OLS_F32) pack_unit<float, SPLIT>(p, g, r, c);
-    else pack_unit<uint16_t, SPLIT>(p, g, r, c);
+    const int64_t units = p.rows * (p.cols8 / 8), i = (int64_t)blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
+    if (g >= p.groups) return;
+    float v[8] = {};
+    if constexpr (!SPLIT) {
+        if (i >= units) return;
+        if (p.dtype == OLS_F32) read_unit<float>(p, g, i, v);
+        else read_unit<uint16_t>(p, g, i, v);
+        store_terms<false>(p.dst + (g * units + i) * 8, v);
+    } else {
+        __shared__ __align__(16) uint16_t stage[256 * 24];
+        if (i < units) read_unit<float>(p, g, i, v);
+        const int lane = threadIdx.x % 64;
+        uint16_t* mine = stage + threadIdx.x / 64 * (64 * 24);
+        store_terms<true>(mine + lane * 24, v);
+        in_wave_order();
+        const int64_t first = i - lane, chunks = min((int64_t)64, units - first) * 3;
+        u4* out = (u4*)(p.dst + (g * units + first) * 24);
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+            if (t * 64 + lane < chunks) out[t * 64 + lane] = *(const u4*)(mine + (t * 64 + lane) * 8);
+    }
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------------
@@ -183,10 +192,11 @@ struct Arena {
     }
 };
 
-// An operand as the products read it: [group][plane][outer][inner8], or the caller's tensor itself.
+// An operand as the products read it: rows of inner8 elements, or of three times as many where each fp32 is three bf16 terms; or
+// the caller's tensor itself.
 struct View {
     const uint16_t* p = nullptr;
-    int64_t pitch = 0, group = 0, plane = 0, inner8 = 0;
+    int64_t pitch = 0, group = 0, inner8 = 0;
 };
 
 bool lies_well(const ols_matrix& m, int dtype, int64_t inner) {
@@ -201,20 +211,20 @@ struct Maker {                         // lays operands out; without a stream it
     PackParams packs = {};
     int n_packs = 0;
     bool split() const { return f.dtype == OLS_F32; }
-    int planes() const { return split() ? 3 : 1; }
+    int terms() const { return split() ? 3 : 1; }
 
     View operand(const ols_matrix& m, int dtype, int64_t outer, int64_t inner, bool may_lie) {
         View v;
-        v.inner8 = up8(inner), v.pitch = up8(inner);
+        v.inner8 = up8(inner), v.pitch = terms() * v.inner8;
         if (may_lie && !split() && lies_well(m, dtype, inner)) {
             v.p = (const uint16_t*)m.dev, v.pitch = m.row, v.group = m.group;
             return v;
         }
         const int64_t per = outer * v.pitch;
         const int groups = m.group == 0 ? 1 : f.groups;      // shared by the workers: laid out once
-        uint16_t* dst = (uint16_t*)ws.take(2 * per * planes() * groups);
-        v.p = dst, v.plane = per, v.group = groups == 1 ? 0 : per * planes();
-        packs.job[n_packs++] = PackJob{m.dev, m.row, m.group, outer, inner, v.inner8, v.pitch, dst, dtype, groups};
+        uint16_t* dst = (uint16_t*)ws.take(2 * per * groups);
+        v.p = dst, v.group = groups == 1 ? 0 : per;
+        packs.job[n_packs++] = PackJob{m.dev, m.row, m.group, outer, inner, v.inner8, dst, dtype, groups};
         return v;
     }
     hipError_t lay_out() const {       // the operands asked for
@@ -236,26 +246,14 @@ struct Maker {                         // lays operands out; without a stream it
     }
     View internal(int64_t rows, int64_t inner, void* at) const {
         View v;
-        v.inner8 = up8(inner), v.pitch = up8(inner), v.plane = rows * v.pitch, v.group = planes() * v.plane, v.p = (const uint16_t*)at;
+        v.inner8 = up8(inner), v.pitch = terms() * v.inner8, v.group = rows * v.pitch, v.p = (const uint16_t*)at;
         return v;
     }
-    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * planes() * f.groups * rows * up8(inner); }
+    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * terms() * f.groups * rows * up8(inner); }
 };
 
-// the planes' products, largest first
-constexpr int kPlanePairs[6][2] = {{0, 0}, {0, 1}, {1, 0}, {1, 1}, {0, 2}, {2, 0}};
-
-void set_segments(Job& j, const View& a, const View& b, const View* a2, const View* b2, bool split) {
-    j.segments = 0, j.seg_second = 0;
-    const int tensors = a2 ? 2 : 1, pairs = split ? 6 : 1;
-    for (int k = 0; k < pairs; ++k)
-        for (int t = 0; t < tensors; ++t) {
-            const int s = j.segments++;
-            j.seg_a[s] = kPlanePairs[k][0] * a.plane + (t ? a2->p - a.p : 0);
-            j.seg_b[s] = kPlanePairs[k][1] * b.plane;
-            if (t) j.seg_second |= 1u << s;
-        }
-    j.big = tensors;
+void set_operands(Job& j, const View& a, const View& b, const View* a2, const View* b2) {
+    j.segments = a2 ? 2 : 1, j.second_a = a2 ? a2->p - a.p : 0;
     j.a = a.p, j.a_group = a.group, j.a_pitch = a.pitch, j.a_inner8 = a.inner8;
     j.b = b.p, j.b_group = b.group, j.b_pitch = b.pitch, j.b_inner8 = b.inner8;
     if (b2) j.b2 = b2->p, j.b2_group = b2->group;
@@ -274,6 +272,9 @@ int64_t count_tiles(const Job* jobs, int n, int groups, int panels, int t) {
     return tiles;
 }
 
+// Workgroups of a round.
+int64_t slots_of(int t, bool split) { return split || t == 256 ? kCus : 2 * kCus; }
+
 // What a product takes, in microseconds, by tile, and by how the tiles of the last round are cut.  Fitted to products of 32 to 8192
 // rows and 256 to 5632 columns over 300 to 8192 indices (within 15 % of most).  A slice of 32 indices takes a workgroup 0.3 us where
 // few run, 0.4 with one on every compute unit and 0.6 with two (tiles of 128); 0.75 to 0.95 with one tile of 256.  Examples,
@@ -281,8 +282,24 @@ int64_t count_tiles(const Job* jobs, int n, int groups, int panels, int t) {
 // 2048 x 5632 over 1024: tiles of 128 39.0, of 256 36.2.  64 x 1024 over 4096: tiles of 128 whole 41.4, cut in 16: 12.8.
 // An epilogue with an activation takes a tile 10 to 25 us more, and less where it is done by the launch that joins ranges
 // (three ragged fp32 workers, 201 x 517 over 131, Gaussian: 39.7 us whole).
-double estimate(const Shape& s, int64_t slices, bool activation) {
-    const int64_t slots = s.t == 256 ? kCus : 2 * kCus;
+//
+// The products of fp32 keep the matrix pipes as busy with one workgroup on a compute unit as with two (a slice of 16: 0.5 us where few
+// run, 0.62 with one on every compute unit, 1.2 with two), so a round is one per compute unit.  Fitted to products of 16 to 2048 rows
+// and 32 to 5248 columns over 64 to 5248 indices.  291 x 1088 over 3192, three workers, 81 tiles: whole 110.7 us, cut in 2 / 3 / 4 / 6:
+// 70.0 / 58.2 / 74.1 / 64.1; 2048 x 1024 over 2816, 128 tiles: whole 101.9, cut in 2: 72.4.
+double estimate(const Shape& s, int64_t slices, bool activation, bool split) {
+    if (split) {
+        auto slice_us = [](double blocks) { return 0.5 + 0.12 * std::min(1.0, blocks / kCus); };
+        const double filled = std::min(1.0, (double)s.whole / kCus), act = activation ? 2.0 : 0.0;
+        double us = 0.0;
+        if (s.whole) us += 1.0 + (double)((s.whole + kCus - 1) / kCus) * (slices * slice_us(s.whole) + 4.5 + act * filled);
+        if (s.rest) {
+            const double blocks = (double)s.rest * s.ranges;
+            us += ((double)slices / s.ranges + 0.5) * slice_us(blocks) + 10.0 + blocks * s.t * s.t * 4.0 / 3.5e6;
+        }
+        return us;
+    }
+    const int64_t slots = slots_of(s.t, false);
     auto slice_us = [&](double blocks) {
         const double one = std::min(1.0, blocks / kCus), two = std::min(1.0, std::max(0.0, blocks / kCus - 1.0));
         return s.t == 256 ? 0.75 + 0.2 * one : 0.3 + 0.1 * one + 0.2 * two;
@@ -301,21 +318,21 @@ double estimate(const Shape& s, int64_t slices, bool activation) {
 Shape choose(const Job* jobs, int n, int groups, int panels, bool split, bool activation) {
     int64_t slices = (int64_t)1 << 40, work = 1;
     for (int i = 0; i < n; ++i) {
-        slices = std::min(slices, tiles_of(jobs[i].K, kBK));
-        work = std::max(work, tiles_of(jobs[i].K, kBK) * jobs[i].segments);
+        const int64_t k = tiles_of(jobs[i].K, split ? kBKF32 : kBK);
+        slices = std::min(slices, k), work = std::max(work, k * jobs[i].segments);
     }
     Shape best{};
     double best_us = 1e300;
-    for (int t = 128; t <= (split ? 128 : 256); t += 128) {          // three planes of every operand leave no registers for large tiles
-        const int64_t slots = t == 256 ? kCus : 2 * kCus, tiles = count_tiles(jobs, n, groups, panels, t);
+    for (int t = 128; t <= (split ? 128 : 256); t += 128) {          // fp32: two sets of sums leave no registers for large tiles
+        const int64_t slots = slots_of(t, split), tiles = count_tiles(jobs, n, groups, panels, t);
         if (tiles > 0x0fffffff) continue;
-        for (int ranges : {1, 2, 3, 4, 6, 8, 12, 16}) {
+        for (int ranges : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             Shape s{t, (int)tiles, 0, 1};
             if (ranges > 1) {
                 s.whole = (int)(tiles / slots * slots), s.rest = (int)(tiles - s.whole), s.ranges = ranges;
                 if (s.rest == 0 || slices < ranges || work / ranges < 4 || (int64_t)s.rest * ranges > slots) continue;
             }
-            const double us = estimate(s, work, activation);
+            const double us = estimate(s, work, activation, split);
             if (us < best_us) best = s, best_us = us;
         }
     }
@@ -345,13 +362,13 @@ hipError_t product(Job* jobs, int n, int groups, bool split, Arena& ws, bool go,
     const unsigned blocks = shape.whole + shape.rest * shape.ranges;
     const dim3 join_grid(shape.rest, (unsigned)(t * (t / PANELS / 8) / 256));
     if (split) {
-        gemm_kernel<A_RC, B_RC, EPI, true, 128><<<blocks, 256, 0, stream>>>(p);
+        gemm_f32_kernel<A_RC, B_RC, EPI><<<blocks, 256, 0, stream>>>(p);
         if (joins) join_kernel<EPI, true, 128><<<join_grid, 256, 0, stream>>>(p);
     } else if (t == 256) {
-        gemm_kernel<A_RC, B_RC, EPI, false, 256><<<blocks, 512, 0, stream>>>(p);
+        gemm_kernel<A_RC, B_RC, EPI, 256><<<blocks, 512, 0, stream>>>(p);
         if (joins) join_kernel<EPI, false, 256><<<join_grid, 256, 0, stream>>>(p);
     } else {
-        gemm_kernel<A_RC, B_RC, EPI, false, 128><<<blocks, 256, 0, stream>>>(p);
+        gemm_kernel<A_RC, B_RC, EPI, 128><<<blocks, 256, 0, stream>>>(p);
         if (joins) join_kernel<EPI, false, 128><<<join_grid, 256, 0, stream>>>(p);
     }
     return hipGetLastError();
@@ -452,14 +469,14 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
 
     Job up = {};
     up.M = f.rows, up.N = f.hidden, up.K = f.width;
-    set_segments(up, x, wg, nullptr, &wu, mk.split());
+    set_operands(up, x, wg, nullptr, &wu);
     up.epi.n = f.hidden, up.epi.n8 = h8, up.epi.pitch = up8(f.hidden), up.epi.m = f.rows, up.epi.act = f.act;
     up.epi.a = saved ? (float*)(saved + s.off_a) : nullptr, up.epi.b = saved ? (float*)(saved + s.off_b) : nullptr, up.epi.h = (uint16_t*)hp;
     e = product<false, true, kUp>(&up, 1, f.groups, mk.split(), ws, go, stream);
     if (e != hipSuccess) return e;
     Job down = {};
     down.M = f.rows, down.N = f.out, down.K = f.hidden;
-    set_segments(down, h, wd, nullptr, nullptr, mk.split());
+    set_operands(down, h, wd, nullptr, nullptr);
     down.epi = store_to(f.y, f.out, f.dtype);
     return product<false, true, kStore>(&down, 1, f.groups, mk.split(), ws, go, stream);
 }
@@ -511,7 +528,7 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         da = mk.internal(f.rows, f.hidden, pa), db = mk.internal(f.rows, f.hidden, pb);
         Job dh = {};
         dh.M = f.rows, dh.N = f.hidden, dh.K = f.out;
-        set_segments(dh, dy, wd, nullptr, nullptr, mk.split());
+        set_operands(dh, dy, wd, nullptr, nullptr);
         dh.epi.n = f.hidden, dh.epi.n8 = h8, dh.epi.pitch = up8(f.hidden), dh.epi.m = f.rows, dh.epi.act = f.act;
         dh.epi.a = (float*)(saved + s.off_a), dh.epi.b = (float*)(saved + s.off_b), dh.epi.h = (uint16_t*)pa, dh.epi.h2 = (uint16_t*)pb;
         e = product<false, false, kGateGrad>(&dh, 1, f.groups, mk.split(), ws, go, stream);
@@ -520,7 +537,7 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
     if (f.dx.dev) {
         Job dx = {};
         dx.M = f.rows, dx.N = f.width, dx.K = f.hidden;
-        set_segments(dx, da, wg, &db, &wu, mk.split());
+        set_operands(dx, da, wg, &db, &wu);
         dx.epi = store_to(f.dx, f.width, f.dtype);
         e = product<false, false, kStore>(&dx, 1, f.groups, mk.split(), ws, go, stream);
         if (e != hipSuccess) return e;
@@ -531,7 +548,7 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         if (!grads[i]->dev) continue;
         Job& j = dw[n++];
         j.M = i < 2 ? f.width : f.hidden, j.N = i < 2 ? f.hidden : f.out, j.K = f.rows;
-        set_segments(j, i < 2 ? x : h, i == 0 ? da : i == 1 ? db : dy, nullptr, nullptr, mk.split());
+        set_operands(j, i < 2 ? x : h, i == 0 ? da : i == 1 ? db : dy, nullptr, nullptr);
         j.epi = store_to(*grads[i], j.N, f.grad_dtype);
     }
     return product<true, true, kStore>(dw, n, f.groups, mk.split(), ws, go, stream);
