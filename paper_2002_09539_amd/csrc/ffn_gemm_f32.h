@@ -14,6 +14,9 @@
 // rows, 1182 by 400: 297 us instead of 472 by six passes.  The copies in front of the products: 3 % slower; next slice's first terms
 // in registers of their own, so that no read is waited for, or wavefront priorities: nothing.
 //
+// PLAIN: the second operand is the caller's fp32 tensor; a lane splits eight elements of a slice on their way to LDS, and two slices
+// are under way in registers.
+//
 // The product of the first terms has accumulators of its own.  An infinite operand has remainders of zero, and the small
 // products would turn infinity times zero into NaN: where the large sum is not finite it is the result.
 #pragma once
@@ -95,17 +98,73 @@ struct TermsRC {
     }
 };
 
-template <bool A_RC, bool B_RC, Epi EPI>
+// The same places in LDS for an operand that lies in memory as plain fp32: a lane takes eight elements of a slice into registers and
+// writes their terms.
+struct PlainKC {
+    unsigned off;
+    int half, place[3];
+    __device__ explicit PlainKC(int64_t pitch) {
+        const int r = threadIdx.x / 2;
+        half = threadIdx.x % 2, off = (unsigned)(r * pitch * 4 + half * 32);
+#pragma unroll
+        for (int n = 0; n < 3; ++n) place[n] = r * 96 + (((3 * half + n) ^ ((r >> 3) & 1)) << 4);
+    }
+    __device__ static Cursor cursor(const float* base, int64_t pitch, int64_t rows, int64_t K, int64_t row0, int64_t k0) {
+        return {(const char*)(base + row0 * pitch + k0), 4 * ((rows - 1 - row0) * pitch + K - k0), 4 * kBKF32};
+    }
+    __device__ bool has(int e, int64_t k_left) const { return half * 8 + e < k_left; }    // behind it lies the next row
+};
+template <int COLS, int PANELS>
+struct PlainRC {
+    unsigned off;
+    int place[3];
+    __device__ explicit PlainRC(int64_t pitch) {
+        using T = TermsRC<COLS, PANELS>;
+        const int i = threadIdx.x % (256 / PANELS), k = i / (COLS / 8), c = i % (COLS / 8);
+        off = (unsigned)(k * pitch * 4 + c * 32);
+#pragma unroll
+        for (int n = 0; n < 3; ++n) place[n] = uniform(threadIdx.x / 64) / (4 / PANELS) * T::kBytes + k * (T::kLine * 16) + ((3 * (c ^ T::swizzle(k)) + n) << 4);
+    }
+    __device__ static Cursor cursor(const float* base, int64_t pitch, int64_t cols, int64_t K, int64_t col0, int64_t k0) {
+        return {(const char*)(base + k0 * pitch + col0), 4 * ((K - 1 - k0) * pitch + cols - col0), 4 * kBKF32 * pitch};
+    }
+    __device__ bool has(int, int64_t) const { return true; }                               // lines past the last one read as zeros
+};
+struct PlainUnit {
+    u4 lo, hi;
+};
+template <typename P>
+__device__ __forceinline__ PlainUnit plain_request(const P& p, const Cursor& c) {
+    const rsrc_t rs = c.window();
+    return {__builtin_amdgcn_raw_buffer_load_b128(rs, (int)p.off, 0, 0), __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(p.off + 16), 0, 0)};
+}
+template <typename P>
+__device__ __forceinline__ void plain_place(const P& p, const PlainUnit& u, int64_t k_left, char* lds) {
+    f4 a = __builtin_bit_cast(f4, u.lo), b = __builtin_bit_cast(f4, u.hi);
+    if (k_left < kBKF32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[e] = p.has(e, k_left) ? a[e] : 0.0f, b[e] = p.has(e + 4, k_left) ? b[e] : 0.0f;
+    }
+    const Split8 s = split8(a, b);
+    *(u4*)(lds + p.place[0]) = s.hi;
+    *(u4*)(lds + p.place[1]) = s.mid;
+    *(u4*)(lds + p.place[2]) = s.lo;
+}
+
+template <bool A_RC, bool B_RC, Epi EPI, bool PLAIN>
 __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs p) {
     constexpr int PANELS = EPI == kUp ? 2 : 1;
     static_assert(PANELS == 1 || B_RC, "two panels are read line by line");
     using TA = typename std::conditional<A_RC, TermsRC<128, 1>, TermsKC>::type;
     using TB = typename std::conditional<B_RC, TermsRC<128 / PANELS, PANELS>, TermsKC>::type;
-    constexpr int kBytes = TA::kBytes + PANELS * TB::kBytes;
-    static_assert(kBytes == 24576, "two wavefronts' results are staged in a buffer");
-    __shared__ __align__(1024) char buf0[kBytes];
-    __shared__ __align__(1024) char buf1[kBytes];
-    __shared__ __align__(1024) char buf2[kBytes];
+    using PB = typename std::conditional<B_RC, PlainRC<128 / PANELS, PANELS>, PlainKC>::type;
+    static_assert(TA::kBytes == 12288 && PANELS * TB::kBytes == 12288, "a wavefront's results are staged in a buffer");
+    __shared__ __align__(1024) char a0[12288];
+    __shared__ __align__(1024) char a1[12288];
+    __shared__ __align__(1024) char a2[12288];
+    __shared__ __align__(1024) char b0[12288];
+    __shared__ __align__(1024) char b1[12288];
+    __shared__ __align__(1024) char b2[12288];
 
     int range;
     const int tile = tile_of_block(p, range);
@@ -113,13 +172,11 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs p) {
     const Job& q = p.job[at.job];
     const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), wm = wave / 2, wn = wave % 2;
     const TA ta(q.a_pitch);
-    const TB tb(q.b_pitch);
+    const typename std::conditional<PLAIN, PB, TB>::type tb(q.b_pitch);
     const int slices = (int)((q.K + kBKF32 - 1) / kBKF32);
     const int from = range < 0 ? 0 : (int)((int64_t)slices * range / p.ranges);
     const int here = (range < 0 ? slices : (int)((int64_t)slices * (range + 1) / p.ranges)) - from;
-    const uint16_t* base_a = q.a + at.group * q.a_group;
-    const uint16_t* base_b = q.b + at.group * q.b_group;
-    const uint16_t* base_b2 = q.b2 + at.group * q.b2_group;
+    const int64_t k0 = (int64_t)from * kBKF32;
 
     f16v big[2][2], small[2][2];
 #pragma unroll
@@ -129,27 +186,58 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs p) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) big[i][t][r] = 0.0f, small[i][t][r] = 0.0f;
 
-    int seg = 0, left_slices = here;                      // of the next copy
-    int64_t k_left;
-    Cursor cur_a, cur_b;
-    auto enter = [&]() {                                  // the segment's first slice of this range
-        const int64_t k0 = (int64_t)from * kBKF32;
-        const uint16_t* a = seg ? base_a + q.second_a : base_a;
-        const uint16_t* b = (PANELS == 1 ? seg != 0 : wave >= 2) ? base_b2 : base_b;
-        cur_a = A_RC ? TA::cursor(a, q.a_pitch, q.a_inner8, q.K, at.m0, k0) : TA::cursor(a, q.a_pitch, q.M, q.a_inner8, at.m0, k0);
-        cur_b = B_RC ? TB::cursor(b, q.b_pitch, q.b_inner8, q.K, at.n0, k0) : TB::cursor(b, q.b_pitch, q.N, q.b_inner8, at.n0, k0);
-        k_left = (A_RC ? q.K : q.a_inner8) - k0;
+    // the next slice of each operand to be read: its segment, the slices left there, the contraction indices left in a row
+    struct Walk {
+        Cursor cur;
+        int seg, slices;
+        int64_t k_left;
     };
-    enter();
-    auto copy = [&](char* lds) {
-        ta.copy(lds, 0, cur_a, k_left);
-        tb.copy(lds, TA::kBytes, cur_b, k_left);
-        cur_a.advance(), cur_b.advance();
-        k_left -= kBKF32;
-        if (--left_slices == 0) {
-            if (++seg < q.segments) left_slices = here, enter();
-            else cur_a.left = cur_b.left = 0, cur_a.step = cur_b.step = 0;   // from here on nothing is read
+    Walk wa, wb;
+    auto enter_a = [&]() {
+        const uint16_t* a = q.a + at.group * q.a_group + (wa.seg ? q.second_a : 0);
+        wa.cur = A_RC ? TA::cursor(a, q.a_pitch, q.a_inner8, q.K, at.m0, k0) : TA::cursor(a, q.a_pitch, q.M, q.a_inner8, at.m0, k0);
+        wa.slices = here, wa.k_left = (A_RC ? q.K : q.a_inner8) - k0;
+    };
+    auto enter_b = [&]() {
+        const bool second = PANELS == 1 ? wb.seg != 0 : wave >= 2;
+        if constexpr (PLAIN) {
+            const float* b = second ? (const float*)q.b2 + at.group * q.b2_group : (const float*)q.b + at.group * q.b_group;
+            wb.cur = PB::cursor(b, q.b_pitch, B_RC ? q.b_inner8 : q.N, q.K, at.n0, k0);
+        } else {
+            const uint16_t* b = second ? q.b2 + at.group * q.b2_group : q.b + at.group * q.b_group;
+            wb.cur = B_RC ? TB::cursor(b, q.b_pitch, q.b_inner8, q.K, at.n0, k0) : TB::cursor(b, q.b_pitch, q.N, q.b_inner8, at.n0, k0);
         }
+        wb.slices = here, wb.k_left = (B_RC || PLAIN ? q.K : q.b_inner8) - k0;
+    };
+    wa.seg = wb.seg = 0;
+    enter_a(), enter_b();
+    auto next = [&](Walk& w, auto& enter) {
+        w.cur.advance();
+        w.k_left -= kBKF32;
+        if (--w.slices == 0) {
+            if (++w.seg < q.segments) enter();
+            else w.cur.left = 0, w.cur.step = 0;          // from here on nothing is read
+        }
+    };
+    auto copy = [&](char* la, char* lb) {
+        ta.copy(la, 0, wa.cur, wa.k_left);
+        next(wa, enter_a);
+        if constexpr (!PLAIN) {
+            tb.copy(lb, 0, wb.cur, wb.k_left);
+            next(wb, enter_b);
+        }
+    };
+    // PLAIN: two slices are under way in registers
+    PlainUnit unit[2];
+    int64_t unit_k[2];
+    auto request = [&](int n) {
+        if constexpr (PLAIN) {
+            unit[n] = plain_request(tb, wb.cur), unit_k[n] = wb.k_left;
+            next(wb, enter_b);
+        }
+    };
+    auto place = [&](int n, char* lb) {
+        if constexpr (PLAIN) plain_place(tb, unit[n], unit_k[n], lb);
     };
     int part_a[2][3], part_b[2][3];
 #pragma unroll
@@ -157,21 +245,21 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs p) {
 #pragma unroll
         for (int n = 0; n < 3; ++n) {
             part_a[i][n] = TA::lane_part(0, wm * 64 + 32 * i, lane, n);
-            part_b[i][n] = PANELS == 2 ? TB::lane_part(TA::kBytes + i * TB::kBytes, wn * 32, lane, n) : TB::lane_part(TA::kBytes, wn * 64 + 32 * i, lane, n);
+            part_b[i][n] = PANELS == 2 ? TB::lane_part(i * TB::kBytes, wn * 32, lane, n) : TB::lane_part(0, wn * 64 + 32 * i, lane, n);
         }
     bf16x8 fa[3][2], fb[3][2];
-    auto fetch = [&](const char* lds, int n) {            // the fragments of a term
+    auto fetch = [&](const char* la, const char* lb, int n) {   // the fragments of a term
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             int part = part_b[i][n];                      // opaque: an array plus one offset
             asm volatile("" : "+v"(part));
-            fb[n][i] = TB::frag(lds, part);
+            fb[n][i] = TB::frag(lb, part);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             int part = part_a[i][n];
             asm volatile("" : "+v"(part));
-            fa[n][i] = TA::frag(lds, part);
+            fa[n][i] = TA::frag(la, part);
         }
     };
     auto multiply = [&](f16v (&to)[2][2], int x, int y) {
@@ -181,43 +269,69 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs p) {
             for (int t = 0; t < 2; ++t) to[i][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[y][t], fa[x][i], to[i][t], 0, 0, 0);
     };
     const int end = here * q.segments;
-    // In front of a slice's products: its fragments are in registers, and this wavefront's copies of the next one have landed (those of
-    // the one behind it may be under way); behind the barrier that holds for all wavefronts, so the next slice can be read and this
-    // one's buffer overwritten.  Copies past the end (windows of no bytes) keep the count the same.
-    auto slice = [&](char* lds, char* next) {
-        __builtin_amdgcn_s_waitcnt(0x0076);               // vmcnt(6) lgkmcnt(0)
+    auto barrier = [&]() {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+    };
+    // In front of slice it's products: its fragments are in registers, and this wavefront's copies of slice it + 1 have landed (those
+    // of slice it + 2 may be under way); behind the barrier that holds for all wavefronts, so slice it + 1 can be read and the buffers
+    // of slice it overwritten.  Copies past the end (windows of no bytes) keep the count the same.  PLAIN: the terms of slice it + 2
+    // are written to the buffer that slice it - 1 had, and slice it + 4 is requested.
+    auto slice = [&](char* la, char* lb, char* la1, char* lb1, char* lb2, int n) {
+        if constexpr (PLAIN) __builtin_amdgcn_s_waitcnt(0x0077);    // vmcnt(7) lgkmcnt(0): requests of two slices and the copies between
+        else __builtin_amdgcn_s_waitcnt(0x0076);                    // vmcnt(6) lgkmcnt(0)
+        barrier();
         multiply(small, 2, 0);
         multiply(small, 0, 2);
-        copy(lds);
+        copy(la, lb);
+        place(n, lb2);
+        request(n);
         __builtin_amdgcn_sched_barrier(0);
-        fetch(next, 2);
+        fetch(la1, lb1, 2);
         multiply(small, 1, 1);
         multiply(small, 1, 0);
         multiply(small, 0, 1);
         __builtin_amdgcn_sched_barrier(0);
-        fetch(next, 1);
+        fetch(la1, lb1, 1);
         multiply(big, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
-        fetch(next, 0);
+        fetch(la1, lb1, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
-    copy(buf0);
-    copy(buf1);
-    copy(buf2);
-    __builtin_amdgcn_s_waitcnt(0x0f7c);                   // vmcnt(12)
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    fetch(buf0, 2);
-    fetch(buf0, 1);
-    fetch(buf0, 0);
-    for (int it = 0; it < end; it += 3) {
-        slice(buf0, buf1);
-        if (it + 1 < end) slice(buf1, buf2);
-        if (it + 2 < end) slice(buf2, buf0);
+    copy(a0, b0);
+    copy(a1, b1);
+    copy(a2, b2);
+    request(0);
+    request(1);
+    place(0, b0);
+    request(0);
+    place(1, b1);
+    request(1);
+    if constexpr (PLAIN) __builtin_amdgcn_s_waitcnt(0x0074);        // vmcnt(4) lgkmcnt(0): the second pair of requests
+    else __builtin_amdgcn_s_waitcnt(0x0f7c);                        // vmcnt(12)
+    barrier();
+    fetch(a0, b0, 2);
+    fetch(a0, b0, 1);
+    fetch(a0, b0, 0);
+    // nested, not side by side: the compiler then knows in all but the first of them which requests are behind those it waits for
+    for (int it = 0; it < end; it += PLAIN ? 6 : 3) {
+        slice(a0, b0, a1, b1, b2, 0);
+        if (it + 1 < end) {
+            slice(a1, b1, a2, b2, b0, 1);
+            if (it + 2 < end) {
+                slice(a2, b2, a0, b0, b1, 0);
+                if constexpr (PLAIN) {
+                    if (it + 3 < end) {
+                        slice(a0, b0, a1, b1, b2, 1);
+                        if (it + 4 < end) {
+                            slice(a1, b1, a2, b2, b0, 0);
+                            if (it + 5 < end) slice(a2, b2, a0, b0, b1, 1);
+                        }
+                    }
+                }
+            }
+        }
     }
     __builtin_amdgcn_s_waitcnt(0x0070);                   // the copies past the end write zeros into LDS
 #pragma unroll
@@ -227,7 +341,7 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs p) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) big[i][t][r] = fabsf(big[i][t][r]) < INFINITY ? big[i][t][r] + small[i][t][r] : big[i][t][r];
     __syncthreads();                                      // everyone is done with the operands
-    float* stage = (float*)(wave < 2 ? buf0 : buf1) + wave % 2 * (32 * 64);
+    float* stage = (float*)(wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? a2 : b0);
     write_tile<EPI, true, 128>(big, stage, p, at, tile, range);
 }
 
