@@ -19,7 +19,8 @@
 // What bounds it, measured warm on products of 8192 rows, 2048 by 5632 (K contiguous in both operands, unless stated): without
 // the copies, on what lies in LDS, 1440 TFLOP/s; the copies alone, at 1.5 times the bytes of a 256 x 256 tile, take as long as
 // 1200 would; together 1110 (1160 with the second operand RC).  Tiles of 256 x 128, two workgroups a compute unit: 974.  Two
-// buffers of 64 indices: 1107.  Four wavefronts of 128 x 128, one a SIMD: a quarter slower than eight.  Wavefront priorities,
+// buffers of 64 indices: 1107.  Four wavefronts of 128 x 128, one a
+// SIMD, with a third less to read from LDS: 4 to 15 % slower than eight, also with the reads between the products.  Wavefront priorities,
 // fragment reads spread between the MFMAs, other orders of tiles, rotated starts, rows apart by other than their length: nothing,
 // or less.  A library's product of these sizes runs at 1100 to 1370.
 //

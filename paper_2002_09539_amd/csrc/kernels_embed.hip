@@ -13,16 +13,17 @@
 //   1. radix sort of (id, position), 9 bits a pass: per-workgroup digit counts, then a stable scatter in which every
 //      wavefront ranks 64 ids at a time by matching ballots.  Up to kSortItems ids per worker take one workgroup and
 //      one launch for all passes.
+//      The sort occupies a few compute units; the other workgroups of its launches meanwhile clear the table, since most ids
+//      of a vocabulary do not occur.
 //   2. the sorted list is cut into runs of kRun positions, a wavefront each, so that the work does not depend on how often
 //      an id occurs.  A sum that lies inside a run is a row of the gradient; one that reaches over its end goes to a partial
 //      row.  (With a wavefront per table row, the row of an id that makes up 6 % of 32 768 tokens took longer than all
 //      the others together: 288 us.)
-//   3. a wavefront takes eight table rows, far apart since the frequent ids are neighbours (in turn: 61 us instead of 44), adds
-//      up the partial rows of an id that several runs hold, and writes zeros for an id that does not occur.  Every row of the
-//      table is written once.
+//   3. the partial rows of an id that several runs hold are added up in order.
 //
-// 32 768 tokens by a law of words, 50 001 rows of 1024, bf16 to fp32: 106 us; sorting 31 in four launches, the runs 25 (63 MB
-// read, 48 written), the rows 44 (170 MB written).  Four workers of 1201 tokens, 5003 rows of 389 fp32: 32 us; 12.6, 12.3 and 8.6.
+// 32 768 tokens by a law of words, 50 001 rows of 1024, bf16 to fp32: 91 us; sorting 47 in four launches, which write 205 MB beside
+// it (31 without; with the table cleared after the sums, by id: 44 more), the runs 24 (63 MB read, 48 written), joining 11.  Sorting in two
+// launches that count all ids in every workgroup: 76.  Four workers of 1201 tokens, 5003 rows of 389 fp32: 30 us; 13.4, 12.1 and 4.3.
 #include "element_io.h"
 #include "ols_internal.h"
 
@@ -38,7 +39,6 @@ constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kPerWave = kSortItems / kSortWaves, kPerLane = kPerWave / 64;
 constexpr int kRun = 16;                    // sorted positions of a run
-constexpr int kRowsPerWave = 8;             // table rows of a wavefront of the last stage
 
 template <typename TI, typename TO>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedParams p, int lanes) {
@@ -63,6 +63,13 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedParams p, int lane
 
 // ---- sorting ------------------------------------------------------------------------------------------------------------
 
+// The gradient's rows as workgroups behind those of the sort clear them: pieces of kClearBytes.
+struct ClearParams {
+    char* out;                   // rows of row_bytes, row_pitch apart; a table without gaps is one long row
+    int64_t rows, row_bytes, row_pitch, group_bytes;
+    int64_t per_row, rows_per;   // pieces of a row, or (short rows) rows of a piece
+    int64_t first;               // this launch's first piece
+};
 struct SortParams {
     const int32_t* ids;          // first pass: the caller's ids; later ones: keys_in
     int64_t ids_group;
@@ -71,18 +78,34 @@ struct SortParams {
     int32_t* keys_out;
     int32_t* pos_out;
     int32_t* counts;             // [group][block][kDigits]
-    int32_t* bounds;             // [group][2][vocab]: cleared by the first launch, see RowsParams
     int64_t n;                   // ids per group
     int blocks, shift;
     int64_t vocab;
+    ClearParams clear;
 };
 
-// Workgroups behind those of the sort clear the table of bounds.
-constexpr int kClearInts = 16384;           // of one workgroup
-__device__ __forceinline__ bool cleared(const SortParams& p, int group, int block) {
-    if (block < 0) return false;
-    const int64_t n = 2 * p.vocab, from = (int64_t)block * kClearInts, to = min(n, from + kClearInts);
-    for (int64_t i = from + threadIdx.x; i < to; i += kSortThreads) p.bounds[group * n + i] = 0;
+constexpr int64_t kClearBytes = 65536;       // of one workgroup; 32 to 256 KiB take the same time
+// bytes [from, to) of a row by some lanes, `lane` of `lanes`
+__device__ __forceinline__ void clear_bytes(char* row, int64_t from, int64_t to, int lane, int lanes) {
+    for (int64_t at = from + 16 * lane; at < to; at += 16 * lanes) {
+        if (at + 16 <= to) {
+            *(u4any*)(row + at) = u4any{0u, 0u, 0u, 0u};
+        } else {
+            for (int64_t e = at; e < to; e += 2) *(uint16_t*)(row + e) = 0;
+        }
+    }
+}
+__device__ __forceinline__ bool cleared(const ClearParams& p, int group, int64_t piece) {
+    if (piece < 0) return false;
+    piece += p.first;
+    char* out = p.out + group * p.group_bytes;
+    if (p.rows_per == 0) {
+        const int64_t r = piece / p.per_row, from = piece % p.per_row * kClearBytes;
+        clear_bytes(out + r * p.row_pitch, from, min(p.row_bytes, from + kClearBytes), threadIdx.x, kSortThreads);
+    } else {
+        const int64_t r0 = piece * p.rows_per, r1 = min(p.rows, r0 + p.rows_per);
+        for (int64_t r = r0 + threadIdx.x / 64; r < r1; r += kSortWaves) clear_bytes(out + r * p.row_pitch, 0, p.row_bytes, threadIdx.x % 64, 64);
+    }
     return true;
 }
 
@@ -200,7 +223,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_one_block_kernel(SortParams
                                                                       int32_t* pos_b, int passes) {
     __shared__ int cnt[kSortWaves][kDigits];
     __shared__ int before[kDigits];
-    if (cleared(p, blockIdx.y, (int)blockIdx.x - 1)) return;
+    if (cleared(p.clear, blockIdx.y, (int64_t)blockIdx.x - 1)) return;
     for (int pass = 0; pass < passes; ++pass) {
         const bool to_a = (passes - 1 - pass) % 2 == 0;   // the last pass ends in a
         p.keys_out = to_a ? keys_a : keys_b;
@@ -219,7 +242,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_one_block_kernel(SortParams
 
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortParams p, int first) {
     __shared__ int hist[kDigits];
-    if (cleared(p, blockIdx.y, (int)blockIdx.x - p.blocks)) return;
+    if (cleared(p.clear, blockIdx.y, (int64_t)blockIdx.x - p.blocks)) return;
     count_block(p, load_items(p, blockIdx.y, blockIdx.x, first, false), hist);
     int32_t* out = p.counts + ((int64_t)blockIdx.y * p.blocks + blockIdx.x) * kDigits;
     for (int d = threadIdx.x; d < kDigits; d += kSortThreads) out[d] = hist[d];
@@ -231,6 +254,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortParams p
     __shared__ int cnt[kSortWaves][kDigits];
     __shared__ int before[kDigits], total[kDigits];
     static_assert(kSortThreads == 2 * kDigits, "two lanes add up a digit's counts");
+    if (cleared(p.clear, blockIdx.y, (int64_t)blockIdx.x - p.blocks)) return;
     const int32_t* counts = p.counts + (int64_t)blockIdx.y * p.blocks * kDigits;
     const int d = threadIdx.x % kDigits, half = threadIdx.x / kDigits, me = blockIdx.x;
     const Items t = load_items(p, blockIdx.y, blockIdx.x, first, true);
@@ -258,40 +282,33 @@ struct RowsParams {
     EmbedGradParams g;
     const int32_t* keys;
     const int32_t* pos;
-    int32_t* bounds;     // [group][2][vocab]: an id's first sorted position and one behind its last; 0, 0 where there is none
+    int32_t* ends;       // [group][vocab]: one behind the last sorted position of an id that several runs hold
     float* partial;      // [group][run][2][width]: the sum that the run begins in the middle of, and the one that it ends in the middle of
     int64_t runs;
 };
 
-// Rows whose loads are in flight together.
-template <typename T, int NV>
-constexpr int row_batch() { return sizeof(T) * NV <= 4 ? 8 : 4; }
-
-// Columns c + 512 t + 8 lane .. of a row of the gradient.
-template <typename TO, int NV>
-__device__ __forceinline__ void write_row(const RowsParams& q, int64_t group, int64_t v, int64_t c, int lane, const float (&sum)[NV][8]) {
-    TO* out = (TO*)q.g.grad + group * q.g.grad_group + v * q.g.grad_row;
+// Eight columns from c of a row of the gradient.
+template <typename TO>
+__device__ __forceinline__ void write_row(const RowsParams& q, int64_t group, int64_t v, int64_t c, const float (&sum)[8]) {
+    if (c >= q.g.width) return;
+    TO* out = (TO*)q.g.grad + group * q.g.grad_group + v * q.g.grad_row + c;
+    const int left = (int)min((int64_t)8, q.g.width - c);
+    float o[8];
+    if (q.g.accumulate) {
+        load_upto8(out, left, 0.0f, o);
 #pragma unroll
-    for (int t = 0; t < NV; ++t) {
-        const int64_t at = c + 512 * t + 8 * lane;
-        if (at >= q.g.width) continue;
-        const int left = (int)min((int64_t)8, q.g.width - at);
-        float o[8];
-        if (q.g.accumulate) {
-            load_upto8(out + at, left, 0.0f, o);
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(q.g.scale, sum[e], o[e]);
+    } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf(q.g.scale, sum[t][e], o[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = q.g.scale * sum[t][e];
-        }
-        store_upto8(out + at, left, o);
+        for (int e = 0; e < 8; ++e) o[e] = q.g.scale * sum[e];
     }
+    store_upto8(out, left, o);
 }
 
-template <typename TI, typename TO, int NV>
+// A wavefront takes a run and 512 columns, eight a lane; B rows are under way together.
+template <typename TI, typename TO>
 __global__ __launch_bounds__(kThreads) void embed_runs_kernel(RowsParams q) {
-    constexpr int B = row_batch<TI, NV>();
+    constexpr int B = sizeof(TI) == 2 ? 16 : 8;
     static_assert(kRun % B == 0 && kRun < 64, "whole batches, and a lane per position");
     const int lane = threadIdx.x % 64;
     const int64_t run = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = blockIdx.y;
@@ -303,114 +320,83 @@ __global__ __launch_bounds__(kThreads) void embed_runs_kernel(RowsParams q) {
     const int key = lane < have || (lane == have && from + have < n) ? keys[lane] : -1;
     const int row = lane < have ? q.pos[group * n + from + lane] : 0;
     const int before = from > 0 ? keys[-1] : -1;
-    const int up = __shfl_up(key, 1), down = __shfl_down(key, 1);
+    const int down = __shfl_down(key, 1);
     const int64_t vocab = q.g.vocab;
-    if (blockIdx.z == 0 && lane < have && key < vocab) {
-        int32_t* b = q.bounds + group * 2 * vocab;
-        if ((lane ? up : before) != key) b[key] = (int)(from + lane);
-        if (down != key) b[vocab + key] = (int)(from + lane + 1);
-    }
-    const int64_t c = (int64_t)blockIdx.z * 512 * NV;
+    if (blockIdx.z == 0 && lane < have && key < vocab && key == before && down != key) q.ends[group * vocab + key] = (int)(from + lane + 1);
+    const int64_t c = (int64_t)blockIdx.z * 512 + 8 * lane;
+    const int left = (int)max((int64_t)0, min((int64_t)8, q.g.width - c));
     const TI* base = (const TI*)q.g.dout + group * q.g.dout_group + c;
-    float sum[NV][8] = {};
+    float sum[8] = {};
     bool open = __builtin_amdgcn_readlane(key, 0) == before;    // the sum began in an earlier run
     for (int k = 0; k < have; k += B) {
-        Raw8<TI> v[B][NV];
+        Raw8<TI> v[B];
 #pragma unroll
-        for (int r = 0; r < B; ++r) {
-            const TI* src = base + __builtin_amdgcn_readlane(row, k + r) * q.g.dout_row;     // positions past the end: row 0
-#pragma unroll
-            for (int t = 0; t < NV; ++t) {
-                const int64_t at = 512 * t + 8 * lane;
-                v[r][t].load(src + at, (int)max((int64_t)0, min((int64_t)8, q.g.width - c - at)));
-            }
-        }
+        for (int r = 0; r < B; ++r) v[r].load(base + __builtin_amdgcn_readlane(row, k + r) * q.g.dout_row, left);   // positions past the end: row 0
 #pragma unroll
         for (int r = 0; r < B; ++r) {
             const int i = k + r, id = __builtin_amdgcn_readlane(key, i);
             if (i >= have || id >= vocab) return;               // sorted: what is no token comes last
 #pragma unroll
-            for (int t = 0; t < NV; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[t][e] += v[r][t].get(e);
+            for (int e = 0; e < 8; ++e) sum[e] += v[r].get(e);
             const bool ends = __builtin_amdgcn_readlane(key, i + 1) != id;
             if (!ends && i + 1 < have) continue;
             if (ends && !open) {
-                write_row<TO, NV>(q, group, id, c, lane, sum);
-            } else {
-                float* out = q.partial + ((group * q.runs + run) * 2 + (open ? 0 : 1)) * q.g.width + c;
-#pragma unroll
-                for (int t = 0; t < NV; ++t) {
-                    const int64_t at = 512 * t + 8 * lane;
-                    if (c + at < q.g.width) store_upto8(out + at, (int)min((int64_t)8, q.g.width - c - at), sum[t]);
-                }
+                write_row<TO>(q, group, id, c, sum);
+            } else if (left > 0) {
+                store_upto8(q.partial + ((group * q.runs + run) * 2 + (open ? 0 : 1)) * q.g.width + c, left, sum);
             }
             open = false;
 #pragma unroll
-            for (int t = 0; t < NV; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[t][e] = 0.0f;
+            for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
         }
     }
 }
 
-template <typename TO, int NV>
-__global__ __launch_bounds__(kThreads) void embed_rows_kernel(RowsParams q) {
-    // a wavefront's rows lie far apart: the frequent ids, whose sums take longest, are mostly neighbours
-    const int lane = threadIdx.x % 64;
-    const int64_t waves = (int64_t)gridDim.x * (kThreads / 64), v0 = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int64_t group = blockIdx.y, vocab = q.g.vocab;
-    const int32_t* b = q.bounds + group * 2 * vocab;
-    const bool mine = lane < kRowsPerWave && v0 + lane * waves < vocab;
-    const int first = mine ? b[v0 + lane * waves] : 0, last = mine ? b[vocab + v0 + lane * waves] : 0;
-    const int64_t c = (int64_t)blockIdx.z * 512 * NV;
-    for (int r = 0; r < kRowsPerWave; ++r) {
-        const int64_t v = v0 + r * waves;
-        if (v >= vocab) break;
-        const int from = __builtin_amdgcn_readlane(first, r), to = __builtin_amdgcn_readlane(last, r);
-        if (to == 0) {
-            if (q.g.accumulate) continue;
-            TO* out = (TO*)q.g.grad + group * q.g.grad_group + v * q.g.grad_row;
-            const int64_t end = min(q.g.width, c + 512 * NV);
-            constexpr int kVec = 16 / sizeof(TO);
-            for (int64_t at = c + lane * kVec; at < end; at += 64 * kVec) {
-                if (at + kVec <= end) {
-                    *(u4any*)(out + at) = u4any{0u, 0u, 0u, 0u};
-                } else {
-                    for (int e = 0; e < end - at; ++e) store1(out + at + e, 0.0f);
-                }
-            }
-            continue;
+// The ids that several runs hold: workgroups of the run that such an id begins in add up its partial rows, 256 columns each.  Every
+// wavefront adds a quarter of them in order, sixteen rows under way together (the most frequent id of a text has a hundred and
+// more), and the quarters are added in order.
+template <typename TO>
+__global__ __launch_bounds__(kThreads) void embed_join_kernel(RowsParams q) {
+    constexpr int B = 16, C = 4, W = kThreads / 64;
+    __shared__ float quarter[W][64 * C];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t run = blockIdx.x, group = blockIdx.y, from = run * kRun, next = from + kRun;
+    const int32_t* keys = q.keys + group * q.g.tokens;
+    const int id = keys[next], first = keys[from], last = keys[next - 1], before = from > 0 ? keys[from - 1] : -1;
+    if (last != id || id >= q.g.vocab || (first == id && before == id)) return;
+    const int64_t all = (q.ends[group * q.g.vocab + id] - 1) / kRun - run + 1, each = all <= B ? B : (all + W - 1) / W;
+    const int64_t width = q.g.width, c = (int64_t)blockIdx.z * (64 * C) + lane, k1 = min(all, (wave + 1) * each);
+    float sum[C] = {};
+    for (int64_t k = wave * each; k < k1; k += B) {
+        float p[B][C];
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const float* part = q.partial + ((group * q.runs + run + k + j) * 2 + (k + j == 0 ? 1 : 0)) * width + c;
+#pragma unroll
+            for (int t = 0; t < C; ++t) p[j][t] = k + j < k1 && c + 64 * t < width ? part[64 * t] : 0.0f;
         }
-        const int64_t run0 = from / kRun, run1 = (to - 1) / kRun;
-        if (run0 == run1) continue;                            // its run has written it
-        float sum[NV][8] = {};
-        for (int64_t k = run0; k <= run1; k += 4) {
-            float p[4][NV][8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float* part = q.partial + ((group * q.runs + k + j) * 2 + (k + j == run0 ? 1 : 0)) * q.g.width + c;
+        for (int j = 0; j < B; ++j)
 #pragma unroll
-                for (int t = 0; t < NV; ++t) {
-                    const int64_t at = 512 * t + 8 * lane;
-                    load_upto8(part + at, k + j <= run1 ? (int)max((int64_t)0, min((int64_t)8, q.g.width - c - at)) : 0, 0.0f, p[j][t]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int t = 0; t < NV; ++t)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[t][e] += p[j][t][e];
-        }
-        write_row<TO, NV>(q, group, v, c, lane, sum);
+            for (int t = 0; t < C; ++t) sum[t] += p[j][t];
     }
+#pragma unroll
+    for (int t = 0; t < C; ++t) quarter[wave][64 * t + lane] = sum[t];
+    __syncthreads();
+    const int64_t at = (int64_t)blockIdx.z * (64 * C) + threadIdx.x;
+    static_assert(64 * C == kThreads, "a column each");
+    if (at >= width) return;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) v += quarter[w][threadIdx.x];
+    TO* out = (TO*)q.g.grad + group * q.g.grad_group + id * q.g.grad_row + at;
+    store1(out, q.g.accumulate ? fmaf(q.g.scale, v, load1(out)) : q.g.scale * v);
 }
 
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
 struct GradPlan {
-    int64_t blocks, runs, off_keys[2], off_pos[2], off_counts, off_bounds, off_partial, bytes;
+    int64_t blocks, runs, off_keys[2], off_pos[2], off_counts, off_ends, off_partial, bytes;
 };
 GradPlan grad_plan(int groups, int64_t tokens, int64_t vocab, int64_t width) {
     GradPlan p;
@@ -422,24 +408,17 @@ GradPlan grad_plan(int groups, int64_t tokens, int64_t vocab, int64_t width) {
         p.off_pos[i] = at, at = up256(at + groups * tokens * 4);
     }
     p.off_counts = at, at = up256(at + (p.blocks > 1 ? groups * p.blocks * kDigits * 4 : 0));
-    p.off_bounds = at, at = up256(at + groups * 2 * vocab * 4);
+    p.off_ends = at, at = up256(at + groups * vocab * 4);
     p.off_partial = at, at = up256(at + groups * p.runs * 2 * width * 4);
     p.bytes = at;
     return p;
 }
 
-template <typename TI, typename TO, int NV>
-void launch_sums(const RowsParams& q, hipStream_t stream) {
-    const int tiles = (int)((q.g.width + 512 * NV - 1) / (512 * NV));
-    if (q.runs)
-        embed_runs_kernel<TI, TO, NV><<<dim3((unsigned)((q.runs + 3) / 4), q.g.groups, tiles), kThreads, 0, stream>>>(q);
-    embed_rows_kernel<TO, NV><<<dim3((unsigned)((q.g.vocab + 4 * kRowsPerWave - 1) / (4 * kRowsPerWave)), q.g.groups, tiles), kThreads, 0, stream>>>(q);
-}
-
 template <typename TI, typename TO>
 void launch_sums(const RowsParams& q, hipStream_t stream) {
-    if (q.g.width <= 512) launch_sums<TI, TO, 1>(q, stream);
-    else launch_sums<TI, TO, 2>(q, stream);
+    if (q.runs == 0) return;
+    embed_runs_kernel<TI, TO><<<dim3((unsigned)((q.runs + kThreads / 64 - 1) / (kThreads / 64)), q.g.groups, (unsigned)((q.g.width + 511) / 512)), kThreads, 0, stream>>>(q);
+    if (q.runs > 1) embed_join_kernel<TO><<<dim3((unsigned)(q.runs - 1), q.g.groups, (unsigned)((q.g.width + 255) / 256)), kThreads, 0, stream>>>(q);
 }
 
 }  // namespace
@@ -471,22 +450,41 @@ hipError_t launch_embed_grad(const EmbedGradParams& g, void* ws, hipStream_t str
     const int passes = (bits + kDigitBits - 1) / kDigitBits;
     SortParams s = {};
     s.ids = g.ids, s.ids_group = g.ids_group, s.n = g.tokens, s.vocab = g.vocab;
-    s.counts = (int32_t*)(w + plan.off_counts), s.bounds = (int32_t*)(w + plan.off_bounds);
-    s.blocks = (int)plan.blocks;
-    const unsigned clear = (unsigned)((2 * g.vocab + kClearInts - 1) / kClearInts);
+    s.counts = (int32_t*)(w + plan.off_counts), s.blocks = (int)plan.blocks;
+    // every launch of the sort, which occupies a few of the compute units, clears its share of the table
+    const int shares = plan.blocks <= 1 ? 1 : 3 * passes;
+    ClearParams& c = s.clear;
+    int64_t pieces = 0;
+    if (!g.accumulate && g.vocab > 0) {
+        const int64_t elem = g.grad_dtype == OLS_F32 ? 4 : 2;
+        c.out = (char*)g.grad, c.group_bytes = g.grad_group * elem, c.rows = g.vocab, c.row_bytes = g.width * elem, c.row_pitch = g.grad_row * elem;
+        if (g.grad_row == g.width) c.row_bytes *= g.vocab, c.rows = 1;
+        c.rows_per = c.rows > 1 && c.row_bytes < kClearBytes ? kClearBytes / c.row_bytes : 0;
+        c.per_row = (c.row_bytes + kClearBytes - 1) / kClearBytes;
+        pieces = c.rows_per ? (c.rows + c.rows_per - 1) / c.rows_per : c.rows * c.per_row;
+    }
+    int done = 0;
+    auto clear = [&](int n) {
+        c.first = pieces * done / shares;
+        done += n;
+        return (unsigned)(pieces * done / shares - c.first);
+    };
     if (plan.blocks <= 1) {          // without ids the passes find none
-        sort_one_block_kernel<<<dim3(1 + clear, g.groups), kSortThreads, 0, stream>>>(s, keys[0], pos[0], keys[1], pos[1], g.tokens > 0 ? passes : 0);
+        const unsigned blocks = 1 + clear(1);
+        sort_one_block_kernel<<<dim3(blocks, g.groups), kSortThreads, 0, stream>>>(s, keys[0], pos[0], keys[1], pos[1], g.tokens > 0 ? passes : 0);
     } else {
         for (int pass = 0; pass < passes; ++pass) {
             const int to = (passes - 1 - pass) % 2;   // the last pass ends in list 0
             s.keys_in = keys[1 - to], s.pos_in = pos[1 - to], s.keys_out = keys[to], s.pos_out = pos[to];
             s.shift = pass * kDigitBits;
-            sort_count_kernel<<<dim3((unsigned)plan.blocks + (pass == 0 ? clear : 0), g.groups), kSortThreads, 0, stream>>>(s, pass == 0);
-            sort_scatter_kernel<<<dim3((unsigned)plan.blocks, g.groups), kSortThreads, 0, stream>>>(s, pass == 0);
+            const unsigned counting = (unsigned)plan.blocks + clear(1);
+            sort_count_kernel<<<dim3(counting, g.groups), kSortThreads, 0, stream>>>(s, pass == 0);
+            const unsigned scattering = (unsigned)plan.blocks + clear(2);       // takes twice as long
+            sort_scatter_kernel<<<dim3(scattering, g.groups), kSortThreads, 0, stream>>>(s, pass == 0);
         }
     }
     RowsParams q;
-    q.g = g, q.keys = keys[0], q.pos = pos[0], q.partial = (float*)(w + plan.off_partial), q.runs = plan.runs, q.bounds = s.bounds;
+    q.g = g, q.keys = keys[0], q.pos = pos[0], q.partial = (float*)(w + plan.off_partial), q.runs = plan.runs, q.ends = (int32_t*)(w + plan.off_ends);
     if (g.dtype == OLS_F32 && g.grad_dtype == OLS_F32) launch_sums<float, float>(q, stream);
     else if (g.dtype == OLS_F32) launch_sums<float, uint16_t>(q, stream);
     else if (g.grad_dtype == OLS_F32) launch_sums<uint16_t, float>(q, stream);
