@@ -440,7 +440,7 @@ OLS_API int64_t ols_embed_grad_workspace_bytes(int groups, int64_t tokens, int64
  * with x [rows][width], w_gate and w_up [width][hidden], w_down [hidden][out], y [rows][out]; no biases.
  *   - dtype: the type of x, y, dy and dx.  OLS_F32: products of fp32 accuracy (every operand as three bf16 terms that add up to
  *     it exactly; weights and their gradients are fp32 too).  OLS_BF16: products of bf16 operands with fp32 sums; h and the
- *     gradients at a and b are rounded to bf16 where they become operands.  The weights are bf16, or fp32 master weights that
+ *     gradients at a and b are rounded to bf16 where they become operands (small blocks of up to 32 rows: two bf16 terms).  The weights are bf16, or fp32 master weights that
  *     are rounded to bf16 on the way (weight_dtype); their gradients are either (grad_dtype).
  *   - ols_gated_ffn reads x and the weights and writes y.  For a later backward pass give it `saved` (ols_gated_ffn_saved_bytes,
  *     256-byte aligned), where it leaves a, b and h; NULL otherwise.  Up to 8 rows without `saved` are read by kernels made for

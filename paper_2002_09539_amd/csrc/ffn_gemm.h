@@ -4,7 +4,7 @@
 // that the block needs.  An operand is a matrix of 16-byte aligned rows; it is read either
 //   * "KC": the contraction index is the contiguous one (memory [rows][K]), or
 //   * "RC": the operand's own index is (memory [K][rows]), transposed by the LDS read.
-// The gradient at the block's input, da Wg^T + db Wu^T, is two segments of one contraction.  Products of fp32 operands are
+// The gradient at the block's input, da Wg^T + db Wu^T, is two segments of one contraction; an operand in two terms doubles them.  Products of fp32 operands are
 // in ffn_gemm_f32.h, on the same tiles, jobs and epilogues.
 //
 // A tile's slices of 32 contraction indices go from memory straight into LDS (16 bytes a lane, no registers in between),
@@ -38,6 +38,7 @@ namespace ffn {
 constexpr int kBK = 32;              // contraction indices of a slice
 constexpr int kRing = 4;             // buffers
 constexpr int kXcds = 8;
+constexpr int kMaxSegments = 4;
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
@@ -153,6 +154,7 @@ struct Epilogue {
     // their own rounding (3.1e-3 against 64 bits where da's and the result's roundings alone make 2.3e-3).
     float *a, *b;
     uint16_t *h, *h2;                   // kUp: h.  kGateGrad: da, db
+    int64_t rest;                       // from a bf16 value to the place of what its rounding has left over; 0: that is not kept
 };
 
 // By the hardware's exponential and reciprocal, each good to a unit in the last place; the argument's rounding adds 2^-24 |a| to
@@ -180,9 +182,19 @@ __device__ __forceinline__ void act_both(int act, float a, float& value, float& 
 
 // eight elements of an internal tensor: bf16, or the three terms that add up to the fp32 values, side by side
 template <bool SPLIT>
-__device__ __forceinline__ void store_terms(uint16_t* p, const float (&v)[8]) {
+__device__ __forceinline__ void store_terms(uint16_t* p, const float (&v)[8], int64_t rest = 0) {
     if constexpr (!SPLIT) {
-        *(u4*)p = u4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        const u4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        *(u4*)p = w;
+        if (rest) {
+            float r[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float hi = i % 2 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+                r[i] = fabsf(hi) < INFINITY ? v[i] - hi : 0.0f;
+            }
+            *(u4*)(p + rest) = u4{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3]), pack_bf16(r[4], r[5]), pack_bf16(r[6], r[7])};
+        }
     } else {
         const Split8 s = split8(f4{v[0], v[1], v[2], v[3]}, f4{v[4], v[5], v[6], v[7]});
         *(u4*)p = s.hi;
@@ -217,7 +229,7 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
                 store8(e.a + at, a);
                 store8(e.b + at, b);
             }
-            store_terms<SPLIT>(e.h + P * at, x);
+            store_terms<SPLIT>(e.h + P * at, x, e.rest);
         } else {
             load8(e.a + at, a);
             load8(e.b + at, b);
@@ -232,8 +244,8 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
                 for (int i = 0; i < 8; ++i)
                     if (i >= real) x[i] = y[i] = 0.0f;
             }
-            store_terms<SPLIT>(e.h + P * at, x);
-            store_terms<SPLIT>(e.h2 + P * at, y);
+            store_terms<SPLIT>(e.h + P * at, x, e.rest);
+            store_terms<SPLIT>(e.h2 + P * at, y, e.rest);
         }
     }
 }
@@ -244,8 +256,9 @@ struct Job {
     const uint16_t *a, *b, *b2;          // b2: kUp's second panel, or the second tensor of segments that say so
     int64_t a_group, b_group, b2_group, a_pitch, b_pitch;
     int64_t M, N, K, a_inner8, b_inner8; // inner extents of the operands as stored, up to 8 elements
-    int64_t second_a;                    // from a to the second segment's operand
-    int segments;                        // 1, or 2: the second one takes b2
+    int64_t seg_a[kMaxSegments], seg_b[kMaxSegments];   // from a and b (or b2) to each segment's operands
+    unsigned seg_second;                 // bit s: segment s takes b2
+    int segments;
     int tiles_m, tiles_n;
     Epilogue epi;
 };
@@ -383,8 +396,8 @@ __global__ __launch_bounds__(gemm_threads<T>(), 2) void gemm_kernel(GemmArgs p) 
     Cursor cur_a, cur_b, cur_b2;
     auto enter = [&]() {                                  // the segment's first slice of this range
         const int64_t k0 = (int64_t)from * kBK;
-        const uint16_t* a = seg ? base_a + q.second_a : base_a;
-        const uint16_t* b = PANELS == 1 && seg ? base_b2 : base_b;
+        const uint16_t* a = base_a + q.seg_a[seg];
+        const uint16_t* b = (PANELS == 1 && ((q.seg_second >> seg) & 1u) ? base_b2 : base_b) + q.seg_b[seg];
         cur_a = A_RC ? TA::cursor(a, q.a_pitch, q.a_inner8, q.K, at.m0, k0) : TA::cursor(a, q.a_pitch, q.M, q.a_inner8, at.m0, k0);
         cur_b = B_RC ? TB::cursor(b, q.b_pitch, q.b_inner8, q.K, at.n0, k0) : TB::cursor(b, q.b_pitch, q.N, q.b_inner8, at.n0, k0);
         if constexpr (PANELS == 2) cur_b2 = TB::cursor(base_b2, q.b_pitch, q.b_inner8, q.K, at.n0, k0);

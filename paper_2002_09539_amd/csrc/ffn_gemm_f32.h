@@ -194,12 +194,12 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs p) {
     };
     Walk wa, wb;
     auto enter_a = [&]() {
-        const uint16_t* a = q.a + at.group * q.a_group + (wa.seg ? q.second_a : 0);
+        const uint16_t* a = q.a + at.group * q.a_group + q.seg_a[wa.seg];
         wa.cur = A_RC ? TA::cursor(a, q.a_pitch, q.a_inner8, q.K, at.m0, k0) : TA::cursor(a, q.a_pitch, q.M, q.a_inner8, at.m0, k0);
         wa.slices = here, wa.k_left = (A_RC ? q.K : q.a_inner8) - k0;
     };
     auto enter_b = [&]() {
-        const bool second = PANELS == 1 ? wb.seg != 0 : wave >= 2;
+        const bool second = PANELS == 1 ? ((q.seg_second >> wb.seg) & 1u) != 0 : wave >= 2;
         if constexpr (PLAIN) {
             const float* b = second ? (const float*)q.b2 + at.group * q.b2_group : (const float*)q.b + at.group * q.b_group;
             wb.cur = PB::cursor(b, q.b_pitch, B_RC ? q.b_inner8 : q.N, q.K, at.n0, k0);

@@ -197,12 +197,19 @@ struct Arena {
 struct View {
     const uint16_t* p = nullptr;
     int64_t pitch = 0, group = 0, inner8 = 0;
+    int64_t rest = 0;                  // to the second term, where it is kept
     bool plain = false;                // fp32 as the caller has it
 };
 
 bool lies_well(const ols_matrix& m, int dtype, int64_t inner) {
     return dtype == OLS_BF16 && inner % 8 == 0 && m.row % 8 == 0 && m.row <= (1 << 22) && m.group % 8 == 0 && ((uintptr_t)m.dev & 15) == 0;
 }
+
+// A small bf16 block of few rows keeps what rounding h, da and db to bf16 leaves over, as a second term: the results of few roundings
+// scatter around 1.41 times the error of their own (up to 1.6), and the longer contractions cost nothing there that shows beside the
+// launches (forward and backward, 17 rows, 104 - 5600 - 22: 71 to 80 us with it, 74 without).  With more weights they do: 32 rows,
+// 1024 - 2816 - 1024: 86, 80; 8 rows, 2048 - 5632 - 2048: 124, 110.
+bool keeps_rest(const ols_ffn& f) { return f.dtype == OLS_BF16 && f.rows <= 32 && f.hidden * (2 * f.width + f.out) <= (1 << 21); }
 
 struct Maker {                         // lays operands out; without a stream it only measures
     const ols_ffn& f;
@@ -259,13 +266,22 @@ struct Maker {                         // lays operands out; without a stream it
     View internal(int64_t rows, int64_t inner, void* at) const {
         View v;
         v.inner8 = up8(inner), v.pitch = terms() * v.inner8, v.group = rows * v.pitch, v.p = (const uint16_t*)at;
+        v.rest = keeps_rest(f) ? f.groups * v.group : 0;
         return v;
     }
-    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * terms() * f.groups * rows * up8(inner); }
+    int64_t internal_bytes(int64_t rows, int64_t inner) const { return 2 * (keeps_rest(f) ? 2 : terms()) * f.groups * rows * up8(inner); }
 };
 
 void set_operands(Job& j, const View& a, const View& b, const View* a2, const View* b2) {
-    j.segments = a2 ? 2 : 1, j.second_a = a2 ? a2->p - a.p : 0;
+    j.segments = 0, j.seg_second = 0;
+    for (int t = 0; t < (a2 ? 2 : 1); ++t) {
+        const View &u = t ? *a2 : a, &v = t ? *b2 : b;
+        for (int k = 0; k < 1 + (u.rest || v.rest); ++k) {        // at most one of the two is in terms
+            const int s = j.segments++;
+            j.seg_a[s] = u.p - a.p + (k ? u.rest : 0), j.seg_b[s] = k ? v.rest : 0;
+            if (t) j.seg_second |= 1u << s;
+        }
+    }
     j.a = a.p, j.a_group = a.group, j.a_pitch = a.pitch, j.a_inner8 = a.inner8;
     j.b = b.p, j.b_group = b.group, j.b_pitch = b.pitch, j.b_inner8 = b.inner8;
     if (b2) j.b2 = b2->p, j.b2_group = b2->group;
@@ -342,6 +358,7 @@ Shape choose(const Job* jobs, int n, int groups, int panels, bool split, bool ac
             Shape s{t, (int)tiles, 0, 1};
             if (ranges > 1) {
                 s.whole = (int)(tiles / slots * slots), s.rest = (int)(tiles - s.whole), s.ranges = ranges;
+                if (t == 256 && activation) continue;      // 8192 x 5632 over 2048: 488 us whole, 485 and 22 to join with the last tiles cut
                 if (s.rest == 0 || slices < ranges || work / ranges < 4 || (int64_t)s.rest * ranges > slots) continue;
             }
             const double us = estimate(s, work, activation, split);
@@ -421,7 +438,7 @@ Saved saved_layout(const ols_ffn& f) {
     s.off_a = 0;
     s.off_b = up256(elems * 4);
     s.off_h = 2 * s.off_b;
-    s.bytes = up256(s.off_h + elems * 2 * (f.dtype == OLS_F32 ? 3 : 1));
+    s.bytes = up256(s.off_h + elems * 2 * (f.dtype == OLS_F32 ? 3 : keeps_rest(f) ? 2 : 1));
     return s;
 }
 
@@ -486,7 +503,7 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
     up.M = f.rows, up.N = f.hidden, up.K = f.width;
     set_operands(up, x, wg, nullptr, &wu);
     up.epi.n = f.hidden, up.epi.n8 = h8, up.epi.pitch = up8(f.hidden), up.epi.m = f.rows, up.epi.act = f.act;
-    up.epi.a = saved ? (float*)(saved + s.off_a) : nullptr, up.epi.b = saved ? (float*)(saved + s.off_b) : nullptr, up.epi.h = (uint16_t*)hp;
+    up.epi.a = saved ? (float*)(saved + s.off_a) : nullptr, up.epi.b = saved ? (float*)(saved + s.off_b) : nullptr, up.epi.h = (uint16_t*)hp, up.epi.rest = h.rest;
     e = product<false, true, kUp>(&up, 1, f.groups, mk.split(), wg.plain, ws, go, stream);
     if (e != hipSuccess) return e;
     Job down = {};
@@ -545,7 +562,7 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         dh.M = f.rows, dh.N = f.hidden, dh.K = f.out;
         set_operands(dh, dy, wd, nullptr, nullptr);
         dh.epi.n = f.hidden, dh.epi.n8 = h8, dh.epi.pitch = up8(f.hidden), dh.epi.m = f.rows, dh.epi.act = f.act;
-        dh.epi.a = (float*)(saved + s.off_a), dh.epi.b = (float*)(saved + s.off_b), dh.epi.h = (uint16_t*)pa, dh.epi.h2 = (uint16_t*)pb;
+        dh.epi.a = (float*)(saved + s.off_a), dh.epi.b = (float*)(saved + s.off_b), dh.epi.h = (uint16_t*)pa, dh.epi.h2 = (uint16_t*)pb, dh.epi.rest = da.rest;
         e = product<false, false, kGateGrad>(&dh, 1, f.groups, mk.split(), wd.plain, ws, go, stream);
         if (e != hipSuccess) return e;
     }
