@@ -1,0 +1,143 @@
+"""Where the token operators change their way of working: sizes on both sides of each rule, against 64 bits.
+
+Tolerances.  fp32 products: 1e-5 of the result's norm (three products good to 2^-23.9 and sums of up to 3000 terms, as for the block's
+other tests).  Small bf16 blocks of few rows keep their inner tensors to 2^-17, so a result is the formula's rounded once: half a
+unit in the last place, 2^-8 at the most, of its own value, and 2^-13 of the results' root mean square for inner terms that cancel (2^-17
+times the square root of some hundred terms).  A gradient entry of the embedding is a sum of k rows in fp32: k 2^-23 of the sum of
+magnitudes, and the storage rounding."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _ops():
+    from paper_2002_09539_amd import operators
+    return operators
+
+
+def _block(x, wg, wu, wd, dy):
+    x, wg, wu, wd, dy = (t.double().cpu() for t in (x, wg, wu, wd, dy))
+    a, b = x @ wg, x @ wu
+    s = torch.sigmoid(a)
+    f, df = a * s, s + a * s * (1 - s)
+    h, dh = f * b, dy @ wd.transpose(-1, -2)
+    da, db = dh * b * df, dh * f
+    t = lambda v: v.transpose(-1, -2)  # noqa: E731
+    return h @ wd, da @ t(wg) + db @ t(wu), t(x) @ da, t(x) @ db, t(h) @ dy
+
+
+def _run(x, wg, wu, wd, dy):
+    y, saved = _ops().gated_ffn(x, wg, wu, wd, save=True)
+    return (y, *_ops().gated_ffn_grad(dy, x, wg, wu, wd, saved))
+
+
+def _inputs(seed, m, rows, width, hidden, out, dtype):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s, std=1.0: (torch.randn(*s, generator=g, device="cuda") * std).to(dtype)  # noqa: E731
+    return r(m, rows, width), r(m, width, hidden, std=width ** -0.5), r(m, width, hidden, std=width ** -0.5), r(m, hidden, out, std=hidden ** -0.5), r(m, rows, out)
+
+
+def _near(got, want):
+    for g, w in zip(got, want):
+        assert float((g.double().cpu() - w).norm()) <= 1e-5 * float(w.norm())
+
+
+@pytest.mark.parametrize("rows", [9, 128, 255, 256, 257, 400])
+def test_fp32_weights_read_in_place_or_laid_out(rows):
+    args = _inputs(rows, 2, rows, 75, 150, 43, F32)
+    _near(_run(*args), _block(*args))
+
+
+@pytest.mark.parametrize("width,hidden,out", [(1, 1, 1), (7, 9, 17), (15, 16, 33), (16, 17, 8), (31, 129, 130), (33, 2049, 3), (2050, 35, 66)])
+def test_fp32_contractions_that_end_inside_a_slice(width, hidden, out):
+    args = _inputs(width, 1, 37, width, hidden, out, F32)
+    _near(_run(*args), _block(*args))
+
+
+def test_fp32_weights_of_other_strides():
+    x, wg, wu, wd, dy = _inputs(5, 2, 40, 24, 70, 18, F32)
+    apart = torch.full((2, 24, 91), math.nan, device="cuda")[:, :, 7:77]      # what lies between the rows is nobody's
+    apart.copy_(wg)
+    _near(_run(x, apart, wu, wd, dy), _block(x, wg, wu, wd, dy))              # gate and up of two pitches
+    down = torch.full((2, 70, 19), math.nan, device="cuda")[:, :, 1:]
+    down.copy_(wd)
+    both = torch.full((2, 24, 2, 71), math.nan, device="cuda")
+    g, u = both[:, :, 0, :70], both[:, :, 1, 1:]
+    g.copy_(wg), u.copy_(wu)
+    _near(_run(x, g, u, down, dy), _block(x, wg, wu, wd, dy))
+    far = torch.zeros(3, (1 << 20) + 40, device="cuda")[:, :32]               # rows further apart than a tile reaches
+    far.copy_(torch.randn(3, 32, device="cuda"))
+    x, _, _, wd, dy = _inputs(6, 1, 40, 3, 32, 18, F32)
+    _near(_run(x[0], far, far, wd[0], dy[0]), _block(x[0], far, far, wd[0], dy[0]))
+
+
+@pytest.mark.parametrize("rows", [20, 300])
+def test_fp32_infinite_weights_reach_their_columns_only(rows):
+    x, wg, wu, wd, _ = _inputs(rows, 1, rows, 50, 40, 30, F32)
+    clean = _ops().gated_ffn(x, wg, wu, wd)
+    wd = wd.clone()
+    wd[0, 3, 7], wd[0, 9, 29], wd[0, 11, 0] = math.inf, -math.inf, math.nan
+    y = _ops().gated_ffn(x, wg, wu, wd)
+    keep = [c for c in range(30) if c not in (0, 7, 29)]
+    assert torch.equal(y[..., keep], clean[..., keep])
+    assert torch.isinf(y[..., 7]).all() and torch.isinf(y[..., 29]).all() and torch.isnan(y[..., 0]).all()
+
+
+@pytest.mark.parametrize("m,rows,width,hidden,out", [(1, 1, 40, 33, 24), (2, 9, 56, 128, 40), (1, 17, 104, 600, 22), (3, 32, 64, 72, 80)])
+def test_small_bf16_blocks_round_once(m, rows, width, hidden, out):
+    args = _inputs(rows, m, rows, width, hidden, out, BF16)
+    for got, want in zip(_run(*args), _block(*args)):
+        off = (got.double().cpu() - want).abs()
+        assert (off <= 2.0 ** -8 * want.abs() + 2.0 ** -13 * float(want.norm()) / math.sqrt(want.numel())).all()
+
+
+@pytest.mark.parametrize("rows", [32, 33])
+def test_bf16_on_both_sides_of_few_rows(rows):
+    args = _inputs(rows, 2, rows, 72, 136, 64, BF16)
+    for got, want in zip(_run(*args), _block(*args)):
+        assert float((got.double().cpu() - want).norm()) <= 1e-2 * float(want.norm())
+
+
+def _counted(counts, seed):
+    """Ids that occur that often, shuffled; between them ids that do not occur."""
+    ids = torch.cat([torch.full((c,), 3 * i + 1) for i, c in enumerate(counts)] + [torch.full((5,), -1)])
+    return ids[torch.randperm(len(ids), generator=torch.Generator().manual_seed(seed))].to(torch.int32).cuda(), 3 * len(counts) + 2
+
+
+@pytest.mark.parametrize("counts", [[16, 16, 16], [15, 1, 17, 31, 33, 2], [1] * 50, [300, 1, 16 * 70 + 3, 8, 40], [5000]])
+@pytest.mark.parametrize("width,dtype,out_dtype", [(129, F32, F32), (260, BF16, F32), (7, F32, BF16), (520, BF16, BF16)])
+def test_ids_that_several_runs_hold(counts, width, dtype, out_dtype):
+    ids, vocab = _counted(counts, len(counts))
+    g = torch.Generator(device="cuda").manual_seed(width)
+    d_out = torch.randn(2, len(ids), width, generator=g, device="cuda").to(dtype)
+    tokens = torch.stack([ids, ids.flip(0)])
+    wide = torch.full((2, vocab, width + 5), 7.0, dtype=out_dtype, device="cuda")
+    views = {"whole": torch.full((2, vocab, width), math.nan, dtype=out_dtype, device="cuda"), "apart": wide[:, :, 2: 2 + width]}
+    for name, out in views.items():
+        _ops().embed_grad(tokens, d_out, vocab, 0.5, out=out, workers=2)
+        start = out.clone()
+        _ops().embed_grad(tokens, d_out, vocab, 0.5, out=out, workers=2, accumulate=True)
+        for w in range(2):
+            t = tokens[w].long().cpu()
+            real = t >= 0
+            rows = d_out[w].double().cpu()[real]
+            want = torch.zeros(vocab, width, dtype=torch.float64).index_add_(0, t[real], rows) * 0.5
+            size = torch.zeros(vocab, width, dtype=torch.float64).index_add_(0, t[real], rows.abs()) * 0.5
+            unit = 2.0 ** -8 if out_dtype == BF16 else 2.0 ** -23
+            assert ((start[w].double().cpu() - want).abs() <= max(counts) * 2.0 ** -23 * size + unit * want.abs()).all(), name
+            twice = start[w].double().cpu() + want
+            assert ((out[w].double().cpu() - twice).abs() <= max(counts) * 2.0 ** -23 * size + unit * twice.abs()).all(), name
+    assert (wide[:, :, :2] == 7.0).all() and (wide[:, :, 2 + width:] == 7.0).all()
+
+
+def test_narrow_rows_that_lie_apart_are_cleared():
+    wide = torch.full((40000, 8), 5.0, device="cuda")
+    out = wide[:, 1:4]
+    _ops().embed_grad(torch.tensor([3, 39999, 3], dtype=torch.int32, device="cuda"), torch.ones(3, 3, device="cuda"), 40000, out=out)
+    assert (out[3] == 2).all() and (out[39999] == 1).all() and float(out.sum()) == 9.0
+    assert (wide[:, 0] == 5).all() and (wide[:, 4:] == 5).all()
