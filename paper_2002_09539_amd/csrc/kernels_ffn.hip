@@ -248,10 +248,15 @@ struct Maker {                         // lays operands out; without a stream it
         else pack_kernel<false><<<grid, 256, 0, stream>>>(packs);
         return hipGetLastError();
     }
-    // A weight.  One of fp32 that at most two rows of tiles read is not laid out: the tiles split it as they read it, which takes
-    // them a quarter longer and saves a pass of 10 bytes an element.  Forward, 43 rows, three workers, 1160 - 3726 - 50: 88 us
+    // A weight.  Large ones of fp32 that at most two rows of tiles read are not laid out: the tiles split them as they read them, which
+    // takes them a quarter longer and saves a pass of 10 bytes an element.  Forward, 43 rows, three workers, 1160 - 3726 - 50: 88 us
     // instead of 115; 128 rows, 1024 - 2816 - 1024: 52, 59; 256: 67, 74; 400 rows, three workers, 500 - 1000 - 700: 73.5, 68.7.
-    bool plain(const ols_matrix& m) const { return split() && f.rows <= 256 && m.row <= (1 << 20); }
+    // Forward and backward, four workers, 128 rows, 512 - 1024 - 512 (6.3 M weights): 124, 134; 200 rows, 800 - 2048 - 800 (4.9 M): 137,
+    // 140; 512 - 1408 - 512 (2.2 M): 110, 106; 20 rows, 128 - 256 - 128: 74, 68.
+    bool plain(const ols_matrix& m) const {
+        const int64_t weights = f.hidden * (2 * f.width + f.out) * (m.group ? f.groups : 1);
+        return split() && f.rows <= 256 && weights >= (3 << 20) && m.row <= (1 << 20);
+    }
     View weight(const ols_matrix& m, int64_t outer, int64_t inner, bool may_lie) {
         if (!may_lie || !plain(m)) return operand(m, f.weight_dtype, outer, inner, may_lie);
         View v;

@@ -141,3 +141,51 @@ def test_narrow_rows_that_lie_apart_are_cleared():
     _ops().embed_grad(torch.tensor([3, 39999, 3], dtype=torch.int32, device="cuda"), torch.ones(3, 3, device="cuda"), 40000, out=out)
     assert (out[3] == 2).all() and (out[39999] == 1).all() and float(out.sum()) == 9.0
     assert (wide[:, 0] == 5).all() and (wide[:, 4:] == 5).all()
+
+
+# more than 3 M weights: split by the tiles that read them, up to 256 rows
+LARGE = [(1021, 1100, 997), (17, 40001, 45), (2050, 770, 5), (31, 33, 100001), (1, 1 << 20, 1)]
+
+
+@pytest.mark.parametrize("width,hidden,out", LARGE)
+@pytest.mark.parametrize("rows", [9, 130])
+def test_fp32_large_weights_of_few_rows(rows, width, hidden, out):
+    args = _inputs(width, 1, rows, width, hidden, out, F32)
+    _near(_run(*args), _block(*args))
+
+
+@pytest.mark.parametrize("rows", [128, 256, 257])
+def test_fp32_large_weights_on_both_sides_of_the_rule(rows):
+    args = _inputs(rows, 2, rows, 331, 1500, 410, F32)
+    _near(_run(*args), _block(*args))
+
+
+def test_fp32_large_weights_of_other_strides():
+    m, rows, width, hidden, out = 2, 40, 331, 1500, 410
+    x, wg, wu, wd, dy = _inputs(5, m, rows, width, hidden, out, F32)
+    want = _block(x, wg, wu, wd, dy)
+    apart = torch.full((m, width, hidden + 21), math.nan, device="cuda")[:, :, 7: 7 + hidden]
+    apart.copy_(wg)
+    _near(_run(x, apart, wu, wd, dy), want)                                   # gate and up of two pitches
+    down = torch.full((m, hidden, out + 1), math.nan, device="cuda")[:, :, 1:]
+    down.copy_(wd)
+    both = torch.full((m, width, 2, hidden + 1), math.nan, device="cuda")
+    g, u = both[:, :, 0, :hidden], both[:, :, 1, 1:]
+    g.copy_(wg), u.copy_(wu)
+    _near(_run(x, g, u, down, dy), want)
+    far = torch.zeros(3, (1 << 20) + 40, device="cuda")                       # rows further apart than a tile reaches
+    far = far[:, :1 << 20]
+    far.copy_(torch.randn(3, 1 << 20, device="cuda"))
+    x, _, _, wd, dy = _inputs(6, 1, 10, 3, 1 << 20, 2, F32)
+    _near(_run(x[0], far, far, wd[0], dy[0]), _block(x[0], far, far, wd[0], dy[0]))
+
+
+def test_fp32_large_infinite_weights_reach_their_columns_only():
+    x, wg, wu, wd, _ = _inputs(20, 1, 20, 500, 2100, 700, F32)
+    clean = _ops().gated_ffn(x, wg, wu, wd)
+    wd = wd.clone()
+    wd[0, 3, 7], wd[0, 9, 699], wd[0, 11, 0] = math.inf, -math.inf, math.nan
+    y = _ops().gated_ffn(x, wg, wu, wd)
+    keep = [c for c in range(700) if c not in (0, 7, 699)]
+    assert torch.equal(y[..., keep], clean[..., keep])
+    assert torch.isinf(y[..., 7]).all() and torch.isinf(y[..., 699]).all() and torch.isnan(y[..., 0]).all()
