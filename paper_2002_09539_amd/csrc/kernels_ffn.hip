@@ -8,7 +8,7 @@
 // registers of the same lanes.  Likewise dh never exists in memory: its tiles become da and db.  The products are those of
 // ffn_gemm.h; storage type fp32 takes them through three bf16 terms per operand (ffn_gemm_f32.h).  An operand whose rows are 16-byte aligned
 // bf16 is read where it lies; others are laid out in the workspace first (rounded to bf16 where the weights are fp32 master
-// weights of a bf16 block), by a streaming pass.
+// weights of a bf16 block), by a streaming pass, except large fp32 weights of few rows, which the tiles split themselves.
 //
 // Few rows (answering token by token) leave nothing to multiply but every weight to read once: there a lane owns eight
 // columns, 32 lanes share the contraction, and several workgroups share it further, so that nearly all weights are under way
@@ -403,7 +403,9 @@ hipError_t product(Job* jobs, int n, int groups, bool split, bool plain, Arena& 
         if (joins) join_kernel<EPI, true, 128><<<join_grid, 256, 0, stream>>>(p);
     } else if (t == 256) {
         gemm_kernel<A_RC, B_RC, EPI, 256><<<blocks, 512, 0, stream>>>(p);
-        if (joins) join_kernel<EPI, false, 256><<<join_grid, 256, 0, stream>>>(p);
+        if constexpr (EPI == kStore) {                   // with an activation large tiles are not cut (choose)
+            if (joins) join_kernel<EPI, false, 256><<<join_grid, 256, 0, stream>>>(p);
+        }
     } else {
         gemm_kernel<A_RC, B_RC, EPI, 128><<<blocks, 256, 0, stream>>>(p);
         if (joins) join_kernel<EPI, false, 128><<<join_grid, 256, 0, stream>>>(p);
