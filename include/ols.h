@@ -484,7 +484,7 @@ OLS_API int64_t ols_gated_ffn_workspace_bytes(const ols_ffn* f, int grad);
  * zeros), which a training loss knows beforehand:
  *     d_logits_j = d_logprob ([j == target] - p_j) - d_entropy p_j (log p_j + entropy);
  * the logits are then read once where a workgroup's registers hold a row (131072 bf16 or 65536 fp32 logits).  It may lie on
- * the logits (same pointer and row stride).  vocab <= 2^24. */
+ * the logits (same pointer and row stride).  Rows lie at least `vocab` elements apart.  vocab <= 2^24. */
 OLS_API int ols_token_logprobs(int64_t rows, int64_t vocab, const void* logits_dev, int dtype, int64_t row_stride, const int32_t* targets_dev,
                                float* logprob_dev, float* entropy_dev, float* logsumexp_dev, float* stats_dev, int top,
                                float* top_logprob_dev, int32_t* top_index_dev, const float* d_logprob_dev, const float* d_entropy_dev, void* d_logits_dev,

@@ -255,7 +255,7 @@ def _logit_rows(t, name):
         _refuse("%s must have a last axis of tokens, got shape %s", name, tuple(t.shape))
     vocab = t.shape[-1]
     if t.dim() == 2 and (t.stride(1) == 1 or vocab == 1):
-        return t, t.shape[0], max(vocab, t.stride(0))
+        return t, t.shape[0], t.stride(0) if t.shape[0] > 1 else vocab     # rows that overlap are refused by the boundary
     if not t.is_contiguous():
         _refuse("%s must be contiguous, or two-dimensional with contiguous rows", name)
     return t, t.numel() // vocab, vocab
@@ -299,7 +299,8 @@ def _logprobs(logits, targets, top, d_logprob, d_entropy, d_logits):
 def token_logprobs(logits, targets=None, top=0):
     """Log probability of targets[...] under logits[..., vocab], the rows' entropy and logsumexp, and the `top` best tokens.
 
-    targets: int32 of shape logits.shape[:-1]; one outside [0, vocab) is none (logprob 0).  Returns TokenLogprobs: logprob,
+    logits: contiguous, or two-dimensional with contiguous rows that do not overlap (an expanded row is refused).  targets: int32 of
+    shape logits.shape[:-1]; one outside [0, vocab) is none (logprob 0).  Returns TokenLogprobs: logprob,
     entropy, logsumexp of that shape, top_logprob and top_index with a last axis of `top` (None with top = 0), and stats
     (the largest logit and the sum of e^(z - it), for token_logprobs_grad)."""
     return _logprobs(logits, targets, top, None, None, None)

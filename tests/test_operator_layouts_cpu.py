@@ -1,0 +1,41 @@
+"""What the tensor functions make of layouts, on the host: the strides that reach the C boundary are the tensors' own, so that rows
+which share memory are refused there before anything is launched."""
+import pytest
+import torch
+
+from paper_2002_09539_amd import binding as B
+from paper_2002_09539_amd import operators as ops
+
+A = 0x7F0000000000      # stand-in for device addresses; never dereferenced
+BIG = 1 << 60
+
+# (tensor, rows that share memory)
+LOGITS = {
+    "one row for all": (torch.zeros(1, 8).expand(4, 8), True),
+    "a window that slides": (torch.zeros(11).as_strided((4, 8), (1, 1)), True),
+    "rows one element short": (torch.zeros(29).as_strided((4, 8), (7, 1)), True),
+    "one logit for all": (torch.zeros(1, 1).expand(4, 1), True),
+    "side by side": (torch.zeros(4, 8), False),
+    "apart": (torch.zeros(4, 11)[:, 2:10], False),
+    "one row": (torch.zeros(8).as_strided((1, 8), (3, 1)), False),
+    "no rows": (torch.zeros(0, 8), False),
+    "a column": (torch.zeros(4, 8)[:, 3:4], False),
+}
+
+
+@pytest.mark.parametrize("name", LOGITS)
+def test_row_strides_of_logits(name):
+    t, shared = LOGITS[name]
+    _, rows, stride = ops._logit_rows(t, "logits")
+    vocab = t.shape[1]
+    assert rows == t.shape[0] and stride == (t.stride(0) if rows > 1 else vocab)
+    last = (rows - 1) * stride + vocab if rows else 0
+    assert shared or t.storage_offset() + last <= t.untyped_storage().nbytes() // 4
+    if not shared:
+        return
+    for call in (lambda: B.ols_token_logprobs(rows, vocab, A, B.OLS_F32, stride, A, A, A, A, A, 0, None, None, None, None, None, 0, A, BIG, None),
+                 lambda: B.ols_token_logprobs(rows, vocab, A, B.OLS_F32, vocab, A, A, A, A, A, 0, None, None, A, A, A + 4096, stride, A, BIG, None),
+                 lambda: B.ols_token_logprobs_grad(rows, vocab, A, B.OLS_F32, stride, A, A, A, A, A, A + 4096, vocab, None),
+                 lambda: B.ols_token_logprobs_grad(rows, vocab, A, B.OLS_F32, vocab, A, A, A, A, A, A + 4096, stride, None)):
+        with pytest.raises(B.OlsError, match="elements apart"):
+            call()
