@@ -1,0 +1,68 @@
+"""The operators at the ends of the sizes that they accept, against plain torch operations.
+
+Tolerances as of the operators' own tests: 4e-6 and 2^-22 of the value for log probabilities (their sums are of positive terms, in short
+partial sums)."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _ops():
+    from paper_2002_09539_amd import operators
+    return operators
+
+
+# 256 parts a row, each with its 32 best
+@pytest.mark.parametrize("rows,vocab,dtype", [(1, 600_011, F32), (2, 600_011, F32), (1, 1_100_003, BF16), (1, 1 << 24, F32)])
+def test_most_alternatives_of_the_longest_rows(rows, vocab, dtype):
+    z = torch.randn(rows, vocab, generator=torch.Generator(device="cuda").manual_seed(rows), device="cuda").to(dtype)
+    r = _ops().token_logprobs(z, None, top=32)
+    d = z.double()
+    lse = torch.logsumexp(d, 1)
+    v, i = torch.sort(d, dim=1, descending=True, stable=True)
+    assert torch.equal(r.top_index, i[:, :32].to(torch.int32))
+    want = v[:, :32] - lse[:, None]
+    assert ((r.top_logprob.double() - want).abs() <= 4e-6 + 2.0 ** -22 * want.abs()).all()
+    assert ((r.logsumexp.double() - lse).abs() <= 4e-6 + 2.0 ** -22 * lse.abs()).all()
+
+
+@pytest.mark.parametrize("vocab", [70_001, 600_011])
+def test_ties_across_all_parts(vocab):
+    """What is equal everywhere, equal from some part on, and equal but for a few."""
+    z = torch.zeros(4, vocab, device="cuda")
+    z[1, vocab // 2:] = 1.0
+    z[2, 5::997] = 2.0
+    z[3, vocab - 3:] = 3.0
+    best = _ops().token_logprobs(z[:2], None, top=32).top_index.tolist() + _ops().token_logprobs(z[2:], None, top=32).top_index.tolist()
+    assert best[0] == list(range(32)) and best[1] == list(range(vocab // 2, vocab // 2 + 32))
+    assert best[2] == list(range(5, 5 + 32 * 997, 997)) and best[3] == [vocab - 3, vocab - 2, vocab - 1, *range(29)]
+    one = torch.full((1, vocab), -math.inf, device="cuda")
+    one[0, vocab - 7] = 0.5
+    assert _ops().token_logprobs(one, None, top=32).top_index.tolist() == [[vocab - 7] + [-1] * 31]
+
+
+def _device_us(call):
+    """Of the least of five runs of ten calls."""
+    call()
+    times = []
+    for _ in range(5):
+        a, b = torch.cuda.Event(True), torch.cuda.Event(True)
+        torch.cuda.synchronize()
+        a.record()
+        for _ in range(10):
+            call()
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b) * 100)
+    return min(times)
+
+
+def test_rows_of_one_value_take_little_longer_than_others():
+    """What ties is not compared pair by pair: 65 us beside 45, and 23 ms where all that the parts hold was."""
+    random, equal = torch.randn(1, 600_011, device="cuda"), torch.zeros(1, 600_011, device="cuda")
+    assert _device_us(lambda: _ops().token_logprobs(equal, None, top=32)) <= 8 * _device_us(lambda: _ops().token_logprobs(random, None, top=32))
