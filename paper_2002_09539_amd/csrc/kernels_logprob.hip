@@ -515,6 +515,20 @@ hipError_t launch_typed(const LogprobParams& p, const RowPlan& r, hipStream_t st
     return r.nv <= 10 ? launch_long<T, 10>(p, r, stream) : r.nv == 13 ? launch_long<T, 13>(p, r, stream) : launch_long<T, 16>(p, r, stream);
 }
 
+// A launch has fewer than 2^32 threads, a row up to 1024 of them.
+constexpr int64_t kMostRows = 1 << 21;
+LogprobParams rows_of(const LogprobParams& p, int64_t first) {
+    const int64_t bytes = p.dtype == OLS_F32 ? 4 : 2;
+    auto at = [&](auto* t, int64_t per) { return t ? t + per * first : t; };
+    LogprobParams q = p;
+    q.rows = std::min(kMostRows, p.rows - first);
+    q.logits = at((const char*)p.logits, p.row_stride * bytes), q.d_logits = at((char*)p.d_logits, p.d_stride * bytes);
+    q.targets = at(p.targets, 1), q.g_logprob = at(p.g_logprob, 1), q.g_entropy = at(p.g_entropy, 1);
+    q.logprob = at(p.logprob, 1), q.entropy = at(p.entropy, 1), q.lse = at(p.lse, 1), q.stats = at(p.stats, 2);
+    q.top_logprob = at(p.top_logprob, p.top), q.top_index = at(p.top_index, p.top);
+    return q;
+}
+
 template <typename T>
 hipError_t launch_grad_typed(const LogprobParams& p, hipStream_t stream) {
     const int64_t span = 256 * 4 * Vec<T>::kN;
@@ -531,23 +545,32 @@ int64_t logprob_workspace_bytes(int dtype, int64_t rows, int64_t vocab, int top)
 }
 
 hipError_t launch_logprob_grad(const LogprobParams& p, hipStream_t stream) {
-    if (p.rows == 0) return hipSuccess;
-    return p.dtype == OLS_F32 ? launch_grad_typed<float>(p, stream) : launch_grad_typed<uint16_t>(p, stream);
+    for (int64_t first = 0; first < p.rows; first += kMostRows) {
+        const LogprobParams q = rows_of(p, first);
+        const hipError_t e = q.dtype == OLS_F32 ? launch_grad_typed<float>(q, stream) : launch_grad_typed<uint16_t>(q, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_logprob(LogprobParams p, void* ws, hipStream_t stream) {
     if (p.rows == 0) return hipSuccess;
     const RowPlan r = row_plan(p.dtype, p.rows, p.vocab);
     p.parts = r.parts, p.part = r.part;
-    p.part_stats = (float*)ws;
-    p.part_val = (float*)ws + 3 * p.rows * r.parts;
-    p.part_idx = (int32_t*)(p.part_val + p.rows * r.parts * p.top);
-    hipError_t e = p.dtype == OLS_F32 ? launch_typed<float>(p, r, stream) : launch_typed<uint16_t>(p, r, stream);
-    if (e != hipSuccess || r.parts == 1) return e;
-    logprob_join_kernel<<<(unsigned)p.rows, 256, (size_t)join_entries(p.top) * 8, stream>>>(p);
-    e = hipGetLastError();
-    if (e != hipSuccess || !p.d_logits) return e;
-    return launch_logprob_grad(p, stream);
+    for (int64_t first = 0; first < p.rows; first += kMostRows) {
+        LogprobParams q = rows_of(p, first);                 // one launch's parts after another's in the same place
+        q.part_stats = (float*)ws;
+        q.part_val = (float*)ws + 3 * q.rows * r.parts;
+        q.part_idx = (int32_t*)(q.part_val + q.rows * r.parts * q.top);
+        hipError_t e = q.dtype == OLS_F32 ? launch_typed<float>(q, r, stream) : launch_typed<uint16_t>(q, r, stream);
+        if (e == hipSuccess && r.parts > 1) {
+            logprob_join_kernel<<<(unsigned)q.rows, 256, (size_t)join_entries(q.top) * 8, stream>>>(q);
+            e = hipGetLastError();
+            if (e == hipSuccess && q.d_logits) e = launch_logprob_grad(q, stream);
+        }
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace ols

@@ -66,3 +66,27 @@ def test_rows_of_one_value_take_little_longer_than_others():
     """What ties is not compared pair by pair: 65 us beside 45, and 23 ms where all that the parts hold was."""
     random, equal = torch.randn(1, 600_011, device="cuda"), torch.zeros(1, 600_011, device="cuda")
     assert _device_us(lambda: _ops().token_logprobs(equal, None, top=32)) <= 8 * _device_us(lambda: _ops().token_logprobs(random, None, top=32))
+
+
+@pytest.mark.parametrize("rows", [1 << 21, (1 << 21) + 3, (1 << 24) + 5])
+def test_rows_of_logits_beyond_a_launch(rows):
+    """A launch has fewer than 2^32 threads, 256 of them for a row."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = torch.randn(rows, 9, generator=g, device="cuda").to(BF16)
+    t = torch.randint(-1, 9, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    up, h = torch.randn(rows, generator=g, device="cuda"), torch.randn(rows, generator=g, device="cuda")
+    r, d = _ops().token_logprobs_with_grad(z, t, up, h, top=2)
+    later = _ops().token_logprobs_grad(z, t, r, up, h)
+    for pick in (slice(0, 1000), slice(rows // 2, rows // 2 + 1000), slice((1 << 21) - 500, (1 << 21) + 500), slice(rows - 1000, rows)):
+        logp = torch.log_softmax(z[pick].double(), 1)
+        real = t[pick] >= 0
+        want = torch.where(real, logp.gather(1, t[pick].long().clamp(min=0)[:, None])[:, 0], 0.0)
+        p, s = logp.exp(), -(logp.exp() * logp).sum(1, keepdim=True)
+        hot = torch.zeros_like(p).scatter_(1, t[pick].long().clamp(min=0)[:, None], 1.0)
+        grad = torch.where(real, up[pick], 0.0).double()[:, None] * (hot - p) - h[pick].double()[:, None] * p * (logp + s)
+        v, i = torch.sort(z[pick], dim=1, descending=True, stable=True)
+        assert ((r.logprob[pick].double() - want).abs() <= 4e-6 + 2.0 ** -22 * want.abs()).all()
+        assert ((r.entropy[pick].double() - s[:, 0]).abs() <= 4e-6).all()
+        assert torch.equal(r.top_index[pick], i[:, :2].to(torch.int32))
+        for got in (d, later):
+            assert ((got[pick].double() - grad).abs() <= 2e-5 + 2.0 ** -8 * grad.abs()).all()
