@@ -24,6 +24,8 @@
 // 32 768 tokens by a law of words, 50 001 rows of 1024, bf16 to fp32: 91 us; sorting 47 in four launches, which write 205 MB beside
 // it (31 without; with the table cleared after the sums, by id: 44 more), the runs 24 (63 MB read, 48 written), joining 11.  Sorting in two
 // launches that count all ids in every workgroup: 76.  Four workers of 1201 tokens, 5003 rows of 389 fp32: 30 us; 13.4, 12.1 and 4.3.
+#include <algorithm>
+
 #include "element_io.h"
 #include "ols_internal.h"
 
@@ -39,6 +41,7 @@ constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kPerWave = kSortItems / kSortWaves, kPerLane = kPerWave / 64;
 constexpr int kRun = 16;                    // sorted positions of a run
+constexpr int kMostBlocks = 1 << 23;        // of kThreads: a launch has fewer than 2^32 threads
 
 template <typename TI, typename TO>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedParams p, int lanes) {
@@ -426,14 +429,20 @@ void launch_sums(const RowsParams& q, hipStream_t stream) {
 hipError_t launch_embed(const EmbedParams& p, hipStream_t stream) {
     int lanes = 1;
     while (lanes < kThreads && (int64_t)lanes * 8 < p.width) lanes *= 2;
-    const int64_t blocks = (p.tokens + kThreads / lanes - 1) / (kThreads / lanes);
-    if (blocks == 0 || p.groups == 0 || p.width == 0) return hipSuccess;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks, p.groups);
-    if (p.dtype == OLS_F32 && p.out_dtype == OLS_F32) embed_kernel<float, float><<<grid, kThreads, 0, stream>>>(p, lanes);
-    else if (p.dtype == OLS_F32) embed_kernel<float, uint16_t><<<grid, kThreads, 0, stream>>>(p, lanes);
-    else if (p.out_dtype == OLS_F32) embed_kernel<uint16_t, float><<<grid, kThreads, 0, stream>>>(p, lanes);
-    else embed_kernel<uint16_t, uint16_t><<<grid, kThreads, 0, stream>>>(p, lanes);
+    if (p.tokens == 0 || p.groups == 0 || p.width == 0) return hipSuccess;
+    const int per = kThreads / lanes;                          // ids of a workgroup
+    const int64_t most = (int64_t)kMostBlocks * per;           // and of a launch
+    for (int64_t first = 0; first < p.tokens; first += most) {
+        EmbedParams q = p;
+        q.tokens = std::min(most, p.tokens - first);
+        q.ids = p.ids + first;
+        q.out = (char*)p.out + first * p.out_row * (p.out_dtype == OLS_F32 ? 4 : 2);
+        const dim3 grid((unsigned)((q.tokens + per - 1) / per), p.groups);
+        if (p.dtype == OLS_F32 && p.out_dtype == OLS_F32) embed_kernel<float, float><<<grid, kThreads, 0, stream>>>(q, lanes);
+        else if (p.dtype == OLS_F32) embed_kernel<float, uint16_t><<<grid, kThreads, 0, stream>>>(q, lanes);
+        else if (p.out_dtype == OLS_F32) embed_kernel<uint16_t, float><<<grid, kThreads, 0, stream>>>(q, lanes);
+        else embed_kernel<uint16_t, uint16_t><<<grid, kThreads, 0, stream>>>(q, lanes);
+    }
     return hipGetLastError();
 }
 

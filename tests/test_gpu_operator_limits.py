@@ -90,3 +90,19 @@ def test_rows_of_logits_beyond_a_launch(rows):
         assert torch.equal(r.top_index[pick], i[:, :2].to(torch.int32))
         for got in (d, later):
             assert ((got[pick].double() - grad).abs() <= 2e-5 + 2.0 ** -8 * grad.abs()).all()
+
+
+def test_lookup_beyond_a_launch():
+    """2^24 ids of rows that take a workgroup each: 34 GB of results."""
+    n, width = 1 << 24, 1025
+    g = torch.Generator(device="cuda").manual_seed(2)
+    table = torch.randn(7, width, generator=g, device="cuda").to(BF16)
+    ids = torch.randint(-1, 7, (n,), generator=g, device="cuda", dtype=torch.int32)
+    out = torch.full((n, width), 9.0, dtype=BF16, device="cuda")
+    _ops().embed(table, ids, 1.0, out=out)
+    rows = torch.cat([table, torch.zeros(1, width, dtype=BF16, device="cuda")])     # -1: the last
+    for first in range(0, n, 1 << 20):
+        part = slice(first, first + (1 << 20))
+        assert torch.equal(out[part], rows[ids[part].long()]), first
+    del out
+    torch.cuda.empty_cache()
