@@ -38,6 +38,7 @@ struct PackJob {
     uint16_t* dst;                   // [group][rows][cols8]
     int dtype, groups;
 };
+constexpr int64_t kMostBlocks = 1 << 23;   // of 256: a launch has fewer than 2^32 threads, and wraps without an error beyond
 constexpr int kMaxPacks = 5;
 struct PackParams {                  // all operands of a call in one launch
     PackJob job[kMaxPacks];
@@ -54,26 +55,29 @@ __device__ __forceinline__ void read_unit(const PackJob& p, int64_t g, int64_t i
 template <bool SPLIT>
 __global__ __launch_bounds__(256) void pack_kernel(PackParams all) {
     const PackJob& p = all.job[blockIdx.z];
-    const int64_t units = p.rows * (p.cols8 / 8), i = (int64_t)blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
+    const int64_t units = p.rows * (p.cols8 / 8), g = blockIdx.y;
     if (g >= p.groups) return;
-    float v[8] = {};
-    if constexpr (!SPLIT) {
-        if (i >= units) return;
-        if (p.dtype == OLS_F32) read_unit<float>(p, g, i, v);
-        else read_unit<uint16_t>(p, g, i, v);
-        store_terms<false>(p.dst + (g * units + i) * 8, v);
-    } else {
-        __shared__ __align__(16) uint16_t stage[256 * 24];
-        if (i < units) read_unit<float>(p, g, i, v);
-        const int lane = threadIdx.x % 64;
-        uint16_t* mine = stage + threadIdx.x / 64 * (64 * 24);
-        store_terms<true>(mine + lane * 24, v);
-        in_wave_order();
-        const int64_t first = i - lane, chunks = min((int64_t)64, units - first) * 3;
-        u4* out = (u4*)(p.dst + (g * units + first) * 24);
+    const int lane = threadIdx.x % 64;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i - lane < units; i += (int64_t)gridDim.x * 256) {
+        float v[8] = {};
+        if constexpr (!SPLIT) {
+            if (i >= units) return;
+            if (p.dtype == OLS_F32) read_unit<float>(p, g, i, v);
+            else read_unit<uint16_t>(p, g, i, v);
+            store_terms<false>(p.dst + (g * units + i) * 8, v);
+        } else {
+            __shared__ __align__(16) uint16_t stage[256 * 24];
+            if (i < units) read_unit<float>(p, g, i, v);
+            uint16_t* mine = stage + threadIdx.x / 64 * (64 * 24);
+            store_terms<true>(mine + lane * 24, v);
+            in_wave_order();
+            const int64_t first = i - lane, chunks = min((int64_t)64, units - first) * 3;
+            u4* out = (u4*)(p.dst + (g * units + first) * 24);
 #pragma unroll
-        for (int t = 0; t < 3; ++t)
-            if (t * 64 + lane < chunks) out[t * 64 + lane] = *(const u4*)(mine + (t * 64 + lane) * 8);
+            for (int t = 0; t < 3; ++t)
+                if (t * 64 + lane < chunks) out[t * 64 + lane] = *(const u4*)(mine + (t * 64 + lane) * 8);
+            in_wave_order();
+        }
     }
 }
 
@@ -243,7 +247,7 @@ struct Maker {                         // lays operands out; without a stream it
             units = std::max(units, packs.job[i].rows * (packs.job[i].cols8 / 8));
             groups = std::max(groups, packs.job[i].groups);
         }
-        const dim3 grid((unsigned)((units + 255) / 256), groups, n_packs);
+        const dim3 grid((unsigned)std::min(kMostBlocks, (units + 255) / 256), groups, n_packs);
         if (split()) pack_kernel<true><<<grid, 256, 0, stream>>>(packs);
         else pack_kernel<false><<<grid, 256, 0, stream>>>(packs);
         return hipGetLastError();
@@ -358,7 +362,7 @@ Shape choose(const Job* jobs, int n, int groups, int panels, bool split, bool ac
     double best_us = 1e300;
     for (int t = 128; t <= (split ? 128 : 256); t += 128) {          // fp32: two sets of sums leave no registers for large tiles
         const int64_t slots = slots_of(t, split), tiles = count_tiles(jobs, n, groups, panels, t);
-        if (tiles > 0x0fffffff) continue;
+        if (tiles * (t == 256 ? 512 : 256) > kMostBlocks * 256) continue;
         for (int ranges : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             Shape s{t, (int)tiles, 0, 1};
             if (ranges > 1) {
@@ -379,7 +383,7 @@ hipError_t product(Job* jobs, int n, int groups, bool split, bool plain, Arena& 
     if (n == 0) return hipSuccess;
     const Shape shape = choose(jobs, n, groups, PANELS, split, EPI != kStore);
     const int t = shape.t;
-    if (t == 0) return hipErrorInvalidValue;              // more tiles than a launch numbers
+    if (t == 0) return hipErrorInvalidValue;              // more tiles than a launch numbers: known before anything is launched
     GemmArgs p = {};
     p.jobs = n, p.groups = groups, p.whole = shape.whole, p.rest = shape.rest, p.ranges = shape.ranges;
     int first = 0;
@@ -416,8 +420,8 @@ hipError_t product(Job* jobs, int n, int groups, bool split, bool plain, Arena& 
 // Adds up the ranges of the kernels for few rows.
 __global__ __launch_bounds__(256) void few_join_kernel(Epilogue e, const float* partial, int64_t rows, int groups, int ranges) {
     const int64_t units = e.n8 / 8, stride = (int64_t)groups * rows * e.n8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= groups * rows * units) return;
-    const int64_t n = i % units * 8, row = i / units;
+    if (i >= rows * units) return;
+    const int64_t n = i % units * 8, row = blockIdx.y * rows + i / units;
     float v[8] = {};
 #pragma unroll 4
     for (int s = 0; s < ranges; ++s) {
@@ -491,7 +495,7 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         few<true>(p, f, stream);
         few<false>(d, f, stream);
         const Epilogue e = store_to(f.y, f.out, f.dtype);
-        few_join_kernel<<<(unsigned)((f.groups * f.rows * (d.n8 / 8) + 255) / 256), 256, 0, stream>>>(e, d.partial, f.rows, f.groups, d.ranges);
+        few_join_kernel<<<dim3((unsigned)((f.rows * (d.n8 / 8) + 255) / 256), f.groups), 256, 0, stream>>>(e, d.partial, f.rows, f.groups, d.ranges);
         return hipGetLastError();
     }
     Maker mk{f, ws, stream, go};
@@ -521,16 +525,17 @@ hipError_t forward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(char* p, int64_t row_bytes, int64_t pitch, int64_t rows, int64_t group, int unit) {
-    const int64_t per = row_bytes / unit, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * per) return;
-    char* at = p + blockIdx.y * group + i / per * pitch + i % per * unit;
-    if (unit == 4) *(float*)at = 0.0f;
-    else *(uint16_t*)at = 0;
+    const int64_t per = row_bytes / unit;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (int64_t)gridDim.x * 256) {
+        char* at = p + blockIdx.y * group + i / per * pitch + i % per * unit;
+        if (unit == 4) *(float*)at = 0.0f;
+        else *(uint16_t*)at = 0;
+    }
 }
 
 hipError_t zero(const ols_matrix& m, int64_t rows, int64_t cols, int dtype, int groups, hipStream_t stream) {
     const int unit = dtype == OLS_F32 ? 4 : 2;
-    zero_kernel<<<dim3((unsigned)((rows * cols + 255) / 256), groups), 256, 0, stream>>>((char*)m.dev, cols * unit, m.row * unit, rows, m.group * unit, unit);
+    zero_kernel<<<dim3((unsigned)std::min(kMostBlocks, (rows * cols + 255) / 256), groups), 256, 0, stream>>>((char*)m.dev, cols * unit, m.row * unit, rows, m.group * unit, unit);
     return hipGetLastError();
 }
 
@@ -598,9 +603,8 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
 int64_t ffn_saved_bytes(const ols_ffn& f) { return f.rows == 0 ? 0 : ffn::saved_layout(f).bytes; }
 int64_t ffn_workspace_bytes(const ols_ffn& f, bool grad) {
     ffn::Arena ws{nullptr};
-    if (grad) (void)ffn::backward(f, ws, false, nullptr);
-    else (void)ffn::forward(f, ws, false, nullptr);
-    return ws.at;
+    const hipError_t e = grad ? ffn::backward(f, ws, false, nullptr) : ffn::forward(f, ws, false, nullptr);
+    return e == hipSuccess ? ws.at : -1;
 }
 hipError_t launch_ffn(const ols_ffn& f, bool grad, hipStream_t stream) {
     ffn::Arena ws{(char*)f.ws};

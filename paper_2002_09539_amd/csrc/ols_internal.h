@@ -502,7 +502,7 @@ hipError_t launch_logprob(LogprobParams p, void* ws, hipStream_t stream);       
 hipError_t launch_logprob_grad(const LogprobParams& p, hipStream_t stream);      // from p.stats and p.entropy
 
 int64_t ffn_saved_bytes(const ols_ffn& f);
-int64_t ffn_workspace_bytes(const ols_ffn& f, bool grad);
+int64_t ffn_workspace_bytes(const ols_ffn& f, bool grad);      // negative: a product has more tiles than a launch numbers
 hipError_t launch_ffn(const ols_ffn& f, bool grad, hipStream_t stream);
 
 // Tensors of one launch, by value in the kernel arguments (4 KiB): no table to upload, nothing to keep alive.

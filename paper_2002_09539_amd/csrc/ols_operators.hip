@@ -86,6 +86,8 @@ int check_ffn(const char* who, const ols_ffn* f) {
     return OLS_OK;
 }
 
+int too_many_tiles(const char* who) { return bad("%s: a product of the workers together has more than 2^23 tiles of 128 x 128 results", who); }
+
 int check_matrix(const char* who, const char* name, const ols_matrix& m, int64_t rows, int64_t cols, int dtype, int groups, bool written) {
     if (!m.dev || !element_aligned(m.dev, dtype)) return bad("%s: %s is null or not aligned to its type", who, name);
     if (!stride_ok(m.row, cols)) return bad("%s: rows of %s, of %lld elements, cannot be %lld apart", who, name, (long long)cols, (long long)m.row);
@@ -234,7 +236,8 @@ int64_t ols_gated_ffn_saved_bytes(const ols_ffn* f) {
 
 int64_t ols_gated_ffn_workspace_bytes(const ols_ffn* f, int grad) {
     if (const int rc = check_ffn("ols_gated_ffn_workspace_bytes", f)) return rc;
-    return ffn_workspace_bytes(*f, grad != 0);
+    const int64_t need = ffn_workspace_bytes(*f, grad != 0);
+    return need < 0 ? too_many_tiles("ols_gated_ffn_workspace_bytes") : need;
 }
 
 int ols_gated_ffn(const ols_ffn* f, void* stream) {
@@ -247,7 +250,9 @@ int ols_gated_ffn(const ols_ffn* f, void* stream) {
         if (f->saved_bytes < ffn_saved_bytes(*f)) return bad("%s: `saved` of %lld bytes, %lld are needed", who, (long long)f->saved_bytes, (long long)ffn_saved_bytes(*f));
         if (!aligned(f->saved, 256)) return bad("%s: `saved` must be 256-byte aligned", who);
     }
-    if (const int rc = check_ws(who, f->ws, f->ws_bytes, ffn_workspace_bytes(*f, false))) return rc;
+    const int64_t need = ffn_workspace_bytes(*f, false);
+    if (need < 0) return too_many_tiles(who);
+    if (const int rc = check_ws(who, f->ws, f->ws_bytes, need)) return rc;
     return done(launch_ffn(*f, false, (hipStream_t)stream), who);
 }
 
@@ -267,7 +272,9 @@ int ols_gated_ffn_grad(const ols_ffn* f, void* stream) {
         if (!f->saved || f->saved_bytes < ffn_saved_bytes(*f))
             return bad("%s: `saved` of %lld bytes, %lld are needed", who, (long long)(f->saved ? f->saved_bytes : 0), (long long)ffn_saved_bytes(*f));
         if (!aligned(f->saved, 256)) return bad("%s: `saved` must be 256-byte aligned", who);
-        if (const int rc = check_ws(who, f->ws, f->ws_bytes, ffn_workspace_bytes(*f, true))) return rc;
+        const int64_t need = ffn_workspace_bytes(*f, true);
+        if (need < 0) return too_many_tiles(who);
+        if (const int rc = check_ws(who, f->ws, f->ws_bytes, need)) return rc;
     }
     return done(launch_ffn(*f, true, (hipStream_t)stream), who);
 }

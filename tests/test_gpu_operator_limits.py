@@ -106,3 +106,38 @@ def test_lookup_beyond_a_launch():
         assert torch.equal(out[part], rows[ids[part].long()]), first
     del out
     torch.cuda.empty_cache()
+
+
+def test_gradients_of_no_rows_beyond_a_launch():
+    """A weight's gradient of more than 2^32 elements is cleared whole: 8.6 GB."""
+    from paper_2002_09539_amd import binding as B
+    width, hidden = 65_537, 65_536
+    g = torch.ones(width, hidden, dtype=BF16, device="cuda")
+    f = B.ols_ffn()
+    f.groups, f.act, f.dtype, f.weight_dtype, f.grad_dtype = 1, B.OLS_ACT_SILU, B.OLS_BF16, B.OLS_BF16, B.OLS_BF16
+    f.rows, f.width, f.hidden, f.out = 0, width, hidden, 1
+    f.g_gate = B.ols_matrix(g.data_ptr(), hidden, 0)
+    B.ols_gated_ffn_grad(f, torch.cuda.current_stream().cuda_stream)
+    assert all(int(torch.count_nonzero(g[i: i + 4096])) == 0 for i in range(0, width, 4096))
+    del g
+    torch.cuda.empty_cache()
+
+
+def test_inputs_laid_out_beyond_a_launch():
+    """More than 2^32 units of eight elements: 69 GB of rows that do not lie on 16 bytes, and as much to lay them out."""
+    rows, width, hidden, out = 1 << 24, 2049, 8, 8
+    g = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *s, std: (torch.randn(*s, generator=g, device="cuda") * std).to(BF16)  # noqa: E731
+    wg, wu, wd = r(width, hidden, std=width ** -0.5), r(width, hidden, std=width ** -0.5), r(hidden, out, std=hidden ** -0.5)
+    x = torch.empty(rows, width, dtype=BF16, device="cuda")
+    for i in range(0, rows, 1 << 20):
+        x[i: i + (1 << 20)] = r(1, width, std=1.0)             # of every 2^20 rows all alike: results as well
+    y = _ops().gated_ffn(x, wg, wu, wd, "relu")
+    for i in range(0, rows, 1 << 20):
+        part = y[i: i + (1 << 20)]
+        a, b = x[i].double() @ wg.double(), x[i].double() @ wu.double()
+        want = (a.clamp(min=0) * b) @ wd.double()
+        assert torch.equal(part, part[:1].expand_as(part)), i
+        assert float((part[0].double() - want).norm()) <= 1e-2 * float(want.norm()), i
+    del x, y
+    torch.cuda.empty_cache()
