@@ -66,10 +66,11 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedParams p, int lane
 
 // ---- sorting ------------------------------------------------------------------------------------------------------------
 
-// The gradient's rows as workgroups behind those of the sort clear them: pieces of kClearBytes.
+// The gradient's rows as workgroups behind those of the sort clear them, a piece each.
 struct ClearParams {
     char* out;                   // rows of row_bytes, row_pitch apart; a table without gaps is one long row
     int64_t rows, row_bytes, row_pitch, group_bytes;
+    int64_t piece;               // bytes
     int64_t per_row, rows_per;   // pieces of a row, or (short rows) rows of a piece
     int64_t first;               // this launch's first piece
 };
@@ -87,7 +88,8 @@ struct SortParams {
     ClearParams clear;
 };
 
-constexpr int64_t kClearBytes = 65536;       // of one workgroup; 32 to 256 KiB take the same time
+constexpr int64_t kClearBytes = 65536;       // of one workgroup, more in tables of more than kMostPieces; 32 to 256 KiB take the same time
+constexpr int64_t kMostPieces = 1 << 21;     // of kSortThreads: a launch has fewer than 2^32 threads
 // bytes [from, to) of a row by some lanes, `lane` of `lanes`
 __device__ __forceinline__ void clear_bytes(char* row, int64_t from, int64_t to, int lane, int lanes) {
     for (int64_t at = from + 16 * lane; at < to; at += 16 * lanes) {
@@ -103,8 +105,8 @@ __device__ __forceinline__ bool cleared(const ClearParams& p, int group, int64_t
     piece += p.first;
     char* out = p.out + group * p.group_bytes;
     if (p.rows_per == 0) {
-        const int64_t r = piece / p.per_row, from = piece % p.per_row * kClearBytes;
-        clear_bytes(out + r * p.row_pitch, from, min(p.row_bytes, from + kClearBytes), threadIdx.x, kSortThreads);
+        const int64_t r = piece / p.per_row, from = piece % p.per_row * p.piece;
+        clear_bytes(out + r * p.row_pitch, from, min(p.row_bytes, from + p.piece), threadIdx.x, kSortThreads);
     } else {
         const int64_t r0 = piece * p.rows_per, r1 = min(p.rows, r0 + p.rows_per);
         for (int64_t r = r0 + threadIdx.x / 64; r < r1; r += kSortWaves) clear_bytes(out + r * p.row_pitch, 0, p.row_bytes, threadIdx.x % 64, 64);
@@ -468,9 +470,12 @@ hipError_t launch_embed_grad(const EmbedGradParams& g, void* ws, hipStream_t str
         const int64_t elem = g.grad_dtype == OLS_F32 ? 4 : 2;
         c.out = (char*)g.grad, c.group_bytes = g.grad_group * elem, c.rows = g.vocab, c.row_bytes = g.width * elem, c.row_pitch = g.grad_row * elem;
         if (g.grad_row == g.width) c.row_bytes *= g.vocab, c.rows = 1;
-        c.rows_per = c.rows > 1 && c.row_bytes < kClearBytes ? kClearBytes / c.row_bytes : 0;
-        c.per_row = (c.row_bytes + kClearBytes - 1) / kClearBytes;
-        pieces = c.rows_per ? (c.rows + c.rows_per - 1) / c.rows_per : c.rows * c.per_row;
+        for (c.piece = kClearBytes;; c.piece *= 2) {
+            c.rows_per = c.rows > 1 && c.row_bytes < c.piece ? c.piece / c.row_bytes : 0;
+            c.per_row = (c.row_bytes + c.piece - 1) / c.piece;
+            pieces = c.rows_per ? (c.rows + c.rows_per - 1) / c.rows_per : c.rows * c.per_row;
+            if (pieces <= kMostPieces) break;
+        }
     }
     int done = 0;
     auto clear = [&](int n) {

@@ -141,3 +141,20 @@ def test_inputs_laid_out_beyond_a_launch():
         assert float((part[0].double() - want).norm()) <= 1e-2 * float(want.norm()), i
     del x, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("apart", [False, True])
+def test_gradient_tables_beyond_a_launch(apart):
+    """137 GB of rows to clear, side by side and a little apart: more pieces of 64 KiB (of one row each) than a launch numbers."""
+    vocab, width = (1 << 22) + 100, 16_385
+    whole = torch.empty(vocab, width + apart, dtype=BF16, device="cuda").fill_(1.0)
+    out = whole[:, :width]
+    ids = torch.tensor([vocab - 1, 5, 5], dtype=torch.int32, device="cuda")
+    _ops().embed_grad(ids, torch.ones(3, width, dtype=BF16, device="cuda"), vocab, out=out)
+    assert (out[5] == 2).all() and (out[vocab - 1] == 1).all()
+    out[5], out[vocab - 1] = 0.0, 0.0
+    step = 1 << 18
+    assert all(int(torch.count_nonzero(out[i: i + step])) == 0 for i in range(0, vocab, step))
+    assert not apart or (whole[:, width] == 1).all()
+    del out, whole
+    torch.cuda.empty_cache()
