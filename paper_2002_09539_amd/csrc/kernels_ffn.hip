@@ -100,6 +100,7 @@ struct FewParams {
 template <typename TX, typename TW, int R, bool FIRST>
 __global__ __launch_bounds__(kFewThreads) void few_kernel(FewParams p) {
     constexpr int PANELS = FIRST ? 2 : 1;
+    constexpr bool ROUND = sizeof(TX) == 2 && sizeof(TW) == 4;  // master weights of a bf16 block: as the products of more rows round them
     __shared__ __align__(16) float xs[kFewSlab][R];
     __shared__ float red[kFewThreads / 64][PANELS][R][kFewCols];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, cl = lane % 8, kl = threadIdx.x / 8;
@@ -148,13 +149,18 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewParams p) {
 #pragma unroll
             for (int j = 0; j < B; ++j) {
                 if (i + 32 * j >= n) continue;
+                float v[PANELS][8];
+#pragma unroll
+                for (int t = 0; t < PANELS; ++t)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[t][e] = ROUND ? of_bf16(bf16_of(u[j][t].get(e))) : u[j][t].get(e);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const float x = xs[i + 32 * j][r];
 #pragma unroll
                     for (int t = 0; t < PANELS; ++t)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) acc[t][r][e] = fmaf(x, u[j][t].get(e), acc[t][r][e]);
+                        for (int e = 0; e < 8; ++e) acc[t][r][e] = fmaf(x, v[t][e], acc[t][r][e]);
                 }
             }
         }
