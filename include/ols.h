@@ -476,7 +476,8 @@ OLS_API int64_t ols_gated_ffn_workspace_bytes(const ols_ffn* f, int grad);
  * and the `top` tokens of the largest logits, best first, ties to the lower index: their log probabilities and indices
  * (top_... are [rows][top], top <= min(OLS_MAX_TOP, vocab); NULL with top == 0).
  *   - A logit of -inf cannot occur: probability 0, gradient 0, never an alternative (index -1, log probability -inf where
- *     fewer than `top` tokens can).  A row of nothing else: logsumexp and logprob -inf, entropy 0, gradient 0.
+ *     fewer than `top` tokens can).  As a target it has logprob -inf, and its gradient is d_logprob as the formula below has it:
+ *     give such rows no target, or a d_logprob of 0.  A row of nothing else: logsumexp and logprob -inf, entropy 0, gradient 0.
  *   - A NaN or +inf in a row makes its results and its gradient NaN and its alternatives' indices -1.
  *   - A target outside [0, vocab) (or targets == NULL) is none: logprob 0 and no part of the gradient.
  * stats ([rows][2]: the largest logit m and the sum of e^(z - m)) is what the gradient alone needs later: unlike the logsumexp

@@ -5,9 +5,9 @@
 //   logsumexp = m + log s      logprob = (z_target - m) - log s      entropy = log s - t / s
 //   dz_j = g_lp ([j = target] - p_j) - g_H p_j (log p_j + entropy),        p_j = e^{z_j - m} / s
 //
-// A logit of -inf is a token that cannot occur: probability 0, never an alternative, gradient 0.  A row of nothing else
-// has logsumexp -inf, logprob -inf, entropy 0, no alternatives and no gradient.  A row with a NaN or +inf has no
-// distribution: its results are NaN and it has no alternatives.  Everything is fp32 whatever the storage type.
+// A logit of -inf is a token that cannot occur: probability 0, never an alternative, gradient 0 (as a target: logprob -inf, gradient
+// g_lp, by the formula).  A row of nothing else has logsumexp -inf, logprob -inf, entropy 0, no alternatives and no gradient.  A row
+// with a NaN or +inf has no distribution: its results are NaN and it has no alternatives.  Everything is fp32 whatever the storage type.
 //
 // What bounds them is reading the logits.  A workgroup loads its part of a row ONCE, into registers (up to 16 vectors of
 // 16 bytes per lane), and takes maximum, sums, the best k and -- where the caller gives the upstream gradients with the

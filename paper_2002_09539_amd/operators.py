@@ -309,7 +309,7 @@ def token_logprobs(logits, targets=None, top=0):
 def token_logprobs_with_grad(logits, targets, d_logprob, d_entropy=None, top=0, out=None):
     """token_logprobs and the gradient at the logits of sum(d_logprob * logprob + d_entropy * entropy), in one call.
 
-    The gradient has the logits' type; out may be the logits themselves.  Returns (TokenLogprobs, gradient)."""
+    The gradient has the logits' type; out may be the logits themselves.  At a target whose logit is -inf it is d_logprob.  Returns (TokenLogprobs, gradient)."""
     if out is None:
         _on_gpu(logits)
         out = torch.empty_like(logits, memory_format=torch.contiguous_format)
