@@ -446,7 +446,8 @@ OLS_API int64_t ols_embed_grad_workspace_bytes(int groups, int64_t tokens, int64
  *     256-byte aligned), where it leaves a, b and h; NULL otherwise.  Up to 8 rows without `saved` are read by kernels made for
  *     single tokens, which round the weights as the others do and keep h in fp32.
  *   - ols_gated_ffn_grad reads dy, x, the weights and `saved` and writes dx, g_gate, g_up and g_down (of the weights' shapes);
- *     one whose dev is NULL is not computed.  Gradients are written, not added to.
+ *     one whose dev is NULL is not computed.  Gradients are written, not added to.  dx may lie on x or on dy, or else the weights'
+ *     gradients on the weights; no other result on an operand, on `saved` or on another result.
  *   - Limits: groups <= 4096; width, hidden and out <= 2^20; rows <= 2^24; a product of all workers has at most 2^23 tiles of 128 x 128
  *     results (128 x 64 of a and b); row strides of dx, y and the gradients must not make
  *     rows or workers overlap. */

@@ -545,6 +545,13 @@ hipError_t zero(const ols_matrix& m, int64_t rows, int64_t cols, int dtype, int 
     return hipGetLastError();
 }
 
+// Whether two matrices of f.rows rows of its type span some of the same memory.
+bool meet(const ols_matrix& a, int64_t a_cols, const ols_matrix& b, int64_t b_cols, const ols_ffn& f) {
+    const int64_t size = f.dtype == OLS_F32 ? 4 : 2;
+    auto end = [&](const ols_matrix& m, int64_t cols) { return (uintptr_t)m.dev + ((f.groups - 1) * m.group + (f.rows - 1) * m.row + cols) * size; };
+    return (uintptr_t)a.dev < end(b, b_cols) && (uintptr_t)b.dev < end(a, a_cols);
+}
+
 hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
     const ols_matrix* grads[3] = {&f.g_gate, &f.g_up, &f.g_down};
     if (f.rows == 0) {                       // sums over no rows
@@ -584,12 +591,17 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         e = product<false, false, kGateGrad>(&dh, 1, f.groups, mk.split(), wd.plain, ws, go, stream);
         if (e != hipSuccess) return e;
     }
-    if (f.dx.dev) {
+    auto to_x = [&]() {
         Job dx = {};
         dx.M = f.rows, dx.N = f.width, dx.K = f.hidden;
         set_operands(dx, da, wg, &db, &wu);
         dx.epi = store_to(f.dx, f.width, f.dtype);
-        e = product<false, false, kStore>(&dx, 1, f.groups, mk.split(), wg.plain, ws, go, stream);
+        return product<false, false, kStore>(&dx, 1, f.groups, mk.split(), wg.plain, ws, go, stream);
+    };
+    // The weights' gradients read x and dy, the one at x reads the weights: whichever may lie on what the other reads comes last.
+    const bool x_last = f.dx.dev && (meet(f.dx, f.width, f.x, f.width, f) || meet(f.dx, f.width, f.dy, f.out, f));
+    if (f.dx.dev && !x_last) {
+        e = to_x();
         if (e != hipSuccess) return e;
     }
     Job dw[kMaxJobs] = {};
@@ -601,7 +613,8 @@ hipError_t backward(const ols_ffn& f, Arena& ws, bool go, hipStream_t stream) {
         set_operands(j, i < 2 ? x : h, i == 0 ? da : i == 1 ? db : dy, nullptr, nullptr);
         j.epi = store_to(*grads[i], j.N, f.grad_dtype);
     }
-    return product<true, true, kStore>(dw, n, f.groups, mk.split(), false, ws, go, stream);
+    e = product<true, true, kStore>(dw, n, f.groups, mk.split(), false, ws, go, stream);
+    return e == hipSuccess && x_last ? to_x() : e;
 }
 
 }  // namespace ffn

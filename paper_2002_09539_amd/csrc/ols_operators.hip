@@ -275,6 +275,9 @@ int ols_gated_ffn_grad(const ols_ffn* f, void* stream) {
         const int64_t need = ffn_workspace_bytes(*f, true);
         if (need < 0) return too_many_tiles(who);
         if (const int rc = check_ws(who, f->ws, f->ws_bytes, need)) return rc;
+        if (f->dx.dev && (f->dx.dev == f->x.dev || f->dx.dev == f->dy.dev) &&
+            ((f->g_gate.dev && f->g_gate.dev == f->w_gate.dev) || (f->g_up.dev && f->g_up.dev == f->w_up.dev)))
+            return bad("%s: dx on x or dy and the gradients of gate or up on the weights, both at once", who);
     }
     return done(launch_ffn(*f, true, (hipStream_t)stream), who);
 }

@@ -214,7 +214,7 @@ def gated_ffn_grad(dy, x, w_gate, w_up, w_down, saved, act="silu", out=None, gra
 
     The weights' gradients are of grad_dtype (the weights' type by default) and have a worker axis if anything has one: a
     shared weight's gradient is each worker's.  out: a FfnGrads of tensors to write to (views of gradient rows, say; None
-    entries are allocated); need_x=False leaves out the gradient at x."""
+    entries are allocated), of which x may be dy or x itself; need_x=False leaves out the gradient at x."""
     f, device, lead = _ffn(x, w_gate, w_up, w_down, act, (dy, saved, *(out or ())))
     if dy.dtype != x.dtype:
         _refuse("dy must be of x's type")

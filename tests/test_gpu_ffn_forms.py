@@ -27,3 +27,23 @@ def test_master_weights_are_rounded_whatever_the_rows(rows, save, width, hidden,
     assert torch.equal(args[0].to(BF16).float(), torch.full_like(args[0], r * 2.0 ** -6))
     want = (width * r * 2.0 ** -6) ** 2 * hidden * r * 2.0 ** -4
     assert ((y.double() - want).abs() <= 2.0 ** -8 * want).all(), float(y[0, 0]) / want
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,rows,width,hidden", [(1, 3, 16, 24), (2, 40, 72, 136), (1, 300, 65, 50)])
+def test_the_gradient_at_x_may_lie_on_x_or_on_dy(dtype, m, rows, width, hidden):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    r = lambda *s: (torch.randn(*s, generator=g, device="cuda") * s[-2] ** -0.5).to(dtype)  # noqa: E731
+    x, dy = torch.randn(m, rows, width, generator=g, device="cuda").to(dtype), torch.randn(m, rows, width, generator=g, device="cuda").to(dtype)
+    w = r(m, width, hidden), r(m, width, hidden), r(m, hidden, width)
+    ops = _ops()
+    _, saved = ops.gated_ffn(x, *w, save=True)
+    want = ops.gated_ffn_grad(dy, x, *w, saved)
+    for name in ("x", "dy"):
+        xs, ds = x.clone(), dy.clone()
+        got = ops.gated_ffn_grad(ds, xs, *w, saved, out=ops.FfnGrads(xs if name == "x" else ds, None, None, None))
+        assert got.x is (xs if name == "x" else ds)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), name
+    here = [t.clone() for t in w]            # the weights' gradients over the weights
+    got = ops.gated_ffn_grad(dy, x, *here, saved, out=ops.FfnGrads(None, *here))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -39,3 +39,22 @@ def test_row_strides_of_logits(name):
                  lambda: B.ols_token_logprobs_grad(rows, vocab, A, B.OLS_F32, vocab, A, A, A, A, A, A + 4096, stride, None)):
         with pytest.raises(B.OlsError, match="elements apart"):
             call()
+
+
+def test_block_gradients_that_need_each_others_operands():
+    """dx over x is written last, gradients over the weights first: both at once would read what is overwritten."""
+    f = B.ols_ffn()
+    f.groups, f.act, f.dtype, f.weight_dtype, f.grad_dtype = 1, B.OLS_ACT_SILU, B.OLS_F32, B.OLS_F32, B.OLS_F32
+    f.rows, f.width, f.hidden, f.out = 40, 16, 32, 16
+    shapes = dict(x=(40, 16), w_gate=(16, 32), w_up=(16, 32), w_down=(32, 16), dy=(40, 16), dx=(40, 16), g_gate=(16, 32), g_up=(16, 32), g_down=(32, 16))
+    for i, (name, (r, c)) in enumerate(shapes.items()):
+        setattr(f, name, B.ols_matrix(A + (i << 20), c, r * c))
+    f.saved, f.saved_bytes, f.ws, f.ws_bytes = A, BIG, A, BIG
+    need = B.ols_gated_ffn_workspace_bytes(f, 1)
+    for on in ("x", "dy"):
+        for grad, weight in (("g_gate", "w_gate"), ("g_up", "w_up")):
+            g = B.ols_ffn.from_buffer_copy(f)
+            g.dx.dev, getattr(g, grad).dev = getattr(g, on).dev, getattr(g, weight).dev
+            assert B.ols_gated_ffn_workspace_bytes(g, 1) == need
+            with pytest.raises(B.OlsError, match="both at once"):
+                B.ols_gated_ffn_grad(g, None)
