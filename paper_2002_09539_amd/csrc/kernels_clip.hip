@@ -6,8 +6,8 @@
 // matrix-free fp64 rate (two operations for four bytes read) is far from what bounds a stream.  Sums have one order: a
 // workgroup's over its chunk, then the chunks of a group in turn.
 //
-// Two launches: the sums of squares of chunks, then the scaled copy, whose workgroups add up their group's sums themselves (a
-// few thousand numbers from the L2) instead of waiting for a launch between.  The gradients are read twice, three
+// Two launches: the sums of squares of chunks, then the scaled copy, whose workgroups add up their group's sums themselves (up to 4096
+// numbers from the L2; groups of more tensors than that get a launch between).  The gradients are read twice, three
 // traversals where two are the least; what bounds both launches is memory.  The copy takes the chunks in the reverse order, each
 // on the XCD that has summed it, so that what was read last is found in the caches.  Sixteen groups of 14.7 M fp32: 158 us to sum
 // (5.9 TB/s) and 354 to copy, 6 us more in the order of the sums.  Taking the groups in batches that fit the 256 MiB memory-side cache costs
@@ -43,11 +43,12 @@ __device__ __forceinline__ double block_sum(double v) {   // the result is in ev
 }
 
 // the sum of a group's chunks: lane i adds up chunks i, i + 256, .. and the workgroup joins the lanes
-__device__ __forceinline__ double group_norm(const double* partial, int64_t first, int64_t count) {
+__device__ __forceinline__ double group_sum(const double* partial, int64_t first, int64_t count) {
     double s = 0.0;
     for (int64_t i = threadIdx.x; i < count; i += kThreads) s += partial[first + i];
-    return sqrt(block_sum(s));
+    return block_sum(s);
 }
+__device__ __forceinline__ double group_norm(const double* partial, int64_t first, int64_t count) { return sqrt(group_sum(partial, first, count)); }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void clip_squares_kernel(ClipTable t, int64_t chunk_elems, double* partial) {
@@ -105,6 +106,12 @@ __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipTable t, int64
     }
 }
 
+// one workgroup a group, which has read all of its chunks before it writes
+__global__ __launch_bounds__(kThreads) void clip_sums_kernel(ClipGroups g, double* partial) {
+    const double sum = group_sum(partial, g.first[blockIdx.x], g.count[blockIdx.x]);
+    if (threadIdx.x == 0) partial[g.first[blockIdx.x]] = sum;
+}
+
 __global__ __launch_bounds__(kThreads) void clip_norms_kernel(ClipGroups g, const double* partial, float* norms) {
     const double norm = group_norm(partial, g.first[blockIdx.x], g.count[blockIdx.x]);
     if (threadIdx.x == 0) norms[g.group[blockIdx.x]] = (float)norm;
@@ -119,6 +126,10 @@ hipError_t launch_clip(const ClipTable& t, int dtype, int64_t chunk_elems, int b
     else if (copy) clip_scale_kernel<uint16_t><<<blocks, kThreads, 0, stream>>>(t, chunk_elems, partial, max_norm, norms);
     else if (dtype == OLS_F32) clip_squares_kernel<float><<<blocks, kThreads, 0, stream>>>(t, chunk_elems, partial);
     else clip_squares_kernel<uint16_t><<<blocks, kThreads, 0, stream>>>(t, chunk_elems, partial);
+    return hipGetLastError();
+}
+hipError_t launch_clip_sums(const ClipGroups& g, int groups, double* partial, hipStream_t stream) {
+    clip_sums_kernel<<<groups, kThreads, 0, stream>>>(g, partial);
     return hipGetLastError();
 }
 hipError_t launch_clip_norms(const ClipGroups& g, int groups, const double* partial, float* norms, hipStream_t stream) {

@@ -522,6 +522,7 @@ struct ClipGroups {
 };
 hipError_t launch_clip(const ClipTable& t, int dtype, int64_t chunk_elems, int blocks, bool copy, double* partial, float max_norm, float* norms,
                        hipStream_t stream);     // the sums of squares, or the scaled copy
+hipError_t launch_clip_sums(const ClipGroups& g, int groups, double* partial, hipStream_t stream);   // a group's sum in the place of its first
 hipError_t launch_clip_norms(const ClipGroups& g, int groups, const double* partial, float* norms, hipStream_t stream);
 
 }  // namespace ols
