@@ -86,7 +86,9 @@ __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipTable t, int64
     T* out = (T*)t.out[k];
     const bool clip = !(norm <= (double)max_norm);      // a NaN clips: it reaches every element
     if (!clip && x == out) return;
-    const float scale = clip ? (float)((double)max_norm / norm) : 1.0f;
+    const double factor = clip ? (double)max_norm / norm : 1.0;
+    const float scale = (float)factor;
+    const bool tiny = factor < 0x1p-126;                 // no normal fp32: what it keeps of it would be the result's precision
     const int64_t from = chunk * chunk_elems, to = min(from + chunk_elems, t.numel[k]);
     for (int64_t i = from + threadIdx.x * 8; i < to; i += 4 * kThreads * 8) {
         float v[4][8];
@@ -99,8 +101,13 @@ __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipTable t, int64
         for (int u = 0; u < 4; ++u) {
             const int64_t at = i + (int64_t)u * kThreads * 8;
             if (at >= to) continue;
+            if (__builtin_expect(tiny, 0)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[u][e] *= scale;
+                for (int e = 0; e < 8; ++e) v[u][e] = (float)((double)v[u][e] * factor);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e] *= scale;
+            }
             store_upto8(out + at, (int)min((int64_t)8, to - at), v[u]);
         }
     }

@@ -79,3 +79,18 @@ def test_many_tensors_are_clipped_in_about_the_time_of_their_norm():
     norm, clip = least(None), least(1.0)
     print("%d tensors: norm %.2f ms, clipping %.2f ms" % (n, norm, clip))
     assert clip <= 5 * norm
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value,max_norm", [(1e36, 1e-3), (1e38, 1.0), (3e38, 1e-6), (1e15, 1e-30), (1e30, 1e-12), (1e-30, 1e-36)])
+def test_factors_below_the_normal_numbers(dtype, value, max_norm):
+    """max_norm / norm may be far below the least normal fp32 where gradients are huge or the limit is tiny; the results are not."""
+    x = (torch.rand(100_000, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda") * value).to(dtype)
+    norm = float(x.double().square().sum().sqrt())
+    want = x.double() * (max_norm / norm)
+    big = want.abs() >= 2.0 ** -110                      # where the result is normal by a margin
+    out = torch.empty_like(x)
+    got = _ops().clip_grad_norm([x], max_norm, out=[out])
+    assert norm > 3.4e38 or abs(float(got[0]) - norm) <= 2.0 ** -23 * norm
+    assert int(big.sum()) > 90_000 or value == 1e-30 or max_norm == 1e-30
+    assert ((out.double() - want).abs()[big] <= (2.0 ** -22 if dtype == F32 else 2.0 ** -8) * want.abs()[big]).all()
