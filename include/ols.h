@@ -502,7 +502,7 @@ OLS_API int ols_token_logprobs_grad(int64_t rows, int64_t vocab, const void* log
  *     norm = sqrt(sum of squares of all its tensors' elements),   out = in * min(1, max_norm / norm).
  * in_dev, out_dev, numel and group are HOST arrays of n entries, read before the call returns; group is non-decreasing
  * (NULL: one group).  norms_dev: [groups] fp32 on the device; 0 for a group without elements.  out_dev[i] may equal
- * in_dev[i]; out_dev == NULL computes the norms only.  Squares are summed in fp64: no gradient of finite elements overflows (a
+ * in_dev[i], outputs must not overlap otherwise; out_dev == NULL computes the norms only.  Squares are summed in fp64: no gradient of finite elements overflows (a
  * norm beyond fp32 reads as an infinity, the outputs are right all the same).
  * A NaN in a group makes its norm and all its outputs NaN; an infinity makes the norm infinite, the infinite elements NaN and
  * the others 0: look at the norm before the step. */

@@ -337,6 +337,14 @@ def token_logprobs_grad(logits, targets, result, d_logprob, d_entropy=None, out=
 
 
 # ---- clipping -----------------------------------------------------------------------------------------------------
+def _distinct(pointers, sizes):
+    """Whether no two tensors that have elements begin at one address."""
+    if len(set(pointers)) == len(pointers):
+        return True
+    real = [p for p, n in zip(pointers, sizes) if n]
+    return len(set(real)) == len(real)
+
+
 def _clip(grads, max_norm, groups, out):
     grads = list(grads)
     if not grads:
@@ -368,8 +376,14 @@ def _clip(grads, max_norm, groups, out):
             grads, out = [grads[i] for i in order], (None if out is grads else [out[i] for i in order])
             out = grads if out is None else out
         group_array = array("i", groups)
-    inputs, numel = array("Q", [t.data_ptr() for t in grads]), array("q", sizes)
-    outputs = None if max_norm is None else inputs if out is grads else array("Q", [t.data_ptr() for t in out])
+    places = [t.data_ptr() for t in grads]
+    inputs, numel, outputs = array("Q", places), array("q", sizes), None
+    if max_norm is not None:
+        if out is not grads:
+            places = [t.data_ptr() for t in out]
+        if not _distinct(places, sizes):
+            _refuse("a tensor cannot be scaled twice in one call")
+        outputs = inputs if out is grads else array("Q", places)
     at = lambda a: None if a is None else a.buffer_info()[0]  # noqa: E731
     nbytes = B.ols_clip_workspace_bytes(n, at(numel), at(group_array), count)
     with _on(place):
@@ -388,5 +402,6 @@ def grad_norm(grads, groups=None):
 def clip_grad_norm(grads, max_norm, groups=None, out=None):
     """Scales each group's tensors by min(1, max_norm / norm), in place or into `out`; returns the norms before that.
 
-    grads: contiguous tensors of one type; groups[i]: the number of tensor i's group (one group by default)."""
+    grads: contiguous tensors of one type; groups[i]: the number of tensor i's group (one group by default).  What is written must not
+    overlap: a gradient that several parameters share is given once."""
     return _clip(grads, max_norm, groups, out)

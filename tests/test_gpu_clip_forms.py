@@ -94,3 +94,19 @@ def test_factors_below_the_normal_numbers(dtype, value, max_norm):
     assert norm > 3.4e38 or abs(float(got[0]) - norm) <= 2.0 ** -23 * norm
     assert int(big.sum()) > 90_000 or value == 1e-30 or max_norm == 1e-30
     assert ((out.double() - want).abs()[big] <= (2.0 ** -22 if dtype == F32 else 2.0 ** -8) * want.abs()[big]).all()
+
+
+def test_a_tensor_is_not_scaled_twice():
+    ops = _ops()
+    x, y, none = torch.ones(50, device="cuda"), torch.ones(7, device="cuda"), torch.zeros(0, device="cuda")
+    for call in (lambda: ops.clip_grad_norm([x, y, x], 1.0), lambda: ops.clip_grad_norm([x, x.clone()], 1.0, out=[x, x]),
+                 lambda: ops.clip_grad_norm([x, y, x], 1.0, groups=[1, 0, 0])):
+        with pytest.raises(B.OlsError, match="twice"):
+            call()
+    assert (x == 1).all()
+    assert abs(float(ops.grad_norm([x, x])[0]) - 10.0) <= 1e-6                      # to read it twice is no harm
+    two = [torch.empty_like(x), torch.empty_like(x)]
+    ops.clip_grad_norm([x, x], 1.0, out=two)
+    assert torch.equal(two[0], two[1]) and ((two[0] - 0.1).abs() <= 1e-7).all()
+    ops.clip_grad_norm([none, x[:0], x, none.clone()], 1.0)
+    assert abs(float(x.norm()) - 1.0) <= 1e-6

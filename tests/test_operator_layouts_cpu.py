@@ -58,3 +58,10 @@ def test_block_gradients_that_need_each_others_operands():
             assert B.ols_gated_ffn_workspace_bytes(g, 1) == need
             with pytest.raises(B.OlsError, match="both at once"):
                 B.ols_gated_ffn_grad(g, None)
+
+
+def test_tensors_that_would_be_scaled_twice():
+    """In one launch two workgroups would scale the same elements, in no order."""
+    assert ops._distinct([], []) and ops._distinct([A, A + 64, 0], [4, 5, 0]) and ops._distinct([0, A, 0], [0, 3, 0])
+    assert ops._distinct([A, A, A + 4], [0, 7, 1])                                  # an empty slice in front of a tensor
+    assert not ops._distinct([A, A + 64, A], [4, 4, 4])
