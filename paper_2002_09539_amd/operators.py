@@ -158,6 +158,13 @@ def _matrix(t, m, shape, name):
     return B.ols_matrix(t.data_ptr(), row, group)
 
 
+def _saved(t):
+    """Address and bytes of what a forward call left."""
+    if t.dtype != torch.uint8 or t.dim() != 1 or not t.is_contiguous():
+        _refuse("saved must be what gated_ffn(..., save=True) returned")
+    return (t.data_ptr() if t.numel() else None), t.numel()
+
+
 _SHARED = ("x", "w_gate", "w_up", "w_down", "dy")    # inputs that may come without a worker axis
 
 
@@ -241,7 +248,7 @@ def gated_ffn_grad(dy, x, w_gate, w_up, w_down, saved, act="silu", out=None, gra
                 _refuse("out.%s must be %s of shape %s", FfnGrads._fields[i], dtype, (*lead, *shape))
             setattr(f, name, _matrix(t, f.groups, shape, name))
             made.append(t)
-        f.saved, f.saved_bytes = (saved.data_ptr() if saved.numel() else None), saved.numel()
+        f.saved, f.saved_bytes = _saved(saved)
         f.ws_bytes = B.ols_gated_ffn_workspace_bytes(f, 1)
         ws = _workspace(f.ws_bytes, device)
         f.ws = _ptr(ws)

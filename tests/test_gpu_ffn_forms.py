@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+from paper_2002_09539_amd import binding as B
+
 pytestmark = pytest.mark.gpu
 
 F32, BF16 = torch.float32, torch.bfloat16
@@ -47,3 +49,12 @@ def test_the_gradient_at_x_may_lie_on_x_or_on_dy(dtype, m, rows, width, hidden):
     here = [t.clone() for t in w]            # the weights' gradients over the weights
     got = ops.gated_ffn_grad(dy, x, *here, saved, out=ops.FfnGrads(None, *here))
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_saved_states_that_are_not_whole_are_refused():
+    ops = _ops()
+    x, w = torch.randn(20, 16, device="cuda"), [torch.randn(16, 16, device="cuda") for _ in range(3)]
+    _, saved = ops.gated_ffn(x, *w, save=True)
+    for t in (saved[:1].expand(saved.numel()), torch.zeros(2 * saved.numel(), dtype=torch.uint8, device="cuda")[::2], saved.float()):
+        with pytest.raises(B.OlsError, match="saved"):
+            ops.gated_ffn_grad(x, x, *w, t)

@@ -65,3 +65,12 @@ def test_tensors_that_would_be_scaled_twice():
     assert ops._distinct([], []) and ops._distinct([A, A + 64, 0], [4, 5, 0]) and ops._distinct([0, A, 0], [0, 3, 0])
     assert ops._distinct([A, A, A + 4], [0, 7, 1])                                  # an empty slice in front of a tensor
     assert not ops._distinct([A, A + 64, A], [4, 4, 4])
+
+
+def test_saved_states_are_whole():
+    """One byte for all, every other byte, another type: fewer bytes lie there than the elements say."""
+    whole = torch.zeros(4096, dtype=torch.uint8)
+    assert ops._saved(whole) == (whole.data_ptr(), 4096) and ops._saved(whole[:0]) == (None, 0)
+    for t in (whole[:1].expand(4096), whole[::2], whole.view(64, 64), whole.float()):
+        with pytest.raises(B.OlsError, match="saved"):
+            ops._saved(t)
