@@ -157,20 +157,32 @@ struct Epilogue {
     int64_t rest;                       // from a bf16 value to the place of what its rounding has left over; 0: that is not kept
 };
 
-// By the hardware's exponential and reciprocal, each good to a unit in the last place; the argument's rounding adds 2^-24 |a| to
-// the exponential's relative error where it is small against one or the activation against its slope's tail.  (With expf and a
-// correctly rounded division the epilogues were bound by the vector unit: 517 and 317 us of the two products that have one.)
+// The hardware's exponential and reciprocal are good to a unit in the last place each, but the argument's rounding adds 2^-24 |a| to the
+// exponential's relative error: 3e-6 of a SiLU far below zero, which is nothing to a bf16's rounding.  (With expf and a correctly rounded
+// division the epilogues of large bf16 blocks were bound by the vector unit: 517 and 317 us of the two products that have one.)
+// FULL, the SiLU of fp32 blocks, is good to four units in the last place whatever its size: the exponential makes up for what its
+// argument's product with log2 e leaves over.  GELU's slope adds its exponential to a distribution function that is good to 2^-24
+// absolutely, so the hardware's is enough there.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
-__device__ __forceinline__ float sigmoid(float a) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-a)); }
+__device__ __forceinline__ float full_exp_of(float x) {
+    constexpr float kHigh = 1.44269502162933349609f, kLow = 1.92596299112661747e-8f;      // log2 e
+    x = fminf(fmaxf(x, -200.0f), 200.0f);                                                  // 0 and infinity; what is left over stays finite
+    const float t = x * kHigh, left = fmaf(x, kLow, fmaf(x, kHigh, -t));
+    return __builtin_amdgcn_exp2f(t) * fmaf(left, 0.69314718055994530942f, 1.0f);
+}
+template <bool FULL>
+__device__ __forceinline__ float sigmoid(float a) { return __builtin_amdgcn_rcpf(1.0f + (FULL ? full_exp_of(-a) : exp_of(-a))); }
 
+template <bool FULL>
 __device__ __forceinline__ float act_value(int act, float a) {
-    if (act == OLS_ACT_SILU) return a * sigmoid(a);
+    if (act == OLS_ACT_SILU) return a * sigmoid<FULL>(a);
     if (act == OLS_ACT_GELU) return 0.5f * a * (1.0f + erff(a * 0.70710678118654752440f));
     return a <= 0.0f ? 0.0f : a;
 }
+template <bool FULL>
 __device__ __forceinline__ void act_both(int act, float a, float& value, float& slope) {
     if (act == OLS_ACT_SILU) {
-        const float g = sigmoid(a);
+        const float g = sigmoid<FULL>(a);
         value = a * g, slope = g * (1.0f + a * (1.0f - g));
     } else if (act == OLS_ACT_GELU) {
         const float cdf = 0.5f * (1.0f + erff(a * 0.70710678118654752440f));
@@ -219,7 +231,7 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
         float a[8], b[8], x[8], y[8];
         if constexpr (EPI == kUp) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = v[i], b[i] = second[i], x[i] = act_value(e.act, v[i]) * second[i];
+            for (int i = 0; i < 8; ++i) a[i] = v[i], b[i] = second[i], x[i] = act_value<SPLIT>(e.act, v[i]) * second[i];
             if (real < 8) {                              // the padding of internal rows is zero whatever the operands hold
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -236,7 +248,7 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t group, int64_t m
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float value, slope;
-                act_both(e.act, a[i], value, slope);
+                act_both<SPLIT>(e.act, a[i], value, slope);
                 x[i] = v[i] * b[i] * slope, y[i] = v[i] * value;
             }
             if (real < 8) {

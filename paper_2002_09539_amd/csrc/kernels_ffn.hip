@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewParams p) {
                         const int64_t step = (int64_t)gridDim.z * p.rows * 2 * p.in8;
 #pragma unroll 4
                         for (int s = 0; s < p.in_ranges; ++s) a += in[s * step], b += in[s * step + p.in8];
-                        v = act_value(p.act, a) * b;
+                        v = act_value<sizeof(TX) == 4>(p.act, a) * b;
                     }
                 }
                 xs[i][r] = v;

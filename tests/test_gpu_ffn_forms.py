@@ -58,3 +58,34 @@ def test_saved_states_that_are_not_whole_are_refused():
     for t in (saved[:1].expand(saved.numel()), torch.zeros(2 * saved.numel(), dtype=torch.uint8, device="cuda")[::2], saved.float()):
         with pytest.raises(B.OlsError, match="saved"):
             ops.gated_ffn_grad(x, x, *w, t)
+
+
+@pytest.mark.parametrize("rows", [1, 5, 60, 300])
+def test_fp32_activations_far_below_zero(rows):
+    """SiLU and its slope are small there but no less precise: an exponential, a sum, a division and a product, each rounded by 2^-24
+    or a little more (2^-21 in all; the slope 2^-20, with two more products and a sum).  a = x w_gate and b = x w_up are exact."""
+    a = torch.linspace(-80.0, -4.0, rows, device="cuda") if rows > 1 else torch.tensor([-61.3], device="cuda")
+    x = torch.stack([a, torch.ones_like(a)], 1)
+    wg, wu, wd = (torch.tensor(v, device="cuda") for v in ([[1.0], [0.0]], [[0.0], [1.0]], [[1.0]]))
+    d = a.double()
+    s = 1 / (1 + torch.exp(-d))
+    want, slope = d * s, s + d * s * (1 - s)
+    y, saved = _ops().gated_ffn(x, wg, wu, wd, save=True)
+    for got in (y, _ops().gated_ffn(x, wg, wu, wd)):
+        assert ((got[:, 0].double() - want).abs() <= 2.0 ** -21 * want.abs()).all()
+    dx = _ops().gated_ffn_grad(torch.ones_like(y), x, wg, wu, wd, saved).x
+    assert ((dx[:, 0].double() - slope).abs() <= 2.0 ** -20 * slope.abs()).all()
+    assert ((dx[:, 1].double() - want).abs() <= 2.0 ** -21 * want.abs()).all()
+
+
+@pytest.mark.parametrize("rows", [4, 40])
+def test_fp32_silu_of_large_arguments(rows):
+    """Where the exponential overflows or vanishes SiLU is its argument or nothing; of an infinite one it is that."""
+    x = torch.ones(rows, 2, device="cuda")
+    x[:4, 0] = torch.tensor([1e30, 300.0, 0.0, -300.0], device="cuda")
+    wg, wu, wd = (torch.tensor(v, device="cuda") for v in ([[1.0], [0.0]], [[0.0], [1.0]], [[1.0]]))
+    for y in (_ops().gated_ffn(x, wg, wu, wd), _ops().gated_ffn(x, wg, wu, wd, save=True)[0]):
+        assert torch.equal(y[:4, 0], torch.tensor([1e30, 300.0, 0.0, 0.0], device="cuda"))
+    one, far = torch.ones(1, 1, device="cuda"), torch.full((rows, 1), float("inf"), device="cuda")
+    for y in (_ops().gated_ffn(far, one, one, one), _ops().gated_ffn(far, one, one, one, save=True)[0]):
+        assert (y == float("inf")).all()
