@@ -149,18 +149,19 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewParams p) {
 #pragma unroll
             for (int j = 0; j < B; ++j) {
                 if (i + 32 * j >= n) continue;
-                float v[PANELS][8];
+                if constexpr (ROUND) {
 #pragma unroll
-                for (int t = 0; t < PANELS; ++t)
+                    for (int t = 0; t < PANELS; ++t)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[t][e] = ROUND ? of_bf16(bf16_of(u[j][t].get(e))) : u[j][t].get(e);
+                        for (int e = 0; e < 8; ++e) u[j][t].v[e] = of_bf16(bf16_of(u[j][t].v[e]));
+                }
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const float x = xs[i + 32 * j][r];
 #pragma unroll
                     for (int t = 0; t < PANELS; ++t)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) acc[t][r][e] = fmaf(x, v[t][e], acc[t][r][e]);
+                        for (int e = 0; e < 8; ++e) acc[t][r][e] = fmaf(x, u[j][t].get(e), acc[t][r][e]);
                 }
             }
         }
