@@ -28,6 +28,7 @@ class Session:
         self.x_alt = z(m, self.ld) if overlap_buffer else None
         self.buf = z(m, self.ld) if mu != 0.0 else None
         self.g = z(m, self.ld) if own_gradient else None
+        self.step_g = None                    # what the next local step reads
         self.z = z(self.ld)
         self.v = None
         self.ws = None
@@ -43,6 +44,7 @@ class Session:
             self.g = g
         B.ols_bind(self.h, _ptr(self.x), _ptr(self.x_alt), _ptr(self.buf), _ptr(self.g), _ptr(self.z), self.ld,
                    self.main.cuda_stream, self.side.cuda_stream)
+        self.step_g = self.g
 
     # ---- configuration -----------------------------------------------------------------------
     def set_option(self, key, value):
@@ -126,16 +128,21 @@ class Session:
     def set_gradient(self, g):
         assert g.is_contiguous() and tuple(g.shape) == (self.m, self.ld) and g.dtype == torch.float32
         B.ols_set_gradient(self.h, _ptr(g))
+        self.step_g = g
 
     def models(self):
         """[m][ld]: the replica buffer that holds the models now (for gradients computed outside the library)."""
         return self.x_alt if B.ols_params_buffer(self.h) else self.x
 
     def clip_gradients(self, max_norm):
-        """Scales every worker's gradient row to a norm of at most max_norm, on the main stream, before local_step; returns
-        the m norms before that (a device tensor)."""
+        """Scales every worker's row of the gradients that local_step reads next (the bound ones, or set_gradient's) to a norm of
+        at most max_norm, on the main stream; returns the m norms before that (a device tensor).  Not with an attached model, which
+        writes its gradients within the step, and not while a deferred step still needs them."""
+        if self.step_g is None:
+            raise B.OlsError(B.OLS_ESTATE, "no gradients are bound")
+        B.ols_set_gradient(self.h, _ptr(self.step_g))       # refuses where the gradients are not the caller's
         with torch.cuda.stream(self.main):
-            return operators.clip_grad_norm([row[: self.d] for row in self.g], max_norm, groups=range(self.m))
+            return operators.clip_grad_norm([row[: self.d] for row in self.step_g], max_norm, groups=range(self.m))
 
     def local_step(self):
         B.ols_local_step(self.h)

@@ -73,7 +73,7 @@ class TokenModel:
     def step(self, s, contexts, targets, max_norm):
         """One iteration of all workers of the Session; returns their losses and the norms of their gradients."""
         with torch.cuda.stream(s.main):
-            losses = self.gradients(s.models(), s.g, contexts, targets)
+            losses = self.gradients(s.models(), s.step_g, contexts, targets)
         norms = s.clip_gradients(max_norm)
         s.run(1)
         return losses, norms
