@@ -38,6 +38,10 @@ constexpr int64_t kMaxTokens = 1 << 24, kMaxVocab = 1 << 24, kMaxWidth = 1 << 20
 
 bool stride_ok(int64_t row, int64_t width) { return row >= width && row <= kMaxStride; }
 bool group_ok(int64_t g) { return g >= 0 && g <= kMaxStride; }
+// Whether the workers' matrices of rows that do not overlap lie behind each other, or side by side within a row's stride.
+bool groups_apart(int groups, int64_t group, int64_t rows, int64_t row, int64_t cols) {
+    return groups == 1 || group >= (rows - 1) * row + cols || (group >= cols && row >= (groups - 1) * group + cols);
+}
 
 // Bytes that a workspace needs, checked against what the caller brought.
 int check_ws(const char* who, const void* ws, int64_t have, int64_t need) {
@@ -92,7 +96,7 @@ int check_matrix(const char* who, const char* name, const ols_matrix& m, int64_t
     if (!m.dev || !element_aligned(m.dev, dtype)) return bad("%s: %s is null or not aligned to its type", who, name);
     if (!stride_ok(m.row, cols)) return bad("%s: rows of %s, of %lld elements, cannot be %lld apart", who, name, (long long)cols, (long long)m.row);
     if (!group_ok(m.group)) return bad("%s: the workers' stride of %s is out of range", who, name);
-    if (written && groups > 1 && m.group < (rows - 1) * m.row + cols) return bad("%s: the workers' %s overlap", who, name);
+    if (written && !groups_apart(groups, m.group, rows, m.row, cols)) return bad("%s: the workers' %s overlap", who, name);
     return OLS_OK;
 }
 
@@ -218,7 +222,7 @@ int ols_embed(int groups, int64_t tokens, int64_t vocab, int64_t width, const in
         return bad("%s: a pointer is not aligned to its type", who);
     if (!stride_ok(table_row, width) || !stride_ok(out_row, width)) return bad("%s: rows of %lld elements overlap at the given strides", who, (long long)width);
     if (!group_ok(ids_group) || !group_ok(table_group) || !group_ok(out_group)) return bad("%s: a worker's stride is out of range", who);
-    if (groups > 1 && out_group < (tokens - 1) * out_row + width) return bad("%s: the workers' outputs overlap", who);
+    if (!groups_apart(groups, out_group, tokens, out_row, width)) return bad("%s: the workers' outputs overlap", who);
     EmbedParams p;
     p.groups = groups, p.dtype = dtype, p.out_dtype = out_dtype, p.tokens = tokens, p.vocab = vocab, p.width = width;
     p.table = table_dev, p.table_row = table_row, p.table_group = table_group, p.ids = ids_dev, p.ids_group = ids_group, p.scale = scale;
@@ -243,7 +247,7 @@ int ols_embed_grad(int groups, int64_t tokens, int64_t vocab, int64_t width, con
         return bad("%s: a pointer is not aligned to its type", who);
     if (!stride_ok(d_out_row, width) || !stride_ok(grad_row, width)) return bad("%s: rows of %lld elements overlap at the given strides", who, (long long)width);
     if (!group_ok(ids_group) || !group_ok(d_out_group) || !group_ok(grad_group)) return bad("%s: a worker's stride is out of range", who);
-    if (groups > 1 && grad_group < (vocab - 1) * grad_row + width) return bad("%s: the workers' gradients overlap", who);
+    if (!groups_apart(groups, grad_group, vocab, grad_row, width)) return bad("%s: the workers' gradients overlap", who);
     if (const int rc = check_ws(who, ws_dev, ws_bytes, embed_grad_workspace_bytes(groups, tokens, vocab, width))) return rc;
     EmbedGradParams p;
     p.groups = groups, p.dtype = dtype, p.grad_dtype = grad_dtype, p.accumulate = accumulate != 0, p.tokens = tokens, p.vocab = vocab, p.width = width;

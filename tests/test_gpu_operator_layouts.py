@@ -32,3 +32,42 @@ def test_logits_and_gradients_whose_rows_share_memory_are_refused(dtype):
         ops.token_logprobs(column, t)
     assert ops.token_logprobs(whole[:, 3:4], t).logprob.tolist() == [0.0] * 4
     assert float(flat.abs().sum()) == 0.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_results_of_workers_side_by_side(dtype):
+    """Workers' matrices within one another's rows ([rows][workers][columns]) do not overlap: same results as elsewhere."""
+    ops = _ops()
+    m, rows, width, hidden, out, vocab = 3, 12, 16, 24, 8, 50
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda *s: (torch.randn(*s, generator=g, device="cuda") * 0.3).to(dtype)  # noqa: E731
+
+    def beside(*shape, fill=7.0):
+        """[m][a][b] in memory [a][m][b + 1], the gap to be left alone"""
+        whole = torch.full((shape[1], shape[0], shape[2] + 1), fill, dtype=dtype, device="cuda")
+        return whole, whole[:, :, : shape[2]].transpose(0, 1)
+    ids = torch.randint(-1, vocab, (m, rows), generator=g, device="cuda", dtype=torch.int32)
+    d = r(m, rows, width)
+    whole, table = beside(m, vocab, width)
+    ops.embed_grad(ids, d, vocab, out=table, workers=m)
+    assert torch.equal(table, ops.embed_grad(ids, d, vocab, dtype=dtype, workers=m)) and (whole[:, :, width] == 7).all()
+    x, w, dy = r(m, rows, width), (r(m, width, hidden), r(m, width, hidden), r(m, hidden, out)), r(m, rows, out)
+    want, saved = ops.gated_ffn(x, *w, save=True)
+    whole, y = beside(m, rows, out)
+    assert torch.equal(ops.gated_ffn(x, *w, save=True, out=y)[0], want) and (whole[:, :, out] == 7).all()
+    grads = ops.gated_ffn_grad(dy, x, *w, saved)
+    places = [beside(*t.shape) for t in grads]
+    got = ops.gated_ffn_grad(dy, x, *w, saved, out=ops.FfnGrads(*(p[1] for p in places)))
+    for a, b, (whole, view) in zip(got, grads, places):
+        assert a is view and torch.equal(a, b) and (whole[:, :, view.shape[2]] == 7).all()
+    none = ops.gated_ffn_grad(dy[:, :0], x[:, :0], *w, saved[:0], out=ops.FfnGrads(None, *(p[1] for p in places[1:])))
+    assert all(float(t.float().abs().sum()) == 0.0 for t in none[1:]) and all((p[0][:, :, -1] == 7).all() for p in places[1:])
+
+
+def test_results_of_workers_that_overlap_are_refused():
+    ops = _ops()
+    x, w = torch.randn(2, 6, 4, device="cuda"), [torch.randn(2, *s, device="cuda") for s in ((4, 8), (4, 8), (8, 4))]
+    flat = torch.zeros(200, device="cuda")
+    for strides in ((3, 8, 1), (4, 7, 1), (23, 4, 1), (0, 4, 1)):
+        with pytest.raises(B.OlsError):
+            ops.gated_ffn(x, *w, out=flat.as_strided((2, 6, 4), strides))
