@@ -5,6 +5,9 @@ stream of the tensors' device (see the section of the same name in include/ols.h
 kept.  Tensors are fp32 or bf16, ids int32.  A leading axis of m workers can stand in front of every tensor, so that
 weights and gradients can be views of the rows of a Session's x and g; rows may be strided, elements of a row may not.
 Tensors that were made on another stream are the caller's to order and to record, as with any torch operation.
+
+Nothing here takes part in automatic differentiation: results carry no graph, also where a tensor requires gradients, and so end any
+graph that leads to them.  Every operator has a function for its gradient, which the caller calls.
 """
 import contextlib
 from array import array
