@@ -81,6 +81,8 @@ def _ptr(t):
 def _ids(tokens, m):
     if tokens.dtype != torch.int32:
         _refuse("ids must be int32, got %s", tokens.dtype)
+    if m < 1:
+        _refuse("at least one worker is needed, got %d", m)
     ids = tokens.reshape(m, -1) if tokens.is_contiguous() else tokens.reshape(m, -1).contiguous()
     return ids, (ids.shape[1] if m > 1 else 0)
 

@@ -74,3 +74,9 @@ def test_saved_states_are_whole():
     for t in (whole[:1].expand(4096), whole[::2], whole.view(64, 64), whole.float()):
         with pytest.raises(B.OlsError, match="saved"):
             ops._saved(t)
+
+
+@pytest.mark.parametrize("m", [0, -1])
+def test_no_workers(m):
+    with pytest.raises(B.OlsError, match="worker"):
+        ops._ids(torch.zeros(0, 3, dtype=torch.int32), m)
