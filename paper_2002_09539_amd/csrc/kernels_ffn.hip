@@ -15,7 +15,8 @@
 // at once.  One row through 2048 - 5632 - 2048 in bf16: 25 us in three launches (12.5, 8 and 4: the first reads 46 MB at 3.7
 // TB/s; with half the workgroups and half the loads in flight 17.5, 11.5 and 3.5).
 //
-// 8192 rows through 2048 - 5632 - 2048, forward and backward, bf16: 1.79 ms, 950 TFLOP/s; ffn_gemm.h says what bounds the products.
+// 8192 rows through 2048 - 5632 - 2048, forward and backward, bf16: 1.73 to 1.84 ms on different cards, 925 to 983 TFLOP/s;
+// ffn_gemm.h says what bounds the products.
 // The two with an epilogue of their own add the time of its memory traffic, since the tiles of a round end together: 461 MB
 // written behind a, b and h, 553 MB read and written behind da and db.
 #include <algorithm>
@@ -216,10 +217,10 @@ bool lies_well(const ols_matrix& m, int dtype, int64_t inner) {
     return dtype == OLS_BF16 && inner % 8 == 0 && m.row % 8 == 0 && m.row <= (1 << 22) && m.group % 8 == 0 && ((uintptr_t)m.dev & 15) == 0;
 }
 
-// A small bf16 block of few rows keeps what rounding h, da and db to bf16 leaves over, as a second term: the results of few roundings
-// scatter around 1.41 times the error of their own (up to 1.6), and the longer contractions cost nothing there that shows beside the
-// launches (forward and backward, 17 rows, 104 - 5600 - 22: 71 to 80 us with it, 74 without).  With more weights they do: 32 rows,
-// 1024 - 2816 - 1024: 86, 80; 8 rows, 2048 - 5632 - 2048: 124, 110.
+// A small bf16 block of few rows keeps what rounding h, da and db to bf16 leaves over, as a second term: its results are the formula's
+// rounded once, where others add roundings of the inner tensors (1.41 times that error, up to 1.6 where few are added up).  It is kept
+// where the longer contractions do not show beside the launches (forward and backward, 17 rows, 104 - 5600 - 22: 71 to 80 us with it,
+// 74 without), and not where they do (32 rows, 1024 - 2816 - 1024: 86 us with it, 80 without; 8 rows, 2048 - 5632 - 2048: 124, 110).
 bool keeps_rest(const ols_ffn& f) { return f.dtype == OLS_BF16 && f.rows <= 32 && f.hidden * (2 * f.width + f.out) <= (1 << 21); }
 
 struct Maker {                         // lays operands out; without a stream it only measures

@@ -16,8 +16,9 @@
 // statistics and best k a second launch joins.
 //
 // The logits stay packed as they were read and are unpacked anew by each pass (kept as fp32 from pass to pass they spill: 1.25 ms
-// instead of 0.43 below).  8192 rows of 50 001 bf16 logits, loss and gradient: 430 us (3.8 TB/s; 396 with rows of 50 000, which
-// start on whole vectors, and 4.85 TB/s with 32 000).  1531 rows of 32 003 bf16 with five alternatives: 34 us, 26 without.  Four
+// instead of 0.43 below).  8192 rows of 50 001 bf16 logits, loss and gradient: 430 us (3.8 TB/s; 364 to 396 with rows of 50 000,
+// which start on whole vectors, and 4.9 TB/s with 32 000), the gradient alone 356.  1531 rows of 32 003 bf16 with five alternatives:
+// 34 us, 25 without.  Four
 // rows of 128 000 fp32 with eight: 8 us in 252 parts, 7 to join them.
 //
 // Best k: the k-th largest of the lanes' maxima is a bound that at least k logits reach and that few others do: fewer
