@@ -448,8 +448,8 @@ OLS_API int64_t ols_embed_grad_workspace_bytes(int groups, int64_t tokens, int64
  *   - ols_gated_ffn_grad reads dy, x, the weights and `saved` and writes dx, g_gate, g_up and g_down (of the weights' shapes);
  *     one whose dev is NULL is not computed.  Gradients are written, not added to.  dx may lie on x or on dy, or else the weights'
  *     gradients on the weights; no other result on an operand, on `saved` or on another result.
- *   - Limits: groups <= 4096; width, hidden and out <= 2^20; rows <= 2^24; a product of all workers has at most 2^23 tiles of 128 x 128
- *     results (128 x 64 of a and b); row strides of dx, y and the gradients must not make
+ *   - Limits: groups <= 4096; width, hidden and out <= 2^20; rows <= 2^24; a product of all workers has fewer than 2^24 - 512 tiles of
+ *     128 x 128 results (128 x 64 of a and b); row strides of dx, y and the gradients must not make
  *     rows or workers overlap. */
 enum { OLS_ACT_SILU = 0, OLS_ACT_GELU = 1 /* x Phi(x), by the error function */, OLS_ACT_RELU = 2 };
 typedef struct ols_matrix {

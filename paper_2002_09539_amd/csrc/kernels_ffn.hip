@@ -370,7 +370,7 @@ Shape choose(const Job* jobs, int n, int groups, int panels, bool split, bool ac
     double best_us = 1e300;
     for (int t = 128; t <= (split ? 128 : 256); t += 128) {          // fp32: two sets of sums leave no registers for large tiles
         const int64_t slots = slots_of(t, split), tiles = count_tiles(jobs, n, groups, panels, t);
-        if (tiles * (t == 256 ? 512 : 256) > kMostBlocks * 256) continue;
+        if ((tiles + slots) * (t == 256 ? 512 : 256) >= (int64_t)1 << 32) continue;      // cut, the tiles of a last round fill it at the most
         for (int ranges : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             Shape s{t, (int)tiles, 0, 1};
             if (ranges > 1) {

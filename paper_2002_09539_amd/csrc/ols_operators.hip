@@ -90,7 +90,7 @@ int check_ffn(const char* who, const ols_ffn* f) {
     return OLS_OK;
 }
 
-int too_many_tiles(const char* who) { return bad("%s: a product of the workers together has more than 2^23 tiles of 128 x 128 results", who); }
+int too_many_tiles(const char* who) { return bad("%s: a product of the workers together has 2^24 - 512 tiles of 128 x 128 results or more", who); }
 
 int check_matrix(const char* who, const char* name, const ols_matrix& m, int64_t rows, int64_t cols, int dtype, int groups, bool written) {
     if (!m.dev || !element_aligned(m.dev, dtype)) return bad("%s: %s is null or not aligned to its type", who, name);

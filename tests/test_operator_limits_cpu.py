@@ -32,5 +32,6 @@ def test_more_tiles_than_a_launch_numbers(groups, rows, width, hidden, out, dtyp
 
 
 def test_many_tiles_that_a_launch_numbers():
+    assert B.ols_gated_ffn_workspace_bytes(block(4096, 9, 8, 64 * 4095, 8, B.OLS_F32), 0) > 0      # 2^24 - 4096
     assert B.ols_gated_ffn_workspace_bytes(block(4096, 9, 8, 1 << 16, 8, B.OLS_F32), 0) > 0
     assert B.ols_gated_ffn_workspace_bytes(block(1, 1 << 24, 8, 8, 4096, B.OLS_BF16), 1) > 0
