@@ -510,6 +510,114 @@ OLS_API int ols_clip_gradients(int n, const void* const* in_dev, void* const* ou
                                int dtype, float max_norm, float* norms_dev, void* ws_dev, int64_t ws_bytes, void* stream);
 OLS_API int64_t ols_clip_workspace_bytes(int n, const int64_t* numel, const int32_t* group, int groups);
 
+/* Distillation: the loss of a student's rows of logits z against lists of a teacher's k best tokens, with the likelihood of a
+ * given token beside it.  With u = z / temperature, p = softmax(u) and the entries (index i_j, value v_j) of a row's list
+ *     q_j = e^{v_j / temperature} / sum of these over the list                                     rest == 0: v are logits or log probabilities
+ *     q_j = e^{v_j},  q_r = max(0, 1 - sum q),  p_r = the sum of p over all that is not listed     rest != 0: v are log probabilities at
+ *                                                                                                  this temperature
+ *     loss = temperature^2 (sum q_j (log q_j - log p_{i_j}) + q_r (log q_r - log p_r)),      logprob = z[target] - log sum e^z.
+ *   - top_value and top_index are [rows][k], without gaps, 1 <= k <= OLS_MAX_TEACHER (ols_token_logprobs writes such lists).  An index
+ *     outside [0, vocab) is no entry.  A list without entries has loss 0 and no gradient.  A token that is listed twice has both q.
+ *   - The rest's term is left out where q_r is 0 or the student allows nothing outside the list (no other logit above -inf).
+ *   - A logit of -inf cannot occur: probability 0.  Where it is listed with q > 0 the loss is infinite and the gradient there -q, by the
+ *     formula; as a target see ols_token_logprobs.  A row of nothing else: loss infinite (0 without any q > 0), logprob -inf, gradient 0.
+ *   - A NaN or +inf in a row, or among a list's values, makes the row's loss and gradient NaN (and the logprob in the first case).
+ *   - targets NULL: none; logprob may be NULL then and is not written.  A target outside [0, vocab) is none: logprob 0.
+ * With d_logits the same call computes the gradient of sum(d_loss loss + d_logprob logprob) (each [rows]; NULL: zeros):
+ *     d_logits_i = d_loss temperature (p_i (sum q + q_r) - q's of i        where i is listed
+ *                                                        - q_r p_i / p_r   elsewhere) + d_logprob ([i == target] - softmax(z)_i).
+ * It may lie on the logits (same pointer and row stride).  stats ([rows][8]) is what the gradient alone needs later, with the same lists,
+ * targets, temperature and rest.  Rows lie at least `vocab` elements apart.  vocab <= 2^24, temperature in [2^-20, 2^20]. */
+#define OLS_MAX_TEACHER 256
+typedef struct ols_distill {
+    int32_t dtype, k, rest;
+    float temperature;
+    int64_t rows, vocab;
+    const void* logits;
+    int64_t row_stride;
+    const float* top_value;
+    const int32_t* top_index;
+    const int32_t* targets;
+    float *loss, *logprob, *stats;
+    const float *d_loss, *d_logprob;
+    void* d_logits;
+    int64_t d_stride;
+    void* ws;
+    int64_t ws_bytes;
+} ols_distill;
+OLS_API int ols_distill_loss(const ols_distill* d, void* stream);
+OLS_API int ols_distill_loss_grad(const ols_distill* d, void* stream);          /* reads stats; loss and logprob are not touched */
+OLS_API int64_t ols_distill_workspace_bytes(int64_t rows, int64_t vocab, int dtype);   /* of ols_distill_loss */
+
+/* One step of beam search: for each of `batch` requests the `beams` best continuations of its in_beams hypotheses.
+ *   - A hypothesis of score s with logits z has the candidates v of value s + z[v] - log sum e^z, one that has ended (finished) itself alone,
+ *     of value s.  They are ordered by value / max(length, 1)^length_penalty, with the length that the candidate has (length + 1, or length
+ *     where it has ended); ties go to the lower hypothesis, then to the lower token.  length may be NULL with a penalty of 0.
+ *   - Results, [batch][beams] each, best first: the value (new_score), the token (eos of an ended one), the hypothesis that it continues
+ *     (parent), whether it has ended (its parent had, or its token is eos; eos < 0: none), and its length (new_length, NULL: not written).
+ *   - A score of -inf is no hypothesis (a search begins with one and beams - 1 of these).  A logit of -inf cannot occur.  Places without a
+ *     candidate: score -inf, token -1, parent its own number (0 from in_beams on), not ended, its parent's length.
+ *   - A score that is NaN or +inf, or a NaN or +inf among the logits of a hypothesis that goes on, makes all scores of its request NaN, its
+ *     tokens -1 and its parents their own numbers.  Logits of ended hypotheses and of none are not read.
+ * logits: [batch][in_beams][vocab], rows beam_stride and requests batch_stride elements apart, which may be anything from 0.
+ * batch < 65536; in_beams and beams in [1, OLS_MAX_TOP]; vocab <= 2^24. */
+typedef struct ols_beam {
+    int32_t dtype, in_beams, beams, eos;
+    int64_t batch, vocab;
+    const void* logits;
+    int64_t batch_stride, beam_stride;
+    const float* score;
+    const uint8_t* finished;        /* NULL: none has ended */
+    const int32_t* length;
+    double length_penalty;
+    float* new_score;
+    int32_t *token, *parent, *new_length;
+    uint8_t* new_finished;
+    void* ws;
+    int64_t ws_bytes;
+} ols_beam;
+OLS_API int ols_beam_select(const ols_beam* b, void* stream);
+OLS_API int64_t ols_beam_workspace_bytes(int64_t batch, int in_beams, int beams, int64_t vocab, int dtype);
+
+/* Moves the states of hypotheses behind a step: state[b][i] = old state[b][parent[b][i]] for n tensors of any type, each of
+ * [batch][in_beams] rows of row_bytes bytes, rows src_beam and requests src_batch bytes apart, to [batch][beams] rows.
+ * All arrays are HOST arrays of n entries, read before the call returns.  dst[i] == src[i] moves in place (the same strides, beams ==
+ * in_beams; hypotheses that stay are not touched); otherwise outputs must not lie on inputs, nor on each other in any case.  A parent outside
+ * [0, in_beams) leaves its place as it was. */
+OLS_API int ols_beam_reorder(int n, const void* const* src, void* const* dst, const int64_t* row_bytes, const int64_t* src_batch, const int64_t* src_beam,
+                             const int64_t* dst_batch, const int64_t* dst_beam, int64_t batch, int in_beams, int beams, const int32_t* parent, void* stream);
+
+/* Products in 8-bit integers:
+ *     y[r][c] = (sum over k of q_x[r][k] q_w[c][k]) x_scale[r] w_scale[c]
+ * The integer sums are exact.  q_w is [out][width]: a channel's weights side by side, in int8; rows at least `width` apart.
+ *   - dtype OLS_F32 or OLS_BF16: x is given in that type, and the call quantises its rows as ols_quantize_rows does; with `up` it takes
+ *     act(x) up in its place, in fp32 (the hidden rows of a gated block).  OLS_I8: x and x_scale are given.  Weights are best with rows that begin on 16
+ *     bytes; others are read more slowly.
+ *   - y is of out_dtype.  Limits: groups <= 4096, width < 2^17, out <= 2^24, rows <= 2^24; fewer than 2^24 tiles of 16 x 16 results. */
+enum { OLS_I8 = 2 };
+typedef struct ols_int8 {
+    int32_t groups, dtype, act, out_dtype;
+    int64_t rows, width, out;
+    ols_matrix x, up, w, y;
+    const float* x_scale;
+    int64_t x_scale_group;
+    const float* w_scale;
+    int64_t w_scale_group;
+    void* ws;
+    int64_t ws_bytes;
+} ols_int8;
+OLS_API int ols_int8_matmul(const ols_int8* f, void* stream);
+OLS_API int64_t ols_int8_workspace_bytes(const ols_int8* f);
+
+/* Rows to 8 bits: scale[r] = fp32(max |x[r]| / 127), q[r][k] = x[r][k] / scale[r] to the nearest whole number, halves to even (of the exact
+ * quotient).  Rows of zeros have scale 0 and q 0, rows with a NaN or an infinity a scale of NaN and q 0.  With up.dev x is act(x) up, in fp32. */
+OLS_API int ols_quantize_rows(int groups, int64_t rows, int64_t width, const ols_matrix* x, const ols_matrix* up, int act, int dtype, int8_t* q, int64_t q_row,
+                              int64_t q_group, float* scale, int64_t scale_group, void* stream);
+/* Weights [width][out] to 8 bits with a scale for each column, laid out for ols_int8_matmul: q [out][width], scale [out]. */
+OLS_API int ols_quantize_weight(int groups, int64_t width, int64_t out, const ols_matrix* w, int dtype, int8_t* q, int64_t q_row, int64_t q_group, float* scale,
+                                int64_t scale_group, void* ws, int64_t ws_bytes, void* stream);
+OLS_API int64_t ols_quantize_weight_workspace_bytes(int groups, int64_t width, int64_t out);
+
 OLS_API const char* ols_last_error(void);
 OLS_API const char* ols_version(void);
 

@@ -10,8 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("OLS_LIBRARY", os.path.join(HERE, "libols.so"))   # override: an alternative build
 
 OLS_OK, OLS_EINVAL, OLS_ESTATE, OLS_EHIP, OLS_ENOMEM = 0, -1, -2, -3, -4
-OLS_F32, OLS_BF16 = 0, 1
-OLS_MAX_TOP = 32
+OLS_F32, OLS_BF16, OLS_I8 = 0, 1, 2
+OLS_MAX_TOP, OLS_MAX_TEACHER = 32, 256
 OLS_ACT_SILU, OLS_ACT_GELU, OLS_ACT_RELU = range(3)
 (OLS_OPT_NESTEROV, OLS_OPT_FUSE_PULL, OLS_OPT_SERIALIZE, OLS_OPT_DRY_RUN, OLS_OPT_KERNEL_TIMING, OLS_OPT_TRACE,
  OLS_OPT_MEAN_SPLIT, OLS_OPT_FUSE_MEAN, OLS_OPT_TUNING) = range(1, 10)
@@ -38,6 +38,27 @@ class ols_ffn(C.Structure):
                 + [(n, C.c_int64) for n in ("rows", "width", "hidden", "out")]
                 + [(n, ols_matrix) for n in ("x", "w_gate", "w_up", "w_down", "y", "dy", "dx", "g_gate", "g_up", "g_down")]
                 + [("saved", C.c_void_p), ("saved_bytes", C.c_int64), ("ws", C.c_void_p), ("ws_bytes", C.c_int64)])
+
+
+class ols_distill(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "k", "rest")] + [("temperature", C.c_float)] + [(n, C.c_int64) for n in ("rows", "vocab")]
+                + [("logits", C.c_void_p), ("row_stride", C.c_int64)]
+                + [(n, C.c_void_p) for n in ("top_value", "top_index", "targets", "loss", "logprob", "stats", "d_loss", "d_logprob", "d_logits")]
+                + [("d_stride", C.c_int64), ("ws", C.c_void_p), ("ws_bytes", C.c_int64)])
+
+
+class ols_beam(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "in_beams", "beams", "eos")] + [(n, C.c_int64) for n in ("batch", "vocab")] + [("logits", C.c_void_p)]
+                + [(n, C.c_int64) for n in ("batch_stride", "beam_stride")] + [(n, C.c_void_p) for n in ("score", "finished", "length")]
+                + [("length_penalty", C.c_double)] + [(n, C.c_void_p) for n in ("new_score", "token", "parent", "new_length", "new_finished", "ws")]
+                + [("ws_bytes", C.c_int64)])
+
+
+class ols_int8(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("groups", "dtype", "act", "out_dtype")] + [(n, C.c_int64) for n in ("rows", "width", "out")]
+                + [(n, ols_matrix) for n in ("x", "up", "w", "y")]
+                + [("x_scale", C.c_void_p), ("x_scale_group", C.c_int64), ("w_scale", C.c_void_p), ("w_scale_group", C.c_int64), ("ws", C.c_void_p),
+                   ("ws_bytes", C.c_int64)])
 
 
 class OlsError(RuntimeError):
@@ -97,6 +118,17 @@ _SIGNATURES = {
     "ols_token_logprobs_grad": (C.c_int, [_I, _I, _P, C.c_int, _I, _P, _P, _P, _P, _P, _P, _I, _P]),
     "ols_clip_gradients": (C.c_int, [C.c_int, _P, _P, _P, _P, C.c_int, C.c_int, C.c_float, _P, _P, _I, _P]),
     "ols_clip_workspace_bytes": (_I, [C.c_int, _P, _P, C.c_int]),
+    "ols_distill_loss": (C.c_int, [_P, _P]),
+    "ols_distill_loss_grad": (C.c_int, [_P, _P]),
+    "ols_distill_workspace_bytes": (_I, [_I, _I, C.c_int]),
+    "ols_beam_select": (C.c_int, [_P, _P]),
+    "ols_beam_workspace_bytes": (_I, [_I, C.c_int, C.c_int, _I, C.c_int]),
+    "ols_beam_reorder": (C.c_int, [C.c_int, _P, _P, _P, _P, _P, _P, _P, _I, C.c_int, C.c_int, _P, _P]),
+    "ols_int8_matmul": (C.c_int, [_P, _P]),
+    "ols_int8_workspace_bytes": (_I, [_P]),
+    "ols_quantize_rows": (C.c_int, [C.c_int, _I, _I, _P, _P, C.c_int, C.c_int, _P, _I, _I, _P, _I, _P]),
+    "ols_quantize_weight": (C.c_int, [C.c_int, _I, _I, _P, C.c_int, _P, _I, _I, _P, _I, _P, _I, _P]),
+    "ols_quantize_weight_workspace_bytes": (_I, [C.c_int, _I, _I]),
     "ols_last_error": (C.c_char_p, []),
     "ols_version": (C.c_char_p, []),
 }
@@ -303,6 +335,37 @@ def ols_clip_gradients(n, inputs, outputs, numel, group, groups, dtype, max_norm
     _check(load().ols_clip_gradients(n, inputs, outputs, numel, group, groups, dtype, max_norm, norms, ws, ws_bytes, stream))
 
 
+def ols_distill_loss(d, stream):
+    _check(load().ols_distill_loss(C.byref(d), stream))
+
+
+def ols_distill_loss_grad(d, stream):
+    _check(load().ols_distill_loss_grad(C.byref(d), stream))
+
+
+def ols_beam_select(b, stream):
+    _check(load().ols_beam_select(C.byref(b), stream))
+
+
+def ols_beam_reorder(n, src, dst, row_bytes, src_batch, src_beam, dst_batch, dst_beam, batch, in_beams, beams, parent, stream):
+    """src to dst_beam: addresses of host arrays of n entries."""
+    _check(load().ols_beam_reorder(n, src, dst, row_bytes, src_batch, src_beam, dst_batch, dst_beam, batch, in_beams, beams, parent, stream))
+
+
+def ols_int8_matmul(f, stream):
+    _check(load().ols_int8_matmul(C.byref(f), stream))
+
+
+def ols_quantize_rows(groups, rows, width, x, up, *rest):
+    """x: an ols_matrix, up: an ols_matrix or None."""
+    _check(load().ols_quantize_rows(groups, rows, width, C.byref(x), None if up is None else C.byref(up), *rest))
+
+
+def ols_quantize_weight(groups, width, out, w, *rest):
+    """w: an ols_matrix."""
+    _check(load().ols_quantize_weight(groups, width, out, C.byref(w), *rest))
+
+
 def _bytes(n):     # a size or an index, or a negative error code
     if n < 0:
         raise OlsError(int(n), last_error())
@@ -323,6 +386,22 @@ def ols_gated_ffn_workspace_bytes(f, grad):
 
 def ols_token_logprobs_workspace_bytes(rows, vocab, dtype, top):
     return _bytes(load().ols_token_logprobs_workspace_bytes(rows, vocab, dtype, top))
+
+
+def ols_distill_workspace_bytes(rows, vocab, dtype):
+    return _bytes(load().ols_distill_workspace_bytes(rows, vocab, dtype))
+
+
+def ols_beam_workspace_bytes(batch, in_beams, beams, vocab, dtype):
+    return _bytes(load().ols_beam_workspace_bytes(batch, in_beams, beams, vocab, dtype))
+
+
+def ols_int8_workspace_bytes(f):
+    return _bytes(load().ols_int8_workspace_bytes(C.byref(f)))
+
+
+def ols_quantize_weight_workspace_bytes(groups, width, out):
+    return _bytes(load().ols_quantize_weight_workspace_bytes(groups, width, out))
 
 
 def ols_clip_workspace_bytes(n, numel, group, groups):

@@ -35,6 +35,9 @@ SOURCES = [
     "kernels_ffn.hip",
     "kernels_logprob.hip",
     "kernels_clip.hip",
+    "kernels_distill.hip",
+    "kernels_beam.hip",
+    "kernels_int8.hip",
 ]
 
 # packed-fp32 VALU forms stay disabled for every device translation unit

@@ -525,4 +525,86 @@ hipError_t launch_clip(const ClipTable& t, int dtype, int64_t chunk_elems, int b
 hipError_t launch_clip_sums(const ClipGroups& g, int groups, double* partial, hipStream_t stream);   // a group's sum in the place of its first
 hipError_t launch_clip_norms(const ClipGroups& g, int groups, const double* partial, float* norms, hipStream_t stream);
 
+struct DistillParams {
+    int dtype, k, rest;
+    float temperature;
+    int64_t rows, vocab;
+    const void* logits;
+    int64_t row_stride;
+    const float* value;                  // [rows][k]
+    const int32_t *index, *targets;
+    float *loss, *logprob, *stats;       // stats: [rows][8]
+    const float *g_loss, *g_logprob;
+    void* d_logits;
+    int64_t d_stride;
+    // set by the launcher
+    int parts;
+    int64_t part;
+    float* part_sums;
+    float hi, lo, hi1, lo1;              // log2 e / temperature and log2 e, each in two terms
+};
+int64_t distill_workspace_bytes(int dtype, int64_t rows, int64_t vocab);
+hipError_t launch_distill(const DistillParams& p, void* ws, hipStream_t stream);     // with d_logits: the gradient as well
+hipError_t launch_distill_grad(const DistillParams& p, hipStream_t stream);          // from p.stats
+
+struct BeamParams {
+    int dtype, in_beams, beams, eos;
+    int64_t batch, vocab;
+    const void* logits;
+    int64_t batch_stride, beam_stride;
+    const float* score;
+    const uint8_t* finished;
+    const int32_t* length;
+    double penalty;
+    float* new_score;
+    int32_t *token, *parent, *new_length;
+    uint8_t* new_finished;
+    // set by the launcher: of each hypothesis' parts
+    int parts;
+    int64_t part;
+    double* part_s;
+    float *part_m, *part_val;
+    int32_t* part_idx;
+};
+int64_t beam_workspace_bytes(int dtype, int64_t batch, int in_beams, int beams, int64_t vocab);
+hipError_t launch_beam(BeamParams p, void* ws, hipStream_t stream);
+
+// Tensors of one launch, by value in the kernel arguments.  Strides and rows in bytes.
+constexpr int kMoveTensors = 60;
+struct BeamMove {
+    int n, in_beams, out_beams;
+    const int32_t* parent;               // of the launch's first request
+    const void* src[kMoveTensors];
+    void* dst[kMoveTensors];
+    int64_t src_batch[kMoveTensors], src_beam[kMoveTensors], dst_batch[kMoveTensors], dst_beam[kMoveTensors], row_bytes[kMoveTensors];
+    int first_block[kMoveTensors];
+};
+static_assert(sizeof(BeamMove) <= 4040, "kernel arguments");
+hipError_t launch_beam_move(const BeamMove& t, unsigned blocks, int64_t batch, hipStream_t stream);
+
+struct QuantRows {                       // x, or act(x) up, of either storage type to 8 bits with a scale for each row
+    int groups, dtype, act;
+    int64_t rows, width;
+    ols_matrix x, up;                    // up.dev NULL: x itself
+    int8_t* q;
+    int64_t q_row, q_group;
+    float* scale;
+    int64_t scale_group;
+    int64_t padded;                      // columns written: zeros behind `width`
+};
+hipError_t launch_quantize_rows(const QuantRows& p, hipStream_t stream);
+struct QuantWeight {
+    int groups, dtype;
+    int64_t width, out;
+    ols_matrix w;
+    int8_t* q;
+    int64_t q_row, q_group;
+    float* scale;
+    int64_t scale_group;
+};
+int64_t quantize_weight_workspace_bytes(int groups, int64_t width, int64_t out);
+hipError_t launch_quantize_weight(const QuantWeight& p, void* ws, hipStream_t stream);
+int64_t int8_workspace_bytes(const ols_int8& f);
+hipError_t launch_int8(const ols_int8& f, hipStream_t stream);
+
 }  // namespace ols

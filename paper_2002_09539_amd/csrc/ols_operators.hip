@@ -207,6 +207,78 @@ hipError_t clip_groups(const ClipCall& c, int groups, Pick pick, Launch launch) 
     return hipSuccess;
 }
 
+// ---- distillation, beam search, products in 8 bits --------------------------------------------------------------------------
+
+int check_distill(const char* who, const ols_distill* d) {
+    if (!d) return bad("%s: null descriptor", who);
+    if (d->k < 1 || d->k > OLS_MAX_TEACHER) return bad("%s: k must be in [1, %d], got %d", who, OLS_MAX_TEACHER, (int)d->k);
+    if (!(d->temperature >= 0x1p-20f && d->temperature <= 0x1p20f)) return bad("%s: the temperature must be in [2^-20, 2^20], got %g", who, (double)d->temperature);
+    if (const int rc = check_logprob(who, d->dtype, d->rows, d->vocab, d->logits, d->row_stride, d->targets)) return rc;
+    if (d->rows == 0) return OLS_OK;
+    if (!d->top_value || !d->top_index) return bad("%s: null list", who);
+    if (!d->stats) return bad("%s: null stats", who);
+    if (!aligned(d->top_value, 4) || !aligned(d->top_index, 4) || !aligned(d->loss, 4) || !aligned(d->logprob, 4) || !aligned(d->stats, 4) || !aligned(d->d_loss, 4) ||
+        !aligned(d->d_logprob, 4))
+        return bad("%s: a pointer is not aligned to its type", who);
+    if (d->d_logits) {
+        if (!element_aligned(d->d_logits, d->dtype)) return bad("%s: the gradient is not aligned to its type", who);
+        if (!stride_ok(d->d_stride, d->vocab)) return bad("%s: rows of %lld gradients cannot be %lld elements apart", who, (long long)d->vocab, (long long)d->d_stride);
+        if (d->d_logits == d->logits && d->d_stride != d->row_stride) return bad("%s: a gradient in place needs the logits' row stride", who);
+    }
+    return OLS_OK;
+}
+DistillParams distill_params(const ols_distill& d) {
+    DistillParams p = {};
+    p.dtype = d.dtype, p.k = d.k, p.rest = d.rest != 0, p.temperature = d.temperature, p.rows = d.rows, p.vocab = d.vocab, p.logits = d.logits, p.row_stride = d.row_stride;
+    p.value = d.top_value, p.index = d.top_index, p.targets = d.targets, p.loss = d.loss, p.logprob = d.logprob, p.stats = d.stats;
+    p.g_loss = d.d_loss, p.g_logprob = d.d_logprob, p.d_logits = d.d_logits, p.d_stride = d.d_stride;
+    return p;
+}
+
+int check_beam(const char* who, int64_t batch, int in_beams, int beams, int64_t vocab, int dtype) {
+    if (!is_dtype(dtype)) return bad("%s: unknown type %d", who, dtype);
+    if (batch < 0 || batch > 65535) return bad("%s: batch must be in [0, 65535], got %lld", who, (long long)batch);
+    if (in_beams < 1 || in_beams > OLS_MAX_TOP || beams < 1 || beams > OLS_MAX_TOP)
+        return bad("%s: hypotheses must be in [1, %d], got %d and %d", who, OLS_MAX_TOP, in_beams, beams);
+    if (vocab < 1 || vocab > kMaxVocab) return bad("%s: vocab must be in [1, 2^24], got %lld", who, (long long)vocab);
+    return OLS_OK;
+}
+
+// Rows [batch][beams] of `bytes`, as far as they reach; at least one row.
+int64_t extent(int64_t batch, int64_t batch_stride, int64_t beams, int64_t beam_stride, int64_t bytes) { return (batch - 1) * batch_stride + (beams - 1) * beam_stride + bytes; }
+
+constexpr int64_t kMaxInt8Width = (1 << 17) - 1;      // of whole sums in 32 bits: 2^17 - 1 products of at most 2^14
+
+int check_int8_matrix(const char* who, const char* name, const void* q, int64_t row, int64_t group, int64_t rows, int64_t cols, int groups, bool written) {
+    if (!q) return bad("%s: %s is null", who, name);
+    if (!stride_ok(row, cols)) return bad("%s: rows of %s, of %lld elements, cannot be %lld apart", who, name, (long long)cols, (long long)row);
+    if (!group_ok(group)) return bad("%s: the workers' stride of %s is out of range", who, name);
+    if (written && !groups_apart(groups, group, rows, row, cols)) return bad("%s: the workers' %s overlap", who, name);
+    return OLS_OK;
+}
+int check_scale(const char* who, const float* scale, int64_t group, int64_t n, int groups, bool written) {
+    if (!scale || !aligned(scale, 4)) return bad("%s: scales are null or not aligned to their type", who);
+    if (!group_ok(group) || (written && groups > 1 && group < n)) return bad("%s: the workers' scales overlap or are out of range", who);
+    return OLS_OK;
+}
+int check_quantize(const char* who, int groups, int64_t rows, int64_t width, int dtype, int act) {
+    if (groups < 1 || groups > kMaxGroups) return bad("%s: groups must be in [1, %d], got %d", who, kMaxGroups, groups);
+    if (!is_dtype(dtype)) return bad("%s: unknown type %d", who, dtype);
+    if (rows < 0 || rows > kMaxTokens) return bad("%s: rows must be in [0, 2^24], got %lld", who, (long long)rows);
+    if (width < 1 || width > kMaxInt8Width) return bad("%s: width must be in [1, 2^17), got %lld", who, (long long)width);
+    if (act < OLS_ACT_SILU || act > OLS_ACT_RELU) return bad("%s: unknown activation %d", who, act);
+    return OLS_OK;
+}
+int check_int8(const char* who, const ols_int8* f) {
+    if (!f) return bad("%s: null descriptor", who);
+    if (const int rc = check_quantize(who, f->groups, f->rows, f->width, f->dtype == OLS_I8 ? OLS_F32 : f->dtype, f->act)) return rc;
+    if (!is_dtype(f->out_dtype)) return bad("%s: unknown type %d of the result", who, (int)f->out_dtype);
+    if (f->out < 1 || f->out > kMaxVocab) return bad("%s: out must be in [1, 2^24], got %lld", who, (long long)f->out);
+    if (f->dtype == OLS_I8 && f->up.dev) return bad("%s: `up` is for rows that the call quantises", who);
+    if ((f->rows + 15) / 16 * ((f->out + 15) / 16) * f->groups >= (1 << 24)) return bad("%s: 2^24 tiles of 16 x 16 results or more", who);
+    return OLS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -398,6 +470,178 @@ int ols_clip_gradients(int n, const void* const* in_dev, void* const* out_dev, c
         e = clip_groups(c, groups, [&](int64_t chunks) { return !out_dev || chunks == 0; },
                         [&](const ClipGroups& t, int k) { return launch_clip_norms(t, k, c.partial, norms_dev, c.stream); });
     return done(e, who);
+}
+
+int64_t ols_distill_workspace_bytes(int64_t rows, int64_t vocab, int dtype) {
+    const char* who = "ols_distill_workspace_bytes";
+    if (const int rc = check_logprob(who, dtype, 0, vocab, nullptr, vocab, nullptr)) return rc;
+    if (rows < 0 || rows > 0x7fffffff) return bad("%s: rows must be in [0, 2^31), got %lld", who, (long long)rows);
+    return distill_workspace_bytes(dtype, rows, vocab);
+}
+
+int ols_distill_loss(const ols_distill* d, void* stream) {
+    const char* who = "ols_distill_loss";
+    if (const int rc = check_distill(who, d)) return rc;
+    if (d->rows == 0) return OLS_OK;
+    if (!d->loss || (d->targets && !d->logprob)) return bad("%s: null result", who);
+    if (const int rc = check_ws(who, d->ws, d->ws_bytes, distill_workspace_bytes(d->dtype, d->rows, d->vocab))) return rc;
+    DistillParams p = distill_params(*d);
+    if (!d->targets) p.logprob = nullptr;
+    return done(launch_distill(p, d->ws, (hipStream_t)stream), who);
+}
+
+int ols_distill_loss_grad(const ols_distill* d, void* stream) {
+    const char* who = "ols_distill_loss_grad";
+    if (const int rc = check_distill(who, d)) return rc;
+    if (d->rows == 0) return OLS_OK;
+    if (!d->d_logits) return bad("%s: null gradient", who);
+    return done(launch_distill_grad(distill_params(*d), (hipStream_t)stream), who);
+}
+
+int64_t ols_beam_workspace_bytes(int64_t batch, int in_beams, int beams, int64_t vocab, int dtype) {
+    if (const int rc = check_beam("ols_beam_workspace_bytes", batch, in_beams, beams, vocab, dtype)) return rc;
+    return beam_workspace_bytes(dtype, batch, in_beams, beams, vocab);
+}
+
+int ols_beam_select(const ols_beam* b, void* stream) {
+    const char* who = "ols_beam_select";
+    if (!b) return bad("%s: null descriptor", who);
+    if (const int rc = check_beam(who, b->batch, b->in_beams, b->beams, b->vocab, b->dtype)) return rc;
+    if (!(b->length_penalty >= -16.0 && b->length_penalty <= 16.0)) return bad("%s: the length penalty must be in [-16, 16], got %g", who, b->length_penalty);
+    if (b->length_penalty != 0.0 && !b->length) return bad("%s: a length penalty needs the lengths", who);
+    if (b->new_length && !b->length) return bad("%s: new lengths need the lengths", who);
+    if (b->batch == 0) return OLS_OK;
+    if (!b->logits || !element_aligned(b->logits, b->dtype)) return bad("%s: logits are null or not aligned to their type", who);
+    if (!group_ok(b->batch_stride) || !group_ok(b->beam_stride)) return bad("%s: a stride of the logits is out of range", who);
+    if (!b->score || !b->new_score || !b->token || !b->parent || !b->new_finished) return bad("%s: null pointer", who);
+    if (!aligned(b->score, 4) || !aligned(b->length, 4) || !aligned(b->new_score, 4) || !aligned(b->token, 4) || !aligned(b->parent, 4) || !aligned(b->new_length, 4))
+        return bad("%s: a pointer is not aligned to its type", who);
+    if (const int rc = check_ws(who, b->ws, b->ws_bytes, beam_workspace_bytes(b->dtype, b->batch, b->in_beams, b->beams, b->vocab))) return rc;
+    BeamParams p = {};
+    p.dtype = b->dtype, p.in_beams = b->in_beams, p.beams = b->beams, p.eos = b->eos, p.batch = b->batch, p.vocab = b->vocab;
+    p.logits = b->logits, p.batch_stride = b->batch_stride, p.beam_stride = b->beam_stride, p.score = b->score, p.finished = b->finished, p.length = b->length;
+    p.penalty = b->length_penalty, p.new_score = b->new_score, p.token = b->token, p.parent = b->parent, p.new_length = b->new_length, p.new_finished = b->new_finished;
+    return done(launch_beam(p, b->ws, (hipStream_t)stream), who);
+}
+
+int ols_beam_reorder(int n, const void* const* src, void* const* dst, const int64_t* row_bytes, const int64_t* src_batch, const int64_t* src_beam,
+                     const int64_t* dst_batch, const int64_t* dst_beam, int64_t batch, int in_beams, int beams, const int32_t* parent, void* stream) {
+    const char* who = "ols_beam_reorder";
+    if (const int rc = check_beam(who, batch, in_beams, beams, 1, OLS_F32)) return rc;
+    if (n < 0 || n > (1 << 20)) return bad("%s: number of tensors must be in [0, 2^20], got %d", who, n);
+    if (n == 0 || batch == 0) return OLS_OK;
+    if (!src || !dst || !row_bytes || !src_batch || !src_beam || !dst_batch || !dst_beam) return bad("%s: null arrays", who);
+    if (!parent || !aligned(parent, 4)) return bad("%s: parents are null or not aligned to their type", who);
+    for (int i = 0; i < n; ++i) {
+        const int64_t bytes = row_bytes[i];
+        if (bytes < 0 || bytes > (int64_t)1 << 35) return bad("%s: rows of tensor %d have %lld bytes", who, i, (long long)bytes);
+        if (bytes == 0) continue;
+        if (!src[i] || !dst[i]) return bad("%s: tensor %d is null", who, i);
+        if (!group_ok(src_batch[i]) || !group_ok(src_beam[i]) || !group_ok(dst_batch[i]) || !group_ok(dst_beam[i])) return bad("%s: a stride of tensor %d is out of range", who, i);
+        if ((beams > 1 && dst_beam[i] < bytes) || !groups_apart((int)batch, dst_batch[i], beams, beams > 1 ? dst_beam[i] : bytes, bytes))
+            return bad("%s: rows of output %d overlap", who, i);
+        if (src[i] == dst[i]) {
+            if (in_beams != beams || (batch > 1 && src_batch[i] != dst_batch[i]) || (beams > 1 && src_beam[i] != dst_beam[i]))
+                return bad("%s: tensor %d in place needs one shape and the same strides", who, i);
+        } else {
+            const char *s = (const char*)src[i], *d = (const char*)dst[i];
+            if (s < d + extent(batch, dst_batch[i], beams, dst_beam[i], bytes) && d < s + extent(batch, src_batch[i], in_beams, src_beam[i], bytes))
+                return bad("%s: output %d lies partly on its input", who, i);
+        }
+    }
+    BeamMove t;
+    t.in_beams = in_beams, t.out_beams = beams, t.n = 0;
+    int64_t blocks = 0;
+    auto launch = [&]() {
+        // a launch has fewer than 2^32 threads
+        const int64_t step = std::max<int64_t>(1, std::min<int64_t>(batch, ((1 << 24) - 1) / std::max<int64_t>(1, blocks)));
+        for (int64_t first = 0; first < batch; first += step) {
+            BeamMove u = t;
+            u.parent = parent + first * beams;
+            for (int i = 0; i < t.n; ++i)
+                u.src[i] = (const char*)t.src[i] + first * t.src_batch[i], u.dst[i] = (char*)t.dst[i] + first * t.dst_batch[i];
+            const hipError_t e = launch_beam_move(u, (unsigned)blocks, std::min(step, batch - first), (hipStream_t)stream);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    };
+    for (int i = 0; i < n; ++i) {
+        if (row_bytes[i] == 0) continue;
+        const int64_t need = (row_bytes[i] + 4095) / 4096;
+        if (t.n == kMoveTensors || (t.n && blocks + need >= (1 << 24))) {
+            if (const hipError_t e = launch()) return done(e, who);
+            t.n = 0, blocks = 0;
+        }
+        const int k = t.n++;
+        t.src[k] = src[i], t.dst[k] = dst[i], t.row_bytes[k] = row_bytes[i], t.first_block[k] = (int)blocks;
+        t.src_batch[k] = src_batch[i], t.src_beam[k] = src_beam[i], t.dst_batch[k] = dst_batch[i], t.dst_beam[k] = dst_beam[i];
+        blocks += need;
+    }
+    return done(t.n ? launch() : hipSuccess, who);
+}
+
+int ols_quantize_rows(int groups, int64_t rows, int64_t width, const ols_matrix* x, const ols_matrix* up, int act, int dtype, int8_t* q, int64_t q_row,
+                      int64_t q_group, float* scale, int64_t scale_group, void* stream) {
+    const char* who = "ols_quantize_rows";
+    if (const int rc = check_quantize(who, groups, rows, width, dtype, act)) return rc;
+    if (rows == 0) return OLS_OK;
+    if (!x) return bad("%s: null x", who);
+    if (const int rc = check_matrix(who, "x", *x, rows, width, dtype, groups, false)) return rc;
+    if (up && up->dev)
+        if (const int rc = check_matrix(who, "up", *up, rows, width, dtype, groups, false)) return rc;
+    if (const int rc = check_int8_matrix(who, "q", q, q_row, q_group, rows, width, groups, true)) return rc;
+    if (const int rc = check_scale(who, scale, scale_group, rows, groups, true)) return rc;
+    QuantRows p = {};
+    p.groups = groups, p.dtype = dtype, p.act = act, p.rows = rows, p.width = width, p.x = *x;
+    if (up) p.up = *up;
+    p.q = q, p.q_row = q_row, p.q_group = q_group, p.scale = scale, p.scale_group = scale_group, p.padded = width;
+    return done(launch_quantize_rows(p, (hipStream_t)stream), who);
+}
+
+int64_t ols_quantize_weight_workspace_bytes(int groups, int64_t width, int64_t out) {
+    const char* who = "ols_quantize_weight_workspace_bytes";
+    if (const int rc = check_quantize(who, groups, 0, width, OLS_F32, OLS_ACT_SILU)) return rc;
+    if (out < 1 || out > kMaxVocab) return bad("%s: out must be in [1, 2^24], got %lld", who, (long long)out);
+    return quantize_weight_workspace_bytes(groups, width, out);
+}
+
+int ols_quantize_weight(int groups, int64_t width, int64_t out, const ols_matrix* w, int dtype, int8_t* q, int64_t q_row, int64_t q_group, float* scale,
+                        int64_t scale_group, void* ws_dev, int64_t ws_bytes, void* stream) {
+    const char* who = "ols_quantize_weight";
+    if (const int rc = check_quantize(who, groups, 0, width, dtype, OLS_ACT_SILU)) return rc;
+    if (out < 1 || out > kMaxVocab) return bad("%s: out must be in [1, 2^24], got %lld", who, (long long)out);
+    if ((out + 63) / 64 * ((width + 63) / 64) * groups >= (1 << 24)) return bad("%s: 2^24 tiles of 64 x 64 weights or more", who);
+    if (!w) return bad("%s: null weights", who);
+    if (const int rc = check_matrix(who, "w", *w, width, out, dtype, groups, false)) return rc;
+    if (const int rc = check_int8_matrix(who, "q", q, q_row, q_group, out, width, groups, true)) return rc;
+    if (const int rc = check_scale(who, scale, scale_group, out, groups, true)) return rc;
+    if (const int rc = check_ws(who, ws_dev, ws_bytes, quantize_weight_workspace_bytes(groups, width, out))) return rc;
+    QuantWeight p = {groups, dtype, width, out, *w, q, q_row, q_group, scale, scale_group};
+    return done(launch_quantize_weight(p, ws_dev, (hipStream_t)stream), who);
+}
+
+int64_t ols_int8_workspace_bytes(const ols_int8* f) {
+    if (const int rc = check_int8("ols_int8_workspace_bytes", f)) return rc;
+    return int8_workspace_bytes(*f);
+}
+
+int ols_int8_matmul(const ols_int8* f, void* stream) {
+    const char* who = "ols_int8_matmul";
+    if (const int rc = check_int8(who, f)) return rc;
+    if (f->rows == 0) return OLS_OK;
+    if (f->dtype == OLS_I8) {
+        if (const int rc = check_int8_matrix(who, "x", f->x.dev, f->x.row, f->x.group, f->rows, f->width, f->groups, false)) return rc;
+        if (const int rc = check_scale(who, f->x_scale, f->x_scale_group, f->rows, f->groups, false)) return rc;
+    } else {
+        if (const int rc = check_matrix(who, "x", f->x, f->rows, f->width, f->dtype, f->groups, false)) return rc;
+        if (f->up.dev)
+            if (const int rc = check_matrix(who, "up", f->up, f->rows, f->width, f->dtype, f->groups, false)) return rc;
+    }
+    if (const int rc = check_int8_matrix(who, "w", f->w.dev, f->w.row, f->w.group, f->out, f->width, f->groups, false)) return rc;
+    if (const int rc = check_scale(who, f->w_scale, f->w_scale_group, f->out, f->groups, false)) return rc;
+    if (const int rc = check_matrix(who, "y", f->y, f->rows, f->out, f->out_dtype, f->groups, true)) return rc;
+    if (const int rc = check_ws(who, f->ws, f->ws_bytes, int8_workspace_bytes(*f))) return rc;
+    return done(launch_int8(*f, (hipStream_t)stream), who);
 }
 
 }  // extern "C"

@@ -1,4 +1,5 @@
-"""Operators of token models on torch tensors: embedding lookup, gated feed-forward block, log probabilities, clipping.
+"""Operators of token models on torch tensors: embedding lookup, gated feed-forward block, log probabilities, clipping, distillation,
+beam search, products in 8-bit integers.
 
 Each function checks its tensors, allocates its results and workspace, and enqueues libols kernels on torch's current
 stream of the tensors' device (see the section of the same name in include/ols.h).  Nothing synchronises and nothing is
@@ -170,7 +171,7 @@ def _saved(t):
     return (t.data_ptr() if t.numel() else None), t.numel()
 
 
-_SHARED = ("x", "w_gate", "w_up", "w_down", "dy")    # inputs that may come without a worker axis
+_SHARED = ("x", "w_gate", "w_up", "w_down", "dy", "up", "weight")    # inputs that may come without a worker axis
 
 
 def _ffn(x, w_gate, w_up, w_down, act, others):
@@ -417,3 +418,283 @@ def clip_grad_norm(grads, max_norm, groups=None, out=None):
     grads: contiguous tensors of one type; groups[i]: the number of tensor i's group (one group by default).  What is written must not
     overlap: a gradient that several parameters share is given once."""
     return _clip(grads, max_norm, groups, out)
+
+
+# ---- distillation -------------------------------------------------------------------------------------------------
+DistillLoss = namedtuple("DistillLoss", "loss logprob stats")
+
+
+def _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperature, rest, d_logits):
+    device = _on_gpu(logits, top_value, top_index, targets, d_loss, d_logprob, d_logits)
+    z, rows, stride = _logit_rows(logits, "logits")
+    shape = logits.shape[:-1]
+    if top_value.dim() < 1 or tuple(top_value.shape[:-1]) != tuple(shape):
+        _refuse("lists of shape %s for logits of shape %s", tuple(top_value.shape), tuple(logits.shape))
+    d = B.ols_distill()
+    d.dtype, d.k, d.rest, d.temperature = _dtype(logits, "logits"), top_value.shape[-1], int(rest), float(temperature)
+    d.rows, d.vocab, d.logits, d.row_stride = rows, logits.shape[-1], z.data_ptr(), stride
+    if targets is None and d_logprob is not None:
+        _refuse("a gradient of log probabilities needs the targets")
+    keep = (_per_row(top_value, top_value.shape, torch.float32, "top_value"), _per_row(top_index, top_value.shape, torch.int32, "top_index"),
+            _per_row(targets, shape, torch.int32, "targets"), _per_row(d_loss, shape, torch.float32, "d_loss"),
+            _per_row(d_logprob, shape, torch.float32, "d_logprob"))
+    d.top_value, d.top_index, d.targets, d.d_loss, d.d_logprob = (_ptr(t) for t in keep)
+    if d_logits is not None:
+        if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype:
+            _refuse("the gradient must have the logits' shape and type")
+        d.d_logits, d.d_stride = d_logits.data_ptr(), _logit_rows(d_logits, "out")[2]
+    return d, shape, device, keep
+
+
+def _distill_loss(logits, top_value, top_index, targets, d_loss, d_logprob, temperature, rest, d_logits):
+    d, shape, device, keep = _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperature, rest, d_logits)
+    d.ws_bytes = B.ols_distill_workspace_bytes(d.rows, d.vocab, d.dtype)
+    with _on(device):
+        ws = _workspace(d.ws_bytes, device)
+        loss = torch.empty(shape, dtype=torch.float32, device=device)
+        logprob = None if targets is None else torch.empty(shape, dtype=torch.float32, device=device)
+        stats = torch.empty(*shape, 8, dtype=torch.float32, device=device)
+        d.loss, d.logprob, d.stats, d.ws = loss.data_ptr(), _ptr(logprob), stats.data_ptr(), _ptr(ws)
+        B.ols_distill_loss(d, _stream(device))
+    return DistillLoss(loss, logprob, stats)
+
+
+def distill_loss(logits, top_value, top_index, targets=None, temperature=1.0, rest=False):
+    """temperature^2 KL(teacher || student) per row, of a student's logits[..., vocab] and lists of the teacher's best tokens.
+
+    top_value (fp32) and top_index (int32): logits.shape[:-1] + (k,), k <= 256, as token_logprobs(..., top=k) returns them; an index outside
+    [0, vocab) is no entry.  rest=False: the teacher's distribution is that of the list alone, softmax(top_value / temperature).  rest=True:
+    top_value are log probabilities at this temperature, and what they leave of one stands against what the student leaves outside the
+    list.  targets (int32, optional): tokens whose log probability at temperature 1 is returned too.  Returns DistillLoss: loss and logprob of
+    shape logits.shape[:-1] (logprob None without targets), and stats for distill_loss_grad."""
+    return _distill_loss(logits, top_value, top_index, targets, None, None, temperature, rest, None)
+
+
+def distill_loss_with_grad(logits, top_value, top_index, d_loss, targets=None, d_logprob=None, temperature=1.0, rest=False, out=None):
+    """distill_loss and the gradient at the logits of sum(d_loss * loss + d_logprob * logprob), in one call.
+
+    d_loss and d_logprob: fp32 of shape logits.shape[:-1], or None.  The gradient has the logits' type; out may be the logits themselves.
+    The teacher has none.  Returns (DistillLoss, gradient)."""
+    if out is None:
+        _on_gpu(logits)
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    return _distill_loss(logits, top_value, top_index, targets, d_loss, d_logprob, temperature, rest, out), out
+
+
+def distill_loss_grad(logits, top_value, top_index, result, d_loss, targets=None, d_logprob=None, temperature=1.0, rest=False, out=None):
+    """The same gradient from an earlier call's DistillLoss (of the same lists, targets, temperature and rest), for upstream gradients that
+    were not known then."""
+    if (targets is None) != (result.logprob is None):
+        _refuse("targets must be those of the earlier call")
+    if out is None:
+        _on_gpu(logits)
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    d, shape, device, keep = _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperature, rest, out)
+    _on_gpu(logits, result.stats)
+    stats = _per_row(result.stats, (*shape, 8), torch.float32, "stats")
+    d.stats = stats.data_ptr()
+    with _on(device):
+        B.ols_distill_loss_grad(d, _stream(device))
+    return out
+
+
+# ---- beam search --------------------------------------------------------------------------------------------------
+Beams = namedtuple("Beams", "score token parent finished length")
+
+
+def beam_select(logits, score, beams=None, finished=None, length=None, eos=-1, length_penalty=0.0):
+    """The best `beams` continuations (as many as there are hypotheses by default) of each request, best first.
+
+    logits: [batch, hypotheses, vocab], the elements of a row contiguous; score: fp32 [batch, hypotheses], the sums of log probabilities so far,
+    -inf for no hypothesis.  finished (bool) and length (int32), both [batch, hypotheses] and optional: a hypothesis that has ended stays in the
+    race as it is; candidates are compared by score / length ** length_penalty.  At most 32 hypotheses; ties go to the lower hypothesis,
+    then to the lower token.  Returns Beams of shape [batch, beams]: score, token (eos behind an ended hypothesis, -1 in places without a
+    candidate), parent (the hypothesis continued, for beam_reorder), finished, and length (None without lengths)."""
+    device = _on_gpu(logits, score, finished, length)
+    if logits.dim() != 3:
+        _refuse("logits are [batch, hypotheses, vocab], got %d axes", logits.dim())
+    batch, have, vocab = logits.shape
+    if vocab > 1 and logits.stride(2) != 1:
+        _refuse("logits: the elements of a row must be contiguous")
+    b = B.ols_beam()
+    b.dtype, b.in_beams, b.beams, b.eos = _dtype(logits, "logits"), have, have if beams is None else int(beams), int(eos)
+    b.batch, b.vocab, b.logits, b.batch_stride, b.beam_stride = batch, vocab, logits.data_ptr(), logits.stride(0), logits.stride(1)
+    keep = (_per_row(score, (batch, have), torch.float32, "score"), _per_row(finished, (batch, have), torch.bool, "finished"),
+            _per_row(length, (batch, have), torch.int32, "length"))
+    b.score, b.finished, b.length = (_ptr(t) for t in keep)
+    b.length_penalty = float(length_penalty)
+    b.ws_bytes = B.ols_beam_workspace_bytes(batch, have, b.beams, vocab, b.dtype)
+    with _on(device):
+        ws = _workspace(b.ws_bytes, device)
+        new_score = torch.empty(batch, b.beams, dtype=torch.float32, device=device)
+        whole = torch.empty(2 if length is None else 3, batch, b.beams, dtype=torch.int32, device=device).unbind(0)
+        ended = torch.empty(batch, b.beams, dtype=torch.bool, device=device)
+        new_length = None if length is None else whole[2]
+        b.new_score, b.token, b.parent, b.new_length, b.new_finished, b.ws = (new_score.data_ptr(), whole[0].data_ptr(), whole[1].data_ptr(), _ptr(new_length),
+                                                                             ended.data_ptr(), _ptr(ws))
+        B.ols_beam_select(b, _stream(device))
+    return Beams(new_score, whole[0], whole[1], ended, new_length)
+
+
+def _state_rows(t, name):
+    """(bytes of a row, bytes between requests, bytes between hypotheses) of a state [batch, hypotheses, ...]."""
+    if t.dim() < 2:
+        _refuse("%s must be [batch, hypotheses, ...], got %d axes", name, t.dim())
+    n, size = 1, t.element_size()
+    for i in range(t.dim() - 1, 1, -1):
+        if t.shape[i] != 1 and t.stride(i) != n:
+            _refuse("%s: what one hypothesis holds must be contiguous", name)
+        n *= t.shape[i]
+    return n * size, t.stride(0) * size, t.stride(1) * size
+
+
+def beam_reorder(states, parent, out=None):
+    """Moves hypotheses' states behind a step: state[b, i] = old state[b, parent[b, i]] for every tensor of `states`; returns the list written.
+
+    states: tensors [batch, hypotheses, ...] of any types, what one hypothesis holds contiguous (a slice of the positions used so far is, where they
+    are the first of these axes).  parent: int32 [batch, beams] (Beams.parent); one outside the hypotheses leaves its place as it was.
+    Without `out` the tensors are written in place, and hypotheses that stay are not touched; `out` holds other tensors of shape
+    [batch, beams, ...], which must not overlap the states or each other."""
+    states = list(states)
+    if not states:
+        return []
+    if parent.dtype != torch.int32 or parent.dim() != 2:
+        _refuse("parent must be int32 [batch, beams], got %s of shape %s", parent.dtype, tuple(parent.shape))
+    outs = states if out is None else list(out)
+    if len(outs) != len(states):
+        _refuse("%d outputs for %d states", len(outs), len(states))
+    device = _on_gpu(parent, *states, *(() if out is None else outs))
+    batch, beams = parent.shape
+    have = states[0].shape[1] if states[0].dim() > 1 else 0
+    row_bytes, strides = array("q"), [array("q") for _ in range(4)]
+    for i, (s, o) in enumerate(zip(states, outs)):
+        n, sb, sh = _state_rows(s, "state %d" % i)
+        if tuple(s.shape[:2]) != (batch, have):
+            _refuse("state %d is of shape %s, for %d requests of %d hypotheses", i, tuple(s.shape), batch, have)
+        ob, oh = sb, sh
+        if o is not s:
+            if o.dtype != s.dtype or tuple(o.shape) != (batch, beams, *s.shape[2:]):
+                _refuse("out %d must be %s of shape %s", i, s.dtype, (batch, beams, *s.shape[2:]))
+            _, ob, oh = _state_rows(o, "out %d" % i)
+        elif have != beams:
+            _refuse("in place, %d hypotheses cannot become %d", have, beams)
+        row_bytes.append(n)
+        for a, v in zip(strides, (sb, sh, ob, oh)):
+            a.append(v)
+    src, dst = array("Q", [t.data_ptr() for t in states]), array("Q", [t.data_ptr() for t in outs])
+    if not _distinct(dst, row_bytes):
+        _refuse("a state cannot be written twice in one call")
+    if out is not None:
+        read = {p: i for i, (p, n) in enumerate(zip(src, row_bytes)) if n}
+        if any(n and read.get(p, i) != i for i, (p, n) in enumerate(zip(dst, row_bytes))):
+            _refuse("an output is another state of the call")
+    parent = parent.contiguous()
+    at = lambda a: a.buffer_info()[0]  # noqa: E731
+    with _on(device):
+        B.ols_beam_reorder(len(states), at(src), at(dst), at(row_bytes), *(at(a) for a in strides), batch, have, beams, parent.data_ptr(), _stream(device))
+    return outs
+
+
+# ---- products in 8-bit integers -----------------------------------------------------------------------------------
+Int8Rows = namedtuple("Int8Rows", "q scale")
+Int8Weight = namedtuple("Int8Weight", "q scale")
+
+
+def _padded(n):
+    return -(-n // 16) * 16          # rows that begin on 16 bytes
+
+
+def _scale(t, m, n, name):
+    """Address and workers' stride of fp32 scales [n] or [m][n]."""
+    if t.dtype != torch.float32 or tuple(t.shape) not in ((n,), (m, n)) or not t.is_contiguous():
+        _refuse("%s must be contiguous float32 of shape %s, got %s of shape %s", name, (m, n), t.dtype, tuple(t.shape))
+    return t.data_ptr(), (n if t.dim() == 2 and m > 1 else 0)
+
+
+def _act_code(act):
+    if act not in _ACT:
+        _refuse("unknown activation %r: one of %s", act, ", ".join(_ACT))
+    return _ACT[act]
+
+
+def quantize_rows(x, up=None, act="silu"):
+    """Rows of x, or of act(x) * up, in 8 bits: q = x / scale to the nearest whole number, scale = max |row| / 127.
+
+    x, up: fp32 or bf16 [rows, width] or [m, rows, width].  Returns Int8Rows(q, scale) for int8_matmul: q int8 of x's shape, scale fp32 of
+    x.shape[:-1].  A row with a NaN or an infinity has q 0 and a scale of NaN."""
+    device = _on_gpu(x, up)
+    if x.dim() not in (2, 3):
+        _refuse("x is [rows, width] or [m, rows, width], got %d axes", x.dim())
+    m, (rows, width) = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2:]
+    if up is not None and (up.shape != x.shape or up.dtype != x.dtype):
+        _refuse("up must be of x's shape and type")
+    mx, mu = _matrix(x, m, (rows, width), "x"), None if up is None else _matrix(up, m, (rows, width), "up")
+    with _on(device):
+        pitch = _padded(width)
+        q = torch.empty(*x.shape[:-1], pitch, dtype=torch.int8, device=device)[..., :width]
+        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
+        B.ols_quantize_rows(m, rows, width, mx, mu, _act_code(act), _dtype(x, "x"), q.data_ptr(), pitch, rows * pitch, scale.data_ptr(), rows, _stream(device))
+    return Int8Rows(q, scale)
+
+
+def quantize_weight(w):
+    """A weight [width, out] or [m, width, out] in 8 bits with a scale for each column, laid out once for int8_matmul.
+
+    Returns Int8Weight(q, scale): q int8 [out, width] or [m, out, width], scale fp32 [out] or [m, out]."""
+    device = _on_gpu(w)
+    if w.dim() not in (2, 3):
+        _refuse("a weight is [width, out] or [m, width, out], got %d axes", w.dim())
+    m, (width, out) = (w.shape[0] if w.dim() == 3 else 1), w.shape[-2:]
+    mw = _matrix(w, m, (width, out), "weight")
+    nbytes = B.ols_quantize_weight_workspace_bytes(m, width, out)
+    with _on(device):
+        ws = _workspace(nbytes, device)
+        pitch = _padded(width)
+        q = torch.empty(*w.shape[:-2], out, pitch, dtype=torch.int8, device=device)[..., :width]
+        scale = torch.empty(*w.shape[:-2], out, dtype=torch.float32, device=device)
+        B.ols_quantize_weight(m, width, out, mw, _dtype(w, "a weight"), q.data_ptr(), pitch, out * pitch, scale.data_ptr(), out, _ptr(ws), nbytes, _stream(device))
+    return Int8Weight(q, scale)
+
+
+def int8_matmul(x, weight, up=None, act="silu", out=None, dtype=None):
+    """y = x w in 8-bit integers: rows of x with a scale each, channels of w with a scale each, exact integer sums.
+
+    x: fp32 or bf16 [rows, width] or [m, rows, width], quantised on the way, or what quantize_rows returned.  With `up` (of x's shape and type)
+    the product is that of act(x) * up: the second one of a gated block, for a = x and b = up.  weight: Int8Weight, from quantize_weight or of any int8
+    q [out, width] or [m, out, width], whose rows are best 16 bytes apart.  y is [rows, out], with the workers' axis if anything has one, of
+    `dtype` (x's by default, bfloat16 for Int8Rows) or in `out`.  width < 2^17."""
+    given = isinstance(x, Int8Rows)
+    xq, (wq, w_scale) = (x.q if given else x), weight
+    device = _on_gpu(xq, wq, w_scale, up, out, *((x.scale,) if given else ()))
+    if wq.dtype != torch.int8 or (given and xq.dtype != torch.int8):
+        _refuse("quantised tensors must be int8")
+    if xq.dim() not in (2, 3) or wq.dim() not in (2, 3):
+        _refuse("x is [rows, width] or [m, rows, width], a quantised weight [out, width] or [m, out, width]")
+    workers = xq.dim() == 3 or wq.dim() == 3
+    m = xq.shape[0] if xq.dim() == 3 else wq.shape[0] if workers else 1
+    rows, width, channels = xq.shape[-2], xq.shape[-1], wq.shape[-2]
+    f = B.ols_int8()
+    f.groups, f.act, f.rows, f.width, f.out = m, _act_code(act), rows, width, channels
+    f.dtype = B.OLS_I8 if given else _dtype(xq, "x")
+    dtype = dtype or (out.dtype if out is not None else torch.bfloat16 if given else xq.dtype)
+    f.out_dtype = _dtype(dtype, "dtype")
+    f.x, f.w = _matrix(xq, m, (rows, width), "x"), _matrix(wq, m, (channels, width), "weight")
+    if up is not None:
+        if given or up.dtype != xq.dtype:
+            _refuse("up must be of x's type, which is not quantised yet")
+        f.up = _matrix(up, m, (rows, width), "up")
+    if given:
+        f.x_scale, f.x_scale_group = _scale(x.scale, m, rows, "the rows' scales")
+    f.w_scale, f.w_scale_group = _scale(w_scale, m, channels, "the channels' scales")
+    shape = ((m,) if workers else ()) + (rows, channels)
+    with _on(device):
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=device)
+        elif tuple(out.shape) != shape or out.dtype != dtype:
+            _refuse("out must be %s of shape %s", dtype, shape)
+        f.y = _matrix(out, m, (rows, channels), "out")
+        f.ws_bytes = B.ols_int8_workspace_bytes(f)
+        ws = _workspace(f.ws_bytes, device)
+        f.ws = _ptr(ws)
+        B.ols_int8_matmul(f, _stream(device))
+    return out

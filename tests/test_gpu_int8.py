@@ -1,0 +1,268 @@
+"""Products in 8-bit integers and their quantisers, against exact sums.
+
+Quantised values have to be equal: a scale is one rounding of a quotient, a value the nearest whole number to an exact quotient.  A result
+is the exact sum converted to fp32 and multiplied by two scales: three roundings of 2^-24, plus the storage's 2^-8 in bf16."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2002_09539_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _ops():
+    from paper_2002_09539_amd import operators
+    return operators
+
+
+def rows_want(x):
+    """(q, scale) of fp64-held rows [..., width], by the definition: round() of the exact quotient, halves to even."""
+    top = x.abs().amax(-1)
+    bad = ~torch.isfinite(x).all(-1)
+    scale = (top / 127).float()
+    s = torch.where(bad | (scale == 0), 1.0, scale.double())[..., None]
+    q = torch.round(x / s).clamp(-127, 127)
+    q = torch.where((bad | (scale == 0))[..., None], 0.0, q)
+    return q.to(torch.int8), torch.where(bad, math.nan, scale)
+
+
+def product_want(q, s, wq, ws):
+    acc = torch.matmul(q.double(), wq.double().transpose(-1, -2))          # below 2^53: exact
+    return acc * s.double()[..., None] * ws.double()[..., None, :]
+
+
+def near(y, want):
+    got = y.double().cpu()
+    bad = torch.isnan(want)
+    assert torch.equal(torch.isnan(got), bad)
+    room = want.abs() * (3 * 2.0 ** -24 + (2.0 ** -8 if y.dtype == BF16 else 0.0)) * (1 + 2.0 ** -7) + 1e-38
+    assert bool(((got - want).abs() <= room)[~bad].all()), float(((got - want).abs() / (want.abs() + 1e-30))[~bad].max())
+
+
+def normal(seed, *shape, std=1.0, dtype=F32):
+    return (torch.randn(*shape, generator=torch.Generator().manual_seed(seed)) * std).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width", [(1, 1), (3, 7), (5, 8), (2, 127), (9, 130), (4, 2048), (2, 8195), (1, 131071)])
+def test_rows(rows, width, dtype):
+    x = normal(rows * width, rows, width, dtype=dtype)
+    r = _ops().quantize_rows(x.cuda())
+    q, s = rows_want(x.double())
+    assert torch.equal(r.scale.cpu(), s) and torch.equal(r.q.cpu(), q) and r.q.shape == x.shape and r.q.dtype == torch.int8
+
+
+def test_rows_on_the_border_and_beyond():
+    """Halves go to even; tiny, huge, empty and unbounded rows."""
+    x = torch.zeros(12, 300)
+    x[0, :255] = torch.arange(-127, 128).float()                            # a scale of one
+    x[1, :254] = torch.arange(-127, 127).float() + 0.5
+    x[1, 254] = 127.0                                                       # halves, to even
+    x[2] = 0.0
+    x[3] = normal(1, 300) * 1e-41                                           # below the normal numbers
+    x[4] = normal(2, 300) * 1e-36
+    x[5] = normal(3, 300) * 1e37
+    x[6, 5] = math.nan
+    x[7, 299] = math.inf
+    x[8, 0] = -math.inf
+    x[9, 3] = 1e-45
+    x[10] = -0.0
+    x[11] = torch.finfo(F32).max
+    r = _ops().quantize_rows(x.cuda())
+    q, s = rows_want(x.double())
+    same = torch.tensor([0, 1, 2, 4, 5, 6, 7, 8, 9, 10, 11])
+    assert torch.equal(torch.isnan(r.scale.cpu()), torch.isnan(s)) and torch.equal(r.scale.cpu()[~torch.isnan(s)], s[~torch.isnan(s)])
+    assert torch.equal(r.q.cpu()[same], q[same]) and torch.equal(r.q.cpu()[3], q[3])
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_rows_of_close_quotients(seed):
+    """Values within a few units in the last place of the borders between two numbers."""
+    g = torch.Generator().manual_seed(seed)
+    top = torch.rand(64, 1, generator=g) * 3 + 0.1
+    scale = (top.double() / 127).float()
+    k = torch.randint(-126, 126, (64, 500), generator=g).double() + 0.5
+    x = (k * scale.double()).float()
+    for _ in range(2):
+        x = torch.where(torch.rand(64, 500, generator=g) < 0.5, torch.nextafter(x, torch.tensor(math.inf)), torch.nextafter(x, torch.tensor(-math.inf)))
+    x = torch.cat([x, top], 1)
+    r = _ops().quantize_rows(x.cuda())
+    q, s = rows_want(x.double())
+    assert torch.equal(r.scale.cpu(), s) and torch.equal(r.q.cpu(), q)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gated_rows(dtype, act):
+    """act(x) up is good to a few 2^-24, so a value may fall to the other side of a border that it is that near."""
+    x, up = normal(1, 3, 9, 333, dtype=dtype), normal(2, 3, 9, 333, dtype=dtype)
+    r = _ops().quantize_rows(x.cuda(), up.cuda(), act)
+    a = x.double()
+    f = a * torch.sigmoid(a) if act == "silu" else 0.5 * a * (1 + torch.erf(a / math.sqrt(2))) if act == "gelu" else a.clamp(min=0)
+    h = f * up.double()
+    s = h.abs().amax(-1) / 127
+    assert bool(((r.scale.cpu().double() / s - 1).abs() <= 1e-6).all())
+    assert bool(((r.q.cpu().double() - h / s[..., None]).abs() <= 0.5 + 127 * 2e-6).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,width,out", [(None, 1, 1), (None, 70, 3), (2, 129, 65), (3, 515, 200), (None, 2048, 96)])
+def test_weights(m, width, out, dtype):
+    lead = () if m is None else (m,)
+    w = normal(width, *lead, width, out, dtype=dtype)
+    w[..., 0, out // 2] = 0.0
+    if out > 2:
+        w[..., :, 1] = 0.0
+        w[..., width // 2, 2] = math.nan
+    r = _ops().quantize_weight(w.cuda())
+    q, s = rows_want(w.double().transpose(-1, -2))
+    assert torch.equal(torch.isnan(r.scale.cpu()), torch.isnan(s)) and torch.equal(r.scale.cpu().nan_to_num(), s.nan_to_num())
+    assert torch.equal(r.q.cpu(), q) and r.q.shape == (*lead, out, width)
+
+
+SIZES = [(1, 1, 1), (1, 64, 16), (1, 2048, 300), (2, 100, 17), (3, 4100, 33), (5, 16, 129), (8, 520, 64), (13, 77, 5), (16, 256, 256), (17, 333, 100), (31, 1024, 48), (33, 129, 257),
+         (64, 640, 130), (65, 96, 64), (100, 1000, 70), (129, 65, 300), (200, 517, 131), (256, 256, 512), (300, 2050, 260), (513, 384, 515), (1000, 144, 24)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width,out", SIZES)
+def test_products(rows, width, out, dtype):
+    ops = _ops()
+    x, w = normal(rows + width, rows, width, dtype=dtype), normal(out + width, width, out, std=width ** -0.5, dtype=dtype)
+    wq = ops.quantize_weight(w.cuda())
+    q, s = rows_want(x.double())
+    want = product_want(q, s, wq.q.cpu(), wq.scale.cpu())
+    y = ops.int8_matmul(x.cuda(), wq)
+    assert y.dtype == dtype and y.shape == (rows, out)
+    near(y, want)
+    given = ops.int8_matmul(ops.quantize_rows(x.cuda()), wq, dtype=F32)
+    near(given, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,rows,width,out", [(2, 1, 200, 50), (3, 20, 130, 70), (3, 201, 517, 131), (2, 300, 1024, 520), (5, 65, 64, 33)])
+def test_workers(m, rows, width, out, dtype):
+    ops = _ops()
+    x, w = normal(m, m, rows, width, dtype=dtype), normal(m + 1, m, width, out, std=0.05, dtype=dtype)
+    wq = ops.quantize_weight(w.cuda())
+    q, s = rows_want(x.double())
+    near(ops.int8_matmul(x.cuda(), wq), product_want(q, s, wq.q.cpu(), wq.scale.cpu()))
+    shared = ops.Int8Weight(wq.q[0], wq.scale[0])                             # one weight for all workers
+    near(ops.int8_matmul(x.cuda(), shared), product_want(q, s, wq.q[:1].cpu(), wq.scale[:1].cpu()))
+    near(ops.int8_matmul(x[0].cuda(), wq), product_want(q[:1], s[:1], wq.q.cpu(), wq.scale.cpu()))         # one input for all
+    r = ops.quantize_rows(x.cuda())
+    near(ops.int8_matmul(r, wq, dtype=F32), product_want(q, s, wq.q.cpu(), wq.scale.cpu()))
+    near(ops.int8_matmul(ops.Int8Rows(r.q[0], r.scale[0]), wq, dtype=dtype), product_want(q[:1], s[:1], wq.q.cpu(), wq.scale.cpu()))
+
+
+@pytest.mark.parametrize("rows,width,out", [(1, 130, 40), (4, 2816, 96), (64, 640, 200), (300, 400, 256)])
+def test_gated_products_are_those_of_their_rows(rows, width, out):
+    ops = _ops()
+    x, up, w = normal(1, rows, width, dtype=BF16).cuda(), normal(2, rows, width, dtype=BF16).cuda(), normal(3, width, out, std=0.05).cuda()
+    wq = ops.quantize_weight(w)
+    for act in ("silu", "gelu", "relu"):
+        y = ops.int8_matmul(x, wq, up=up, act=act, dtype=F32)
+        r = ops.quantize_rows(x, up, act)
+        near(y, product_want(r.q.cpu(), r.scale.cpu(), wq.q.cpu(), wq.scale.cpu()))
+
+
+@pytest.mark.parametrize("rows", [1, 7, 40, 150, 300])
+def test_whole_range_of_values_and_long_sums(rows):
+    """Weights of -128 to 127 that were made elsewhere, the longest sums, rows of zeros and rows that are not finite."""
+    ops = _ops()
+    width = 131071 if rows <= 7 else 4112
+    g = torch.Generator().manual_seed(rows)
+    wq = torch.randint(-128, 128, (20, width), generator=g).to(torch.int8)
+    wq[3] = -128
+    xq = torch.randint(-128, 128, (rows, width), generator=g).to(torch.int8)
+    xq[0] = -128
+    s, ws = torch.rand(rows, generator=g), torch.rand(20, generator=g)
+    s[rows // 2] = math.nan if rows > 1 else 1.0
+    want = product_want(xq, s, wq, ws)
+    y = ops.int8_matmul(ops.Int8Rows(xq.cuda(), s.cuda()), ops.Int8Weight(wq.cuda(), ws.cuda()), dtype=F32)
+    near(y, want)
+    x = normal(5, rows, width)
+    x[0] = 0.0
+    if rows > 1:
+        x[1, 3] = math.inf
+    q, sx = rows_want(x.double())
+    near(ops.int8_matmul(x.cuda(), ops.Int8Weight(wq.cuda(), ws.cuda())), product_want(q, sx, wq, ws))
+
+
+@pytest.mark.parametrize("rows", [1, 8, 50, 260])
+def test_strides_and_what_lies_around(rows):
+    ops = _ops()
+    width, out = 200, 150
+    big = normal(1, rows, 300).cuda()
+    wbig = torch.randint(-127, 128, (out, 333), generator=torch.Generator().manual_seed(2), dtype=torch.int32).to(torch.int8).cuda()
+    ws = torch.rand(out).cuda()
+    ybig = torch.full((rows, 400), 5.0, dtype=BF16, device="cuda")
+    x, wq, y = big[:, 51:51 + width], wbig[:, 77:77 + width], ybig[:, 101:101 + out]        # nothing begins on 16 bytes
+    back = ops.int8_matmul(x, ops.Int8Weight(wq, ws), out=y)
+    assert back is y
+    q, s = rows_want(x.cpu().double())
+    near(y, product_want(q, s, wq.cpu(), ws.cpu()))
+    assert bool((ybig[:, :101] == 5).all()) and bool((ybig[:, 101 + out:] == 5).all())
+    qbig = torch.full((rows, 333), 99, dtype=torch.int8, device="cuda")
+    qbig[:, 9:9 + width] = q.cuda()
+    near(ops.int8_matmul(ops.Int8Rows(qbig[:, 9:9 + width], s.cuda()), ops.Int8Weight(wq, ws), dtype=F32), product_want(q, s, wq.cpu(), ws.cpu()))
+
+
+@pytest.mark.parametrize("rows,width,out", [(1, 512, 100), (40, 300, 64), (300, 256, 300)])
+def test_streams_and_capture(rows, width, out):
+    ops = _ops()
+    x, w = normal(1, rows, width, dtype=BF16).cuda(), ops.quantize_weight(normal(2, width, out).cuda())
+    plain = ops.int8_matmul(x, w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = ops.int8_matmul(x, w)
+    side.synchronize()
+    assert torch.equal(other, plain)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = ops.int8_matmul(x, w)
+        z = ops.int8_matmul(y, ops.quantize_weight(torch.zeros(out, 40, device="cuda")))
+    for seed in (4, 5, 6):
+        x.copy_(normal(seed, rows, width, dtype=BF16))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, ops.int8_matmul(x, w)) and bool((z == 0).all())
+
+
+def test_a_gated_block_in_eight_bits():
+    """Quantised against the block in 64 bits: rounding to 1 / 254 of a row's largest value is 1 % of a normal row's spread."""
+    ops = _ops()
+    n, width, hidden, out = 60, 256, 704, 256
+    x, g, u, d = normal(1, n, width), normal(2, width, hidden, std=width ** -0.5), normal(3, width, hidden, std=width ** -0.5), normal(4, hidden, out, std=hidden ** -0.5)
+    gu, down = ops.quantize_weight(torch.cat([g, u], 1).cuda()), ops.quantize_weight(d.cuda())
+    ab = ops.int8_matmul(x.cuda(), gu)
+    y = ops.int8_matmul(ab[:, :hidden], down, up=ab[:, hidden:], act="silu")
+    a, b = x.double() @ g.double(), x.double() @ u.double()
+    want = (a * torch.sigmoid(a) * b) @ d.double()
+    assert float((y.cpu().double() - want).norm() / want.norm()) < 0.05
+    assert np.isfinite(y.cpu().numpy()).all()
+
+
+def test_refusals():
+    ops = _ops()
+    x = normal(1, 4, 32).cuda()
+    w = ops.quantize_weight(normal(2, 32, 8).cuda())
+    for call in (lambda: ops.int8_matmul(x[:, :31], w), lambda: ops.int8_matmul(x.half(), w), lambda: ops.int8_matmul(x, ops.Int8Weight(w.q.int(), w.scale)),
+                 lambda: ops.int8_matmul(x, ops.Int8Weight(w.q, w.scale[:7])), lambda: ops.int8_matmul(x, ops.Int8Weight(w.q, w.scale.double())),
+                 lambda: ops.int8_matmul(x, w, up=x.bfloat16()), lambda: ops.int8_matmul(x, w, up=x[:3]), lambda: ops.int8_matmul(x, w, up=x, act="tanh"),
+                 lambda: ops.int8_matmul(ops.quantize_rows(x), w, up=x), lambda: ops.int8_matmul(x, w, out=torch.empty(4, 9, device="cuda")),
+                 lambda: ops.int8_matmul(x, w, out=torch.empty(4, 8, device="cuda"), dtype=BF16), lambda: ops.int8_matmul(x, w, dtype=torch.float16),
+                 lambda: ops.int8_matmul(x.cpu(), w), lambda: ops.int8_matmul(x.t().contiguous().t(), w), lambda: ops.int8_matmul(x[0], w),
+                 lambda: ops.int8_matmul(torch.zeros(1, 131072, device="cuda"), ops.Int8Weight(torch.zeros(4, 131072, dtype=torch.int8, device="cuda"), torch.ones(4, device="cuda"))),
+                 lambda: ops.quantize_rows(x[0]), lambda: ops.quantize_rows(x, x[:2]), lambda: ops.quantize_rows(x.int()), lambda: ops.quantize_weight(x[0]),
+                 lambda: ops.quantize_weight(x.cpu())):
+        with pytest.raises(B.OlsError):
+            call()
+    assert ops.int8_matmul(x[:0], w).shape == (0, 8) and ops.quantize_rows(x[:0]).q.shape == (0, 32)
