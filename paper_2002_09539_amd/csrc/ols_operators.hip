@@ -275,7 +275,8 @@ int check_int8(const char* who, const ols_int8* f) {
     if (!is_dtype(f->out_dtype)) return bad("%s: unknown type %d of the result", who, (int)f->out_dtype);
     if (f->out < 1 || f->out > kMaxVocab) return bad("%s: out must be in [1, 2^24], got %lld", who, (long long)f->out);
     if (f->dtype == OLS_I8 && f->up.dev) return bad("%s: `up` is for rows that the call quantises", who);
-    if ((f->rows + 15) / 16 * ((f->out + 15) / 16) * f->groups >= (1 << 24)) return bad("%s: 2^24 tiles of 16 x 16 results or more", who);
+    const int64_t tile = f->rows <= 64 ? 16 : 128;        // a launch has fewer than 2^32 threads
+    if ((f->rows + tile - 1) / tile * ((f->out + tile - 1) / tile) * f->groups >= (1 << 23)) return bad("%s: 2^23 tiles of %d x %d results or more", who, (int)tile, (int)tile);
     return OLS_OK;
 }
 

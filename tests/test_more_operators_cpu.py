@@ -109,12 +109,12 @@ def matrix(dev=A, row=64, group=6400):
     return B.ols_matrix(dev, row, group)
 
 
-INT8 = dict(groups=2, dtype=BF16, act=0, out_dtype=F32, rows=5, width=40, out=30, x=matrix(), up=matrix(None), w=matrix(), y=matrix(), x_scale=A, x_scale_group=5,
+INT8 = dict(groups=2, dtype=BF16, act=0, out_dtype=F32, rows=70, width=40, out=30, x=matrix(), up=matrix(None), w=matrix(), y=matrix(), x_scale=A, x_scale_group=70,
             w_scale=A, w_scale_group=30, ws=A, ws_bytes=BIG)
 
 
 @pytest.mark.parametrize("change", [dict(groups=0), dict(groups=4097), dict(dtype=3), dict(out_dtype=2), dict(act=3), dict(rows=-1), dict(rows=2 ** 24 + 1), dict(width=0),
-                                    dict(width=2 ** 17), dict(out=0), dict(out=2 ** 24 + 1), dict(rows=2 ** 20, out=2 ** 13), dict(x=matrix(None)), dict(x=matrix(A + 1)),
+                                    dict(width=2 ** 17), dict(out=0), dict(out=2 ** 24 + 1), dict(rows=2 ** 24, out=2 ** 13, y=matrix(row=2 ** 13)), dict(rows=64, out=2 ** 24), dict(x=matrix(None)), dict(x=matrix(A + 1)),
                                     dict(x=matrix(row=39)), dict(x=matrix(group=-1)), dict(up=matrix(A + 1)), dict(up=matrix(row=39)), dict(w=matrix(None)), dict(w=matrix(row=39)),
                                     dict(w=matrix(group=1 << 41)), dict(w_scale=None), dict(w_scale=A + 2), dict(w_scale_group=-1), dict(y=matrix(None)), dict(y=matrix(A + 2)),
                                     dict(y=matrix(row=29)), dict(y=matrix(group=29)), dict(ws=A + 128), dict(dtype=I8, up=matrix()), dict(dtype=I8, x_scale=None),
@@ -126,7 +126,7 @@ def test_int8_refuses(change):
 def test_int8_workspace():
     f = filled(B.ols_int8, INT8, {})
     need = B.ols_int8_workspace_bytes(f)
-    assert need >= 2 * 5 * 40
+    assert need >= 2 * 70 * 40
     refused(lambda: B.ols_int8_matmul(filled(B.ols_int8, INT8, dict(ws_bytes=need - 1)), None), B.OLS_ENOMEM, str(need))
     assert B.ols_int8_workspace_bytes(filled(B.ols_int8, INT8, dict(rows=0))) == 0
     refused(lambda: B.ols_int8_workspace_bytes(filled(B.ols_int8, INT8, dict(width=0))))
