@@ -14,18 +14,22 @@ namespace ols {
 namespace {
 
 typedef int i4 __attribute__((ext_vector_type(4)));
+using ffn::uniform;
 
 // ---- quantisers -----------------------------------------------------------------------------------------------------------
 
 // A row's scale, and x / scale rounded.  x times the reciprocal can miss the border between two numbers, so the remainder x - q s
-// decides, which is exact in fp32: next to a border it has fewer than 24 bits.  Tiny rows are raised to where the reciprocal exists.
+// decides, which is exact in fp32: next to a border it has fewer than 24 bits.  Eight values whose remainders all stay clear of half a
+// step need no more than that; tiny rows are raised to where the reciprocal exists.
+__device__ __forceinline__ unsigned size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }     // in order of size, then infinities, then NaN
 struct RowScale {
-    float scale, raise, s, inv;
-    __device__ RowScale(float top, bool bad) {
-        scale = bad ? NAN : (float)((double)top / 127.0);
+    float scale, raise, s, inv, clear;
+    __device__ RowScale(unsigned top) {        // size_bits of the row's largest value
+        scale = top >= 0x7f800000u ? NAN : (float)((double)__uint_as_float(top) / 127.0);
         raise = scale < 1e-30f ? 0x1p64f : 1.0f;
         s = scale * raise;
         inv = s > 0.0f ? 1.0f / s : 0.0f;                      // NaN > 0 is false: q is 0
+        clear = raise == 1.0f && s > 0.0f ? 0.5f * s * (1.0f - 0x1p-16f) : 0.0f;
     }
     __device__ int q(float x) const {
         const float v = x * raise;
@@ -42,6 +46,17 @@ struct RowScale {
 __device__ __forceinline__ unsigned pack4(const RowScale& s, float a, float b, float c, float d) {
     return (unsigned)(s.q(a) & 255) | (unsigned)(s.q(b) & 255) << 8 | (unsigned)(s.q(c) & 255) << 16 | (unsigned)(s.q(d) & 255) << 24;
 }
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u2 pack8(const RowScale& s, const float (&v)[8]) {
+    float q[8], far = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = rintf(v[e] * s.inv), far = fmaxf(far, fabsf(fmaf(-q[e], s.s, v[e])));
+    if (!(far < s.clear)) return u2{pack4(s, v[0], v[1], v[2], v[3]), pack4(s, v[4], v[5], v[6], v[7])};
+    u2 w = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e / 4] = __builtin_amdgcn_cvt_pk_u8_f32(q[e] + 128.0f, e % 4, w[e / 4]);
+    return w ^ 0x80808080u;
+}
 
 typedef unsigned u2any __attribute__((ext_vector_type(2), aligned(1)));
 
@@ -57,33 +72,33 @@ __device__ __forceinline__ void values(const QuantRows& p, const T* x, const T* 
     for (int e = 0; e < 8; ++e) v[e] = ffn::act_value<true>(p.act, v[e]) * u[e];
 }
 
+template <int THREADS>
+__device__ __forceinline__ unsigned largest(unsigned top, unsigned* tops) {      // of all threads of a workgroup
+    for (int o = 32; o; o >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
+    if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) top = max(top, tops[w]);
+    return top;
+}
 // The scale of a row, by all threads of a workgroup.
 template <typename T, int THREADS>
-__device__ __forceinline__ RowScale row_scale(const QuantRows& p, const T* x, const T* up, float* tops, int* bads) {
-    float top = 0.0f;
-    bool bad = false;
+__device__ __forceinline__ RowScale row_scale(const QuantRows& p, const T* x, const T* up, unsigned* tops) {
+    unsigned top = 0;
     for (int64_t c = threadIdx.x * 8; c < p.width; c += THREADS * 8) {
         float v[8];
         values<T>(p, x, up, c, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e])), bad |= !(fabsf(v[e]) < INFINITY);
+        for (int e = 0; e < 8; ++e) top = max(top, size_bits(v[e]));
     }
-    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const unsigned long long any = __ballot(bad);
-    __syncthreads();                                           // the places may still be read for the row before
-    if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top, bads[threadIdx.x / 64] = any != 0;
-    __syncthreads();
-    top = 0.0f, bad = false;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, tops[w]), bad |= bads[w] != 0;
-    return RowScale(top, bad);
+    return RowScale(largest<THREADS>(top, tops));
 }
 
-__device__ __forceinline__ void store_packed(int8_t* q, int64_t left, unsigned lo, unsigned hi) {
+__device__ __forceinline__ void store_packed(int8_t* q, int64_t left, u2 w) {
     if (left >= 8) {
-        *(u2any*)q = u2any{lo, hi};
+        *(u2any*)q = w;
     } else {
-        for (int e = 0; e < left; ++e) q[e] = (int8_t)((e < 4 ? lo >> (8 * e) : hi >> (8 * (e - 4))) & 255);
+        for (int e = 0; e < left; ++e) q[e] = (int8_t)(w[e / 4] >> (8 * (e % 4)) & 255);
     }
 }
 
@@ -91,43 +106,34 @@ __device__ __forceinline__ void store_packed(int8_t* q, int64_t left, unsigned l
 // NV = 0: longer rows are read again.
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void quantize_rows_kernel(QuantRows p) {
-    __shared__ float tops[THREADS / 64];
-    __shared__ int bads[THREADS / 64];
+    __shared__ unsigned tops[THREADS / 64];
     const int64_t group = blockIdx.x / p.rows, row = blockIdx.x % p.rows;
     const T* x = (const T*)p.x.dev + group * p.x.group + row * p.x.row;
     const T* up = p.up.dev ? (const T*)p.up.dev + group * p.up.group + row * p.up.row : nullptr;
     int8_t* q = p.q + group * p.q_group + row * p.q_row;
     if constexpr (NV == 0) {
-        const RowScale s = row_scale<T, THREADS>(p, x, up, tops, bads);
+        const RowScale s = row_scale<T, THREADS>(p, x, up, tops);
         if (threadIdx.x == 0) p.scale[group * p.scale_group + row] = s.scale;
         for (int64_t c = threadIdx.x * 8; c < p.padded; c += THREADS * 8) {
             float v[8];
             values<T>(p, x, up, c, v);
-            store_packed(q + c, p.padded - c, pack4(s, v[0], v[1], v[2], v[3]), pack4(s, v[4], v[5], v[6], v[7]));
+            store_packed(q + c, p.padded - c, pack8(s, v));
         }
     } else {
         float v[NV][8];
 #pragma unroll
         for (int j = 0; j < NV; ++j) values<T>(p, x, up, (int64_t)(j * THREADS + threadIdx.x) * 8, v[j]);
-        float top = 0.0f;
-        bool bad = false;
+        unsigned top = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[j][e])), bad |= !(fabsf(v[j][e]) < INFINITY);
-        for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        const unsigned long long any = __ballot(bad);
-        if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top, bads[threadIdx.x / 64] = any != 0;
-        __syncthreads();
-        top = 0.0f, bad = false;
-#pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, tops[w]), bad |= bads[w] != 0;
-        const RowScale s(top, bad);
+            for (int e = 0; e < 8; ++e) top = max(top, size_bits(v[j][e]));
+        const RowScale s(largest<THREADS>(top, tops));
         if (threadIdx.x == 0) p.scale[group * p.scale_group + row] = s.scale;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int64_t c = (int64_t)(j * THREADS + threadIdx.x) * 8;
-            if (c < p.padded) store_packed(q + c, p.padded - c, pack4(s, v[j][0], v[j][1], v[j][2], v[j][3]), pack4(s, v[j][4], v[j][5], v[j][6], v[j][7]));
+            if (c < p.padded) store_packed(q + c, p.padded - c, pack8(s, v[j]));
         }
     }
 }
@@ -138,7 +144,7 @@ void launch_rows_typed(const QuantRows& p, unsigned blocks, hipStream_t stream) 
     if (units <= 64) quantize_rows_kernel<T, 64, 1><<<blocks, 64, 0, stream>>>(p);
     else if (units <= 256) quantize_rows_kernel<T, 256, 1><<<blocks, 256, 0, stream>>>(p);
     else if (units <= 512) quantize_rows_kernel<T, 256, 2><<<blocks, 256, 0, stream>>>(p);
-    else if (units <= 1024) quantize_rows_kernel<T, 512, 2><<<blocks, 512, 0, stream>>>(p);
+    else if (units <= 1024) quantize_rows_kernel<T, 1024, 1><<<blocks, 1024, 0, stream>>>(p);
     else if (units <= 2048) quantize_rows_kernel<T, 1024, 2><<<blocks, 1024, 0, stream>>>(p);
     else quantize_rows_kernel<T, 1024, 0><<<blocks, 1024, 0, stream>>>(p);
 }
@@ -173,7 +179,7 @@ __global__ __launch_bounds__(256) void weight_kernel(QuantWeight p, const float*
     float t = 0.0f;
     if (c < p.out)
         for (int r = 0; r < ranges; ++r) t = fmaxf(t, top[((int64_t)r * gridDim.z + group) * p.out + c]);
-    const RowScale s(t, !(t < INFINITY));
+    const RowScale s(size_bits(t));
     if (c < p.out) {
         if (blockIdx.y == 0 && threadIdx.x < 64) p.scale[group * p.scale_group + c] = s.scale;
         const T* w = (const T*)p.w.dev + group * p.w.group + c;
@@ -215,6 +221,8 @@ __device__ __forceinline__ i4 load_16(const int8_t* row, int64_t k, int64_t widt
     return i4{(int)v[0], (int)v[1], (int)v[2], (int)v[3]};
 }
 
+__device__ __forceinline__ i4 whole_16(const int8_t* at) { return __builtin_bit_cast(i4, (u4)*(const u4bytes*)at); }
+
 template <int N>
 __device__ __forceinline__ void store_scaled(const Product& p, int64_t group, int64_t r, int64_t c, const float (&v)[N]) {   // columns c .. of row r
     const int64_t at = group * p.y_group + r * p.y_row + c;
@@ -231,63 +239,87 @@ __device__ __forceinline__ void store_scaled(const Product& p, int64_t group, in
     }
 }
 
-// Few rows: a workgroup for 16 channels and 16 R rows, whose wavefronts share the contraction, 64 indices at a time in turn; up to kAhead
-// of its turns' weights are under way before anything is waited for.  FUSED: the workgroup quantises the rows itself, into LDS.
+// Few rows: a workgroup for 16 channels and 16 R rows, whose wavefronts share the contraction in ranges; kAhead turns of 64 indices are
+// under way before anything is waited for.  FUSED: the workgroup quantises the one row itself, into LDS,
+// which saves 1.5 us of a launch's 3; of two rows and more it saves nothing.
 constexpr int kAhead = 8;
 template <typename TX, int R, int WAVES, bool FUSED>
 __global__ __launch_bounds__(WAVES * 64) void few_kernel(Product p) {
     extern __shared__ __align__(16) char lds[];
-    __shared__ float scales[16 * R];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t group = blockIdx.z, c0 = (int64_t)blockIdx.x * 16, r0 = (int64_t)blockIdx.y * (16 * R);
-    const int64_t c = min(c0 + lane % 16, p.out - 1);
-    const int8_t* w = p.w + group * p.w_group + c * p.w_row;
-    const int turns = (int)((p.width + 63) / 64);
-    i4 a[kAhead];
+    const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
+    const int64_t group = blockIdx.z, c0 = (int64_t)blockIdx.x * 16;
+    // channels and rows that do not exist are the last one again: what comes of them is not written
+    const int8_t* w = p.w + group * p.w_group + min(c0 + lane % 16, p.out - 1) * p.w_row + 16 * (lane / 16);
+    const int8_t* x[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) x[i] = p.x + group * p.x_group + min((int64_t)16 * i + lane % 16, p.rows - 1) * p.x_row + 16 * (lane / 16);
+    const int turns = (int)(p.width / 64), from = turns * wave / WAVES, to = turns * (wave + 1) / WAVES;      // whole turns: no bounds to look at
+    const int tail = turns * 64;
+    constexpr int AX = kAhead / (2 * R);                           // turns whose rows are under way: registers
+    i4 a[kAhead], b[FUSED ? 1 : AX][R];
     auto request = [&](int first) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int64_t k = ((int64_t)first + j * WAVES + wave) * 64 + 16 * (lane / 16);
-            a[j] = load_16(w, k, p.width, true);
+        for (int j = 0; j < kAhead; ++j)
+            if (first + j < to) a[j] = whole_16(w + (int64_t)(first + j) * 64);
+    };
+    auto request_rows = [&](int first) {
+        if constexpr (!FUSED) {
+#pragma unroll
+            for (int j = 0; j < AX; ++j)
+                if (first + j < to) {
+#pragma unroll
+                    for (int i = 0; i < R; ++i) b[j][i] = whole_16(x[i] + (int64_t)(first + j) * 64);
+                }
         }
     };
-    request(0);
-    const int pitch = (int)((p.width + 63) / 64 * 64) + 16;        // of a row in LDS: rows on different banks
-    if constexpr (FUSED) {
-        const int here = (int)min((int64_t)16 * R, p.rows - r0);
-        __shared__ float tops[WAVES];
-        __shared__ int bads[WAVES];
-        for (int r = 0; r < here; ++r) {
-            const TX* x = (const TX*)p.quant.x.dev + group * p.quant.x.group + (r0 + r) * p.quant.x.row;
-            const TX* up = p.quant.up.dev ? (const TX*)p.quant.up.dev + group * p.quant.up.group + (r0 + r) * p.quant.up.row : nullptr;
-            const RowScale s = row_scale<TX, WAVES * 64>(p.quant, x, up, tops, bads);
-            if (threadIdx.x == 0) scales[r] = s.scale;
-            for (int64_t k = threadIdx.x * 8; k < pitch - 16; k += WAVES * 64 * 8) {
-                float v[8];
-                values<TX>(p.quant, x, up, k, v);
-                *(u2any*)(lds + r * pitch + k) = u2any{pack4(s, v[0], v[1], v[2], v[3]), pack4(s, v[4], v[5], v[6], v[7])};
-            }
+    request(from);
+    i4 a_tail = {};
+    const bool has_tail = wave == WAVES - 1 && p.width % 64 != 0;
+    const int64_t behind = p.width - tail - 16 * (lane / 16);      // of the lane's sixteen bytes of the tail, those that exist
+    if (has_tail) a_tail = load_16(w + tail, 0, behind, true);
+    float scale = 0.0f;
+    if constexpr (FUSED) {                                         // one row
+        __shared__ unsigned tops[WAVES];
+        const TX* row = (const TX*)p.quant.x.dev + group * p.quant.x.group;
+        const TX* up = p.quant.up.dev ? (const TX*)p.quant.up.dev + group * p.quant.up.group : nullptr;
+        const RowScale s = row_scale<TX, WAVES * 64>(p.quant, row, up, tops);
+        scale = s.scale;
+        for (int64_t k = threadIdx.x * 8; k < (p.width + 63) / 64 * 64; k += WAVES * 64 * 8) {
+            float v[8];
+            values<TX>(p.quant, row, up, k, v);
+            *(u2*)(lds + k) = pack8(s, v);
         }
         __syncthreads();
     }
     i4 acc[R] = {};
-    const int8_t* x = p.x + group * p.x_group;
-    for (int first = 0; first < turns; first += kAhead * WAVES) {
-        if (first) request(first);
+    const int row = 16 * (lane / 16);
+    for (int first = from; first < to; first += kAhead) {
+        if (first > from) request(first);
+        if constexpr (FUSED) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int turn = first + j * WAVES + wave;
-            if (turn >= turns) continue;
-            const int64_t k = (int64_t)turn * 64 + 16 * (lane / 16);
+            for (int j = 0; j < kAhead; ++j)
+                if (first + j < to) acc[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[j], *(const i4*)(lds + row + (first + j) * 64), acc[0], 0, 0, 0);
+        } else {
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                // rows that do not exist are the last one again: what comes of them is not written
-                const int64_t r = min(r0 + 16 * i + lane % 16, p.rows - 1);
-                i4 b;
-                if constexpr (FUSED) b = *(const i4*)(lds + (int)(r - r0) * pitch + k);
-                else b = load_16(x + r * p.x_row, k, p.width, true);
-                acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[j], b, acc[i], 0, 0, 0);
+            for (int h = 0; h < kAhead; h += AX) {
+                if (first + h >= to) continue;
+                request_rows(first + h);
+#pragma unroll
+                for (int j = 0; j < AX; ++j)
+                    if (first + h + j < to) {
+#pragma unroll
+                        for (int i = 0; i < R; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[h + j], b[j][i], acc[i], 0, 0, 0);
+                    }
             }
+        }
+    }
+    if (has_tail) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            i4 v;
+            if constexpr (FUSED) v = *(const i4*)(lds + row + tail);
+            else v = load_16(x[i] + tail, 0, behind, true);
+            acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a_tail, v, acc[i], 0, 0, 0);
         }
     }
     i4* sums = (i4*)lds;                                           // [wave][R][lane]
@@ -299,9 +331,9 @@ __global__ __launch_bounds__(WAVES * 64) void few_kernel(Product p) {
         i4 sum = {};
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) sum += sums[(k * R + i) * 64 + lane];
-        const int64_t r = r0 + 16 * i + lane % 16, o = c0 + 4 * (lane / 16);
+        const int64_t r = 16 * i + lane % 16, o = c0 + 4 * (lane / 16);
         if (r >= p.rows || o >= p.out) continue;
-        const float s = FUSED ? scales[r - r0] : p.x_scale[group * p.x_scale_group + r];
+        const float s = FUSED ? scale : p.x_scale[group * p.x_scale_group + r];
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = o + e < p.out ? (float)sum[e] * s * p.w_scale[group * p.w_scale_group + o + e] : 0.0f;
@@ -313,7 +345,6 @@ __global__ __launch_bounds__(WAVES * 64) void few_kernel(Product p) {
 
 constexpr int kSlice = 64;               // indices of a slice: as many bytes as the bf16 tiles' 32
 using ffn::Cursor;
-using ffn::uniform;
 typedef int i16v __attribute__((ext_vector_type(16)));
 
 struct Place {
@@ -341,17 +372,22 @@ __device__ __forceinline__ int tile_of_block(const Product& p, int& range) {
     return p.whole + u % p.rest;
 }
 
-// T x T tiles: 256 with eight wavefronts of 64 x 128, 128 with four of 64 x 64.  The tiles, their ring in LDS and the order of copies,
-// barriers and reads are those of the bf16 products (ffn_gemm.h): sixteen bytes of a lane are sixteen indices here instead of eight.
+// T x T tiles: 256 with eight wavefronts of 64 x 128, 128 with four of 64 x 64, 64 with four of 32 x 32.  The tiles, their ring in LDS and
+// the order of copies, barriers and reads are those of the bf16 products (ffn_gemm.h): sixteen bytes of a lane are sixteen indices here
+// instead of eight.  Tiles of 64 have a ring of eight slices, since few of them run.
 template <int T>
 __global__ __launch_bounds__(ffn::gemm_threads<T>(), 2) void tile_kernel(Product p) {
-    constexpr int THREADS = ffn::gemm_threads<T>(), TM = 2, TN = T / 64;
+    constexpr int THREADS = ffn::gemm_threads<T>(), TM = T == 64 ? 1 : 2, TN = T / 64, D = T == 64 ? 8 : 4;
     using Tile = ffn::TileKC<T, THREADS>;
-    constexpr int kBytes = 2 * Tile::kBytes;
+    constexpr int kBytes = 2 * Tile::kBytes, kMore = D == 8 ? kBytes : 16;
     __shared__ __align__(1024) char buf0[kBytes];
     __shared__ __align__(1024) char buf1[kBytes];
     __shared__ __align__(1024) char buf2[kBytes];
     __shared__ __align__(1024) char buf3[kBytes];
+    __shared__ __align__(1024) char buf4[kMore];
+    __shared__ __align__(1024) char buf5[kMore];
+    __shared__ __align__(1024) char buf6[kMore];
+    __shared__ __align__(1024) char buf7[kMore];
 
     int range;
     const int tile = tile_of_block(p, range);
@@ -409,8 +445,9 @@ __global__ __launch_bounds__(ffn::gemm_threads<T>(), 2) void tile_kernel(Product
 #pragma unroll
             for (int t = 0; t < TN; ++t) acc[i][t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[s & 1][t], fa[s & 1][i], acc[i][t], 0, 0, 0);
     };
-    // Counts as in ffn_gemm.h: four copies a slice and wavefront; copies past the end (windows of no bytes) keep the count the same.
-    static_assert(2 * Tile::kCopies == 4 && ffn::kRing == 4, "the counts below are of four copies a slice");
+    // Counts as in ffn_gemm.h; copies past the end (windows of no bytes) keep the count the same.
+    constexpr int kPerSlice = 2 * Tile::kCopies;
+    static_assert((D - 1) * kPerSlice < 16, "counts of four bits");
     auto barrier = [&]() {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -420,7 +457,7 @@ __global__ __launch_bounds__(ffn::gemm_threads<T>(), 2) void tile_kernel(Product
         fetch(lds, 1);
         multiply(0);
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0078);                   // vmcnt(8) lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt(0x0070 | (D - 2) * kPerSlice);   // vmcnt, lgkmcnt(0): the next slice has landed
         barrier();
         fetch(next, 0);
         multiply(1);
@@ -431,25 +468,37 @@ __global__ __launch_bounds__(ffn::gemm_threads<T>(), 2) void tile_kernel(Product
     copy(buf1);
     copy(buf2);
     copy(buf3);
-    __builtin_amdgcn_s_waitcnt(0x0f7c);                       // vmcnt(12)
+    if constexpr (D == 8) {
+        copy(buf4);
+        copy(buf5);
+        copy(buf6);
+        copy(buf7);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (D - 1) * kPerSlice);       // vmcnt
     barrier();
     fetch(buf0, 0);
-    for (int it = 0; it < end; it += ffn::kRing) {
+    for (int it = 0; it < end; it += D) {
         slice(buf0, buf1);
         if (it + 1 < end) slice(buf1, buf2);
         if (it + 2 < end) slice(buf2, buf3);
-        if (it + 3 < end) slice(buf3, buf0);
+        if (it + 3 < end) slice(buf3, D == 8 ? buf4 : buf0);
+        if constexpr (D == 8) {
+            if (it + 4 < end) slice(buf4, buf5);
+            if (it + 5 < end) slice(buf5, buf6);
+            if (it + 6 < end) slice(buf6, buf7);
+            if (it + 7 < end) slice(buf7, buf0);
+        }
     }
     __builtin_amdgcn_s_waitcnt(0x0070);                       // the copies past the end write zeros into LDS
 
     __syncthreads();                                          // everyone is done with the operands
     constexpr int kCols = TN * 32, kUnits = kCols / 8, kRows = 64 / kUnits;
-    constexpr int kPart = THREADS / 64 / ffn::kRing, kInts = 32 * kCols;   // wavefronts that stage in one buffer
+    constexpr int kPart = THREADS / 64 / 4, kInts = 32 * kCols, kSwizzle = kCols >= 64 ? 15 : 7;   // wavefronts that stage in one buffer
     static_assert(kBytes >= kPart * kInts * 4, "the results of 32 rows of every wavefront are staged in the buffers");
-    char* bufs[ffn::kRing] = {buf0, buf1, buf2, buf3};
+    char* bufs[4] = {buf0, buf1, buf2, buf3};
     int* stage = (int*)bufs[0] + wave % kPart * kInts;
 #pragma unroll
-    for (int i = 1; i < ffn::kRing; ++i) stage = wave / kPart == i ? (int*)bufs[i] + wave % kPart * kInts : stage;
+    for (int i = 1; i < 4; ++i) stage = wave / kPart == i ? (int*)bufs[i] + wave % kPart * kInts : stage;
     const int lane_row = lane % 32, out_row = lane / kUnits, unit = lane % kUnits, col = wn * (T / 2) + 8 * unit;
     float cs[8];
     if (range < 0) load_upto8(p.w_scale + at.group * p.w_scale_group + at.n0 + col, (int)max((int64_t)0, min((int64_t)8, p.out - at.n0 - col)), 0.0f, cs);
@@ -460,13 +509,13 @@ __global__ __launch_bounds__(ffn::gemm_threads<T>(), 2) void tile_kernel(Product
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int chunk = 8 * t + 2 * g + lane / 32;
-                *(i4*)(stage + lane_row * kCols + 4 * (chunk ^ (lane_row & 15))) = i4{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
+                *(i4*)(stage + lane_row * kCols + 4 * (chunk ^ (lane_row & kSwizzle))) = i4{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
             }
         in_wave_order();                                      // written and read by one wavefront: LDS keeps its order
 #pragma unroll 1
         for (int r0 = 0; r0 < 32; r0 += kRows) {
             const int r = r0 + out_row, row = wm * (32 * TM) + 32 * i + r;
-            const i4 lo = *(const i4*)(stage + r * kCols + 4 * ((2 * unit) ^ (r & 15))), hi = *(const i4*)(stage + r * kCols + 4 * ((2 * unit + 1) ^ (r & 15)));
+            const i4 lo = *(const i4*)(stage + r * kCols + 4 * ((2 * unit) ^ (r & kSwizzle))), hi = *(const i4*)(stage + r * kCols + 4 * ((2 * unit + 1) ^ (r & kSwizzle)));
             if (range >= 0) {
                 int* out = p.partial + ((int64_t)range * p.rest + (tile - p.whole)) * (T * T) + row * T + col;
                 *(i4*)out = lo;
@@ -534,28 +583,53 @@ struct Plan {
 
 bool lies_well(const ols_matrix& m) { return m.row % 16 == 0 && m.row <= (1 << 22) && m.group % 16 == 0 && ((uintptr_t)m.dev & 15) == 0; }
 
-constexpr int kFewRows = 64;              // at most: weights go straight into registers
 constexpr int kCus = 256;
+// Up to this many rows weights go straight into registers.  Products alone, in us, few_kernel / tiles: 32 rows, 2048 to 2048: 6.6 / 9.5; to
+// 11 264: 12.3 / 11.7; 64 rows, 5632 to 2048: 11.3 / 11.2, 2048 to 11 264: 15.9 / 11.7, to 32 000: 36 / 18.
+constexpr int kFewRows = 32;
+constexpr int kFewWaves = 4096;           // of all workgroups together, where the contraction is long enough
+
+// What a product in tiles takes, in microseconds: a start, and for each round of tiles its slices, which take longer the more tiles run
+// beside each other; cut contractions add a launch and their sums' traffic.  Fitted to products of 64 to 8192 rows and 700 to 32 000
+// channels over 1000 to 5632 indices (within 20 % of all but one).  Tiles of 64 / 128 / 256 whole: 512 rows, 2048 to 2048: 11.8 / 16.8 / 33;
+// 1024, 2048 to 5632: 38 / 24.5 / 35; 8192, 4096 to 4096 in 256: 161.  128 rows, 5632 to 2048 in tiles of 64, cut in 1 / 2 / 4 / 8: 22.5 /
+// 17.2 / 13.2 / 14.7.
+struct Cost {
+    int tile, slots;                      // tiles of a round
+    double start, least, more;            // a slice: least + more x (share of the slots that are taken)
+};
+constexpr Cost kCosts[3] = {{64, 2 * kCus, 4.6, 0.17, 0.14}, {128, 2 * kCus, 6.0, 0.30, 0.42}, {256, kCus, 9.6, 0.45, 0.75}};
+
+double cost_of(const Cost& c, int64_t tiles, int64_t slices, int ranges) {
+    const int64_t rounds = tiles / c.slots, rest = tiles % c.slots;
+    double us = c.start + (double)(rounds * slices) * (c.least + c.more);
+    if (!rest) return us;
+    const int64_t run = rest * ranges, last = run % c.slots ? run % c.slots : c.slots;
+    us += (double)((slices + ranges - 1) / ranges) * ((double)((run - 1) / c.slots) * (c.least + c.more) + c.least + c.more * (double)last / c.slots);
+    return ranges == 1 ? us : us + 3.0 + (double)run * c.tile * c.tile * 8 / 4e6;
+}
 
 Plan plan_of(const ols_int8& f) {
     Plan p = {};
     const int64_t turns = (f.width + 63) / 64;
     p.ranges = 1;
     if (f.rows <= kFewRows) {
-        const int64_t channels = (f.out + 15) / 16 * f.groups;
         p.R = f.rows <= 16 ? 1 : 2;
-        const int64_t blocks = channels * ((f.rows + 16 * p.R - 1) / (16 * p.R));
-        p.waves = blocks <= 2 * kCus && turns >= 32 ? 16 : turns >= 8 ? 8 : 4;
-        p.fused = f.dtype != OLS_I8 && f.rows <= 16 && f.rows * (turns * 64 + 16) <= 32768 && f.rows * f.width * blocks <= (1 << 23);
+        const int64_t blocks = (f.out + 15) / 16 * f.groups;
+        p.waves = 2;
+        while (p.waves < 16 && 2 * p.waves * blocks <= kFewWaves && 4 * p.waves <= turns) p.waves *= 2;
+        p.fused = f.dtype != OLS_I8 && f.rows == 1 && f.width <= 32768 && f.width * blocks <= (1 << 23);
     } else {
-        int64_t tiles = (f.rows + 255) / 256 * ((f.out + 255) / 256) * f.groups;
-        p.tile = tiles >= 192 ? 256 : 128;
-        p.tiles_m = (int)((f.rows + p.tile - 1) / p.tile), p.tiles_n = (int)((f.out + p.tile - 1) / p.tile);
-        tiles = (int64_t)p.tiles_m * p.tiles_n * f.groups;
-        p.whole = (int)tiles;
-        if (tiles <= kCus) {
-            p.ranges = (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCus / tiles, turns / 4));
-            if (p.ranges > 1) p.whole = 0, p.rest = (int)tiles;
+        double best = 1e30;
+        for (const Cost& c : kCosts) {
+            const int64_t tiles_m = (f.rows + c.tile - 1) / c.tile, tiles_n = (f.out + c.tile - 1) / c.tile, tiles = tiles_m * tiles_n * f.groups;
+            for (int ranges = 1; ranges <= 16 && (ranges == 1 || 4 * ranges <= turns); ranges *= 2) {
+                const double us = cost_of(c, tiles, turns, ranges);
+                if (us >= best) continue;
+                best = us;
+                p.tile = c.tile, p.tiles_m = (int)tiles_m, p.tiles_n = (int)tiles_n, p.ranges = ranges;
+                p.rest = ranges > 1 ? (int)(tiles % c.slots) : 0, p.whole = (int)tiles - p.rest;
+            }
         }
         p.lay_w = !lies_well(f.w);
     }
@@ -573,25 +647,20 @@ Plan plan_of(const ols_int8& f) {
 
 template <typename TX, int R, int WAVES, bool FUSED>
 void launch_few_sized(const Product& p, hipStream_t stream) {
-    const size_t sums = (size_t)WAVES * R * 1024, rows = FUSED ? (size_t)p.rows * ((p.width + 63) / 64 * 64 + 16) : 0;
-    const dim3 grid((unsigned)((p.out + 15) / 16), (unsigned)((p.rows + 16 * R - 1) / (16 * R)), p.groups);
-    few_kernel<TX, R, WAVES, FUSED><<<grid, WAVES * 64, std::max(sums, rows), stream>>>(p);
+    const size_t sums = (size_t)WAVES * R * 1024, row = FUSED ? (size_t)(p.width + 63) / 64 * 64 : 0;
+    few_kernel<TX, R, WAVES, FUSED><<<dim3((unsigned)((p.out + 15) / 16), 1, p.groups), WAVES * 64, std::max(sums, row), stream>>>(p);
+}
+template <typename TX, int R, bool FUSED>
+void launch_few_waves(const Product& p, const Plan& plan, hipStream_t stream) {
+    if (plan.waves == 16) launch_few_sized<TX, R, 16, FUSED>(p, stream);
+    else if (plan.waves == 8) launch_few_sized<TX, R, 8, FUSED>(p, stream);
+    else if (plan.waves == 4) launch_few_sized<TX, R, 4, FUSED>(p, stream);
+    else launch_few_sized<TX, R, 2, FUSED>(p, stream);
 }
 template <typename TX, bool FUSED>
 void launch_few(const Product& p, const Plan& plan, hipStream_t stream) {
-    if constexpr (FUSED) {                // at most 16 rows
-        if (plan.waves == 16) launch_few_sized<TX, 1, 16, true>(p, stream);
-        else if (plan.waves == 8) launch_few_sized<TX, 1, 8, true>(p, stream);
-        else launch_few_sized<TX, 1, 4, true>(p, stream);
-    } else if (plan.R == 1) {
-        if (plan.waves == 16) launch_few_sized<TX, 1, 16, false>(p, stream);
-        else if (plan.waves == 8) launch_few_sized<TX, 1, 8, false>(p, stream);
-        else launch_few_sized<TX, 1, 4, false>(p, stream);
-    } else {
-        if (plan.waves == 16) launch_few_sized<TX, 2, 16, false>(p, stream);
-        else if (plan.waves == 8) launch_few_sized<TX, 2, 8, false>(p, stream);
-        else launch_few_sized<TX, 2, 4, false>(p, stream);
-    }
+    if (FUSED || plan.R == 1) launch_few_waves<TX, 1, FUSED>(p, plan, stream);      // fused: one row
+    else if constexpr (!FUSED) launch_few_waves<TX, 2, false>(p, plan, stream);
 }
 
 hipError_t launch_pack(const Pack& p, int groups, hipStream_t stream) {
@@ -682,12 +751,14 @@ hipError_t launch_int8(const ols_int8& f, hipStream_t stream) {
     }
     const unsigned blocks = (unsigned)(plan.whole + plan.rest * plan.ranges);
     if (plan.tile == 256) tile_kernel<256><<<blocks, 512, 0, stream>>>(p);
-    else tile_kernel<128><<<blocks, 256, 0, stream>>>(p);
+    else if (plan.tile == 128) tile_kernel<128><<<blocks, 256, 0, stream>>>(p);
+    else tile_kernel<64><<<blocks, 256, 0, stream>>>(p);
     e = hipGetLastError();
     if (e != hipSuccess || !plan.rest) return e;
     const dim3 grid(plan.rest, plan.tile * plan.tile / 8 / 256);
     if (plan.tile == 256) join_kernel<256><<<grid, 256, 0, stream>>>(p);
-    else join_kernel<128><<<grid, 256, 0, stream>>>(p);
+    else if (plan.tile == 128) join_kernel<128><<<grid, 256, 0, stream>>>(p);
+    else join_kernel<64><<<grid, 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 
