@@ -547,7 +547,7 @@ typedef struct ols_distill {
 } ols_distill;
 OLS_API int ols_distill_loss(const ols_distill* d, void* stream);
 OLS_API int ols_distill_loss_grad(const ols_distill* d, void* stream);          /* reads stats; loss and logprob are not touched */
-OLS_API int64_t ols_distill_workspace_bytes(int64_t rows, int64_t vocab, int dtype);   /* of ols_distill_loss */
+OLS_API int64_t ols_distill_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int k);   /* of ols_distill_loss */
 
 /* One step of beam search: for each of `batch` requests the `beams` best continuations of its in_beams hypotheses.
  *   - A hypothesis of score s with logits z has the candidates v of value s + z[v] - log sum e^z, one that has ended (finished) itself alone,

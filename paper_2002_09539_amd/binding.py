@@ -120,7 +120,7 @@ _SIGNATURES = {
     "ols_clip_workspace_bytes": (_I, [C.c_int, _P, _P, C.c_int]),
     "ols_distill_loss": (C.c_int, [_P, _P]),
     "ols_distill_loss_grad": (C.c_int, [_P, _P]),
-    "ols_distill_workspace_bytes": (_I, [_I, _I, C.c_int]),
+    "ols_distill_workspace_bytes": (_I, [_I, _I, C.c_int, C.c_int]),
     "ols_beam_select": (C.c_int, [_P, _P]),
     "ols_beam_workspace_bytes": (_I, [_I, C.c_int, C.c_int, _I, C.c_int]),
     "ols_beam_reorder": (C.c_int, [C.c_int, _P, _P, _P, _P, _P, _P, _P, _I, C.c_int, C.c_int, _P, _P]),
@@ -388,8 +388,8 @@ def ols_token_logprobs_workspace_bytes(rows, vocab, dtype, top):
     return _bytes(load().ols_token_logprobs_workspace_bytes(rows, vocab, dtype, top))
 
 
-def ols_distill_workspace_bytes(rows, vocab, dtype):
-    return _bytes(load().ols_distill_workspace_bytes(rows, vocab, dtype))
+def ols_distill_workspace_bytes(rows, vocab, dtype, k):
+    return _bytes(load().ols_distill_workspace_bytes(rows, vocab, dtype, k))
 
 
 def ols_beam_workspace_bytes(batch, in_beams, beams, vocab, dtype):

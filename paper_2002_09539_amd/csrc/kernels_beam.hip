@@ -19,11 +19,6 @@ namespace ols {
 
 namespace {
 
-__device__ __forceinline__ double sum_lanes(double v) {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-
 // e^d as a power of two; log2 e = hi + lo, both positive, so that -inf stays -inf
 __device__ __forceinline__ float exp_of(float d) {
     constexpr float kHi = 1.44269502162933349609f, kLo = 1.92596299112661747e-8f;
@@ -72,7 +67,7 @@ __global__ __launch_bounds__(THREADS, 4) void beam_part_kernel(BeamParams p) {
         for (int e = 0; e < N; ++e) s0 += exp_of(Vec<T>::get(v[j], e) - base);
         s += (double)s0;
     }
-    s = sum_lanes(s);
+    s = wave_sum(s);
     if (lane == 0) red_s[wave] = s;
     keep_packed(v);
     __syncthreads();
@@ -112,7 +107,7 @@ __global__ __launch_bounds__(64) void beam_join_kernel(BeamParams p) {
         const double base = m == -INFINITY ? 0.0 : (double)m;
         double sum = 0.0;
         for (int j = lane; j < p.parts; j += 64) sum += p.part_s[row * p.parts + j] * exp((double)p.part_m[row * p.parts + j] - base);
-        sum = sum_lanes(sum);
+        sum = wave_sum(sum);
         if (lane == 0) tops[i] = m, sums[i] = sum;
     }
     in_wave_order();

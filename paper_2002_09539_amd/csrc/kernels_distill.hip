@@ -11,7 +11,6 @@
 // For that the listed logits are struck out of the registers that hold the row (a bit per logit in LDS says which; a set bit met
 // again says that a list names a token twice), the sums are taken over the others against the others' own maximum, and one wavefront
 // adds the listed ones.  Maximum and sums are fp32; what a list adds up to and the loss, a difference of like numbers, are fp64.
-// Exponents are products with log2 e / T in two terms: its rounding alone would move every far logit the same way.
 //
 // What bounds it is one read and one write of the logits.  A workgroup holds its part of a row in registers and forms the
 // gradient from there; all logits get the gradient of an unlisted one, and behind a barrier the entries of the list and the target
@@ -24,13 +23,8 @@ namespace {
 
 constexpr int kMaxList = OLS_MAX_TEACHER;
 
-// e^{d x} as a power of two: x log2 e = hi + lo, both positive, so that -inf stays -inf
-__device__ __forceinline__ float power(float d, float hi, float lo) { return __builtin_amdgcn_exp2f(fmaf(d, hi, d * lo)); }
-
-__device__ __forceinline__ double sum_lanes(double v) {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
+// e^{d x} as a power of two, x log2 e rounded: the exponent of a far logit is off by 2^-25 of itself
+__device__ __forceinline__ float power(float d, float scale) { return __builtin_amdgcn_exp2f(d * scale); }
 
 struct Sums {            // over some of a row: maximum, sum of e^{(z - m) / T}, sum of e^{z - m}
     float m, s, s1;
@@ -38,103 +32,95 @@ struct Sums {            // over some of a row: maximum, sum of e^{(z - m) / T},
 __device__ __forceinline__ Sums join(const DistillParams& p, const Sums& a, const Sums& b) {
     const float m = fmaxf(a.m, b.m), base = m == -INFINITY ? 0.0f : m;
     const float da = a.m - base, db = b.m - base;                         // -inf where a side is empty
-    return {m, a.s * power(da, p.hi, p.lo) + b.s * power(db, p.hi, p.lo), a.s1 * power(da, p.hi1, p.lo1) + b.s1 * power(db, p.hi1, p.lo1)};
+    return {m, a.s * power(da, p.scale) + b.s * power(db, p.scale), a.s1 * power(da, p.scale1) + b.s1 * power(db, p.scale1)};
 }
 
-// A row's list in LDS: places in the row (-1: none), q, and the student's logits; entry k is the target.
+// A row's list in LDS: places in the row (-1: none), q, and the student's logits.
 struct List {
-    int index[kMaxList + 1];
-    float q[kMaxList + 1], z[kMaxList + 1];
-    int twice, target_listed;            // a token is named twice; the target is in the list
+    int index[kMaxList];
+    float q[kMaxList], z[kMaxList];
 };
 
-// What one wavefront knows of a list.
+// What is known of a row from its list and target alone.
 struct Teacher {
-    double w, rest, self;                // sum of q, q_r, sum of q log q
+    double w, rest, self, cross;         // sum of q, q_r, sums of q log q and of q (z - m) / T
+    float m, s, s1;                      // of the listed tokens, each once: largest logit, sums of e^{(z - m) / T} and e^{z - m}
+    float z_target;
     float top, scale;                    // q_j = e^{(v_j - top) / T or v_j} scale
+    int target;                          // -1: none
+    int target_listed, twice, any;       // the target is in the list; a token is named twice; some q is positive
 };
 
-// Reads entries and target; entries outside [start, end) are none.
+// Reads a row's list and target; by one wavefront.
 template <typename T>
-__device__ __forceinline__ void read_list(const DistillParams& p, List& l, int64_t row, const T* z, int64_t start, int64_t end) {
-    const int lane = threadIdx.x % 64;
+__device__ __forceinline__ void read_list(const DistillParams& p, List& l, Teacher& t, int64_t row, const T* z) {
     const int target = p.targets ? p.targets[row] : -1;
+    t.target = target >= 0 && target < p.vocab ? target : -1;
     bool met = false;
-    for (int i = lane; i < p.k; i += 64) {
+    for (int i = threadIdx.x % 64; i < p.k; i += 64) {
         const int at = p.index[row * p.k + i];
-        const bool there = at >= start && at < end;
+        const bool there = at >= 0 && at < p.vocab;
         l.index[i] = there ? at : -1;
         l.z[i] = there ? load1(z + at) : -INFINITY;
-        met |= there && at == target;
+        met |= there && at == t.target;
     }
-    const unsigned long long any = __ballot(met);
-    if (lane == 0) {
-        const bool there = target >= start && target < end;
-        l.index[p.k] = there ? target : -1;
-        l.z[p.k] = there ? load1(z + target) : -INFINITY;
-        l.q[p.k] = 0.0f;
-        l.target_listed = any != 0;
-    }
+    t.target_listed = __ballot(met) != 0;
+    t.z_target = t.target >= 0 ? load1(z + t.target) : -INFINITY;
+    in_wave_order();
 }
 
-// One bit per logit of [start, ..), set where it is listed.
-__device__ __forceinline__ void mark(const DistillParams& p, List& l, unsigned* bits, int64_t start) {
-    bool again = false;
-    for (int i = threadIdx.x % 64; i < p.k; i += 64) {
-        if (l.index[i] < 0) continue;
-        const int at = (int)(l.index[i] - start);
-        again |= (atomicOr(&bits[at / 32], 1u << (at % 32)) >> (at % 32)) & 1u;
-    }
-    const unsigned long long any = __ballot(again);
-    if (threadIdx.x % 64 == 0) l.twice = any != 0;
-}
-// Whether entry i is its token's first.
-__device__ __forceinline__ bool first_of(const List& l, int i) {
-    for (int j = 0; j < i; ++j)
-        if (l.index[j] == l.index[i]) return false;
-    return true;
-}
-
-// The teacher's probabilities into l.q, by one wavefront.  A NaN or +inf among the values makes them all NaN.
-__device__ __forceinline__ Teacher weigh(const DistillParams& p, List& l, int64_t row) {
+// The teacher's probabilities into l.q and the sums over the list, by one wavefront.  A NaN or +inf among the values makes them all NaN.
+__device__ __forceinline__ void weigh(const DistillParams& p, List& l, Teacher& t, int64_t row) {
     const int lane = threadIdx.x % 64;
     const float* value = p.value + row * p.k;
-    Teacher t;
-    float top = -INFINITY;
-    bool some = false, bad = false;
+    float top = -INFINITY, m = -INFINITY;
+    bool some = false, bad = false, again = false;
     for (int i = lane; i < p.k; i += 64) {
         if (l.index[i] < 0) continue;
         const float v = value[i];
         some = true, bad |= !(v < INFINITY);
-        top = fmaxf(top, v);
+        top = fmaxf(top, v), m = fmaxf(m, l.z[i]);
     }
     some = __ballot(some) != 0, bad = __ballot(bad) != 0;
     top = wave_max(top);
+    t.m = wave_max(m);
     t.top = p.rest || top == -INFINITY ? 0.0f : top;
-    const double inv_t = p.rest ? 1.0 : 1.0 / (double)p.temperature;
-    double w = 0.0, self = 0.0;
+    const float base = t.m == -INFINITY ? 0.0f : t.m;
+    const double inv_t = 1.0 / (double)p.temperature, inv_v = p.rest ? 1.0 : inv_t;
+    double w = 0.0, self = 0.0, cross = 0.0;
+    float s = 0.0f, s1 = 0.0f;
     for (int i = lane; i < p.k; i += 64) {
         float q = 0.0f;
         if (l.index[i] >= 0) {
-            const double u = ((double)value[i] - t.top) * inv_t, e = exp(u);
-            w += e, self += e > 0.0 ? e * u : 0.0;
+            const double u = ((double)value[i] - t.top) * inv_v, e = exp(u);
+            w += e, self += e > 0.0 ? e * u : 0.0, cross += e > 0.0 ? e * (((double)l.z[i] - (double)base) * inv_t) : 0.0;
             q = (float)e;
+            bool first = true;
+            for (int j = 0; j < i; j += 4) {                   // whether the token was named before
+                const int4 at = *(const int4*)(l.index + j);
+                first &= !(at.x == l.index[i] || (at.y == l.index[i] && j + 1 < i) || (at.z == l.index[i] && j + 2 < i) || (at.w == l.index[i] && j + 3 < i));
+            }
+            again |= !first;
+            if (first) s += power(l.z[i] - base, p.scale), s1 += power(l.z[i] - base, p.scale1);
         }
         l.q[i] = q;
     }
-    w = sum_lanes(w), self = sum_lanes(self);
+    w = wave_sum(w), self = wave_sum(self), cross = wave_sum(cross);
+    t.s = wave_sum(s), t.s1 = wave_sum(s1);
+    t.twice = __ballot(again) != 0;
+    t.any = w > 0.0;
     t.scale = 1.0f, t.rest = 0.0;
     if (p.rest) {
         t.rest = some ? fmax(1.0 - w, 0.0) : 0.0;
     } else if (w > 0.0) {
         t.scale = (float)(1.0 / w);
-        self = self / w - log(w);
+        self = self / w - log(w), cross /= w;
         for (int i = lane; i < p.k; i += 64) l.q[i] *= t.scale;
         w = 1.0;
     }
     if (bad) w = self = NAN, t.scale = NAN;
-    t.w = w, t.self = self;
-    return t;
+    t.w = w, t.self = self, t.cross = cross;
+    in_wave_order();
 }
 
 // What the gradient needs of a row; p.stats holds it for a later call.
@@ -146,284 +132,320 @@ struct Coefs {
     float s, s1;         // the sums, against m
     bool empty, held;    // nothing is allowed; the rest counts
 };
-// u: over what is not struck out, listed: over the others, against the larger maximum
+// u: over what is not struck out, which are all where the rest does not count.
 __device__ __forceinline__ Coefs coefs(const DistillParams& p, const Sums& u, const Sums& listed, float w, float rest) {
     Coefs c;
-    c.m = fmaxf(u.m, listed.m);
+    const Sums all = p.rest ? join(p, u, listed) : u;
+    c.m = all.m, c.s = all.s, c.s1 = all.s1;
     const float m = c.m == -INFINITY ? 0.0f : c.m;
-    const float f = power(u.m - m, p.hi, p.lo), f1 = power(u.m - m, p.hi1, p.lo1);
-    c.s = u.s * f + listed.s, c.s1 = u.s1 * f1 + listed.s1;
     c.base = u.m == -INFINITY ? 0.0f : u.m;
     c.empty = c.m == -INFINITY && c.s == 0.0f;
     c.held = rest > 0.0f && u.s > 0.0f;
-    const float all = c.held ? w + rest : w;
-    c.listed = c.empty ? 0.0f * all : all / c.s;              // a list with a NaN stays one
+    const float both = c.held ? w + rest : w;
+    c.listed = c.empty ? 0.0f * both : both / c.s;             // a list with a NaN stays one
     c.inv_s1 = c.empty ? 0.0f : 1.0f / c.s1;
-    c.others = c.listed * f - (c.held ? rest / u.s : 0.0f);
-    c.hard = c.inv_s1 * f1;
+    c.others = c.listed * power(u.m - m, p.scale) - (c.held ? rest / u.s : 0.0f);
+    c.hard = c.inv_s1 * power(u.m - m, p.scale1);
     return c;
 }
+__device__ __forceinline__ Coefs coefs(const DistillParams& p, const Sums& u, const Teacher& t) { return coefs(p, u, Sums{t.m, t.s, t.s1}, (float)t.w, (float)t.rest); }
 
-// Sums over the listed tokens, each once, against max(m_u, their own maximum), by one wavefront.
-__device__ __forceinline__ Sums sum_list(const DistillParams& p, const List& l, float m_u, bool twice) {
-    const int lane = threadIdx.x % 64;
-    float m = -INFINITY;
-    for (int i = lane; i < p.k; i += 64) m = fmaxf(m, l.z[i]);
-    m = wave_max(m);
-    const float all = fmaxf(m, m_u), base = all == -INFINITY ? 0.0f : all;
-    float s = 0.0f, s1 = 0.0f;
-    for (int i = lane; i < p.k; i += 64) {
-        if (l.index[i] < 0 || (twice && !first_of(l, i))) continue;
-        s += power(l.z[i] - base, p.hi, p.lo), s1 += power(l.z[i] - base, p.hi1, p.lo1);
-    }
-    return {m, wave_sum(s), wave_sum(s1)};
-}
-
-// Loss, likelihood and stats of a row, by one wavefront.
-__device__ __forceinline__ void finish_row(const DistillParams& p, const List& l, const Teacher& t, const Sums& u, const Coefs& c, int64_t row) {
-    const int lane = threadIdx.x % 64;
-    const double inv_t = 1.0 / (double)p.temperature;
-    double cross = 0.0;
-    bool some = false;
-    for (int i = lane; i < p.k; i += 64) {
-        if (!(l.q[i] > 0.0f)) continue;                                  // a NaN comes by t.self
-        some = true;
-        cross += (double)l.q[i] * (((double)l.z[i] - (double)c.m) * inv_t);
-    }
-    cross = sum_lanes(cross);
-    some = __ballot(some) != 0;
-    if (lane != 0) return;
-    const double log_s = log((double)c.s);
-    double loss = t.self - cross + t.w * log_s;
+// Loss, likelihood and stats of a row, by one lane.
+__device__ __forceinline__ void finish_row(const DistillParams& p, const Teacher& t, const Sums& u, const Coefs& c, int64_t row) {
+    const double inv_t = 1.0 / (double)p.temperature, log_s = log((double)c.s);
+    // t.cross is against the listed tokens' own maximum
+    double loss = t.self + t.w * log_s;
+    if (t.any) loss -= t.cross + t.w * (((t.m == -INFINITY ? 0.0 : (double)t.m) - (double)c.m) * inv_t);
     if (c.held) loss += t.rest * (log(t.rest) - (((double)u.m - (double)c.m) * inv_t + log((double)u.s) - log_s));
-    if (c.empty) loss = t.w != t.w ? NAN : some ? INFINITY : 0.0;
+    if (c.empty) loss = t.w != t.w ? NAN : t.any ? INFINITY : 0.0;
     else if (!(c.s < INFINITY)) loss = NAN;
     p.loss[row] = (float)(loss * (double)p.temperature * (double)p.temperature);
     if (p.logprob) {
         float given = 0.0f;
-        if (l.index[p.k] >= 0) given = c.empty ? -INFINITY : !(c.s1 < INFINITY) ? NAN : (float)((double)l.z[p.k] - (double)c.m - log((double)c.s1));
+        if (t.target >= 0) given = c.empty ? -INFINITY : !(c.s1 < INFINITY) ? NAN : (float)((double)t.z_target - (double)c.m - log((double)c.s1));
         p.logprob[row] = given;
     }
     float* o = p.stats + 8 * row;
     o[0] = c.base, o[1] = c.others, o[2] = c.hard, o[3] = c.m, o[4] = c.listed, o[5] = c.inv_s1, o[6] = t.top, o[7] = c.empty && t.w == t.w ? 0.0f : t.scale;
 }
 
-// The gradient of a listed token or of the target (entry k, where it is not listed).
-__device__ __forceinline__ float entry_grad(const DistillParams& p, const List& l, const Coefs& c, int i, float g_loss, float g_hard) {
-    const bool hard = l.index[p.k] == l.index[i];
-    const float at_m = l.z[i] - (c.m == -INFINITY ? 0.0f : c.m);
-    float soft;
-    if (i == p.k) {
-        soft = c.others * power(l.z[i] - c.base, p.hi, p.lo);
-    } else {
-        float q = l.q[i];
-        if (l.twice) {
-            q = 0.0f;
-            for (int j = 0; j < p.k; ++j) q += l.index[j] == l.index[i] ? l.q[j] : 0.0f;
-        }
-        soft = c.listed * power(at_m, p.hi, p.lo) - q;
-    }
-    const float d = g_loss * soft + g_hard * ((hard ? 1.0f : 0.0f) - c.inv_s1 * power(at_m, p.hi1, p.lo1));
+// The gradient of a listed token (q: of all its entries) or of an unlisted target.
+__device__ __forceinline__ float entry_grad(const DistillParams& p, const Coefs& c, float z, bool listed, float q, bool target, float g_loss, float g_hard) {
+    const float at_m = z - (c.m == -INFINITY ? 0.0f : c.m);
+    const float soft = listed ? c.listed * power(at_m, p.scale) - q : c.others * power(z - c.base, p.scale);
+    const float d = g_loss * soft + g_hard * ((target ? 1.0f : 0.0f) - c.inv_s1 * power(at_m, p.scale1));
     return c.empty ? (soft != soft ? NAN : 0.0f) : d;
 }
 
-// Sixteen bytes of logits with the marked ones struck out.
-template <typename T>
-__device__ __forceinline__ void strike(u4& v, const unsigned* bits, int64_t at) {       // at: the first one's place in the part
-    constexpr int N = Vec<T>::kN;
-    const unsigned b = (((const uint8_t*)bits)[at / 8] >> (at % 8)) & ((1u << N) - 1);
-    if (!b) return;
-    float x[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (b >> e) & 1u ? -INFINITY : Vec<T>::get(v, e);
-    v = Vec<T>::pack(x);
-}
-
-template <typename T, int NV, int THREADS>
-__device__ __forceinline__ void write_grad(const DistillParams& p, u4 (&v)[NV], const Coefs& c, T* d, int64_t start, int64_t end, float g_loss, float g_hard) {
-    constexpr int N = Vec<T>::kN;
-    const bool two = p.targets && p.temperature != 1.0f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int64_t i = start + ((int64_t)j * THREADS + threadIdx.x) * N;
-        if (i >= end) continue;
-        float x[N];
-        if (two) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float a = Vec<T>::get(v[j], e) - c.base;
-                x[e] = g_loss * (c.others * power(a, p.hi, p.lo)) - g_hard * (c.hard * power(a, p.hi1, p.lo1));
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float w = power(Vec<T>::get(v[j], e) - c.base, p.hi, p.lo);
-                x[e] = g_loss * (c.others * w) - g_hard * (c.hard * w);
-            }
-        }
-        store_vec<T>(d, i, end, x);
-    }
-}
-
+// A row, or a part of one, in the registers of a workgroup: whole vectors, and of what is left of the last one a logit in each of the
+// first lanes.  Addresses are a uniform pointer and a lane's offset: kept for every vector, as 64-bit numbers, they spill.
 template <typename T, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS, 4) void distill_kernel(DistillParams p) {
-    constexpr int N = Vec<T>::kN, WAVES = THREADS / 64;
-    extern __shared__ unsigned bits[];
-    __shared__ List list;
-    __shared__ float red_m[WAVES], red_s[WAVES], red_s1[WAVES];
-    __shared__ Sums listed;
-    __shared__ float list_w, list_rest;
-    const int64_t row = blockIdx.x;
-    const int part = blockIdx.y, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const T* z = (const T*)p.logits + row * p.row_stride;
-    const int64_t start = (int64_t)part * p.part, end = min(start + p.part, p.vocab);
-    const bool whole = p.parts == 1;
+struct Held {
+    static constexpr int kN = Vec<T>::kN;
     u4 v[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = load_vec<T>(z, start + ((int64_t)j * THREADS + threadIdx.x) * N, end);
-    for (int i = threadIdx.x; i < (int)((p.part + 31) / 32); i += THREADS) bits[i] = 0;
-    __syncthreads();
-    Teacher teacher = {};
-    if (wave == 0) {
-        read_list<T>(p, list, row, z, start, end);
-        in_wave_order();
-        mark(p, list, bits, start);
+    float tail;                          // -inf where there is none
+
+    __device__ static void load_one(u4& v, int j, const T* row, int length) {
+        v = u4{Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone};
+        if ((int)threadIdx.x < length / kN - j * THREADS) v = *(const u4any*)((const char*)row + (size_t)j * THREADS * 16 + threadIdx.x * 16u);
     }
-    if (p.rest) {
-        __syncthreads();
+    __device__ void load_tail(const T* row, int length) { tail = (int)threadIdx.x < length % kN ? load1(row + length / kN * kN + threadIdx.x) : -INFINITY; }
+    __device__ void load(const T* row, int length) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) load_one(v[j], j, row, length);
+        load_tail(row, length);
+    }
+    // The logits whose bits are set become -inf.
+    __device__ void strike(const unsigned* bits, int length) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t at = ((int64_t)j * THREADS + threadIdx.x) * N;
-            if (start + at < end) strike<T>(v[j], bits, at);
+            const int at = (j * THREADS + (int)threadIdx.x) * kN;
+            if (at + kN > length) continue;
+            const unsigned b = (((const uint8_t*)bits)[at / 8] >> (at % 8)) & ((1u << kN) - 1);
+            if (!b) continue;
+            float x[kN];
+#pragma unroll
+            for (int e = 0; e < kN; ++e) x[e] = (b >> e) & 1u ? -INFINITY : Vec<T>::get(v[j], e);
+            v[j] = Vec<T>::pack(x);
         }
+        const int at = length / kN * kN + (int)threadIdx.x;
+        if (at < length && (bits[at / 32] >> (at % 32)) & 1u) tail = -INFINITY;
     }
-    if (wave == 0 && whole) {
-        teacher = weigh(p, list, row);
-        if (lane == 0) list_w = (float)teacher.w, list_rest = (float)teacher.rest;
+    __device__ float largest() const {
+        float m = tail;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < kN; ++e) m = fmaxf(m, Vec<T>::get(v[j], e));
+        return m;
     }
-    float m = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int e = 0; e < N; ++e) m = fmaxf(m, Vec<T>::get(v[j], e));
-    keep_packed(v);
-    m = wave_max(m);
-    if (lane == 0) red_m[wave] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, red_m[w]);
-    if (wave == 0 && whole) {
-        Sums l{-INFINITY, 0.0f, 0.0f};
-        if (p.rest) l = sum_list(p, list, m, list.twice);
-        if (lane == 0) listed = l;
-    }
-    const float base = m == -INFINITY ? 0.0f : m;
-    const bool two = p.targets && p.temperature != 1.0f;
-    float s = 0.0f, s1 = 0.0f;
+};
+
+// What e^{z - base} takes: nothing more, a square, or an exponential of its own.
+enum Second { kNone, kSquare, kOther };
+__host__ __device__ __forceinline__ Second second_of(const DistillParams& p) { return !p.targets || p.temperature == 1.0f ? kNone : p.temperature == 2.0f ? kSquare : kOther; }
+
+// Adds up e^{(z - base) / T} and, where it is another, e^{z - base}.  Short sums first: fewer roundings of the long ones.
+template <Second SECOND>
+__device__ __forceinline__ void add_one(const DistillParams& p, float d, float& a, float& b) {
+    const float w = power(d, p.scale);
+    a += w;
+    if constexpr (SECOND == kSquare) b = fmaf(w, w, b);
+    if constexpr (SECOND == kOther) b += power(d, p.scale1);
+}
+template <Second SECOND, typename T, int THREADS, int NV>
+__device__ __forceinline__ void add_up(const DistillParams& p, const Held<T, THREADS, NV>& h, float base, float& s, float& s1) {
+    add_one<SECOND>(p, h.tail - base, s, s1);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        float s0 = 0.0f;                   // short sums first: fewer roundings of the long ones
+        float a = 0.0f, b = 0.0f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) s0 += power(Vec<T>::get(v[j], e) - base, p.hi, p.lo);
-        s += s0;
-        if (two) {
-            s0 = 0.0f;
-#pragma unroll
-            for (int e = 0; e < N; ++e) s0 += power(Vec<T>::get(v[j], e) - base, p.hi1, p.lo1);
-            s1 += s0;
-        }
+        for (int e = 0; e < Vec<T>::kN; ++e) add_one<SECOND>(p, Vec<T>::get(h.v[j], e) - base, a, b);
+        s += a, s1 += b;
     }
-    s = wave_sum(s), s1 = wave_sum(s1);
-    if (lane == 0) red_s[wave] = s, red_s1[wave] = s1;
-    __syncthreads();
-    s = s1 = 0.0f;
+}
+
+// Writes the gradient of logits that are not listed; a register that is done with is filled from the next row.
+template <Second SECOND>
+__device__ __forceinline__ float one_grad(const DistillParams& p, float d, float soft, float hard) {
+    const float w = power(d, p.scale);
+    if constexpr (SECOND == kNone) return soft * w;
+    if constexpr (SECOND == kSquare) return w * fmaf(-hard, w, soft);
+    return fmaf(-hard, power(d, p.scale1), soft * w);
+}
+template <Second SECOND, typename T, int THREADS, int NV>
+__device__ __forceinline__ void write_grad(const DistillParams& p, Held<T, THREADS, NV>& h, const Coefs& c, T* d, const T* next, int length, float g_loss, float g_hard) {
+    constexpr int N = Vec<T>::kN;
+    const float hard = g_hard * c.hard, soft = SECOND == kNone ? g_loss * c.others - hard : g_loss * c.others;    // factors of at most about one
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) s += red_s[w], s1 += red_s1[w];
-    keep_packed(v);
-    const Sums u{m, s, two ? s1 : s};
-    if (!whole) {
+    for (int j = 0; j < NV; ++j) {
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = one_grad<SECOND>(p, Vec<T>::get(h.v[j], e) - c.base, soft, hard);
+        if ((int)threadIdx.x < length / N - j * THREADS) *(u4any*)((char*)d + (size_t)j * THREADS * 16 + threadIdx.x * 16u) = Vec<T>::pack(x);
+        if (next) Held<T, THREADS, NV>::load_one(h.v[j], j, next, length);
+        __builtin_amdgcn_sched_barrier(0);       // registers
+    }
+    if ((int)threadIdx.x < length % N) store1(d + length / N * N + threadIdx.x, one_grad<SECOND>(p, h.tail - c.base, soft, hard));
+    if (next) h.load_tail(next, length);
+}
+// The teacher's side of whole rows, a wavefront for each: lists' sums, q and logits go to the workspace.  In a kernel of its own, since fp64
+// functions take the registers that hold rows.
+template <typename T>
+__global__ __launch_bounds__(256) void distill_list_kernel(DistillParams p) {
+    __shared__ __align__(16) List lists[4];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+    if (row >= p.rows) return;
+    List& l = lists[wave];
+    Teacher t;
+    read_list<T>(p, l, t, row, (const T*)p.logits + row * p.row_stride);
+    weigh(p, l, t, row);
+    if (lane == 0) ((Teacher*)p.teachers)[row] = t;
+    for (int i = lane; i < p.k; i += 64) p.list_q[row * p.k + i] = l.q[i], p.list_z[row * p.k + i] = l.z[i];
+}
+// ... and its end, a lane for each row.
+__global__ __launch_bounds__(64) void distill_loss_kernel(DistillParams p) {
+    const int64_t row = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    if (row >= p.rows) return;
+    const Teacher t = ((const Teacher*)p.teachers)[row];
+    const float* in = p.part_sums + 3 * row;
+    const Sums u{in[0], in[1], in[2]};
+    finish_row(p, t, u, coefs(p, u, t), row);
+}
+
+// Whole rows: a workgroup takes every gridDim.x-th, and reads the next one while it writes the gradient of this.  Parts of rows: one each.
+template <typename T, int THREADS, int NV, Second SECOND>
+__global__ __launch_bounds__(THREADS, 4) void distill_kernel(DistillParams p) {
+    constexpr int WAVES = THREADS / 64;
+    extern __shared__ unsigned bits[];
+    __shared__ float red_m[WAVES], red_s[WAVES], red_s1[WAVES];
+    const int part = blockIdx.y, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t start = (int64_t)part * p.part, end = min(start + p.part, p.vocab);
+    const int length = (int)(end - start);
+    const bool whole = p.parts == 1;
+    Held<T, THREADS, NV> h;
+    h.load((const T*)p.logits + (int64_t)blockIdx.x * p.row_stride + start, length);
+    if (p.rest)
+        for (int i = threadIdx.x; i < (length + 31) / 32; i += THREADS) bits[i] = 0;
+    auto place = [&](int64_t row) {            // of the lane's entry of a list; no list is longer than a workgroup
+        if ((int)threadIdx.x >= p.k || row >= p.rows) return -1;
+        const int at = p.index[row * p.k + threadIdx.x];
+        return at >= start && at < end ? (int)(at - start) : -1;
+    };
+    int at = place(blockIdx.x);
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        if (p.rest) {
+            __syncthreads();                   // the bits are clear
+            if (at >= 0) atomicOr(&bits[at / 32], 1u << (at % 32));
+            __syncthreads();
+            h.strike(bits, length);
+        }
+        float m = wave_max(h.largest());
+        keep_packed(h.v);
+        if (lane == 0) red_m[wave] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, red_m[w]);
+        float s = 0.0f, s1 = 0.0f;
+        add_up<SECOND>(p, h, m == -INFINITY ? 0.0f : m, s, s1);
+        keep_packed(h.v);
+        s = wave_sum(s), s1 = wave_sum(s1);
+        if (lane == 0) red_s[wave] = s, red_s1[wave] = s1;
+        __syncthreads();
+        s = s1 = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) s += red_s[w], s1 += red_s1[w];
+        const Sums u{m, s, SECOND == kNone ? s : s1};
         if (threadIdx.x == 0) {
             float* o = p.part_sums + 3 * (row * p.parts + part);
             o[0] = u.m, o[1] = u.s, o[2] = u.s1;
         }
-        return;
+        if (!whole || !p.d_logits) return;     // without a gradient there is a workgroup for each row
+        const T* next = row + gridDim.x < p.rows ? (const T*)p.logits + (row + gridDim.x) * p.row_stride : nullptr;
+        const int next_at = place(row + gridDim.x);
+        const Teacher& t = ((const Teacher*)p.teachers)[row];
+        const Coefs c = coefs(p, u, t);
+        const float g_loss = p.g_loss ? p.g_loss[row] * p.temperature : 0.0f, g_hard = t.target >= 0 && p.g_logprob ? p.g_logprob[row] : 0.0f;
+        T* d = (T*)p.d_logits + row * p.d_stride;
+        const float entry_q = at >= 0 ? p.list_q[row * p.k + threadIdx.x] : 0.0f, entry_z = at >= 0 ? p.list_z[row * p.k + threadIdx.x] : 0.0f;
+        write_grad<SECOND>(p, h, c, d, next, length, g_loss, g_hard);
+        __syncthreads();                   // the list and the target are written over
+        if (at >= 0) {
+            float q = entry_q;
+            if (t.twice) {
+                q = 0.0f;
+                for (int j = 0; j < p.k; ++j) q += p.index[row * p.k + j] == at ? p.list_q[row * p.k + j] : 0.0f;
+            }
+            store1(d + at, entry_grad(p, c, entry_z, true, q, at == t.target, g_loss, g_hard));
+        }
+        if (threadIdx.x == 0 && t.target >= 0 && !t.target_listed) store1(d + t.target, entry_grad(p, c, t.z_target, false, 0.0f, true, g_loss, g_hard));
+        if (p.rest && at >= 0) bits[at / 32] = 0;
+        at = next_at;
     }
-    const Coefs c = coefs(p, u, listed, list_w, list_rest);
-    if (wave == 0) finish_row(p, list, teacher, u, c, row);
-    if (!p.d_logits) return;
-    const float g_loss = p.g_loss ? p.g_loss[row] * p.temperature : 0.0f, g_hard = list.index[p.k] >= 0 && p.g_logprob ? p.g_logprob[row] : 0.0f;
-    T* d = (T*)p.d_logits + row * p.d_stride;
-    write_grad<T, NV, THREADS>(p, v, c, d, start, end, g_loss, g_hard);
-    __syncthreads();
-    for (int i = threadIdx.x; i <= p.k; i += THREADS)
-        if (list.index[i] >= 0 && !(i == p.k && list.target_listed)) store1(d + list.index[i], entry_grad(p, list, c, i, g_loss, g_hard));
 }
 
-// Joins the parts of a row and finishes it.
-template <typename T>
-__global__ __launch_bounds__(64) void distill_join_kernel(DistillParams p) {
-    __shared__ List list;
-    const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x;
-    const float* in = p.part_sums + 3 * row * p.parts;
-    Sums a{-INFINITY, 0.0f, 0.0f};
-    for (int i = lane; i < p.parts; i += 64) a = join(p, a, Sums{in[3 * i], in[3 * i + 1], in[3 * i + 2]});
-    for (int o = 32; o; o >>= 1) {
-        const Sums b{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.s1, o)};
-        a = lane & o ? join(p, b, a) : join(p, a, b);       // the same order in every lane
-    }
-    read_list<T>(p, list, row, (const T*)p.logits + row * p.row_stride, 0, p.vocab);
-    in_wave_order();
-    const Teacher teacher = weigh(p, list, row);
-    in_wave_order();
-    Sums l{-INFINITY, 0.0f, 0.0f};
-    if (p.rest) l = sum_list(p, list, a.m, true);
-    const Coefs c = coefs(p, a, l, (float)teacher.w, (float)teacher.rest);
-    finish_row(p, list, teacher, a, c, row);
-}
-
-// The gradient from the logits and what the forward call left.
-template <typename T>
-__global__ __launch_bounds__(256) void distill_grad_kernel(DistillParams p) {
-    constexpr int N = Vec<T>::kN, NV = 4, kSpan = 256 * N * NV;
-    __shared__ unsigned bits[kSpan / 32];
-    __shared__ List list;
+// The rest of a call behind the parts, with JOIN: every workgroup joins the parts of its row, the first one writes its results, and all write
+// their logits' gradient.  Otherwise the gradient from what an earlier call left.
+template <typename T, bool JOIN>
+__global__ __launch_bounds__(256) void distill_finish_kernel(DistillParams p) {
+    constexpr int NV = 4, kSpan = 256 * Vec<T>::kN * NV;
+    __shared__ __align__(16) List list;
+    __shared__ Coefs shared;
+    __shared__ int listed, twice;
     const int64_t row = blockIdx.x;
     const T* z = (const T*)p.logits + row * p.row_stride;
-    T* d = (T*)p.d_logits + row * p.d_stride;
+    T* d = p.d_logits ? (T*)p.d_logits + row * p.d_stride : nullptr;
     const int64_t start = (int64_t)blockIdx.y * kSpan, end = min(start + kSpan, p.vocab);
-    u4 v[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = load_vec<T>(z, start + (j * 256 + threadIdx.x) * N, end);
-    for (int i = threadIdx.x; i < kSpan / 32; i += 256) bits[i] = 0;
-    __syncthreads();
+    const int length = (int)(end - start), lane = threadIdx.x;
+    Held<T, 256, NV> h;
+    if (d) h.load(z + start, length);
     const float* in = p.stats + 8 * row;
-    if (threadIdx.x < 64) {
-        read_list<T>(p, list, row, z, start, end);
-        in_wave_order();
-        mark(p, list, bits, start);
-        const float top = in[6], scale = in[7], inv_t = p.rest ? 1.0f : 1.0f / p.temperature;
-        for (int i = threadIdx.x; i < p.k; i += 64) {
-            const float q = expf((p.value[row * p.k + i] - top) * inv_t) * scale;
-            list.q[i] = list.index[i] < 0 || scale == 0.0f ? 0.0f : q;
+    if (lane < 64) {
+        Teacher t;
+        read_list<T>(p, list, t, row, z);
+        if constexpr (JOIN) {
+            const float* sums = p.part_sums + 3 * row * p.parts;
+            Sums a{-INFINITY, 0.0f, 0.0f};
+            for (int i = lane; i < p.parts; i += 64) a = join(p, a, Sums{sums[3 * i], sums[3 * i + 1], sums[3 * i + 2]});
+            for (int o = 32; o; o >>= 1) {
+                const Sums b{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.s1, o)};
+                a = lane & o ? join(p, b, a) : join(p, a, b);       // the same order in every lane
+            }
+            weigh(p, list, t, row);
+            const Coefs c = coefs(p, a, t);
+            if (lane == 0) {
+                if (blockIdx.y == 0) finish_row(p, t, a, c, row);
+                shared = c, listed = t.target_listed, twice = t.twice;
+            }
+        } else {
+            const float top = in[6], scale = in[7], inv_t = p.rest ? 1.0f : 1.0f / p.temperature;
+            for (int i = lane; i < p.k; i += 64) {
+                const float q = expf((p.value[row * p.k + i] - top) * inv_t) * scale;
+                list.q[i] = list.index[i] < 0 || scale == 0.0f ? 0.0f : q;
+            }
+            if (lane == 0) {
+                Coefs c = {};
+                c.base = in[0], c.others = in[1], c.hard = in[2], c.m = in[3], c.listed = in[4], c.inv_s1 = in[5], c.empty = c.inv_s1 == 0.0f;
+                shared = c, listed = t.target_listed, twice = 1;
+            }
         }
     }
-    Coefs c = {};
-    c.base = in[0], c.others = in[1], c.hard = in[2], c.m = in[3], c.listed = in[4], c.inv_s1 = in[5];
-    c.empty = c.inv_s1 == 0.0f;
+    if (!d) return;
     const int target = p.targets ? p.targets[row] : -1;
+    const bool has_target = target >= start && target < end;
+    const float z_target = has_target ? load1(z + target) : 0.0f;
     const float g_loss = p.g_loss ? p.g_loss[row] * p.temperature : 0.0f;
     const float g_hard = target >= 0 && target < p.vocab && p.g_logprob ? p.g_logprob[row] : 0.0f;
-    __syncthreads();                       // every logit of the list is read: the gradient may lie on them
-    write_grad<T, NV, 256>(p, v, c, d, start, end, g_loss, g_hard);
+    __syncthreads();                           // every logit of the list is read: the gradient may lie on them
+    const Coefs c = shared;
+    const Second second = second_of(p);
+    if (second == kNone) write_grad<kNone>(p, h, c, d + start, (const T*)nullptr, length, g_loss, g_hard);
+    else if (second == kSquare) write_grad<kSquare>(p, h, c, d + start, (const T*)nullptr, length, g_loss, g_hard);
+    else write_grad<kOther>(p, h, c, d + start, (const T*)nullptr, length, g_loss, g_hard);
     __syncthreads();
-    for (int i = threadIdx.x; i <= p.k; i += 256)
-        if (list.index[i] >= 0 && !(i == p.k && list.target_listed)) store1(d + list.index[i], entry_grad(p, list, c, i, g_loss, g_hard));
+    for (int i = lane; i < p.k; i += 256) {
+        const int at = list.index[i];
+        if (at < start || at >= end) continue;
+        float q = list.q[i];
+        if (twice) {
+            q = 0.0f;
+            for (int j = 0; j < p.k; ++j) q += list.index[j] == at ? list.q[j] : 0.0f;
+        }
+        store1(d + at, entry_grad(p, c, list.z[i], true, q, at == target, g_loss, g_hard));
+    }
+    if (lane == 0 && has_target && !listed) store1(d + target, entry_grad(p, c, z_target, false, 0.0f, true, g_loss, g_hard));
 }
 
 template <typename T, int THREADS, int NV>
 hipError_t launch_rows(const DistillParams& p, hipStream_t stream) {
-    distill_kernel<T, THREADS, NV><<<dim3((unsigned)p.rows, p.parts), THREADS, (size_t)((p.part + 31) / 32) * 4, stream>>>(p);
+    const int64_t fill = (int64_t)256 * (1024 / THREADS) * (NV <= 4 ? 2 : 1);     // workgroups that run beside each other
+    const dim3 grid((unsigned)(p.parts > 1 || !p.d_logits ? p.rows : std::min(p.rows, fill)), p.parts);
+    const size_t lds = p.rest ? (size_t)((p.part + 31) / 32) * 4 : 0;
+    const Second second = second_of(p);
+    if (second == kNone) distill_kernel<T, THREADS, NV, kNone><<<grid, THREADS, lds, stream>>>(p);
+    else if (second == kSquare) distill_kernel<T, THREADS, NV, kSquare><<<grid, THREADS, lds, stream>>>(p);
+    else distill_kernel<T, THREADS, NV, kOther><<<grid, THREADS, lds, stream>>>(p);
     return hipGetLastError();
 }
 template <typename T, int NV>
@@ -455,42 +477,34 @@ DistillParams rows_of(const DistillParams& p, int64_t first) {
     return q;
 }
 
-template <typename T>
-hipError_t launch_grad_typed(const DistillParams& p, hipStream_t stream) {
+template <typename T, bool JOIN>
+hipError_t launch_finish(const DistillParams& p, hipStream_t stream) {
     const int64_t span = 256 * 4 * Vec<T>::kN;
-    distill_grad_kernel<T><<<dim3((unsigned)p.rows, (unsigned)((p.vocab + span - 1) / span)), 256, 0, stream>>>(p);
+    distill_finish_kernel<T, JOIN><<<dim3((unsigned)p.rows, p.d_logits ? (unsigned)((p.vocab + span - 1) / span) : 1), 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 
-// log2 e / T as hi + lo, both positive
-void split_exponent(double x, float& hi, float& lo) {
-    hi = (float)x;
-    if ((double)hi >= x) hi = nextafterf(hi, 0.0f);
-    lo = (float)(x - (double)hi);
-}
 DistillParams with_exponents(DistillParams p) {
     constexpr double kLog2 = 1.4426950408889634074;
-    split_exponent(kLog2 / (double)p.temperature, p.hi, p.lo);
-    split_exponent(kLog2, p.hi1, p.lo1);
+    p.scale = (float)(kLog2 / (double)p.temperature), p.scale1 = (float)kLog2;
     return p;
-}
-
-hipError_t grad_rows(const DistillParams& p, hipStream_t stream) {
-    return p.dtype == OLS_F32 ? launch_grad_typed<float>(p, stream) : launch_grad_typed<uint16_t>(p, stream);
 }
 
 }  // namespace
 
-int64_t distill_workspace_bytes(int dtype, int64_t rows, int64_t vocab) {
+// Whole rows: of each what its list adds up to, q and z, and the sums.  Parts: their sums.
+int64_t distill_workspace_bytes(int dtype, int64_t rows, int64_t vocab, int k) {
     if (rows == 0) return 0;
     const RowPlan r = row_plan(dtype, rows, vocab);
-    return r.parts > 1 ? std::min(kMostRows, rows) * r.parts * 12 : 0;
+    rows = std::min(kMostRows, rows);
+    return rows * (r.parts > 1 ? r.parts * 12 : (int64_t)sizeof(Teacher) + 12 + 8 * k);
 }
 
 hipError_t launch_distill_grad(const DistillParams& params, hipStream_t stream) {
     const DistillParams p = with_exponents(params);
     for (int64_t first = 0; first < p.rows; first += kMostRows) {
-        const hipError_t e = grad_rows(rows_of(p, first), stream);
+        const DistillParams q = rows_of(p, first);
+        const hipError_t e = q.dtype == OLS_F32 ? launch_finish<float, false>(q, stream) : launch_finish<uint16_t, false>(q, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -500,15 +514,27 @@ hipError_t launch_distill(const DistillParams& params, void* ws, hipStream_t str
     if (params.rows == 0) return hipSuccess;
     DistillParams p = with_exponents(params);
     const RowPlan r = row_plan(p.dtype, p.rows, p.vocab);
-    p.parts = r.parts, p.part = r.part, p.part_sums = (float*)ws;      // one launch's parts after another's in the same place
+    p.parts = r.parts, p.part = r.part;
     for (int64_t first = 0; first < p.rows; first += kMostRows) {
-        const DistillParams q = rows_of(p, first);
-        hipError_t e = q.dtype == OLS_F32 ? launch_typed<float>(q, r, stream) : launch_typed<uint16_t>(q, r, stream);
-        if (e == hipSuccess && r.parts > 1) {
-            if (q.dtype == OLS_F32) distill_join_kernel<float><<<(unsigned)q.rows, 64, 0, stream>>>(q);
-            else distill_join_kernel<uint16_t><<<(unsigned)q.rows, 64, 0, stream>>>(q);
+        DistillParams q = rows_of(p, first);                           // one launch's rows after another's in the same place
+        hipError_t e = hipSuccess;
+        if (r.parts > 1) {
+            q.part_sums = (float*)ws;
+        } else {
+            q.teachers = ws;
+            q.part_sums = (float*)((char*)ws + q.rows * sizeof(Teacher)), q.list_q = q.part_sums + 3 * q.rows, q.list_z = q.list_q + q.rows * q.k;
+            const unsigned blocks = (unsigned)((q.rows + 3) / 4);
+            if (q.dtype == OLS_F32) distill_list_kernel<float><<<blocks, 256, 0, stream>>>(q);
+            else distill_list_kernel<uint16_t><<<blocks, 256, 0, stream>>>(q);
             e = hipGetLastError();
-            if (e == hipSuccess && q.d_logits) e = grad_rows(q, stream);
+        }
+        if (e == hipSuccess) e = q.dtype == OLS_F32 ? launch_typed<float>(q, r, stream) : launch_typed<uint16_t>(q, r, stream);
+        if (e != hipSuccess) return e;
+        if (r.parts > 1) {
+            e = q.dtype == OLS_F32 ? launch_finish<float, true>(q, stream) : launch_finish<uint16_t, true>(q, stream);
+        } else {
+            distill_loss_kernel<<<(unsigned)((q.rows + 63) / 64), 64, 0, stream>>>(q);
+            e = hipGetLastError();
         }
         if (e != hipSuccess) return e;
     }

@@ -540,10 +540,11 @@ struct DistillParams {
     // set by the launcher
     int parts;
     int64_t part;
-    float* part_sums;
-    float hi, lo, hi1, lo1;              // log2 e / temperature and log2 e, each in two terms
+    void* teachers;
+    float *part_sums, *list_q, *list_z;
+    float scale, scale1;                 // log2 e / temperature and log2 e
 };
-int64_t distill_workspace_bytes(int dtype, int64_t rows, int64_t vocab);
+int64_t distill_workspace_bytes(int dtype, int64_t rows, int64_t vocab, int k);
 hipError_t launch_distill(const DistillParams& p, void* ws, hipStream_t stream);     // with d_logits: the gradient as well
 hipError_t launch_distill_grad(const DistillParams& p, hipStream_t stream);          // from p.stats
 

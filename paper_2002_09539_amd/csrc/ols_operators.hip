@@ -473,11 +473,12 @@ int ols_clip_gradients(int n, const void* const* in_dev, void* const* out_dev, c
     return done(e, who);
 }
 
-int64_t ols_distill_workspace_bytes(int64_t rows, int64_t vocab, int dtype) {
+int64_t ols_distill_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int k) {
     const char* who = "ols_distill_workspace_bytes";
     if (const int rc = check_logprob(who, dtype, 0, vocab, nullptr, vocab, nullptr)) return rc;
     if (rows < 0 || rows > 0x7fffffff) return bad("%s: rows must be in [0, 2^31), got %lld", who, (long long)rows);
-    return distill_workspace_bytes(dtype, rows, vocab);
+    if (k < 1 || k > OLS_MAX_TEACHER) return bad("%s: k must be in [1, %d], got %d", who, OLS_MAX_TEACHER, k);
+    return distill_workspace_bytes(dtype, rows, vocab, k);
 }
 
 int ols_distill_loss(const ols_distill* d, void* stream) {
@@ -485,7 +486,7 @@ int ols_distill_loss(const ols_distill* d, void* stream) {
     if (const int rc = check_distill(who, d)) return rc;
     if (d->rows == 0) return OLS_OK;
     if (!d->loss || (d->targets && !d->logprob)) return bad("%s: null result", who);
-    if (const int rc = check_ws(who, d->ws, d->ws_bytes, distill_workspace_bytes(d->dtype, d->rows, d->vocab))) return rc;
+    if (const int rc = check_ws(who, d->ws, d->ws_bytes, distill_workspace_bytes(d->dtype, d->rows, d->vocab, d->k))) return rc;
     DistillParams p = distill_params(*d);
     if (!d->targets) p.logprob = nullptr;
     return done(launch_distill(p, d->ws, (hipStream_t)stream), who);

@@ -448,7 +448,7 @@ def _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperatu
 
 def _distill_loss(logits, top_value, top_index, targets, d_loss, d_logprob, temperature, rest, d_logits):
     d, shape, device, keep = _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperature, rest, d_logits)
-    d.ws_bytes = B.ols_distill_workspace_bytes(d.rows, d.vocab, d.dtype)
+    d.ws_bytes = B.ols_distill_workspace_bytes(d.rows, d.vocab, d.dtype, d.k)
     with _on(device):
         ws = _workspace(d.ws_bytes, device)
         loss = torch.empty(shape, dtype=torch.float32, device=device)

@@ -46,11 +46,13 @@ def test_distill_grad_refuses(change):
 
 def test_distill_workspace_and_no_rows():
     bytes_of = B.ols_distill_workspace_bytes
-    assert bytes_of(0, 100, F32) == 0 and bytes_of(4096, 50000, BF16) == 0 and bytes_of(1, 1 << 24, BF16) > 0
-    refused(lambda: bytes_of(-1, 100, F32))
-    refused(lambda: bytes_of(1, 0, F32))
-    refused(lambda: bytes_of(1, 10, I8))
-    need = bytes_of(1, 1 << 17, F32)
+    assert bytes_of(0, 100, F32, 4) == 0 and bytes_of(1, 1 << 24, BF16, 4) > 0 and 0 < bytes_of(4096, 50000, BF16, 64) < 4096 * 1024
+    refused(lambda: bytes_of(-1, 100, F32, 4))
+    refused(lambda: bytes_of(1, 0, F32, 4))
+    refused(lambda: bytes_of(1, 10, I8, 4))
+    refused(lambda: bytes_of(1, 10, F32, 0))
+    refused(lambda: bytes_of(1, 10, F32, 257))
+    need = bytes_of(1, 1 << 17, F32, 4)
     few = dict(rows=1, vocab=1 << 17, row_stride=1 << 17, d_stride=1 << 17)
     refused(lambda: B.ols_distill_loss(filled(B.ols_distill, DISTILL, dict(**few, ws_bytes=need - 1)), None), B.OLS_ENOMEM, str(need))
     refused(lambda: B.ols_distill_loss(filled(B.ols_distill, DISTILL, dict(**few, ws=None)), None), B.OLS_ENOMEM)
