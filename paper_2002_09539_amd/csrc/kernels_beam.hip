@@ -83,104 +83,131 @@ __global__ __launch_bounds__(THREADS, 4) void beam_part_kernel(BeamParams p) {
     for (int i = threadIdx.x; i < p.beams; i += THREADS) p.part_val[slot * p.beams + i] = best_val[i], p.part_idx[slot * p.beams + i] = best_idx[i];
 }
 
-// Largest first; a lane's candidate is one of its lists' heads.
-struct Head {
-    double key;
-    int list;               // -1: none
-};
-__device__ __forceinline__ bool before(const Head& a, const Head& b) { return a.list >= 0 && (b.list < 0 || a.key > b.key || (a.key == b.key && a.list < b.list)); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved_or_own(double v) {
+    const unsigned long long b = __double_as_longlong(v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp((int)(unsigned)b, (int)(unsigned)b, CTRL, ROWS, 0xf, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp((int)(unsigned)(b >> 32), (int)(unsigned)(b >> 32), CTRL, ROWS, 0xf, false);
+    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+__device__ __forceinline__ double lane_of(double v, int lane) {
+    const unsigned long long b = __double_as_longlong(v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)b, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(b >> 32), lane);
+    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+__device__ __forceinline__ double wave_max(double v) {
+    v = fmax(v, moved_or_own<0x111, 0xf>(v));
+    v = fmax(v, moved_or_own<0x112, 0xf>(v));
+    v = fmax(v, moved_or_own<0x114, 0xf>(v));
+    v = fmax(v, moved_or_own<0x118, 0xf>(v));
+    v = fmax(v, moved_or_own<0x142, 0xa>(v));
+    v = fmax(v, moved_or_own<0x143, 0xc>(v));
+    return lane_of(v, 63);
+}
 
-// One wavefront for each request.
-__global__ __launch_bounds__(64) void beam_join_kernel(BeamParams p) {
-    // Of a hypothesis: what comes to a logit's distance from the largest (-inf: it has no candidates), that one, and length^penalty.
-    __shared__ double lead[kMaxTop], sums[kMaxTop], scale[kMaxTop];
-    __shared__ float tops[kMaxTop];
-    extern __shared__ uint16_t used[];                        // of each list: how many are taken
+// What is known of a hypothesis.
+struct Hypothesis {
+    double lead, scale, sum;   // what comes to a logit's distance from the largest (-inf: it has no candidates), length^penalty, sum of e^{z - top}
+    float top;
+    int length, ended;
+};
+
+// A workgroup for each request: its wavefronts add up the parts, then one merges the parts' lists, each in order; a lane looks after every
+// 64th.  LISTS: they lie in LDS.
+template <bool LISTS>
+__global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
+    __shared__ Hypothesis of[kMaxTop];
+    extern __shared__ __align__(8) char dyn[];
     const int64_t batch = blockIdx.x;
-    const int lane = threadIdx.x, lists = p.in_beams * p.parts, k = p.beams;
-    for (int i = 0; i < p.in_beams && p.parts > 1; ++i) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, k = p.beams, lists = p.in_beams * p.parts, entries = lists * k;
+    uint8_t* used = (uint8_t*)dyn;                            // of each list: how many are taken
+    const float* val = p.part_val + batch * entries;
+    const int* idx = p.part_idx + batch * entries;
+    for (int l = threadIdx.x; l < lists; l += 256) used[l] = 0;
+    if constexpr (LISTS) {
+        float* v = (float*)(dyn + (lists + 7) / 8 * 8);
+        int* at = (int*)(v + entries);
+        for (int i = threadIdx.x; i < entries; i += 256) v[i] = val[i], at[i] = idx[i];
+        val = v, idx = at;
+    }
+    for (int i = wave; i < p.in_beams; i += 4) {
         const int64_t row = batch * p.in_beams + i;
         if (!goes_on(p, row)) continue;
         float m = -INFINITY;
         for (int j = lane; j < p.parts; j += 64) m = fmaxf(m, p.part_m[row * p.parts + j]);
-        m = wave_max(m);
+        m = ols::wave_max(m);
         const double base = m == -INFINITY ? 0.0 : (double)m;
         double sum = 0.0;
         for (int j = lane; j < p.parts; j += 64) sum += p.part_s[row * p.parts + j] * exp((double)p.part_m[row * p.parts + j] - base);
         sum = wave_sum(sum);
-        if (lane == 0) tops[i] = m, sums[i] = sum;
+        if (lane == 0) of[i].top = m, of[i].sum = sum;
     }
-    in_wave_order();
+    __syncthreads();
+    if (wave) return;
     bool bad = false;
     if (lane < p.in_beams) {
+        Hypothesis& h = of[lane];
         const int64_t row = batch * p.in_beams + lane;
         const float score = p.score[row];
         const bool dead = score == -INFINITY, ended = !dead && !goes_on(p, row);
-        if (p.parts == 1 && !dead && !ended) tops[lane] = p.part_m[row], sums[lane] = p.part_s[row];
-        const double sum = dead || ended ? 1.0 : sums[lane];
+        const double sum = dead || ended ? 1.0 : h.sum;
         bad = !dead && (!(score < INFINITY) || !(sum < INFINITY));
-        lead[lane] = dead || !(sum > 0.0) ? (double)-INFINITY : (double)score - log(sum);
-        const int before = p.length ? p.length[row] : 0, after = ended ? before : before + 1;
-        scale[lane] = p.penalty == 0.0 ? 1.0 : pow((double)max(after, 1), p.penalty);
+        h.lead = dead || !(sum > 0.0) ? (double)-INFINITY : (double)score - log(sum);
+        h.ended = ended, h.length = p.length ? p.length[row] : 0;
+        h.scale = p.penalty == 0.0 ? 1.0 : exp(p.penalty * log((double)max(ended ? h.length : h.length + 1, 1)));     // pow takes 4 us
     }
     const bool poisoned = __ballot(bad) != 0;
-    for (int l = lane; l < lists; l += 64) used[l] = 0;
     in_wave_order();
-    // value and key of the head of list l
-    auto value_of = [&](int l, int& token) {
-        const int i = l / p.parts, at = used[l];
-        const int64_t row = batch * p.in_beams + i, slot = batch * lists + l;
-        token = -1;
-        if (lead[i] == -INFINITY || at >= k) return (double)-INFINITY;
-        if (p.finished && p.finished[row]) {
-            if (at > 0 || l % p.parts) return (double)-INFINITY;
-            token = 0;
-            return lead[i];
-        }
-        token = p.part_idx[slot * k + at];
-        return token < 0 ? (double)-INFINITY : lead[i] + ((double)p.part_val[slot * k + at] - (double)tops[i]);
+    // Token of the head of list l, -1 where there is none, and its value.
+    auto token_of = [&](int l) {
+        const Hypothesis& h = of[l / p.parts];
+        const int at = used[l];
+        if (h.lead == -INFINITY || at >= k) return -1;
+        if (h.ended) return at == 0 && l % p.parts == 0 ? 0 : -1;
+        return idx[l * k + at];
     };
-    auto head_of = [&](int l) {
-        int token;
-        const double v = value_of(l, token);
-        return token < 0 ? Head{0.0, -1} : Head{v / scale[l / p.parts], l};
+    auto value_of = [&](int l) {
+        const Hypothesis& h = of[l / p.parts];
+        return h.ended ? h.lead : h.lead + ((double)val[l * k + used[l]] - (double)h.top);
     };
-    auto best_of = [&]() {
-        Head h{0.0, -1};
+    int list = -1;                                            // of the lane's lists the one whose head is first
+    double key = -INFINITY;
+    auto look = [&]() {
+        list = -1, key = -INFINITY;
         for (int l = lane; l < lists; l += 64) {
-            const Head g = head_of(l);
-            if (before(g, h)) h = g;
+            if (token_of(l) < 0) continue;
+            const double v = value_of(l) / of[l / p.parts].scale;
+            if (list < 0 || v > key) list = l, key = v;       // ties: the lower list
         }
-        return h;
     };
-    Head mine = best_of();
-    for (int turn = 0; turn < k; ++turn) {
-        Head h = mine;
-        for (int o = 32; o; o >>= 1) {
-            const Head g{__shfl_xor(h.key, o), __shfl_xor(h.list, o)};
-            if (before(g, h)) h = g;
-        }
-        const int64_t out = batch * k + turn;
-        if (poisoned || h.list < 0) {
-            if (lane == 0) {
-                const int slot = turn < p.in_beams ? turn : 0;
-                p.new_score[out] = poisoned ? NAN : -INFINITY, p.token[out] = -1, p.parent[out] = slot, p.new_finished[out] = 0;
-                if (p.new_length) p.new_length[out] = p.length[batch * p.in_beams + slot];
-            }
-            continue;
-        }
-        if (h.list % 64 == lane) {
-            int token;
-            const double v = value_of(h.list, token);
-            const int i = h.list / p.parts;
-            const int64_t row = batch * p.in_beams + i;
-            const bool ended = p.finished && p.finished[row];
-            p.new_score[out] = (float)v, p.token[out] = ended ? p.eos : token, p.parent[out] = i;
-            p.new_finished[out] = ended || (p.eos >= 0 && token == p.eos);
-            if (p.new_length) p.new_length[out] = p.length[row] + (ended ? 0 : 1);
-            used[h.list] += 1;
-            mine = best_of();
-        }
+    look();
+    // Of place `lane` of the result.
+    int from = -1, token = -1;
+    double value = 0.0;
+    for (int turn = 0; turn < k && !poisoned; ++turn) {
+        const double best = wave_max(key);
+        const unsigned long long at = __ballot(list >= 0 && key == best);
+        if (!at) break;
+        int first = __builtin_amdgcn_readlane(list, __ffsll(at) - 1);
+        for (unsigned long long more = at & (at - 1); more; more &= more - 1) first = min(first, __builtin_amdgcn_readlane(list, __ffsll(more) - 1));
+        const int said = token_of(first);
+        const double v = value_of(first);
+        if (lane == turn) from = first, token = said, value = v;
+        in_wave_order();
+        if (first % 64 == lane) used[first] += 1, look();
+        in_wave_order();
+    }
+    if (lane >= k) return;
+    const int64_t out = batch * k + lane;
+    if (from < 0) {
+        const int slot = lane < p.in_beams ? lane : 0;
+        p.new_score[out] = poisoned ? NAN : -INFINITY, p.token[out] = -1, p.parent[out] = slot, p.new_finished[out] = 0;
+        if (p.new_length) p.new_length[out] = of[slot].length;
+    } else {
+        const Hypothesis& h = of[from / p.parts];
+        p.new_score[out] = (float)value, p.token[out] = h.ended ? p.eos : token, p.parent[out] = from / p.parts;
+        p.new_finished[out] = h.ended || (p.eos >= 0 && token == p.eos);
+        if (p.new_length) p.new_length[out] = h.length + (h.ended ? 0 : 1);
     }
 }
 
@@ -190,35 +217,60 @@ hipError_t launch_rows(const BeamParams& p, hipStream_t stream) {
     beam_part_kernel<T, THREADS, NV><<<dim3((unsigned)(p.batch * p.in_beams), p.parts), THREADS, lds, stream>>>(p);
     return hipGetLastError();
 }
-template <typename T, int NV>
-hipError_t launch_long(const BeamParams& p, const RowPlan& r, hipStream_t stream) {
-    if (r.threads == 256) return launch_rows<T, 256, NV>(p, stream);
-    return r.threads == 512 ? launch_rows<T, 512, NV>(p, stream) : launch_rows<T, 1024, NV>(p, stream);
-}
 template <typename T>
 hipError_t launch_typed(const BeamParams& p, const RowPlan& r, hipStream_t stream) {
-    if (r.threads == 256) {
-        if (r.nv == 2) return launch_rows<T, 256, 2>(p, stream);
-        if (r.nv == 4) return launch_rows<T, 256, 4>(p, stream);
-        if (r.nv == 8) return launch_rows<T, 256, 8>(p, stream);
-    }
-    return r.nv <= 10 ? launch_long<T, 10>(p, r, stream) : r.nv == 13 ? launch_long<T, 13>(p, r, stream) : launch_long<T, 16>(p, r, stream);
+    if (r.nv == 2) return launch_rows<T, 256, 2>(p, stream);
+    if (r.nv == 4) return launch_rows<T, 256, 4>(p, stream);
+    if (r.nv == 8) return launch_rows<T, 256, 8>(p, stream);
+    return r.nv == 10 ? launch_rows<T, 256, 10>(p, stream) : r.nv == 13 ? launch_rows<T, 256, 13>(p, stream) : launch_rows<T, 256, 16>(p, stream);
 }
 
 // ---- states ---------------------------------------------------------------------------------------------------------------
 
-typedef unsigned int u4bytes __attribute__((ext_vector_type(4), aligned(1)));   // sixteen bytes at any address
+// BYTES at any address, of up to S hypotheses at once.  Places that are not written read the first row again.
+template <int BYTES>
+struct Piece;
+template <>
+struct Piece<16> {
+    typedef unsigned int type __attribute__((ext_vector_type(4), aligned(1)));
+};
+template <>
+struct Piece<8> {
+    typedef unsigned int type __attribute__((ext_vector_type(2), aligned(1)));
+};
+template <>
+struct Piece<4> {
+    typedef unsigned int type __attribute__((aligned(1)));
+};
+template <>
+struct Piece<2> {
+    typedef unsigned short type __attribute__((aligned(1)));
+};
+template <>
+struct Piece<1> {
+    typedef unsigned char type;
+};
+template <int BYTES, int S>
+struct Pieces {
+    typename Piece<BYTES>::type v[S];
+    __device__ void read(const char* src, int64_t row, const int (&from)[S]) {
+#pragma unroll
+        for (int i = 0; i < S; ++i) v[i] = *(const typename Piece<BYTES>::type*)(src + max(from[i], 0) * row);
+    }
+    __device__ void write(char* dst, int64_t row, const int (&from)[S]) const {
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+            if (from[i] >= 0) *(typename Piece<BYTES>::type*)(dst + i * row) = v[i];
+    }
+};
 
-// The pieces of up to S hypotheses at once in registers; the last piece of a row may be shorter.
+// A thread for each sixteen bytes of a request's rows; what is left of a row goes in pieces of eight, four, two and one, all read first.
 template <int S>
 __global__ __launch_bounds__(256) void beam_move_kernel(BeamMove t) {
     int k = 0;
     while (k + 1 < t.n && (int)blockIdx.x >= t.first_block[k + 1]) ++k;
     const int64_t batch = blockIdx.y, at = ((int64_t)(blockIdx.x - t.first_block[k]) * 256 + threadIdx.x) * 16, left = t.row_bytes[k] - at;
-    if (left <= 0) return;
     const int32_t* parent = t.parent + batch * t.out_beams;
-    const char* src = (const char*)t.src[k] + batch * t.src_batch[k] + at;
-    char* dst = (char*)t.dst[k] + batch * t.dst_batch[k] + at;
     const bool in_place = t.src[k] == t.dst[k];
     int from[S];
 #pragma unroll
@@ -226,40 +278,48 @@ __global__ __launch_bounds__(256) void beam_move_kernel(BeamMove t) {
         from[i] = i < t.out_beams ? parent[i] : -1;
         if (from[i] >= t.in_beams || (in_place && from[i] == i)) from[i] = -1;
     }
+    if (left <= 0) return;
+    const char* src = (const char*)t.src[k] + batch * t.src_batch[k] + at;
+    char* dst = (char*)t.dst[k] + batch * t.dst_batch[k] + at;
+    const int64_t src_row = t.src_beam[k], dst_row = t.dst_beam[k];
     if (left >= 16) {
-        u4 piece[S];
-#pragma unroll
-        for (int i = 0; i < S; ++i)
-            if (from[i] >= 0) piece[i] = *(const u4bytes*)(src + from[i] * t.src_beam[k]);
-#pragma unroll
-        for (int i = 0; i < S; ++i)
-            if (from[i] >= 0) *(u4bytes*)(dst + i * t.dst_beam[k]) = piece[i];
-    } else {
-        for (int b = 0; b < left; ++b) {
-            char piece[S];
-#pragma unroll
-            for (int i = 0; i < S; ++i)
-                if (from[i] >= 0) piece[i] = src[from[i] * t.src_beam[k] + b];
-#pragma unroll
-            for (int i = 0; i < S; ++i)
-                if (from[i] >= 0) dst[i * t.dst_beam[k] + b] = piece[i];
-        }
+        Pieces<16, S> p;
+        p.read(src, src_row, from);
+        p.write(dst, dst_row, from);
+        return;
     }
+    const int four = left & 8, two = four + (left & 4), one = two + (left & 2);      // where they begin
+    Pieces<8, S> p8;
+    Pieces<4, S> p4;
+    Pieces<2, S> p2;
+    Pieces<1, S> p1;
+    if (left & 8) p8.read(src, src_row, from);
+    if (left & 4) p4.read(src + four, src_row, from);
+    if (left & 2) p2.read(src + two, src_row, from);
+    if (left & 1) p1.read(src + one, src_row, from);
+    if (left & 8) p8.write(dst, dst_row, from);
+    if (left & 4) p4.write(dst + four, dst_row, from);
+    if (left & 2) p2.write(dst + two, dst_row, from);
+    if (left & 1) p1.write(dst + one, dst_row, from);
 }
 
 }  // namespace
+
+// Workgroups of four wavefronts: several run on a compute unit, and one's search for its best overlaps with another's loads.  512 rows of
+// 128 000 bf16 in workgroups that hold whole rows: 49 us.
+static RowPlan beam_plan(int dtype, int64_t rows, int64_t vocab) { return row_plan(dtype, rows, vocab, 256); }
 
 // All parts of a call lie in the workspace.
 int64_t beam_workspace_bytes(int dtype, int64_t batch, int in_beams, int beams, int64_t vocab) {
     if (batch == 0) return 0;
     const int64_t rows = batch * in_beams;
-    return rows * row_plan(dtype, rows, vocab).parts * (12 + 8 * (int64_t)beams);
+    return rows * beam_plan(dtype, rows, vocab).parts * (12 + 8 * (int64_t)beams);
 }
 
 hipError_t launch_beam(BeamParams p, void* ws, hipStream_t stream) {
     if (p.batch == 0) return hipSuccess;
     const int64_t rows = p.batch * p.in_beams;
-    const RowPlan r = row_plan(p.dtype, rows, p.vocab);
+    const RowPlan r = beam_plan(p.dtype, rows, p.vocab);
     p.parts = r.parts, p.part = r.part;
     p.part_s = (double*)ws;
     p.part_m = (float*)(p.part_s + rows * r.parts);
@@ -267,7 +327,9 @@ hipError_t launch_beam(BeamParams p, void* ws, hipStream_t stream) {
     p.part_idx = (int32_t*)(p.part_val + rows * r.parts * p.beams);
     hipError_t e = p.dtype == OLS_F32 ? launch_typed<float>(p, r, stream) : launch_typed<uint16_t>(p, r, stream);
     if (e != hipSuccess) return e;
-    beam_join_kernel<<<(unsigned)p.batch, 64, (size_t)p.in_beams * r.parts * 2, stream>>>(p);
+    const int64_t lists = (int64_t)p.in_beams * r.parts, counts = (lists + 7) / 8 * 8, whole = counts + lists * p.beams * 8;
+    if (whole <= 48 << 10) beam_join_kernel<true><<<(unsigned)p.batch, 256, (size_t)whole, stream>>>(p);
+    else beam_join_kernel<false><<<(unsigned)p.batch, 256, (size_t)counts, stream>>>(p);
     return hipGetLastError();
 }
 

@@ -233,10 +233,10 @@ struct RowPlan {
 // Parts of a row: one, where a workgroup's registers hold it and the rows fill the device by themselves; otherwise so many
 // that about kFill workgroups run, of at least 2 vectors per lane.
 constexpr int64_t kFill = 512, kMostParts = 256;
-inline RowPlan row_plan(int dtype, int64_t rows, int64_t vocab) {
+inline RowPlan row_plan(int dtype, int64_t rows, int64_t vocab, int threads = 1024) {      // of the largest workgroup
     const int n = dtype == OLS_F32 ? 4 : 8;
     const int64_t unit = 256 * n;                       // one vector per lane of the smallest workgroup
-    const int64_t most = 1024 * 16 * n;                 // the largest workgroup's registers
+    const int64_t most = (int64_t)threads * 16 * n;     // the largest workgroup's registers
     int64_t parts = (vocab + most - 1) / most;
     if (rows < kFill) parts = std::max(parts, std::min(std::min(kMostParts, (kFill + rows - 1) / rows), (vocab + 2 * unit - 1) / (2 * unit)));
     RowPlan r;

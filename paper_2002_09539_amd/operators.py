@@ -430,19 +430,19 @@ def _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperatu
     shape = logits.shape[:-1]
     if top_value.dim() < 1 or tuple(top_value.shape[:-1]) != tuple(shape):
         _refuse("lists of shape %s for logits of shape %s", tuple(top_value.shape), tuple(logits.shape))
-    d = B.ols_distill()
-    d.dtype, d.k, d.rest, d.temperature = _dtype(logits, "logits"), top_value.shape[-1], int(rest), float(temperature)
-    d.rows, d.vocab, d.logits, d.row_stride = rows, logits.shape[-1], z.data_ptr(), stride
     if targets is None and d_logprob is not None:
         _refuse("a gradient of log probabilities needs the targets")
     keep = (_per_row(top_value, top_value.shape, torch.float32, "top_value"), _per_row(top_index, top_value.shape, torch.int32, "top_index"),
             _per_row(targets, shape, torch.int32, "targets"), _per_row(d_loss, shape, torch.float32, "d_loss"),
             _per_row(d_logprob, shape, torch.float32, "d_logprob"))
-    d.top_value, d.top_index, d.targets, d.d_loss, d.d_logprob = (_ptr(t) for t in keep)
+    value, index, given, g_loss, g_hard = [_ptr(t) for t in keep]
+    d_stride = 0
     if d_logits is not None:
         if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype:
             _refuse("the gradient must have the logits' shape and type")
-        d.d_logits, d.d_stride = d_logits.data_ptr(), _logit_rows(d_logits, "out")[2]
+        d_stride = _logit_rows(d_logits, "out")[2]
+    d = B.ols_distill(_dtype(logits, "logits"), top_value.shape[-1], int(rest), float(temperature), rows, logits.shape[-1], z.data_ptr(), stride, value, index, given,
+                      None, None, None, g_loss, g_hard, _ptr(d_logits), d_stride)
     return d, shape, device, keep
 
 
@@ -516,35 +516,41 @@ def beam_select(logits, score, beams=None, finished=None, length=None, eos=-1, l
     batch, have, vocab = logits.shape
     if vocab > 1 and logits.stride(2) != 1:
         _refuse("logits: the elements of a row must be contiguous")
-    b = B.ols_beam()
-    b.dtype, b.in_beams, b.beams, b.eos = _dtype(logits, "logits"), have, have if beams is None else int(beams), int(eos)
-    b.batch, b.vocab, b.logits, b.batch_stride, b.beam_stride = batch, vocab, logits.data_ptr(), logits.stride(0), logits.stride(1)
-    keep = (_per_row(score, (batch, have), torch.float32, "score"), _per_row(finished, (batch, have), torch.bool, "finished"),
-            _per_row(length, (batch, have), torch.int32, "length"))
-    b.score, b.finished, b.length = (_ptr(t) for t in keep)
-    b.length_penalty = float(length_penalty)
-    b.ws_bytes = B.ols_beam_workspace_bytes(batch, have, b.beams, vocab, b.dtype)
+    code, beams = _dtype(logits, "logits"), have if beams is None else int(beams)
+    rows = (batch, have)
+    score, finished = _per_row(score, rows, torch.float32, "score"), _per_row(finished, rows, torch.bool, "finished")
+    length = _per_row(length, rows, torch.int32, "length")
+    nbytes = B.ols_beam_workspace_bytes(batch, have, beams, vocab, code)
     with _on(device):
-        ws = _workspace(b.ws_bytes, device)
-        new_score = torch.empty(batch, b.beams, dtype=torch.float32, device=device)
-        whole = torch.empty(2 if length is None else 3, batch, b.beams, dtype=torch.int32, device=device).unbind(0)
-        ended = torch.empty(batch, b.beams, dtype=torch.bool, device=device)
+        ws = _workspace(nbytes, device)
+        new_score = torch.empty(batch, beams, dtype=torch.float32, device=device)
+        whole = torch.empty(2 if length is None else 3, batch, beams, dtype=torch.int32, device=device).unbind(0)
+        ended = torch.empty(batch, beams, dtype=torch.bool, device=device)
         new_length = None if length is None else whole[2]
-        b.new_score, b.token, b.parent, b.new_length, b.new_finished, b.ws = (new_score.data_ptr(), whole[0].data_ptr(), whole[1].data_ptr(), _ptr(new_length),
-                                                                             ended.data_ptr(), _ptr(ws))
+        b = B.ols_beam(code, have, beams, int(eos), batch, vocab, logits.data_ptr(), logits.stride(0), logits.stride(1), score.data_ptr(), _ptr(finished),
+                       _ptr(length), float(length_penalty), new_score.data_ptr(), whole[0].data_ptr(), whole[1].data_ptr(), _ptr(new_length), ended.data_ptr(),
+                       _ptr(ws), nbytes)
         B.ols_beam_select(b, _stream(device))
     return Beams(new_score, whole[0], whole[1], ended, new_length)
 
 
-def _state_rows(t, name):
-    """(bytes of a row, bytes between requests, bytes between hypotheses) of a state [batch, hypotheses, ...]."""
-    if t.dim() < 2:
-        _refuse("%s must be [batch, hypotheses, ...], got %d axes", name, t.dim())
-    n, size = 1, t.element_size()
-    for i in range(t.dim() - 1, 1, -1):
-        if t.shape[i] != 1 and t.stride(i) != n:
+def _state_rows(t, batch, beams, name):
+    """(bytes of a row, bytes between requests, bytes between hypotheses) of a state [batch, beams, ...]."""
+    shape, size = t.shape, t.element_size()
+    if len(shape) < 2:
+        _refuse("%s must be [batch, hypotheses, ...], got %d axes", name, len(shape))
+    if shape[0] != batch or shape[1] != beams:
+        _refuse("%s is of shape %s, for %d requests of %d hypotheses", name, tuple(shape), batch, beams)
+    if batch * beams == 0:
+        return 0, 0, 0
+    if t.is_contiguous():
+        n = t.numel() // (batch * beams) * size
+        return n, n * beams, n
+    n = 1
+    for i in range(len(shape) - 1, 1, -1):
+        if shape[i] != 1 and t.stride(i) != n:
             _refuse("%s: what one hypothesis holds must be contiguous", name)
-        n *= t.shape[i]
+        n *= shape[i]
     return n * size, t.stride(0) * size, t.stride(1) * size
 
 
@@ -566,32 +572,29 @@ def beam_reorder(states, parent, out=None):
     device = _on_gpu(parent, *states, *(() if out is None else outs))
     batch, beams = parent.shape
     have = states[0].shape[1] if states[0].dim() > 1 else 0
-    row_bytes, strides = array("q"), [array("q") for _ in range(4)]
-    for i, (s, o) in enumerate(zip(states, outs)):
-        n, sb, sh = _state_rows(s, "state %d" % i)
-        if tuple(s.shape[:2]) != (batch, have):
-            _refuse("state %d is of shape %s, for %d requests of %d hypotheses", i, tuple(s.shape), batch, have)
-        ob, oh = sb, sh
-        if o is not s:
-            if o.dtype != s.dtype or tuple(o.shape) != (batch, beams, *s.shape[2:]):
-                _refuse("out %d must be %s of shape %s", i, s.dtype, (batch, beams, *s.shape[2:]))
-            _, ob, oh = _state_rows(o, "out %d" % i)
-        elif have != beams:
+    src, dst = [t.data_ptr() for t in states], [t.data_ptr() for t in outs]
+    rows = [_state_rows(t, batch, have, "a state") for t in states]
+    row_bytes, src_batch, src_beam = zip(*rows)
+    if out is None:
+        if have != beams:
             _refuse("in place, %d hypotheses cannot become %d", have, beams)
-        row_bytes.append(n)
-        for a, v in zip(strides, (sb, sh, ob, oh)):
-            a.append(v)
-    src, dst = array("Q", [t.data_ptr() for t in states]), array("Q", [t.data_ptr() for t in outs])
-    if not _distinct(dst, row_bytes):
-        _refuse("a state cannot be written twice in one call")
-    if out is not None:
+        dst_batch, dst_beam = src_batch, src_beam
+    else:
+        for s, o in zip(states, outs):
+            if o.dtype != s.dtype or o.shape[2:] != s.shape[2:]:
+                _refuse("an output is %s of shape %s, for a state of %s and shape %s", o.dtype, tuple(o.shape), s.dtype, tuple(s.shape))
+        _, dst_batch, dst_beam = zip(*[_state_rows(t, batch, beams, "an output") for t in outs])
         read = {p: i for i, (p, n) in enumerate(zip(src, row_bytes)) if n}
         if any(n and read.get(p, i) != i for i, (p, n) in enumerate(zip(dst, row_bytes))):
             _refuse("an output is another state of the call")
+    if not _distinct(dst, row_bytes):
+        _refuse("a state cannot be written twice in one call")
     parent = parent.contiguous()
-    at = lambda a: a.buffer_info()[0]  # noqa: E731
+    n = len(states)
+    numbers = array("q", (*src, *dst, *row_bytes, *src_batch, *src_beam, *dst_batch, *dst_beam))      # seven arrays of n entries
+    at = numbers.buffer_info()[0]
     with _on(device):
-        B.ols_beam_reorder(len(states), at(src), at(dst), at(row_bytes), *(at(a) for a in strides), batch, have, beams, parent.data_ptr(), _stream(device))
+        B.ols_beam_reorder(n, *range(at, at + 7 * 8 * n, 8 * n), batch, have, beams, parent.data_ptr(), _stream(device))
     return outs
 
 
