@@ -5,7 +5,7 @@
 //   order:       by value / length^penalty, largest first; ties to the lower hypothesis, then to the lower token
 //
 // Within a hypothesis that is the order of its logits, which is exact.  Between hypotheses it hangs on the last bits of the sums:
-// these are added up in fp64 from exponentials whose argument's rounding does not lean to a side, and candidates are compared in fp64.
+// these are added up in fp64, and candidates are compared in fp64.
 //
 // What bounds the choice is one read of the logits: a workgroup holds its part of a hypothesis' row in registers, takes the sum
 // and the part's best from there (logit_rows.h), and one wavefront for each request merges the parts' lists, each in order: a lane
@@ -19,11 +19,9 @@ namespace ols {
 
 namespace {
 
-// e^d as a power of two; log2 e = hi + lo, both positive, so that -inf stays -inf
-__device__ __forceinline__ float exp_of(float d) {
-    constexpr float kHi = 1.44269502162933349609f, kLo = 1.92596299112661747e-8f;
-    return __builtin_amdgcn_exp2f(fmaf(d, kHi, d * kLo));
-}
+// log2 e is rounded by 2^-26 of itself, which moves a row's logarithm by 1e-8 of its logits' mean distance from the largest: rows of one
+// model by nearly the same.
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 
 // A hypothesis that is read: it has a score and has not ended.
 __device__ __forceinline__ bool goes_on(const BeamParams& p, int64_t row) {
@@ -107,9 +105,9 @@ __device__ __forceinline__ double wave_max(double v) {
 
 // What is known of a hypothesis.
 struct Hypothesis {
-    double lead, scale, sum;   // what comes to a logit's distance from the largest (-inf: it has no candidates), length^penalty, sum of e^{z - top}
-    float top;
-    int length, ended;
+    double lead, scale, sum;   // what comes to a logit's distance from the largest (-inf: it has no candidates), 1 / length^penalty, sum of e^{z - top}
+    float score, top;
+    int length, ended, dead;
 };
 
 // A workgroup for each request: its wavefronts add up the parts, then one merges the parts' lists, each in order; a lane looks after every
@@ -121,24 +119,33 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
     const int64_t batch = blockIdx.x;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, k = p.beams, lists = p.in_beams * p.parts, entries = lists * k;
     uint8_t* used = (uint8_t*)dyn;                            // of each list: how many are taken
-    const float* val = p.part_val + batch * entries;
+    const float *val = p.part_val + batch * entries, *part_m = p.part_m + batch * lists;
+    const double* part_s = p.part_s + batch * lists;
     const int* idx = p.part_idx + batch * entries;
     for (int l = threadIdx.x; l < lists; l += 256) used[l] = 0;
-    if constexpr (LISTS) {
-        float* v = (float*)(dyn + (lists + 7) / 8 * 8);
+    if constexpr (LISTS) {                                    // all that is read, in one round trip
+        double* s = (double*)(dyn + (lists + 7) / 8 * 8);
+        float *m = (float*)(s + lists), *v = m + lists;
         int* at = (int*)(v + entries);
+        for (int i = threadIdx.x; i < lists; i += 256) s[i] = part_s[i], m[i] = part_m[i];
         for (int i = threadIdx.x; i < entries; i += 256) v[i] = val[i], at[i] = idx[i];
-        val = v, idx = at;
+        part_s = s, part_m = m, val = v, idx = at;
     }
+    if ((int)threadIdx.x < p.in_beams) {
+        Hypothesis& h = of[threadIdx.x];
+        const int64_t row = batch * p.in_beams + threadIdx.x;
+        h.score = p.score[row], h.length = p.length ? p.length[row] : 0;
+        h.dead = h.score == -INFINITY, h.ended = !h.dead && p.finished && p.finished[row], h.sum = 1.0;
+    }
+    __syncthreads();
     for (int i = wave; i < p.in_beams; i += 4) {
-        const int64_t row = batch * p.in_beams + i;
-        if (!goes_on(p, row)) continue;
+        if (of[i].dead || of[i].ended) continue;
         float m = -INFINITY;
-        for (int j = lane; j < p.parts; j += 64) m = fmaxf(m, p.part_m[row * p.parts + j]);
+        for (int j = lane; j < p.parts; j += 64) m = fmaxf(m, part_m[i * p.parts + j]);
         m = ols::wave_max(m);
         const double base = m == -INFINITY ? 0.0 : (double)m;
         double sum = 0.0;
-        for (int j = lane; j < p.parts; j += 64) sum += p.part_s[row * p.parts + j] * exp((double)p.part_m[row * p.parts + j] - base);
+        for (int j = lane; j < p.parts; j += 64) sum += part_s[i * p.parts + j] * exp((double)part_m[i * p.parts + j] - base);
         sum = wave_sum(sum);
         if (lane == 0) of[i].top = m, of[i].sum = sum;
     }
@@ -147,54 +154,47 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
     bool bad = false;
     if (lane < p.in_beams) {
         Hypothesis& h = of[lane];
-        const int64_t row = batch * p.in_beams + lane;
-        const float score = p.score[row];
-        const bool dead = score == -INFINITY, ended = !dead && !goes_on(p, row);
-        const double sum = dead || ended ? 1.0 : h.sum;
-        bad = !dead && (!(score < INFINITY) || !(sum < INFINITY));
-        h.lead = dead || !(sum > 0.0) ? (double)-INFINITY : (double)score - log(sum);
-        h.ended = ended, h.length = p.length ? p.length[row] : 0;
-        h.scale = p.penalty == 0.0 ? 1.0 : exp(p.penalty * log((double)max(ended ? h.length : h.length + 1, 1)));     // pow takes 4 us
+        bad = !h.dead && (!(h.score < INFINITY) || !(h.sum < INFINITY));
+        h.lead = h.dead || !(h.sum > 0.0) ? (double)-INFINITY : (double)h.score - log_of(h.sum);
+        h.scale = p.penalty == 0.0 ? 1.0 : exp(-p.penalty * log_of((double)max(h.ended ? h.length : h.length + 1, 1)));
     }
     const bool poisoned = __ballot(bad) != 0;
     in_wave_order();
-    // Token of the head of list l, -1 where there is none, and its value.
-    auto token_of = [&](int l) {
-        const Hypothesis& h = of[l / p.parts];
-        const int at = used[l];
-        if (h.lead == -INFINITY || at >= k) return -1;
-        if (h.ended) return at == 0 && l % p.parts == 0 ? 0 : -1;
-        return idx[l * k + at];
-    };
-    auto value_of = [&](int l) {
-        const Hypothesis& h = of[l / p.parts];
-        return h.ended ? h.lead : h.lead + ((double)val[l * k + used[l]] - (double)h.top);
-    };
-    int list = -1;                                            // of the lane's lists the one whose head is first
-    double key = -INFINITY;
-    auto look = [&]() {
-        list = -1, key = -INFINITY;
-        for (int l = lane; l < lists; l += 64) {
-            if (token_of(l) < 0) continue;
-            const double v = value_of(l) / of[l / p.parts].scale;
-            if (list < 0 || v > key) list = l, key = v;       // ties: the lower list
-        }
-    };
-    look();
-    // Of place `lane` of the result.
-    int from = -1, token = -1;
-    double value = 0.0;
+    // The hypothesis of list l: quotients are at least 1 / 2048 off a whole number and below 32, where the product is off by 2^-18.  (Divisions of
+    // whole numbers were most of a turn.)
+    const float per = 1.0f / (float)p.parts;
+    auto owner = [&](int l) { return (int)(((float)l + 0.5f) * per); };
+    // Of the lane's lists the one whose head is first, and of place `lane` of the result what it is.
+    int list = -1, token = -1, from = -1, said = -1;
+    double key = -INFINITY, value = 0.0, score = 0.0;
+    bool stale = true;
+#pragma unroll 1
     for (int turn = 0; turn < k && !poisoned; ++turn) {
+        if (stale) {
+            list = -1, key = -INFINITY;
+#pragma unroll 1
+            for (int l = lane; l < lists; l += 64) {          // two round trips to LDS, whatever the head is
+                const int i = owner(l), at = used[l], entry = l * k + min(at, k - 1);
+                const Hypothesis h = of[i];
+                const int said_here = idx[entry];
+                const double v = h.ended ? h.lead : h.lead + ((double)val[entry] - (double)h.top), ranked = v * h.scale;
+                const bool there = h.lead > -INFINITY && (h.ended ? at == 0 && l == i * p.parts : at < k && said_here >= 0);
+                if (there && (list < 0 || ranked > key)) list = l, key = ranked, value = v, token = h.ended ? 0 : said_here;   // ties: the lower list
+            }
+        }
         const double best = wave_max(key);
         const unsigned long long at = __ballot(list >= 0 && key == best);
         if (!at) break;
-        int first = __builtin_amdgcn_readlane(list, __ffsll(at) - 1);
-        for (unsigned long long more = at & (at - 1); more; more &= more - 1) first = min(first, __builtin_amdgcn_readlane(list, __ffsll(more) - 1));
-        const int said = token_of(first);
-        const double v = value_of(first);
-        if (lane == turn) from = first, token = said, value = v;
-        in_wave_order();
-        if (first % 64 == lane) used[first] += 1, look();
+        int who = __ffsll(at) - 1, first = __builtin_amdgcn_readlane(list, who);
+        for (unsigned long long more = at & (at - 1); more; more &= more - 1) {
+            const int other = __ffsll(more) - 1, l = __builtin_amdgcn_readlane(list, other);
+            if (l < first) first = l, who = other;
+        }
+        const int token_first = __builtin_amdgcn_readlane(token, who);
+        const double value_first = lane_of(value, who);
+        if (lane == turn) from = first, said = token_first, score = value_first;
+        stale = lane == who;
+        if (stale) used[first] += 1;
         in_wave_order();
     }
     if (lane >= k) return;
@@ -204,9 +204,9 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
         p.new_score[out] = poisoned ? NAN : -INFINITY, p.token[out] = -1, p.parent[out] = slot, p.new_finished[out] = 0;
         if (p.new_length) p.new_length[out] = of[slot].length;
     } else {
-        const Hypothesis& h = of[from / p.parts];
-        p.new_score[out] = (float)value, p.token[out] = h.ended ? p.eos : token, p.parent[out] = from / p.parts;
-        p.new_finished[out] = h.ended || (p.eos >= 0 && token == p.eos);
+        const Hypothesis& h = of[owner(from)];
+        p.new_score[out] = (float)score, p.token[out] = h.ended ? p.eos : said, p.parent[out] = owner(from);
+        p.new_finished[out] = h.ended || (p.eos >= 0 && said == p.eos);
         if (p.new_length) p.new_length[out] = h.length + (h.ended ? 0 : 1);
     }
 }
@@ -327,7 +327,7 @@ hipError_t launch_beam(BeamParams p, void* ws, hipStream_t stream) {
     p.part_idx = (int32_t*)(p.part_val + rows * r.parts * p.beams);
     hipError_t e = p.dtype == OLS_F32 ? launch_typed<float>(p, r, stream) : launch_typed<uint16_t>(p, r, stream);
     if (e != hipSuccess) return e;
-    const int64_t lists = (int64_t)p.in_beams * r.parts, counts = (lists + 7) / 8 * 8, whole = counts + lists * p.beams * 8;
+    const int64_t lists = (int64_t)p.in_beams * r.parts, counts = (lists + 7) / 8 * 8, whole = counts + lists * (12 + 8 * (int64_t)p.beams);
     if (whole <= 48 << 10) beam_join_kernel<true><<<(unsigned)p.batch, 256, (size_t)whole, stream>>>(p);
     else beam_join_kernel<false><<<(unsigned)p.batch, 256, (size_t)counts, stream>>>(p);
     return hipGetLastError();

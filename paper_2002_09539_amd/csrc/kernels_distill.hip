@@ -35,7 +35,7 @@ __device__ __forceinline__ Sums join(const DistillParams& p, const Sums& a, cons
     return {m, a.s * power(da, p.scale) + b.s * power(db, p.scale), a.s1 * power(da, p.scale1) + b.s1 * power(db, p.scale1)};
 }
 
-// A row's list in LDS: places in the row (-1: none), q, and the student's logits.
+// A row's list in LDS: places in the row (-1: none), the teacher's values and then q, and the student's logits.
 struct List {
     int index[kMaxList];
     float q[kMaxList], z[kMaxList];
@@ -59,8 +59,10 @@ __device__ __forceinline__ void read_list(const DistillParams& p, List& l, Teach
     bool met = false;
     for (int i = threadIdx.x % 64; i < p.k; i += 64) {
         const int at = p.index[row * p.k + i];
+        const float value = p.value[row * p.k + i];            // under way with the index, not behind what follows from it
         const bool there = at >= 0 && at < p.vocab;
         l.index[i] = there ? at : -1;
+        l.q[i] = value;
         l.z[i] = there ? load1(z + at) : -INFINITY;
         met |= there && at == t.target;
     }
@@ -70,14 +72,13 @@ __device__ __forceinline__ void read_list(const DistillParams& p, List& l, Teach
 }
 
 // The teacher's probabilities into l.q and the sums over the list, by one wavefront.  A NaN or +inf among the values makes them all NaN.
-__device__ __forceinline__ void weigh(const DistillParams& p, List& l, Teacher& t, int64_t row) {
+__device__ __forceinline__ void weigh(const DistillParams& p, List& l, Teacher& t) {
     const int lane = threadIdx.x % 64;
-    const float* value = p.value + row * p.k;
     float top = -INFINITY, m = -INFINITY;
     bool some = false, bad = false, again = false;
     for (int i = lane; i < p.k; i += 64) {
         if (l.index[i] < 0) continue;
-        const float v = value[i];
+        const float v = l.q[i];
         some = true, bad |= !(v < INFINITY);
         top = fmaxf(top, v), m = fmaxf(m, l.z[i]);
     }
@@ -92,7 +93,7 @@ __device__ __forceinline__ void weigh(const DistillParams& p, List& l, Teacher& 
     for (int i = lane; i < p.k; i += 64) {
         float q = 0.0f;
         if (l.index[i] >= 0) {
-            const double u = ((double)value[i] - t.top) * inv_v, e = exp(u);
+            const double u = ((double)l.q[i] - t.top) * inv_v, e = exp(u);
             w += e, self += e > 0.0 ? e * u : 0.0, cross += e > 0.0 ? e * (((double)l.z[i] - (double)base) * inv_t) : 0.0;
             q = (float)e;
             bool first = true;
@@ -114,7 +115,7 @@ __device__ __forceinline__ void weigh(const DistillParams& p, List& l, Teacher& 
         t.rest = some ? fmax(1.0 - w, 0.0) : 0.0;
     } else if (w > 0.0) {
         t.scale = (float)(1.0 / w);
-        self = self / w - log(w), cross /= w;
+        self = self / w - log_of(w), cross /= w;
         for (int i = lane; i < p.k; i += 64) l.q[i] *= t.scale;
         w = 1.0;
     }
@@ -152,17 +153,17 @@ __device__ __forceinline__ Coefs coefs(const DistillParams& p, const Sums& u, co
 
 // Loss, likelihood and stats of a row, by one lane.
 __device__ __forceinline__ void finish_row(const DistillParams& p, const Teacher& t, const Sums& u, const Coefs& c, int64_t row) {
-    const double inv_t = 1.0 / (double)p.temperature, log_s = log((double)c.s);
+    const double inv_t = 1.0 / (double)p.temperature, log_s = log_of((double)c.s);
     // t.cross is against the listed tokens' own maximum
     double loss = t.self + t.w * log_s;
     if (t.any) loss -= t.cross + t.w * (((t.m == -INFINITY ? 0.0 : (double)t.m) - (double)c.m) * inv_t);
-    if (c.held) loss += t.rest * (log(t.rest) - (((double)u.m - (double)c.m) * inv_t + log((double)u.s) - log_s));
+    if (c.held) loss += t.rest * (log_of(t.rest) - (((double)u.m - (double)c.m) * inv_t + log_of((double)u.s) - log_s));
     if (c.empty) loss = t.w != t.w ? NAN : t.any ? INFINITY : 0.0;
     else if (!(c.s < INFINITY)) loss = NAN;
     p.loss[row] = (float)(loss * (double)p.temperature * (double)p.temperature);
     if (p.logprob) {
         float given = 0.0f;
-        if (t.target >= 0) given = c.empty ? -INFINITY : !(c.s1 < INFINITY) ? NAN : (float)((double)t.z_target - (double)c.m - log((double)c.s1));
+        if (t.target >= 0) given = c.empty ? -INFINITY : !(c.s1 < INFINITY) ? NAN : (float)((double)t.z_target - (double)c.m - log_of((double)c.s1));
         p.logprob[row] = given;
     }
     float* o = p.stats + 8 * row;
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(256) void distill_list_kernel(DistillParams p) {
     List& l = lists[wave];
     Teacher t;
     read_list<T>(p, l, t, row, (const T*)p.logits + row * p.row_stride);
-    weigh(p, l, t, row);
+    weigh(p, l, t);
     if (lane == 0) ((Teacher*)p.teachers)[row] = t;
     for (int i = lane; i < p.k; i += 64) p.list_q[row * p.k + i] = l.q[i], p.list_z[row * p.k + i] = l.z[i];
 }
@@ -381,27 +382,25 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillParams p) {
     Held<T, 256, NV> h;
     if (d) h.load(z + start, length);
     const float* in = p.stats + 8 * row;
+    Teacher t;
+    Sums a{-INFINITY, 0.0f, 0.0f};
     if (lane < 64) {
-        Teacher t;
+        const float* sums = JOIN ? p.part_sums + 3 * row * p.parts : nullptr;
+        if (JOIN && lane < p.parts) a = Sums{sums[3 * lane], sums[3 * lane + 1], sums[3 * lane + 2]};
         read_list<T>(p, list, t, row, z);
         if constexpr (JOIN) {
-            const float* sums = p.part_sums + 3 * row * p.parts;
-            Sums a{-INFINITY, 0.0f, 0.0f};
-            for (int i = lane; i < p.parts; i += 64) a = join(p, a, Sums{sums[3 * i], sums[3 * i + 1], sums[3 * i + 2]});
+            for (int i = lane + 64; i < p.parts; i += 64) a = join(p, a, Sums{sums[3 * i], sums[3 * i + 1], sums[3 * i + 2]});
             for (int o = 32; o; o >>= 1) {
                 const Sums b{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.s1, o)};
                 a = lane & o ? join(p, b, a) : join(p, a, b);       // the same order in every lane
             }
-            weigh(p, list, t, row);
+            weigh(p, list, t);
             const Coefs c = coefs(p, a, t);
-            if (lane == 0) {
-                if (blockIdx.y == 0) finish_row(p, t, a, c, row);
-                shared = c, listed = t.target_listed, twice = t.twice;
-            }
+            if (lane == 0) shared = c, listed = t.target_listed, twice = t.twice;
         } else {
             const float top = in[6], scale = in[7], inv_t = p.rest ? 1.0f : 1.0f / p.temperature;
             for (int i = lane; i < p.k; i += 64) {
-                const float q = expf((p.value[row * p.k + i] - top) * inv_t) * scale;
+                const float q = expf((list.q[i] - top) * inv_t) * scale;
                 list.q[i] = list.index[i] < 0 || scale == 0.0f ? 0.0f : q;
             }
             if (lane == 0) {
@@ -411,7 +410,10 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillParams p) {
             }
         }
     }
-    if (!d) return;
+    auto finish = [&]() {                      // behind the gradient, which waits for it nowhere
+        if (JOIN && blockIdx.y == 0 && lane == 0) finish_row(p, t, a, shared, row);
+    };
+    if (!d) return finish();
     const int target = p.targets ? p.targets[row] : -1;
     const bool has_target = target >= start && target < end;
     const float z_target = has_target ? load1(z + target) : 0.0f;
@@ -435,6 +437,7 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillParams p) {
         store1(d + at, entry_grad(p, c, list.z[i], true, q, at == target, g_loss, g_hard));
     }
     if (lane == 0 && has_target && !listed) store1(d + target, entry_grad(p, c, z_target, false, 0.0f, true, g_loss, g_hard));
+    finish();
 }
 
 template <typename T, int THREADS, int NV>

@@ -105,6 +105,20 @@ __device__ __forceinline__ double wave_sum(double v) {
     return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
 }
 
+// log x in fp64, by log m = 2 atanh((m - 1) / (m + 1)) for m in [sqrt 1/2, sqrt 2) and its series up to the 17th power (2e-16).  Not inlined:
+// kernels of one wavefront's work wait for their instructions longer than for the arithmetic.
+__device__ __attribute__((noinline)) double log_of(double x) {
+    if (!(x > 0.0 && x < (double)INFINITY)) return x == 0.0 ? (double)-INFINITY : x > 0.0 ? x : (double)NAN;
+    double m = __builtin_amdgcn_frexp_mant(x);
+    int e = __builtin_amdgcn_frexp_exp(x);
+    if (m < 0.70710678118654752440) m *= 2.0, e -= 1;
+    const double f = (m - 1.0) / (m + 1.0), s = f * f;
+    double v = 1.0 / 17;
+    v = fma(v, s, 1.0 / 15), v = fma(v, s, 1.0 / 13), v = fma(v, s, 1.0 / 11), v = fma(v, s, 1.0 / 9);
+    v = fma(v, s, 1.0 / 7), v = fma(v, s, 1.0 / 5), v = fma(v, s, 1.0 / 3), v = fma(v, s, 1.0);
+    return fma((double)e, 0.69314718055994530942, 2.0 * f * v);
+}
+
 // places among the listed: value descending, index ascending
 __device__ __forceinline__ bool beats(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
 

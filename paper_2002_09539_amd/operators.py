@@ -277,9 +277,13 @@ def _logit_rows(t, name):
 def _per_row(t, shape, dtype, name):
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         _refuse("%s must be %s of shape %s, got %s of shape %s", name, dtype, tuple(shape), t.dtype, tuple(t.shape))
     return t.contiguous()
+
+
+def _floats(device, *shape):
+    return torch.empty(*shape, dtype=torch.float32, device=device) if shape else torch.empty((), dtype=torch.float32, device=device)
 
 
 def _logprobs(logits, targets, top, d_logprob, d_entropy, d_logits):
@@ -428,21 +432,24 @@ def _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperatu
     device = _on_gpu(logits, top_value, top_index, targets, d_loss, d_logprob, d_logits)
     z, rows, stride = _logit_rows(logits, "logits")
     shape = logits.shape[:-1]
-    if top_value.dim() < 1 or tuple(top_value.shape[:-1]) != tuple(shape):
+    if top_value.dim() < 1 or top_value.shape[:-1] != shape:
         _refuse("lists of shape %s for logits of shape %s", tuple(top_value.shape), tuple(logits.shape))
     if targets is None and d_logprob is not None:
         _refuse("a gradient of log probabilities needs the targets")
-    keep = (_per_row(top_value, top_value.shape, torch.float32, "top_value"), _per_row(top_index, top_value.shape, torch.int32, "top_index"),
-            _per_row(targets, shape, torch.int32, "targets"), _per_row(d_loss, shape, torch.float32, "d_loss"),
-            _per_row(d_logprob, shape, torch.float32, "d_logprob"))
-    value, index, given, g_loss, g_hard = [_ptr(t) for t in keep]
+    listed = top_value.shape
+    top_value, top_index = _per_row(top_value, listed, torch.float32, "top_value"), _per_row(top_index, listed, torch.int32, "top_index")
+    targets, d_loss = _per_row(targets, shape, torch.int32, "targets"), _per_row(d_loss, shape, torch.float32, "d_loss")
+    d_logprob = _per_row(d_logprob, shape, torch.float32, "d_logprob")
+    keep = top_value, top_index, targets, d_loss, d_logprob
     d_stride = 0
-    if d_logits is not None:
+    if d_logits is logits:
+        d_stride = stride
+    elif d_logits is not None:
         if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype:
             _refuse("the gradient must have the logits' shape and type")
         d_stride = _logit_rows(d_logits, "out")[2]
-    d = B.ols_distill(_dtype(logits, "logits"), top_value.shape[-1], int(rest), float(temperature), rows, logits.shape[-1], z.data_ptr(), stride, value, index, given,
-                      None, None, None, g_loss, g_hard, _ptr(d_logits), d_stride)
+    d = B.ols_distill(_dtype(logits, "logits"), listed[-1], int(rest), float(temperature), rows, logits.shape[-1], z.data_ptr(), stride, top_value.data_ptr(),
+                      top_index.data_ptr(), _ptr(targets), None, None, None, _ptr(d_loss), _ptr(d_logprob), _ptr(d_logits), d_stride)
     return d, shape, device, keep
 
 
@@ -451,9 +458,8 @@ def _distill_loss(logits, top_value, top_index, targets, d_loss, d_logprob, temp
     d.ws_bytes = B.ols_distill_workspace_bytes(d.rows, d.vocab, d.dtype, d.k)
     with _on(device):
         ws = _workspace(d.ws_bytes, device)
-        loss = torch.empty(shape, dtype=torch.float32, device=device)
-        logprob = None if targets is None else torch.empty(shape, dtype=torch.float32, device=device)
-        stats = torch.empty(*shape, 8, dtype=torch.float32, device=device)
+        loss, stats = _floats(device, *shape), _floats(device, *shape, 8)
+        logprob = None if targets is None else _floats(device, *shape)
         d.loss, d.logprob, d.stats, d.ws = loss.data_ptr(), _ptr(logprob), stats.data_ptr(), _ptr(ws)
         B.ols_distill_loss(d, _stream(device))
     return DistillLoss(loss, logprob, stats)
@@ -603,6 +609,9 @@ Int8Rows = namedtuple("Int8Rows", "q scale")
 Int8Weight = namedtuple("Int8Weight", "q scale")
 
 
+_NO_MATRIX = B.ols_matrix(None, 0, 0)
+
+
 def _padded(n):
     return -(-n // 16) * 16          # rows that begin on 16 bytes
 
@@ -676,28 +685,24 @@ def int8_matmul(x, weight, up=None, act="silu", out=None, dtype=None):
     workers = xq.dim() == 3 or wq.dim() == 3
     m = xq.shape[0] if xq.dim() == 3 else wq.shape[0] if workers else 1
     rows, width, channels = xq.shape[-2], xq.shape[-1], wq.shape[-2]
-    f = B.ols_int8()
-    f.groups, f.act, f.rows, f.width, f.out = m, _act_code(act), rows, width, channels
-    f.dtype = B.OLS_I8 if given else _dtype(xq, "x")
+    code = B.OLS_I8 if given else _dtype(xq, "x")
     dtype = dtype or (out.dtype if out is not None else torch.bfloat16 if given else xq.dtype)
-    f.out_dtype = _dtype(dtype, "dtype")
-    f.x, f.w = _matrix(xq, m, (rows, width), "x"), _matrix(wq, m, (channels, width), "weight")
+    mx, mw, mu = _matrix(xq, m, (rows, width), "x"), _matrix(wq, m, (channels, width), "weight"), _NO_MATRIX
     if up is not None:
         if given or up.dtype != xq.dtype:
             _refuse("up must be of x's type, which is not quantised yet")
-        f.up = _matrix(up, m, (rows, width), "up")
-    if given:
-        f.x_scale, f.x_scale_group = _scale(x.scale, m, rows, "the rows' scales")
-    f.w_scale, f.w_scale_group = _scale(w_scale, m, channels, "the channels' scales")
-    shape = ((m,) if workers else ()) + (rows, channels)
+        mu = _matrix(up, m, (rows, width), "up")
+    xs = _scale(x.scale, m, rows, "the rows' scales") if given else (None, 0)
+    ws = _scale(w_scale, m, channels, "the channels' scales")
+    shape = (m, rows, channels) if workers else (rows, channels)
     with _on(device):
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=device)
-        elif tuple(out.shape) != shape or out.dtype != dtype:
+        elif out.shape != shape or out.dtype != dtype:
             _refuse("out must be %s of shape %s", dtype, shape)
-        f.y = _matrix(out, m, (rows, channels), "out")
+        f = B.ols_int8(m, code, _act_code(act), _dtype(dtype, "dtype"), rows, width, channels, mx, mu, mw, _matrix(out, m, (rows, channels), "out"), *xs, *ws)
         f.ws_bytes = B.ols_int8_workspace_bytes(f)
-        ws = _workspace(f.ws_bytes, device)
-        f.ws = _ptr(ws)
+        space = _workspace(f.ws_bytes, device)
+        f.ws = _ptr(space)
         B.ols_int8_matmul(f, _stream(device))
     return out
