@@ -28,6 +28,60 @@ __device__ __forceinline__ bool goes_on(const BeamParams& p, int64_t row) {
     return !(p.score[row] == -INFINITY) && !(p.finished && p.finished[row]);
 }
 
+// The best k of what a workgroup of 256 holds, as best_of_part does it, from a bound that is quicker to find: of 16 (k <= 8) or 32 groups of
+// lanes the k-th largest of their maxima, which at least k logits reach and few others.  Where more do than the list holds (many equal
+// ones, or one lane that holds them all) best_of_part takes over.  512 rows of 128 000 bf16, 8 of each: best_of_part 15 us of 39.
+template <typename T, int NV>
+__device__ __forceinline__ void best_of_groups(const u4 (&v)[NV], float lane_max, int64_t start, int k, int room, float* list_val, int* list_idx, float* best_val,
+                                               int* best_idx) {
+    constexpr int N = Vec<T>::kN;
+    __shared__ float tops[32];
+    __shared__ int listed;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    float m = lane_max;
+    m = fmaxf(m, moved<0x111, 0xf>(m, -INFINITY));
+    m = fmaxf(m, moved<0x112, 0xf>(m, -INFINITY));
+    m = fmaxf(m, moved<0x114, 0xf>(m, -INFINITY));             // the lane's and the seven in front of it, of a row of 16
+    const bool wide = k <= 8;
+    if (wide) m = fmaxf(m, moved<0x118, 0xf>(m, -INFINITY));
+    const int size = wide ? 16 : 8, groups = 256 / size;
+    if (lane % size == size - 1) tops[(wave * 64 + lane) / size] = m;
+    if (threadIdx.x == 0) listed = 0;
+    __syncthreads();
+    const float mine = lane < groups ? tops[lane] : -INFINITY;
+    int above = 0, with = 0;                                   // groups above the lane's, and with those equal to it
+    for (int i = 0; i < groups; ++i) {
+        const float other = lane_of(mine, i);
+        above += other > mine ? 1 : 0, with += other >= mine ? 1 : 0;
+    }
+    const unsigned long long at = __ballot(lane < groups && above < k && with >= k);
+    const float limit = at ? lane_of(mine, __ffsll(at) - 1) : -INFINITY;
+    if (__ballot(lane_max >= limit && lane_max > -INFINITY)) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float top = Vec<T>::get(v[j], 0);
+#pragma unroll
+            for (int e = 1; e < N; ++e) top = fmaxf(top, Vec<T>::get(v[j], e));
+            if (!(top >= limit && top > -INFINITY)) continue;
+            const int64_t first = start + ((int64_t)j * 256 + threadIdx.x) * N;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float x = Vec<T>::get(v[j], e);
+                if (!(x >= limit && x > -INFINITY)) continue;
+                const int to = atomicAdd(&listed, 1);
+                if (to < room) list_val[to] = x, list_idx[to] = (int)(first + e);
+            }
+        }
+    }
+    __syncthreads();
+    if (listed > room) {
+        best_of_part<T, 256, NV>(v, lane_max, start, k, list_val, list_idx, best_val, best_idx);
+        return;
+    }
+    write_best<256>(list_val, list_idx, listed, k, best_val, best_idx);
+    __syncthreads();
+}
+
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS, 4) void beam_part_kernel(BeamParams p) {
     constexpr int N = Vec<T>::kN, WAVES = THREADS / 64;
@@ -70,8 +124,9 @@ __global__ __launch_bounds__(THREADS, 4) void beam_part_kernel(BeamParams p) {
     keep_packed(v);
     __syncthreads();
     float* list_val = (float*)dyn;
-    int* list_idx = (int*)(list_val + list_entries<T, THREADS, NV>(p.beams));
-    best_of_part<T, THREADS, NV>(v, lane_max, start, p.beams, list_val, list_idx, best_val, best_idx);
+    const int room = list_entries<T, THREADS, NV>(p.beams);
+    int* list_idx = (int*)(list_val + room);
+    best_of_groups<T, NV>(v, lane_max, start, p.beams, room, list_val, list_idx, best_val, best_idx);
     const int64_t slot = row * p.parts + part;
     if (threadIdx.x == 0) {
         s = 0.0;
