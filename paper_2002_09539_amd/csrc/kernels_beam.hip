@@ -364,11 +364,11 @@ __global__ __launch_bounds__(256) void beam_move_kernel(BeamMove t) {
 // 128 000 bf16 in workgroups that hold whole rows: 49 us.
 static RowPlan beam_plan(int dtype, int64_t rows, int64_t vocab) { return row_plan(dtype, rows, vocab, 256); }
 
-// All parts of a call lie in the workspace.
+// All parts of a call lie in the workspace; negative: they are more than a launch numbers (fewer than 2^32 threads, 256 for each).
 int64_t beam_workspace_bytes(int dtype, int64_t batch, int in_beams, int beams, int64_t vocab) {
     if (batch == 0) return 0;
-    const int64_t rows = batch * in_beams;
-    return rows * beam_plan(dtype, rows, vocab).parts * (12 + 8 * (int64_t)beams);
+    const int64_t rows = batch * in_beams, parts = rows * beam_plan(dtype, rows, vocab).parts;
+    return parts >= (1 << 24) ? -1 : parts * (12 + 8 * (int64_t)beams);
 }
 
 hipError_t launch_beam(BeamParams p, void* ws, hipStream_t stream) {

@@ -466,13 +466,13 @@ hipError_t launch_typed(const DistillParams& p, const RowPlan& r, hipStream_t st
     return r.nv <= 10 ? launch_long<T, 10>(p, r, stream) : r.nv == 13 ? launch_long<T, 13>(p, r, stream) : launch_long<T, 16>(p, r, stream);
 }
 
-// A launch has fewer than 2^32 threads, a row up to 1024 of them.
-constexpr int64_t kMostRows = 1 << 21;
+// A launch has fewer than 2^32 threads: a row up to 1024 for each of its parts, or 256 for each of its pieces in the gradient from memory.
+int64_t most_rows(int dtype, int64_t vocab) { return std::max<int64_t>(1, (1 << 21) / ((vocab + (dtype == OLS_F32 ? 4095 : 8191)) / (dtype == OLS_F32 ? 4096 : 8192))); }
 DistillParams rows_of(const DistillParams& p, int64_t first) {
     const int64_t bytes = p.dtype == OLS_F32 ? 4 : 2;
     auto at = [&](auto* t, int64_t per) { return t ? t + per * first : t; };
     DistillParams q = p;
-    q.rows = std::min(kMostRows, p.rows - first);
+    q.rows = std::min(most_rows(p.dtype, p.vocab), p.rows - first);
     q.logits = at((const char*)p.logits, p.row_stride * bytes), q.d_logits = at((char*)p.d_logits, p.d_stride * bytes);
     q.value = at(p.value, p.k), q.index = at(p.index, p.k), q.targets = at(p.targets, 1);
     q.g_loss = at(p.g_loss, 1), q.g_logprob = at(p.g_logprob, 1);
@@ -499,13 +499,13 @@ DistillParams with_exponents(DistillParams p) {
 int64_t distill_workspace_bytes(int dtype, int64_t rows, int64_t vocab, int k) {
     if (rows == 0) return 0;
     const RowPlan r = row_plan(dtype, rows, vocab);
-    rows = std::min(kMostRows, rows);
+    rows = std::min(most_rows(dtype, vocab), rows);
     return rows * (r.parts > 1 ? r.parts * 12 : (int64_t)sizeof(Teacher) + 12 + 8 * k);
 }
 
 hipError_t launch_distill_grad(const DistillParams& params, hipStream_t stream) {
     const DistillParams p = with_exponents(params);
-    for (int64_t first = 0; first < p.rows; first += kMostRows) {
+    for (int64_t first = 0; first < p.rows; first += most_rows(p.dtype, p.vocab)) {
         const DistillParams q = rows_of(p, first);
         const hipError_t e = q.dtype == OLS_F32 ? launch_finish<float, false>(q, stream) : launch_finish<uint16_t, false>(q, stream);
         if (e != hipSuccess) return e;
@@ -518,7 +518,7 @@ hipError_t launch_distill(const DistillParams& params, void* ws, hipStream_t str
     DistillParams p = with_exponents(params);
     const RowPlan r = row_plan(p.dtype, p.rows, p.vocab);
     p.parts = r.parts, p.part = r.part;
-    for (int64_t first = 0; first < p.rows; first += kMostRows) {
+    for (int64_t first = 0; first < p.rows; first += most_rows(p.dtype, p.vocab)) {
         DistillParams q = rows_of(p, first);                           // one launch's rows after another's in the same place
         hipError_t e = hipSuccess;
         if (r.parts > 1) {

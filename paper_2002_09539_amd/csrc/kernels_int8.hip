@@ -623,6 +623,7 @@ Plan plan_of(const ols_int8& f) {
         double best = 1e30;
         for (const Cost& c : kCosts) {
             const int64_t tiles_m = (f.rows + c.tile - 1) / c.tile, tiles_n = (f.out + c.tile - 1) / c.tile, tiles = tiles_m * tiles_n * f.groups;
+            if (tiles >= (1 << 23)) continue;                  // a launch has fewer than 2^32 threads
             for (int ranges = 1; ranges <= 16 && (ranges == 1 || 4 * ranges <= turns); ranges *= 2) {
                 const double us = cost_of(c, tiles, turns, ranges);
                 if (us >= best) continue;

@@ -567,7 +567,7 @@ struct BeamParams {
     float *part_m, *part_val;
     int32_t* part_idx;
 };
-int64_t beam_workspace_bytes(int dtype, int64_t batch, int in_beams, int beams, int64_t vocab);
+int64_t beam_workspace_bytes(int dtype, int64_t batch, int in_beams, int beams, int64_t vocab);      // negative: more parts than a launch numbers
 hipError_t launch_beam(BeamParams p, void* ws, hipStream_t stream);
 
 // Tensors of one launch, by value in the kernel arguments.  Strides and rows in bytes.

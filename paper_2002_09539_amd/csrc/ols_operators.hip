@@ -244,6 +244,8 @@ int check_beam(const char* who, int64_t batch, int in_beams, int beams, int64_t 
     return OLS_OK;
 }
 
+int too_many_parts(const char* who) { return bad("%s: 2^24 parts of 32768 bf16 or 16384 fp32 logits or more", who); }
+
 // Rows [batch][beams] of `bytes`, as far as they reach; at least one row.
 int64_t extent(int64_t batch, int64_t batch_stride, int64_t beams, int64_t beam_stride, int64_t bytes) { return (batch - 1) * batch_stride + (beams - 1) * beam_stride + bytes; }
 
@@ -502,7 +504,8 @@ int ols_distill_loss_grad(const ols_distill* d, void* stream) {
 
 int64_t ols_beam_workspace_bytes(int64_t batch, int in_beams, int beams, int64_t vocab, int dtype) {
     if (const int rc = check_beam("ols_beam_workspace_bytes", batch, in_beams, beams, vocab, dtype)) return rc;
-    return beam_workspace_bytes(dtype, batch, in_beams, beams, vocab);
+    const int64_t need = beam_workspace_bytes(dtype, batch, in_beams, beams, vocab);
+    return need < 0 ? too_many_parts("ols_beam_workspace_bytes") : need;
 }
 
 int ols_beam_select(const ols_beam* b, void* stream) {
@@ -518,7 +521,9 @@ int ols_beam_select(const ols_beam* b, void* stream) {
     if (!b->score || !b->new_score || !b->token || !b->parent || !b->new_finished) return bad("%s: null pointer", who);
     if (!aligned(b->score, 4) || !aligned(b->length, 4) || !aligned(b->new_score, 4) || !aligned(b->token, 4) || !aligned(b->parent, 4) || !aligned(b->new_length, 4))
         return bad("%s: a pointer is not aligned to its type", who);
-    if (const int rc = check_ws(who, b->ws, b->ws_bytes, beam_workspace_bytes(b->dtype, b->batch, b->in_beams, b->beams, b->vocab))) return rc;
+    const int64_t need = beam_workspace_bytes(b->dtype, b->batch, b->in_beams, b->beams, b->vocab);
+    if (need < 0) return too_many_parts(who);
+    if (const int rc = check_ws(who, b->ws, b->ws_bytes, need)) return rc;
     BeamParams p = {};
     p.dtype = b->dtype, p.in_beams = b->in_beams, p.beams = b->beams, p.eos = b->eos, p.batch = b->batch, p.vocab = b->vocab;
     p.logits = b->logits, p.batch_stride = b->batch_stride, p.beam_stride = b->beam_stride, p.score = b->score, p.finished = b->finished, p.length = b->length;

@@ -91,7 +91,7 @@ def test_selection(batch, have, vocab, beams, dtype):
     check(z, score, beams, length=length, penalty=-0.5)
 
 
-@pytest.mark.parametrize("dtype,batch,have,vocab", [(F32, 1, 2, 70001), (BF16, 1, 3, 140001), (BF16, 128, 4, 20011), (BF16, 64, 8, 70001), (F32, 64, 8, 40001), (BF16, 64, 8, 33001)])
+@pytest.mark.parametrize("dtype,batch,have,vocab", [(F32, 1, 32, 20011), (BF16, 2, 31, 9000), (F32, 1, 3, (1 << 20) + 5), (F32, 1, 2, 70001), (BF16, 1, 3, 140001), (BF16, 128, 4, 20011), (BF16, 64, 8, 70001), (F32, 64, 8, 40001), (BF16, 64, 8, 33001)])
 def test_long_rows(dtype, batch, have, vocab):
     """Rows in parts, and each size of workgroup; some requests of the many are looked at."""
     g = torch.Generator(device="cuda").manual_seed(vocab)
@@ -138,6 +138,23 @@ def test_ties_go_to_the_lower_hypothesis_and_token(parts):
     b = _ops().beam_select(z.cuda(), score.cuda(), beams=8)
     assert b.token[0].tolist() == [40, 100, 40, 100, 40, 100, 0, 1] and b.parent[0].tolist() == [0, 0, 1, 1, 2, 2, 0, 0]
     assert torch.equal(b.token, b.token[:1].expand_as(b.token))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k", [3, 8, 9, 32])
+def test_best_that_one_lane_holds(k, dtype):
+    """The best all side by side, in one lane's registers and its neighbours', and the same value everywhere else: lists longer than their room."""
+    vocab = 32768 if dtype == BF16 else 16384
+    z = torch.full((2, 1, vocab), -3.0)
+    z[0, 0, 4096: 4096 + 40] = torch.arange(40).float() / 8
+    z[1, 0, ::1] = torch.where(torch.arange(vocab) % 3 == 0, 2.0, -5.0)
+    score = torch.zeros(2, 1)
+    z = z.to(dtype)
+    check(z, score, beams=k)
+    many = _ops().beam_select(z.repeat(300, 1, 1).cuda(), score.repeat(300, 1).cuda(), beams=k)        # whole rows in a workgroup
+    few = _ops().beam_select(z.cuda(), score.cuda(), beams=k)
+    assert torch.equal(many.token, few.token.repeat(300, 1))
+    assert float((many.score - few.score.repeat(300, 1)).abs().max()) <= 2e-6 + 2.0 ** -22 * 9      # each within the tolerance above: sums of other parts
 
 
 def test_what_is_not_finite_stays_in_its_request():

@@ -80,6 +80,9 @@ def test_beam_workspace():
     refused(lambda: B.ols_beam_select(filled(B.ols_beam, BEAM, dict(ws_bytes=need - 1)), None), B.OLS_ENOMEM, str(need))
     refused(lambda: B.ols_beam_workspace_bytes(2, 33, 4, 100, F32))
     assert B.ols_beam_workspace_bytes(0, 3, 4, 100, F32) == 0
+    shared = dict(batch=65535, in_beams=32, vocab=1 << 20, batch_stride=0, beam_stride=0)          # one row of logits for all
+    refused(lambda: B.ols_beam_workspace_bytes(65535, 32, 4, 1 << 20, F32), part="2^24 parts")
+    refused(lambda: B.ols_beam_select(filled(B.ols_beam, BEAM, shared), None), part="2^24 parts")
     B.ols_beam_select(filled(B.ols_beam, BEAM, dict(batch=0, logits=None)), None)
 
 
