@@ -28,28 +28,29 @@ __device__ __forceinline__ bool goes_on(const BeamParams& p, int64_t row) {
     return !(p.score[row] == -INFINITY) && !(p.finished && p.finished[row]);
 }
 
-// The best k of what a workgroup of 256 holds, as best_of_part does it, from a bound that is quicker to find: of 16 (k <= 8) or 32 groups of
-// lanes the k-th largest of their maxima, which at least k logits reach and few others.  Where more do than the list holds (many equal
+// The best k of what a workgroup of 256 holds, as best_of_part does it, from a bound that is quicker to find: of 16, 32 or 64 groups of
+// lanes, at least 2 k, the k-th largest of their maxima, which at least k logits reach and few others (of 32 groups the 32nd is the smallest: in the worst of
+// 512 parts 300 logits lie above it, whose order took 28 us).  Where more do than the list holds (many equal
 // ones, or one lane that holds them all) best_of_part takes over.  512 rows of 128 000 bf16, 8 of each: best_of_part 15 us of 39.
 template <typename T, int NV>
 __device__ __forceinline__ void best_of_groups(const u4 (&v)[NV], float lane_max, int64_t start, int k, int room, float* list_val, int* list_idx, float* best_val,
                                                int* best_idx) {
     constexpr int N = Vec<T>::kN;
-    __shared__ float tops[32];
+    __shared__ float tops[64];
     __shared__ int listed;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     float m = lane_max;
     m = fmaxf(m, moved<0x111, 0xf>(m, -INFINITY));
     m = fmaxf(m, moved<0x112, 0xf>(m, -INFINITY));
-    m = fmaxf(m, moved<0x114, 0xf>(m, -INFINITY));             // the lane's and the seven in front of it, of a row of 16
-    const bool wide = k <= 8;
-    if (wide) m = fmaxf(m, moved<0x118, 0xf>(m, -INFINITY));
-    const int size = wide ? 16 : 8, groups = 256 / size;
+    if (k <= 16) m = fmaxf(m, moved<0x114, 0xf>(m, -INFINITY));
+    if (k <= 8) m = fmaxf(m, moved<0x118, 0xf>(m, -INFINITY));
+    const int size = k <= 8 ? 16 : k <= 16 ? 8 : 4, groups = 256 / size;       // lane size - 1 of a group has seen all of it
     if (lane % size == size - 1) tops[(wave * 64 + lane) / size] = m;
     if (threadIdx.x == 0) listed = 0;
     __syncthreads();
     const float mine = lane < groups ? tops[lane] : -INFINITY;
     int above = 0, with = 0;                                   // groups above the lane's, and with those equal to it
+#pragma unroll 16
     for (int i = 0; i < groups; ++i) {
         const float other = lane_of(mine, i);
         above += other > mine ? 1 : 0, with += other >= mine ? 1 : 0;
@@ -78,14 +79,32 @@ __device__ __forceinline__ void best_of_groups(const u4 (&v)[NV], float lane_max
         best_of_part<T, 256, NV>(v, lane_max, start, k, list_val, list_idx, best_val, best_idx);
         return;
     }
-    write_best<256>(list_val, list_idx, listed, k, best_val, best_idx);
+    if (listed <= 64) {
+        write_best<256>(list_val, list_idx, listed, k, best_val, best_idx);
+    } else {                                                   // four listed ones at a time; there is room for four (k >= 9 here, or many are equal)
+        const int count = listed, whole = (count + 3) / 4;
+        if ((int)threadIdx.x < 4 * whole - count) list_val[count + threadIdx.x] = -INFINITY, list_idx[count + threadIdx.x] = 0x7fffffff;
+        __syncthreads();
+        for (int i = threadIdx.x; i < count; i += 256) {
+            const float x = list_val[i];
+            const int at_x = list_idx[i];
+            int place = 0;
+#pragma unroll 2
+            for (int j = 0; j < whole; ++j) {
+                const f4 y = ((const f4*)list_val)[j];
+                const int4 at_y = ((const int4*)list_idx)[j];
+                place += (beats(y[0], at_y.x, x, at_x) ? 1 : 0) + (beats(y[1], at_y.y, x, at_x) ? 1 : 0) + (beats(y[2], at_y.z, x, at_x) ? 1 : 0) + (beats(y[3], at_y.w, x, at_x) ? 1 : 0);
+            }
+            if (place < k) best_val[place] = x, best_idx[place] = at_x;
+        }
+    }
     __syncthreads();
 }
 
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS, 4) void beam_part_kernel(BeamParams p) {
     constexpr int N = Vec<T>::kN, WAVES = THREADS / 64;
-    extern __shared__ char dyn[];
+    extern __shared__ __align__(16) char dyn[];
     __shared__ float red_m[WAVES];
     __shared__ double red_s[WAVES];
     __shared__ float best_val[kMaxTop];
@@ -124,7 +143,7 @@ __global__ __launch_bounds__(THREADS, 4) void beam_part_kernel(BeamParams p) {
     keep_packed(v);
     __syncthreads();
     float* list_val = (float*)dyn;
-    const int room = list_entries<T, THREADS, NV>(p.beams);
+    const int room = list_entries<T, THREADS, NV>(p.beams);       // a multiple of four
     int* list_idx = (int*)(list_val + room);
     best_of_groups<T, NV>(v, lane_max, start, p.beams, room, list_val, list_idx, best_val, best_idx);
     const int64_t slot = row * p.parts + part;
@@ -165,21 +184,22 @@ struct Hypothesis {
     int length, ended, dead;
 };
 
-// A workgroup for each request: its wavefronts add up the parts, then one merges the parts' lists, each in order; a lane looks after every
-// 64th.  LISTS: they lie in LDS.
+// A workgroup for each request: its wavefronts add up the parts and rank the heads of the parts' lists, then one merges these, each in order.  A
+// lane looks after every 64th list; after a turn only the list that was taken from is ranked anew.  LISTS: all lie in LDS.
 template <bool LISTS>
 __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
     __shared__ Hypothesis of[kMaxTop];
     extern __shared__ __align__(8) char dyn[];
     const int64_t batch = blockIdx.x;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, k = p.beams, lists = p.in_beams * p.parts, entries = lists * k;
-    uint8_t* used = (uint8_t*)dyn;                            // of each list: how many are taken
+    double* key = LISTS ? (double*)dyn : p.part_key + batch * lists;      // of each list: its head's rank, -inf where there is none
+    uint8_t* used = (uint8_t*)(dyn + (LISTS ? 8 * lists : 0));            // and how many are taken
     const float *val = p.part_val + batch * entries, *part_m = p.part_m + batch * lists;
     const double* part_s = p.part_s + batch * lists;
     const int* idx = p.part_idx + batch * entries;
     for (int l = threadIdx.x; l < lists; l += 256) used[l] = 0;
     if constexpr (LISTS) {                                    // all that is read, in one round trip
-        double* s = (double*)(dyn + (lists + 7) / 8 * 8);
+        double* s = key + lists + (lists + 7) / 8;
         float *m = (float*)(s + lists), *v = m + lists;
         int* at = (int*)(v + entries);
         for (int i = threadIdx.x; i < lists; i += 256) s[i] = part_s[i], m[i] = part_m[i];
@@ -205,51 +225,92 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
         if (lane == 0) of[i].top = m, of[i].sum = sum;
     }
     __syncthreads();
-    if (wave) return;
-    bool bad = false;
-    if (lane < p.in_beams) {
-        Hypothesis& h = of[lane];
-        bad = !h.dead && (!(h.score < INFINITY) || !(h.sum < INFINITY));
-        h.lead = h.dead || !(h.sum > 0.0) ? (double)-INFINITY : (double)h.score - log_of(h.sum);
-        h.scale = p.penalty == 0.0 ? 1.0 : exp(-p.penalty * log_of((double)max(h.ended ? h.length : h.length + 1, 1)));
+    bool poisoned = false;
+    if (wave == 0) {
+        bool bad = false;
+        if (lane < p.in_beams) {
+            Hypothesis& h = of[lane];
+            bad = !h.dead && (!(h.score < INFINITY) || !(h.sum < INFINITY));
+            h.lead = h.dead || !(h.sum > 0.0) ? (double)-INFINITY : (double)h.score - log_of(h.sum);
+            h.scale = p.penalty == 0.0 ? 1.0 : exp(-p.penalty * log_of((double)max(h.ended ? h.length : h.length + 1, 1)));
+        }
+        poisoned = __ballot(bad) != 0;
+        in_wave_order();
     }
-    const bool poisoned = __ballot(bad) != 0;
-    in_wave_order();
     // The hypothesis of list l: quotients are at least 1 / 2048 off a whole number and below 32, where the product is off by 2^-18.  (Divisions of
     // whole numbers were most of a turn.)
     const float per = 1.0f / (float)p.parts;
     auto owner = [&](int l) { return (int)(((float)l + 0.5f) * per); };
-    // Of the lane's lists the one whose head is first, and of place `lane` of the result what it is.
-    int list = -1, token = -1, from = -1, said = -1;
-    double key = -INFINITY, value = 0.0, score = 0.0;
-    bool stale = true;
+    // Entry `at` of list l: whether it is there, its token and value.  Two round trips to LDS.
+    struct Candidate {
+        int token;                                            // -1: none
+        double value, rank;
+    };
+    auto candidate = [&](int l, int at) {
+        const int i = owner(l), entry = l * k + min(at, k - 1);
+        const Hypothesis h = of[i];
+        const int said = idx[entry];
+        const float z = val[entry];
+        Candidate c;
+        c.value = h.ended ? h.lead : h.lead + ((double)z - (double)h.top);
+        c.rank = c.value * h.scale;
+        c.token = !(h.lead > -INFINITY) ? -1 : h.ended ? (at == 0 && l == i * p.parts ? 0 : -1) : at < k ? said : -1;
+        return c;
+    };
+    auto rank_of = [&](int l, int at) {
+        const Candidate c = candidate(l, at);
+        return c.token < 0 ? (double)-INFINITY : c.rank;
+    };
+    const bool single = lists <= 64;                          // a list for each lane
+    if (!single) {
+        __syncthreads();
+        for (int l = threadIdx.x; l < lists; l += 256) key[l] = rank_of(l, 0);
+        __syncthreads();
+    }
+    if (wave) return;
+    // The lane's best list, and of place `lane` of the result its list and entry.
+    constexpr int kMine = 9;                                  // lists of a lane whose ranks stay in registers: 512 and a few parts for one request
+    const bool held = lists <= 64 * kMine;
+    const int per_lane = (lists + 63) / 64;
+    double mine[kMine];
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) mine[j] = held && !single && lane + 64 * j < lists ? key[lane + 64 * j] : -INFINITY;
+    if (single && lane < lists) mine[0] = rank_of(lane, 0);
+    int list = -1, from = -1, entry = 0;
+    double best = -INFINITY;
 #pragma unroll 1
     for (int turn = 0; turn < k && !poisoned; ++turn) {
-        if (stale) {
-            list = -1, key = -INFINITY;
-#pragma unroll 1
-            for (int l = lane; l < lists; l += 64) {          // two round trips to LDS, whatever the head is
-                const int i = owner(l), at = used[l], entry = l * k + min(at, k - 1);
-                const Hypothesis h = of[i];
-                const int said_here = idx[entry];
-                const double v = h.ended ? h.lead : h.lead + ((double)val[entry] - (double)h.top), ranked = v * h.scale;
-                const bool there = h.lead > -INFINITY && (h.ended ? at == 0 && l == i * p.parts : at < k && said_here >= 0);
-                if (there && (list < 0 || ranked > key)) list = l, key = ranked, value = v, token = h.ended ? 0 : said_here;   // ties: the lower list
+        list = -1, best = -INFINITY;
+        if (held) {
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                if (j >= per_lane) break;
+                const bool more = mine[j] > best;             // ties: the lower list
+                list = more ? lane + 64 * j : list, best = more ? mine[j] : best;
+            }
+        } else {
+            for (int l = lane; l < lists; l += 64) {
+                const double v = key[l];
+                if (v > best) list = l, best = v;
             }
         }
-        const double best = wave_max(key);
-        const unsigned long long at = __ballot(list >= 0 && key == best);
+        const double first = wave_max(best);
+        const unsigned long long at = __ballot(list >= 0 && best == first);
         if (!at) break;
-        int who = __ffsll(at) - 1, first = __builtin_amdgcn_readlane(list, who);
+        int who = __ffsll(at) - 1, taken = __builtin_amdgcn_readlane(list, who);
         for (unsigned long long more = at & (at - 1); more; more &= more - 1) {
             const int other = __ffsll(more) - 1, l = __builtin_amdgcn_readlane(list, other);
-            if (l < first) first = l, who = other;
+            if (l < taken) taken = l, who = other;
         }
-        const int token_first = __builtin_amdgcn_readlane(token, who);
-        const double value_first = lane_of(value, who);
-        if (lane == turn) from = first, said = token_first, score = value_first;
-        stale = lane == who;
-        if (stale) used[first] += 1;
+        const int place = used[taken];
+        if (lane == turn) from = taken, entry = place;
+        if (lane == who) {
+            const double rank = rank_of(taken, place + 1);
+            used[taken] = (uint8_t)(place + 1);
+            if (!held) key[taken] = rank;
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) mine[j] = taken == lane + 64 * j ? rank : mine[j];
+        }
         in_wave_order();
     }
     if (lane >= k) return;
@@ -260,8 +321,9 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
         if (p.new_length) p.new_length[out] = of[slot].length;
     } else {
         const Hypothesis& h = of[owner(from)];
-        p.new_score[out] = (float)score, p.token[out] = h.ended ? p.eos : said, p.parent[out] = owner(from);
-        p.new_finished[out] = h.ended || (p.eos >= 0 && said == p.eos);
+        const Candidate c = candidate(from, entry);
+        p.new_score[out] = (float)c.value, p.token[out] = h.ended ? p.eos : c.token, p.parent[out] = owner(from);
+        p.new_finished[out] = h.ended || (p.eos >= 0 && c.token == p.eos);
         if (p.new_length) p.new_length[out] = h.length + (h.ended ? 0 : 1);
     }
 }
@@ -360,6 +422,8 @@ __global__ __launch_bounds__(256) void beam_move_kernel(BeamMove t) {
 
 }  // namespace
 
+constexpr int64_t kLds = 152 << 10;       // of a compute unit's 160 KiB, beside what the join declares
+
 // Workgroups of four wavefronts: several run on a compute unit, and one's search for its best overlaps with another's loads.  512 rows of
 // 128 000 bf16 in workgroups that hold whole rows: 49 us.
 static RowPlan beam_plan(int dtype, int64_t rows, int64_t vocab) { return row_plan(dtype, rows, vocab, 256); }
@@ -368,7 +432,7 @@ static RowPlan beam_plan(int dtype, int64_t rows, int64_t vocab) { return row_pl
 int64_t beam_workspace_bytes(int dtype, int64_t batch, int in_beams, int beams, int64_t vocab) {
     if (batch == 0) return 0;
     const int64_t rows = batch * in_beams, parts = rows * beam_plan(dtype, rows, vocab).parts;
-    return parts >= (1 << 24) ? -1 : parts * (12 + 8 * (int64_t)beams);
+    return parts >= (1 << 24) ? -1 : parts * (20 + 8 * (int64_t)beams);
 }
 
 hipError_t launch_beam(BeamParams p, void* ws, hipStream_t stream) {
@@ -377,14 +441,20 @@ hipError_t launch_beam(BeamParams p, void* ws, hipStream_t stream) {
     const RowPlan r = beam_plan(p.dtype, rows, p.vocab);
     p.parts = r.parts, p.part = r.part;
     p.part_s = (double*)ws;
-    p.part_m = (float*)(p.part_s + rows * r.parts);
+    p.part_key = p.part_s + rows * r.parts;
+    p.part_m = (float*)(p.part_key + rows * r.parts);
     p.part_val = p.part_m + rows * r.parts;
     p.part_idx = (int32_t*)(p.part_val + rows * r.parts * p.beams);
     hipError_t e = p.dtype == OLS_F32 ? launch_typed<float>(p, r, stream) : launch_typed<uint16_t>(p, r, stream);
     if (e != hipSuccess) return e;
-    const int64_t lists = (int64_t)p.in_beams * r.parts, counts = (lists + 7) / 8 * 8, whole = counts + lists * (12 + 8 * (int64_t)p.beams);
-    if (whole <= 48 << 10) beam_join_kernel<true><<<(unsigned)p.batch, 256, (size_t)whole, stream>>>(p);
-    else beam_join_kernel<false><<<(unsigned)p.batch, 256, (size_t)counts, stream>>>(p);
+    const int64_t lists = (int64_t)p.in_beams * r.parts, counts = (lists + 7) / 8 * 8, whole = counts + lists * (20 + 8 * (int64_t)p.beams);
+    if (whole > kLds) {
+        beam_join_kernel<false><<<(unsigned)p.batch, 256, (size_t)counts, stream>>>(p);        // at most 32 KiB
+        return hipGetLastError();
+    }
+    if (whole > (60 << 10)) e = ensure_dynamic_lds((const void*)beam_join_kernel<true>, kLds);
+    if (e != hipSuccess) return e;
+    beam_join_kernel<true><<<(unsigned)p.batch, 256, (size_t)whole, stream>>>(p);
     return hipGetLastError();
 }
 

@@ -563,7 +563,7 @@ struct BeamParams {
     // set by the launcher: of each hypothesis' parts
     int parts;
     int64_t part;
-    double* part_s;
+    double *part_s, *part_key;
     float *part_m, *part_val;
     int32_t* part_idx;
 };

@@ -91,7 +91,7 @@ def test_selection(batch, have, vocab, beams, dtype):
     check(z, score, beams, length=length, penalty=-0.5)
 
 
-@pytest.mark.parametrize("dtype,batch,have,vocab", [(F32, 1, 32, 20011), (BF16, 2, 31, 9000), (F32, 1, 3, (1 << 20) + 5), (F32, 1, 2, 70001), (BF16, 1, 3, 140001), (BF16, 128, 4, 20011), (BF16, 64, 8, 70001), (F32, 64, 8, 40001), (BF16, 64, 8, 33001)])
+@pytest.mark.parametrize("dtype,batch,have,vocab", [(F32, 1, 32, 20011), (BF16, 2, 31, 9000), (F32, 1, 3, (1 << 20) + 5), (F32, 1, 17, (1 << 20) + 5), (F32, 1, 2, 70001), (BF16, 1, 3, 140001), (BF16, 128, 4, 20011), (BF16, 64, 8, 70001), (F32, 64, 8, 40001), (BF16, 64, 8, 33001)])
 def test_long_rows(dtype, batch, have, vocab):
     """Rows in parts, and each size of workgroup; some requests of the many are looked at."""
     g = torch.Generator(device="cuda").manual_seed(vocab)
