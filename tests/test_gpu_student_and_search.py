@@ -126,6 +126,32 @@ def test_search_in_eight_bits():
         s.sync()
 
 
+def test_calls_on_two_streams_at_once():
+    from paper_2002_09539_amd import operators as ops
+    g = torch.Generator(device="cuda").manual_seed(3)
+    z = [torch.randn(n, 30011, generator=g, device="cuda").bfloat16() for n in (7, 600)]
+    lists = [ops.token_logprobs(t, None, top=16) for t in z]
+    x, w = [torch.randn(n, 1030, generator=g, device="cuda") for n in (20, 300)], ops.quantize_weight(torch.randn(1030, 700, generator=g, device="cuda"))
+    beams = [t[: t.shape[0] // 6 * 6].view(-1, 6, 30011) if t.shape[0] >= 600 else t[None, :6].contiguous() for t in z]
+    scores = [torch.randn(b.shape[:2], generator=g, device="cuda") for b in beams]
+
+    def calls(i):
+        r, d = ops.distill_loss_with_grad(z[i], lists[i].top_logprob, lists[i].top_index, torch.ones(len(z[i]), device="cuda"), rest=True)
+        b = ops.beam_select(beams[i], scores[i])
+        return [r.loss, d, b.score, b.token, b.parent, ops.int8_matmul(x[i], w)]
+    want = [calls(0), calls(1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        got = [None, None]
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                got[i] = calls(i)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
 def test_the_command_runs(capsys, monkeypatch):
     from paper_2002_09539_amd import token_model
     monkeypatch.setattr("sys.argv", ["token_model", "--rounds", "5", "--workers", "2", "--batch", "32", "--vocab", "64", "--width", "16", "--hidden", "48", "--student", "24",
