@@ -51,9 +51,9 @@ struct Teacher {
     int target_listed, twice, any;       // the target is in the list; a token is named twice; some q is positive
 };
 
-// Reads a row's list and target; by one wavefront.
+// Reads a row's list and target; by one wavefront.  kept: their logits, where the launch may write over them.
 template <typename T>
-__device__ __forceinline__ void read_list(const DistillParams& p, List& l, Teacher& t, int64_t row, const T* z) {
+__device__ __forceinline__ void read_list(const DistillParams& p, List& l, Teacher& t, int64_t row, const T* z, const float* kept = nullptr) {
     const int target = p.targets ? p.targets[row] : -1;
     t.target = target >= 0 && target < p.vocab ? target : -1;
     bool met = false;
@@ -63,11 +63,11 @@ __device__ __forceinline__ void read_list(const DistillParams& p, List& l, Teach
         const bool there = at >= 0 && at < p.vocab;
         l.index[i] = there ? at : -1;
         l.q[i] = value;
-        l.z[i] = there ? load1(z + at) : -INFINITY;
+        l.z[i] = !there ? -INFINITY : kept ? kept[i] : load1(z + at);
         met |= there && at == t.target;
     }
     t.target_listed = __ballot(met) != 0;
-    t.z_target = t.target >= 0 ? load1(z + t.target) : -INFINITY;
+    t.z_target = t.target < 0 ? -INFINITY : kept ? kept[p.k] : load1(z + t.target);
     in_wave_order();
 }
 
@@ -315,6 +315,14 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(DistillParams p) {
         return at >= start && at < end ? (int)(at - start) : -1;
     };
     int at = place(blockIdx.x);
+    if (!whole) {
+        // The listed logits and the target's, for the workgroups that finish the row: the gradient of one may lie on what another reads.
+        float* kept = p.list_z + (int64_t)blockIdx.x * (p.k + 1);
+        const T* z = (const T*)p.logits + (int64_t)blockIdx.x * p.row_stride;
+        if (at >= 0) kept[threadIdx.x] = load1(z + start + at);
+        const int target = threadIdx.x == 0 && p.targets ? p.targets[blockIdx.x] : -1;
+        if (target >= start && target < end) kept[p.k] = load1(z + target);
+    }
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
         if (p.rest) {
             __syncthreads();                   // the bits are clear
@@ -387,7 +395,7 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillParams p) {
     if (lane < 64) {
         const float* sums = JOIN ? p.part_sums + 3 * row * p.parts : nullptr;
         if (JOIN && lane < p.parts) a = Sums{sums[3 * lane], sums[3 * lane + 1], sums[3 * lane + 2]};
-        read_list<T>(p, list, t, row, z);
+        read_list<T>(p, list, t, row, z, JOIN ? p.list_z + row * (p.k + 1) : nullptr);
         if constexpr (JOIN) {
             for (int i = lane + 64; i < p.parts; i += 64) a = join(p, a, Sums{sums[3 * i], sums[3 * i + 1], sums[3 * i + 2]});
             for (int o = 32; o; o >>= 1) {
@@ -419,7 +427,7 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillParams p) {
     const float z_target = has_target ? load1(z + target) : 0.0f;
     const float g_loss = p.g_loss ? p.g_loss[row] * p.temperature : 0.0f;
     const float g_hard = target >= 0 && target < p.vocab && p.g_logprob ? p.g_logprob[row] : 0.0f;
-    __syncthreads();                           // every logit of the list is read: the gradient may lie on them
+    __syncthreads();                           // the logits of the part are read: the gradient may lie on them
     const Coefs c = shared;
     const Second second = second_of(p);
     if (second == kNone) write_grad<kNone>(p, h, c, d + start, (const T*)nullptr, length, g_loss, g_hard);
@@ -513,12 +521,12 @@ DistillParams with_exponents(DistillParams p) {
 
 }  // namespace
 
-// Whole rows: of each what its list adds up to, q and z, and the sums.  Parts: their sums.
+// Whole rows: of each what its list adds up to, q and z, and the sums.  Parts: their sums, and the listed logits and the target's.
 int64_t distill_workspace_bytes(int dtype, int64_t rows, int64_t vocab, int k) {
     if (rows == 0) return 0;
     const RowPlan r = distill_plan(dtype, rows, vocab, k);
     rows = std::min(most_rows(dtype, vocab), rows);
-    return rows * (r.parts > 1 ? r.parts * 12 : (int64_t)sizeof(Teacher) + 12 + 8 * k);
+    return rows * (r.parts > 1 ? r.parts * 12 + 4 * (k + 1) : (int64_t)sizeof(Teacher) + 12 + 8 * k);
 }
 
 hipError_t launch_distill_grad(const DistillParams& params, hipStream_t stream) {
@@ -540,7 +548,7 @@ hipError_t launch_distill(const DistillParams& params, void* ws, hipStream_t str
         DistillParams q = rows_of(p, first);                           // one launch's rows after another's in the same place
         hipError_t e = hipSuccess;
         if (r.parts > 1) {
-            q.part_sums = (float*)ws;
+            q.part_sums = (float*)ws, q.list_z = q.part_sums + 3 * q.rows * r.parts;
         } else {
             q.teachers = ws;
             q.part_sums = (float*)((char*)ws + q.rows * sizeof(Teacher)), q.list_q = q.part_sums + 3 * q.rows, q.list_z = q.list_q + q.rows * q.k;

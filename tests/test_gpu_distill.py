@@ -176,6 +176,24 @@ def test_long_rows(rows, vocab, dtype, rest):
             assert bool(((grad[i].cpu().double() - w).abs() <= room).all())
 
 
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,vocab,dtype", [(2048, 66001, F32), (2048, 140003, BF16), (31, 20011, F32)])
+def test_gradient_on_the_logits_of_many_rows_in_parts(rows, vocab, dtype, rest):
+    """Workgroups that write a row's gradient late need what others wrote over early: lists in all parts, or in the first one alone."""
+    g = torch.Generator(device="cuda").manual_seed(rows + rest)
+    z = (torch.randn(rows, vocab, generator=g, device="cuda") * 2.0).to(dtype)
+    index = torch.randint(0, vocab, (rows, 24), generator=g, device="cuda", dtype=torch.int32)
+    index[::2] %= 4000
+    value = torch.log_softmax(torch.randn(rows, 25, generator=g, device="cuda"), 1)[:, :24].contiguous()
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    t[::3] %= 4000
+    gl, gh = torch.rand(rows, generator=g, device="cuda"), torch.rand(rows, generator=g, device="cuda")
+    apart, d = _ops().distill_loss_with_grad(z, value, index, gl, targets=t, d_logprob=gh, temperature=1.5, rest=rest)
+    on = _ops().distill_loss_with_grad(z, value, index, gl, targets=t, d_logprob=gh, temperature=1.5, rest=rest, out=z)
+    assert torch.equal(apart.loss, on[0].loss) and torch.equal(apart.logprob, on[0].logprob) and torch.equal(apart.stats, on[0].stats)
+    assert on[1] is z and torch.equal(d, z)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("rows,vocab", [(9, 300), (530, 600)])
