@@ -593,7 +593,8 @@ OLS_API int ols_beam_reorder(int n, const void* const* src, void* const* dst, co
  *   - dtype OLS_F32 or OLS_BF16: x is given in that type, and the call quantises its rows as ols_quantize_rows does; with `up` it takes
  *     act(x) up in its place, in fp32 (the hidden rows of a gated block).  OLS_I8: x and x_scale are given.  Weights are best with rows that begin on 16
  *     bytes; others are read more slowly.
- *   - y is of out_dtype.  Limits: groups <= 4096, width < 2^17, out <= 2^24, rows <= 2^24; fewer than 2^23 tiles of
+ *   - y is of out_dtype.  It may lie on x or `up` where the call quantises them, which it does first, and on nothing else that is read.
+ *     The workspace's size is that of the descriptor with its pointers.  Limits: groups <= 4096, width < 2^17, out <= 2^24, rows <= 2^24; fewer than 2^23 tiles of
  *     16 x 16 results (up to 64 rows) or 128 x 128. */
 enum { OLS_I8 = 2 };
 typedef struct ols_int8 {

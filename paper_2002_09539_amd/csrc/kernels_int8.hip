@@ -2,7 +2,13 @@
 //
 //   s_r = fp32(max |x_r| / 127),  q_rk = x_rk / s_r to the nearest whole number, halves to even,   y_rc = (sum_k q_rk w_ck) s_r t_c
 //
-// The sums are whole numbers, exact in 32 bits whatever their order (width < 2^17).
+// The sums are whole numbers, exact in 32 bits whatever their order (width < 2^17); the two scales are applied to them in fp32, and the
+// result is rounded once.
+//
+// Few rows are bound by the weights' bytes: they go from memory straight into the registers of the matrix instruction (a row of 2048 to
+// 32 000, 65 MB: 15.4 us, 4.3 TB/s).  Many rows are bound by the matrix pipes: both operands go through tiles in LDS (8192 rows, 4096 to
+// 4096: 147 to 164 us as the clock allows, 1680 to 1880 TOP/s, where a library's product of 8192^3 reaches 2046).  Between them, some
+// dozens of tiles, a launch is a chain of waits.
 #include <algorithm>
 
 #include "element_io.h"
@@ -107,7 +113,7 @@ __device__ __forceinline__ void store_packed(int8_t* q, int64_t left, u2 w) {
 }
 
 // A workgroup for each row.  Up to NV vectors of eight a lane stay in registers from the search for the largest value to the rounding;
-// NV = 0: longer rows are read again.
+// NV = 0: longer rows are read again.  Bound by bytes: 8192 rows of 4096 bf16 25.5 us, 3.9 TB/s.
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void quantize_rows_kernel(QuantRows p) {
     __shared__ unsigned tops[THREADS / 64];
@@ -271,8 +277,9 @@ __device__ __forceinline__ void store_scaled(const Product& p, int64_t group, in
 }
 
 // Few rows: a workgroup for 16 channels and 16 R rows, whose wavefronts share the contraction in ranges; kAhead turns of 64 indices are
-// under way before anything is waited for.  FUSED: the workgroup quantises the one row itself, into LDS,
-// which saves 1.5 us of a launch's 3; of two rows and more it saves nothing.
+// under way before anything is waited for.  FUSED: the workgroup quantises the one row itself, into LDS, and a launch falls away (1.5 us
+// of a call).  Of more rows every workgroup would have more to do than the launch takes (all of a call on the device, quantised here / by
+// themselves: 8 rows, 2048 to 2048 9.7 / 8.5 us, 16 rows, 1024 to 8000 12.5 / 9.2).
 constexpr int kAhead = 8;
 template <typename TX, int R, int WAVES, bool FUSED>
 __global__ __launch_bounds__(WAVES * 64) void few_kernel(Product p) {
@@ -614,6 +621,13 @@ struct Plan {
 
 bool lies_well(const ols_matrix& m) { return m.row % 16 == 0 && m.row <= (1 << 22) && m.group % 16 == 0 && ((uintptr_t)m.dev & 15) == 0; }
 
+// Whether y lies away from the one row of each group that m holds.
+bool away(const ols_int8& f, const ols_matrix& m) {
+    const char *a = (const char*)m.dev, *y = (const char*)f.y.dev;
+    const int64_t size = f.dtype == OLS_F32 ? 4 : 2, y_size = f.out_dtype == OLS_F32 ? 4 : 2;
+    return a >= y + ((f.groups - 1) * f.y.group + f.out) * y_size || y >= a + ((f.groups - 1) * m.group + f.width) * size;
+}
+
 constexpr int kCus = 256;
 // Up to this many rows weights go straight into registers.  Products alone, in us, few_kernel / tiles: 32 rows, 2048 to 2048: 6.6 / 9.5; to
 // 11 264: 12.3 / 11.7; 64 rows, 5632 to 2048: 11.3 / 11.2, 2048 to 11 264: 15.9 / 11.7, to 32 000: 36 / 18.
@@ -650,6 +664,7 @@ Plan plan_of(const ols_int8& f) {
         p.waves = 2;
         while (p.waves < 16 && 2 * p.waves * blocks <= kFewWaves && 4 * p.waves <= turns) p.waves *= 2;
         p.fused = f.dtype != OLS_I8 && f.rows == 1 && f.width <= 32768 && f.width * blocks <= (1 << 23);
+        p.fused = p.fused && away(f, f.x) && (!f.up.dev || away(f, f.up));      // while some quantise, others write
     } else {
         double best = 1e30;
         for (const Cost& c : kCosts) {

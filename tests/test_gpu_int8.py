@@ -213,6 +213,21 @@ def test_strides_and_what_lies_around(rows):
     near(ops.int8_matmul(ops.Int8Rows(qbig[:, 9:9 + width], s.cuda()), ops.Int8Weight(wq, ws), dtype=F32), product_want(q, s, wq.cpu(), ws.cpu()))
 
 
+@pytest.mark.parametrize("m,rows,width", [(1, 1, 4096), (1, 1, 32768), (3, 1, 2000), (1, 5, 512), (1, 40, 2048), (2, 300, 640)])
+def test_result_on_what_is_quantised(m, rows, width):
+    """The result takes the place of x, of up, or of both by halves: rows are quantised before anything is written."""
+    ops = _ops()
+    x, up = normal(1, m, rows, width, dtype=BF16).cuda(), normal(2, m, rows, width, dtype=BF16).cuda()
+    w = ops.Int8Weight(torch.randint(-127, 128, (m, width, (width + 15) // 16 * 16), dtype=torch.int8, device="cuda")[..., :width], torch.rand(m, width, device="cuda"))
+    plain, gated = ops.int8_matmul(x, w), ops.int8_matmul(x, w, up=up)
+    on_x, on_up = x.clone(), up.clone()
+    assert torch.equal(ops.int8_matmul(on_x, w, out=on_x), plain) and torch.equal(ops.int8_matmul(x, w, up=on_up, out=on_up), gated)
+    both = torch.cat([x, up], -1)
+    shifted = both[..., width // 2:width // 2 + width]
+    ops.int8_matmul(both[..., :width], w, up=both[..., width:], out=shifted)
+    assert torch.equal(shifted, gated)
+
+
 @pytest.mark.parametrize("rows,width,out", [(1, 512, 100), (40, 300, 64), (300, 256, 300)])
 def test_streams_and_capture(rows, width, out):
     ops = _ops()
