@@ -194,6 +194,20 @@ def test_whole_range_of_values_and_long_sums(rows):
     near(ops.int8_matmul(x.cuda(), ops.Int8Weight(wq.cuda(), ws.cuda())), product_want(q, sx, wq, ws))
 
 
+@pytest.mark.parametrize("rows,width,out", [(1, 300, 40), (9, 512, 70), (40, 4096, 64), (300, 640, 300)])
+@pytest.mark.parametrize("size", [1e36, 1e-36])
+def test_scales_whose_products_with_the_sums_leave_the_range(rows, width, out, size):
+    """Large rows with small channels and small rows with large channels: the result is an ordinary number."""
+    ops = _ops()
+    g = torch.Generator().manual_seed(rows)
+    wq, xq = torch.randint(-127, 128, (out, width), generator=g).to(torch.int8), torch.randint(-127, 128, (rows, width), generator=g).to(torch.int8)
+    s, ws = (torch.rand(rows, generator=g) + 0.5) * size, (torch.rand(out, generator=g) + 0.5) / size
+    for a, b in ((s, ws), (ws.new_full((rows,), 1.0 / size), ws.new_full((out,), size))):
+        y = ops.int8_matmul(ops.Int8Rows(xq.cuda(), a.cuda()), ops.Int8Weight(wq.cuda(), b.cuda()), dtype=F32)
+        assert bool(torch.isfinite(y).all())
+        near(y, product_want(xq, a, wq, b))
+
+
 @pytest.mark.parametrize("rows", [1, 8, 50, 260])
 def test_strides_and_what_lies_around(rows):
     ops = _ops()
