@@ -51,7 +51,7 @@ _SAME = contextlib.nullcontext()
 def _on(device):
     """The tensors' device as the current one, which it mostly is."""
     index = device if isinstance(device, int) else device.index
-    return _SAME if index == torch.cuda.current_device() else torch.cuda.device(index)
+    return _SAME if index == torch._C._cuda_getDevice() else torch.cuda.device(index)
 
 
 def _stream(device):
@@ -155,13 +155,19 @@ _ACT = {"silu": B.OLS_ACT_SILU, "gelu": B.OLS_ACT_GELU, "relu": B.OLS_ACT_RELU}
 
 def _matrix(t, m, shape, name):
     """A tensor as the C boundary takes it: [m][rows][cols], without the worker axis [rows][cols] shared by the workers."""
-    have = tuple(t.shape)
-    if have == shape and (m == 1 or name in _SHARED):
-        t = t.unsqueeze(0)
-    elif have != (m, *shape):
-        _refuse("%s must be of shape %s, got %s", name, (m, *shape), have)
-    group, row = _rows(t, name)
-    return B.ols_matrix(t.data_ptr(), row, group)
+    have, stride = t.shape, t.stride()
+    rows, width = shape
+    group = 0
+    if have != shape or not (m == 1 or name in _SHARED):
+        if have != (m, rows, width):
+            _refuse("%s must be of shape %s, got %s", name, (m, *shape), tuple(have))
+        group = stride[0] if m > 1 else 0
+    if stride[-1] != 1 and width > 1:
+        _refuse("%s: the elements of a row must be contiguous", name)
+    if 0 in have:
+        return B.ols_matrix(t.data_ptr(), max(1, width), 0)
+    row = stride[-2]
+    return B.ols_matrix(t.data_ptr(), row if rows > 1 or row > width else width, group)
 
 
 def _saved(t):
@@ -264,11 +270,14 @@ def gated_ffn_grad(dy, x, w_gate, w_up, w_down, saved, act="silu", out=None, gra
 
 # ---- log probabilities --------------------------------------------------------------------------------------------
 def _logit_rows(t, name):
-    if t.dim() < 1 or t.shape[-1] < 1:
-        _refuse("%s must have a last axis of tokens, got shape %s", name, tuple(t.shape))
-    vocab = t.shape[-1]
-    if t.dim() == 2 and (t.stride(1) == 1 or vocab == 1):
-        return t, t.shape[0], t.stride(0) if t.shape[0] > 1 else vocab     # rows that overlap are refused by the boundary
+    shape = t.shape
+    if not shape or shape[-1] < 1:
+        _refuse("%s must have a last axis of tokens, got shape %s", name, tuple(shape))
+    vocab = shape[-1]
+    if len(shape) == 2:
+        row, step = t.stride()
+        if step == 1 or vocab == 1:
+            return t, shape[0], row if shape[0] > 1 else vocab     # rows that overlap are refused by the boundary
     if not t.is_contiguous():
         _refuse("%s must be contiguous, or two-dimensional with contiguous rows", name)
     return t, t.numel() // vocab, vocab
@@ -519,8 +528,8 @@ def beam_select(logits, score, beams=None, finished=None, length=None, eos=-1, l
     device = _on_gpu(logits, score, finished, length)
     if logits.dim() != 3:
         _refuse("logits are [batch, hypotheses, vocab], got %d axes", logits.dim())
-    batch, have, vocab = logits.shape
-    if vocab > 1 and logits.stride(2) != 1:
+    (batch, have, vocab), stride = logits.shape, logits.stride()
+    if vocab > 1 and stride[2] != 1:
         _refuse("logits: the elements of a row must be contiguous")
     code, beams = _dtype(logits, "logits"), have if beams is None else int(beams)
     rows = (batch, have)
@@ -529,15 +538,14 @@ def beam_select(logits, score, beams=None, finished=None, length=None, eos=-1, l
     nbytes = B.ols_beam_workspace_bytes(batch, have, beams, vocab, code)
     with _on(device):
         ws = _workspace(nbytes, device)
-        new_score = torch.empty(batch, beams, dtype=torch.float32, device=device)
-        whole = torch.empty(2 if length is None else 3, batch, beams, dtype=torch.int32, device=device).unbind(0)
+        parts = torch.empty(3 if length is None else 4, batch, beams, dtype=torch.int32, device=device).unbind(0)
+        new_score, token, parent = parts[0].view(torch.float32), parts[1], parts[2]
+        new_length = None if length is None else parts[3]
         ended = torch.empty(batch, beams, dtype=torch.bool, device=device)
-        new_length = None if length is None else whole[2]
-        b = B.ols_beam(code, have, beams, int(eos), batch, vocab, logits.data_ptr(), logits.stride(0), logits.stride(1), score.data_ptr(), _ptr(finished),
-                       _ptr(length), float(length_penalty), new_score.data_ptr(), whole[0].data_ptr(), whole[1].data_ptr(), _ptr(new_length), ended.data_ptr(),
-                       _ptr(ws), nbytes)
+        b = B.ols_beam(code, have, beams, int(eos), batch, vocab, logits.data_ptr(), stride[0], stride[1], score.data_ptr(), _ptr(finished), _ptr(length),
+                       float(length_penalty), new_score.data_ptr(), token.data_ptr(), parent.data_ptr(), _ptr(new_length), ended.data_ptr(), _ptr(ws), nbytes)
         B.ols_beam_select(b, _stream(device))
-    return Beams(new_score, whole[0], whole[1], ended, new_length)
+    return Beams(new_score, token, parent, ended, new_length)
 
 
 def _state_rows(t, batch, beams, name):
@@ -587,12 +595,13 @@ def beam_reorder(states, parent, out=None):
         dst_batch, dst_beam = src_batch, src_beam
     else:
         for s, o in zip(states, outs):
-            if o.dtype != s.dtype or o.shape[2:] != s.shape[2:]:
+            if o.dtype != s.dtype or (o.shape != s.shape and o.shape[2:] != s.shape[2:]):
                 _refuse("an output is %s of shape %s, for a state of %s and shape %s", o.dtype, tuple(o.shape), s.dtype, tuple(s.shape))
         _, dst_batch, dst_beam = zip(*[_state_rows(t, batch, beams, "an output") for t in outs])
-        read = {p: i for i, (p, n) in enumerate(zip(src, row_bytes)) if n}
-        if any(n and read.get(p, i) != i for i, (p, n) in enumerate(zip(dst, row_bytes))):
-            _refuse("an output is another state of the call")
+        if not set(src).isdisjoint(dst):
+            read = {p: i for i, (p, n) in enumerate(zip(src, row_bytes)) if n}
+            if any(n and read.get(p, i) != i for i, (p, n) in enumerate(zip(dst, row_bytes))):
+                _refuse("an output is another state of the call")
     if not _distinct(dst, row_bytes):
         _refuse("a state cannot be written twice in one call")
     parent = parent.contiguous()
@@ -618,9 +627,10 @@ def _padded(n):
 
 def _scale(t, m, n, name):
     """Address and workers' stride of fp32 scales [n] or [m][n]."""
-    if t.dtype != torch.float32 or tuple(t.shape) not in ((n,), (m, n)) or not t.is_contiguous():
-        _refuse("%s must be contiguous float32 of shape %s, got %s of shape %s", name, (m, n), t.dtype, tuple(t.shape))
-    return t.data_ptr(), (n if t.dim() == 2 and m > 1 else 0)
+    shape = t.shape
+    if t.dtype != torch.float32 or not (shape == (n,) or shape == (m, n)) or not t.is_contiguous():
+        _refuse("%s must be contiguous float32 of shape %s, got %s of shape %s", name, (m, n), t.dtype, tuple(shape))
+    return t.data_ptr(), (n if len(shape) == 2 and m > 1 else 0)
 
 
 def _act_code(act):
@@ -680,11 +690,12 @@ def int8_matmul(x, weight, up=None, act="silu", out=None, dtype=None):
     device = _on_gpu(xq, wq, w_scale, up, out, *((x.scale,) if given else ()))
     if wq.dtype != torch.int8 or (given and xq.dtype != torch.int8):
         _refuse("quantised tensors must be int8")
-    if xq.dim() not in (2, 3) or wq.dim() not in (2, 3):
+    x_shape, w_shape = xq.shape, wq.shape
+    if len(x_shape) not in (2, 3) or len(w_shape) not in (2, 3):
         _refuse("x is [rows, width] or [m, rows, width], a quantised weight [out, width] or [m, out, width]")
-    workers = xq.dim() == 3 or wq.dim() == 3
-    m = xq.shape[0] if xq.dim() == 3 else wq.shape[0] if workers else 1
-    rows, width, channels = xq.shape[-2], xq.shape[-1], wq.shape[-2]
+    workers = len(x_shape) == 3 or len(w_shape) == 3
+    m = x_shape[0] if len(x_shape) == 3 else w_shape[0] if workers else 1
+    rows, width, channels = x_shape[-2], x_shape[-1], w_shape[-2]
     code = B.OLS_I8 if given else _dtype(xq, "x")
     dtype = dtype or (out.dtype if out is not None else torch.bfloat16 if given else xq.dtype)
     mx, mw, mu = _matrix(xq, m, (rows, width), "x"), _matrix(wq, m, (channels, width), "weight"), _NO_MATRIX
@@ -697,7 +708,7 @@ def int8_matmul(x, weight, up=None, act="silu", out=None, dtype=None):
     shape = (m, rows, channels) if workers else (rows, channels)
     with _on(device):
         if out is None:
-            out = torch.empty(shape, dtype=dtype, device=device)
+            out = torch.empty(*shape, dtype=dtype, device=device)
         elif out.shape != shape or out.dtype != dtype:
             _refuse("out must be %s of shape %s", dtype, shape)
         f = B.ols_int8(m, code, _act_code(act), _dtype(dtype, "dtype"), rows, width, channels, mx, mu, mw, _matrix(out, m, (rows, channels), "out"), *xs, *ws)
