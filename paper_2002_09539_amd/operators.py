@@ -440,12 +440,13 @@ DistillLoss = namedtuple("DistillLoss", "loss logprob stats")
 def _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperature, rest, d_logits):
     device = _on_gpu(logits, top_value, top_index, targets, d_loss, d_logprob, d_logits)
     z, rows, stride = _logit_rows(logits, "logits")
-    shape = logits.shape[:-1]
-    if top_value.dim() < 1 or top_value.shape[:-1] != shape:
-        _refuse("lists of shape %s for logits of shape %s", tuple(top_value.shape), tuple(logits.shape))
+    *shape, vocab = logits.shape
+    listed = top_value.shape
+    shape = tuple(shape)
+    if not listed or listed[:-1] != shape:
+        _refuse("lists of shape %s for logits of shape %s", tuple(listed), tuple(logits.shape))
     if targets is None and d_logprob is not None:
         _refuse("a gradient of log probabilities needs the targets")
-    listed = top_value.shape
     top_value, top_index = _per_row(top_value, listed, torch.float32, "top_value"), _per_row(top_index, listed, torch.int32, "top_index")
     targets, d_loss = _per_row(targets, shape, torch.int32, "targets"), _per_row(d_loss, shape, torch.float32, "d_loss")
     d_logprob = _per_row(d_logprob, shape, torch.float32, "d_logprob")
@@ -457,7 +458,7 @@ def _distill(logits, top_value, top_index, targets, d_loss, d_logprob, temperatu
         if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype:
             _refuse("the gradient must have the logits' shape and type")
         d_stride = _logit_rows(d_logits, "out")[2]
-    d = B.ols_distill(_dtype(logits, "logits"), listed[-1], int(rest), float(temperature), rows, logits.shape[-1], z.data_ptr(), stride, top_value.data_ptr(),
+    d = B.ols_distill(_dtype(logits, "logits"), listed[-1], int(rest), float(temperature), rows, vocab, z.data_ptr(), stride, top_value.data_ptr(),
                       top_index.data_ptr(), _ptr(targets), None, None, None, _ptr(d_loss), _ptr(d_logprob), _ptr(d_logits), d_stride)
     return d, shape, device, keep
 
