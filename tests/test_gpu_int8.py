@@ -57,6 +57,17 @@ def test_rows(rows, width, dtype):
     assert torch.equal(r.scale.cpu(), s) and torch.equal(r.q.cpu(), q) and r.q.shape == x.shape and r.q.dtype == torch.int8
 
 
+@pytest.mark.parametrize("rows", [6, 1025])
+@pytest.mark.parametrize("width,dtype", [(300, F32), (1000, BF16), (1999, F32), (3001, BF16), (4096, F32), (5003, BF16), (8190, F32), (8193, BF16), (16001, BF16), (16390, F32)])
+def test_each_size_of_workgroup(rows, width, dtype):
+    x = normal(width, rows, width, dtype=dtype)
+    x[rows // 2] = 0.0
+    x[rows - 1, width - 1] = 50.0                           # the largest of its row is the last
+    r = _ops().quantize_rows(x.cuda())
+    q, s = rows_want(x.double())
+    assert torch.equal(r.scale.cpu(), s) and torch.equal(r.q.cpu(), q)
+
+
 def test_rows_on_the_border_and_beyond():
     """Halves go to even; tiny, huge, empty and unbounded rows."""
     x = torch.zeros(12, 300)
