@@ -665,22 +665,23 @@ constexpr int kCus = 256;
 constexpr int kFewRows = 32;
 constexpr int kFewWaves = 4096;           // of all workgroups together, where the contraction is long enough
 
-// What a product in tiles takes, in microseconds: a start, and for each round of tiles its slices, which take longer the more tiles run
-// beside each other; cut contractions add a launch and their sums' traffic.  Fitted to products of 64 to 8192 rows and 700 to 32 000
-// channels over 1000 to 5632 indices (within 20 % of all but one).  Tiles of 64 / 128 / 256 whole: 512 rows, 2048 to 2048: 11.8 / 16.8 / 33;
+// What a product in tiles takes, in microseconds: a start (of later rounds a part of it is hidden), and for each round of tiles its slices,
+// which take longer the more tiles run beside each other; cut contractions add a launch and their sums' traffic.  Fitted to products of 64 to 8192 rows and 700 to 32 000
+// channels over 100 to 8192 indices.  Tiles of 64 / 128 / 256 whole: 512 rows, 2048 to 2048: 11.8 / 16.8 / 33;
 // 1024, 2048 to 5632: 38 / 24.5 / 35; 8192, 4096 to 4096 in 256: 161.  128 rows, 5632 to 2048 in tiles of 64, cut in 1 / 2 / 4 / 8: 22.5 /
-// 17.2 / 13.2 / 14.7.
+// 17.2 / 13.2 / 14.7.  2000 rows, 512 to 2000, where tiles of 64 take two rounds: 14.7 / 10.4 / 16.9.
 struct Cost {
     int tile, slots;                      // tiles of a round
-    double start, least, more;            // a slice: least + more x (share of the slots that are taken)
+    double start, again, least, more;     // of the first round and of others; a slice: least + more x (share of the slots that are taken)
 };
-constexpr Cost kCosts[3] = {{64, 2 * kCus, 4.6, 0.17, 0.14}, {128, 2 * kCus, 6.0, 0.30, 0.42}, {256, kCus, 9.6, 0.45, 0.75}};
+constexpr Cost kCosts[3] = {{64, 2 * kCus, 4.6, 3.0, 0.17, 0.14}, {128, 2 * kCus, 6.0, 4.0, 0.30, 0.42}, {256, kCus, 9.6, 7.0, 0.45, 0.75}};
 
 double cost_of(const Cost& c, int64_t tiles, int64_t slices, int ranges) {
     const int64_t rounds = tiles / c.slots, rest = tiles % c.slots;
-    double us = c.start + (double)(rounds * slices) * (c.least + c.more);
+    double us = c.start - c.again + (double)rounds * (c.again + (double)slices * (c.least + c.more));
     if (!rest) return us;
     const int64_t run = rest * ranges, last = run % c.slots ? run % c.slots : c.slots;
+    us += (double)((run + c.slots - 1) / c.slots) * c.again;
     us += (double)((slices + ranges - 1) / ranges) * ((double)((run - 1) / c.slots) * (c.least + c.more) + c.least + c.more * (double)last / c.slots);
     return ranges == 1 ? us : us + 3.0 + (double)run * c.tile * c.tile * 8 / 4e6;
 }
