@@ -7,7 +7,7 @@
 //
 // Few rows are bound by the weights' bytes: they go from memory straight into the registers of the matrix instruction (a row of 2048 to
 // 32 000, 65 MB: 15.4 us, 4.3 TB/s).  Many rows are bound by the matrix pipes: both operands go through tiles in LDS (8192 rows, 4096 to
-// 4096: 147 to 164 us as the clock allows, 1680 to 1880 TOP/s, where a library's product of 8192^3 reaches 2046).  Between them, some
+// 4096: 138 to 160 us as the clock allows, 1720 to 1990 TOP/s, where a library's product of 8192^3 reaches 2046).  Between them, some
 // dozens of tiles, a launch is a chain of waits.
 #include <algorithm>
 
@@ -666,9 +666,9 @@ constexpr int kFewRows = 32;
 constexpr int kFewWaves = 4096;           // of all workgroups together, where the contraction is long enough
 
 // What a product in tiles takes, in microseconds: a start (of later rounds a part of it is hidden), and for each round of tiles its slices,
-// which take longer the more tiles run beside each other; cut contractions add a launch and their sums' traffic.  Fitted to products of 64 to 8192 rows and 700 to 32 000
-// channels over 100 to 8192 indices.  Tiles of 64 / 128 / 256 whole: 512 rows, 2048 to 2048: 11.8 / 16.8 / 33;
-// 1024, 2048 to 5632: 38 / 24.5 / 35; 8192, 4096 to 4096 in 256: 161.  128 rows, 5632 to 2048 in tiles of 64, cut in 1 / 2 / 4 / 8: 22.5 /
+// which take longer the more tiles run beside each other; cut contractions add a launch and their sums' traffic.
+// Fitted to products of 64 to 8192 rows and 56 to 32 000 channels over 100 to 8192 indices.  Tiles of 64 / 128 / 256 whole: 512 rows, 2048 to
+// 2048: 11.8 / 16.8 / 33; 1024, 2048 to 5632: 38 / 24.5 / 35; 1319, 1184 to 13 224: 81 / 53 / 55; 4096, 1536 to 4096: 77 / 44 / 36.  128 rows, 5632 to 2048 in tiles of 64, cut in 1 / 2 / 4 / 8: 22.5 /
 // 17.2 / 13.2 / 14.7.  2000 rows, 512 to 2000, where tiles of 64 take two rounds: 14.7 / 10.4 / 16.9.
 struct Cost {
     int tile, slots;                      // tiles of a round
