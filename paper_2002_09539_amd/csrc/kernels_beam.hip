@@ -179,9 +179,23 @@ __device__ __forceinline__ double wave_max(double v) {
     return lane_of(v, 63);
 }
 
+// length^a, a in [0, 16], exact where it is a whole number below 2^53: equal quotients are equal numbers then.  A rounded reciprocal or a multiple
+// of a logarithm makes two numbers of most pairs of equal averages (of 6844 pairs of lengths up to 59, 4925).  So whole powers are products,
+// and sixteenths go by roots, which are rounded correctly; a finer fraction of a length below 2^32 is no whole number.
+__device__ __forceinline__ double power_of(double length, double a) {
+    if (16.0 * a != floor(16.0 * a)) return exp(a * log_of(length));
+    double v = 1.0, left = a, root = length;
+    for (; left >= 1.0; left -= 1.0) v *= length;
+    while (left > 0.0) {
+        root = sqrt(root), left *= 2.0;
+        if (left >= 1.0) v *= root, left -= 1.0;
+    }
+    return v;
+}
+
 // What is known of a hypothesis.
 struct Hypothesis {
-    double lead, scale, sum;   // what comes to a logit's distance from the largest (-inf: it has no candidates), 1 / length^penalty, sum of e^{z - top}
+    double lead, power, sum;   // what comes to a logit's distance from the largest (-inf: it has no candidates), length^|penalty|, sum of e^{z - top}
     float score, top;
     int length, ended, dead;
 };
@@ -234,7 +248,7 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
             Hypothesis& h = of[lane];
             bad = !h.dead && (!(h.score < INFINITY) || !(h.sum < INFINITY));
             h.lead = h.dead || !(h.sum > 0.0) ? (double)-INFINITY : (double)h.score - log_of(h.sum);
-            h.scale = p.penalty == 0.0 ? 1.0 : exp(-p.penalty * log_of((double)max(h.ended ? h.length : h.length + 1, 1)));
+            h.power = p.penalty == 0.0 ? 1.0 : power_of((double)max(h.ended ? h.length : h.length + 1, 1), fabs(p.penalty));
         }
         poisoned = __ballot(bad) != 0;
         in_wave_order();
@@ -255,7 +269,7 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
         const float z = val[entry];
         Candidate c;
         c.value = h.ended ? h.lead : h.lead + ((double)z - (double)h.top);
-        c.rank = c.value * h.scale;
+        c.rank = p.penalty > 0.0 ? c.value / h.power : c.value * h.power;
         c.token = !(h.lead > -INFINITY) ? -1 : h.ended ? (at == 0 && l == i * p.parts ? 0 : -1) : at < k ? said : -1;
         return c;
     };
