@@ -4,8 +4,9 @@
 //   candidates:  (i, v) of value score_i + logp_iv and length length_i + 1;  of an ended hypothesis only itself, (i, 0) of value score_i
 //   order:       by value / length^penalty, largest first; ties to the lower hypothesis, then to the lower token
 //
-// Within a hypothesis that is the order of its logits, which is exact.  Between hypotheses it hangs on the last bits of the sums:
-// these are added up in fp64, and candidates are compared in fp64.
+// Within a hypothesis that is the order of its logits, which is exact: in a part's list, and in the merge where heads of two parts have the same
+// value in fp64 (a score that swallows the logits, logits that are tiny beside it).  Between hypotheses it hangs on the last bits of the
+// sums: these are added up in fp64, and candidates are compared in fp64.
 //
 // What bounds the choice is one read of the logits: a workgroup holds its part of a hypothesis' row in registers, takes the sum
 // and the part's best from there (logit_rows.h), and one wavefront for each request merges the parts' lists, each in order: a lane
@@ -198,6 +199,7 @@ struct Hypothesis {
     double lead, power, sum;   // what comes to a logit's distance from the largest (-inf: it has no candidates), length^|penalty|, sum of e^{z - top}
     float score, top;
     int length, ended, dead;
+    int close;                 // two of its logits may have one value in fp64
 };
 
 // A workgroup for each request: its wavefronts add up the parts and rank the heads of the parts' lists, then one merges these, each in order.  A
@@ -238,19 +240,29 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
         double sum = 0.0;
         for (int j = lane; j < p.parts; j += 64) sum += part_s[i * p.parts + j] * exp((double)part_m[i * p.parts + j] - base);
         sum = wave_sum(sum);
-        if (lane == 0) of[i].top = m, of[i].sum = sum;
+        // Logits are 0 or of sizes in [2^-16, 2^8): they differ by 2^-39 at least, and so do their values, by 2^-50 of themselves if the score is below
+        // 2^10, which no rounding makes equal.  Otherwise every turn looks at the logits of the heads that share the best rank.
+        bool close = !LISTS;
+        if constexpr (LISTS)
+            for (int e = lane; e < p.parts * k; e += 64) {
+                const unsigned size = __float_as_uint(val[i * p.parts * k + e]) & 0x7fffffffu;
+                close |= size - 0x37800000u >= 0x0c000000u && size != 0u && size != 0x7f800000u;      // -inf: none
+            }
+        close = __ballot(close) != 0;
+        if (lane == 0) of[i].top = m, of[i].sum = sum, of[i].close = close;
     }
     __syncthreads();
-    bool poisoned = false;
+    bool poisoned = false, look = false;
     if (wave == 0) {
-        bool bad = false;
+        bool bad = false, close = false;
         if (lane < p.in_beams) {
             Hypothesis& h = of[lane];
             bad = !h.dead && (!(h.score < INFINITY) || !(h.sum < INFINITY));
             h.lead = h.dead || !(h.sum > 0.0) ? (double)-INFINITY : (double)h.score - log_of(h.sum);
             h.power = p.penalty == 0.0 ? 1.0 : power_of((double)max(h.ended ? h.length : h.length + 1, 1), fabs(p.penalty));
         }
-        poisoned = __ballot(bad) != 0;
+        if (lane < p.in_beams && !of[lane].dead && !of[lane].ended) close = of[lane].close || !(fabs(of[lane].lead) < 1024.0);
+        poisoned = __ballot(bad) != 0, look = p.parts > 1 && __ballot(close) != 0;
         in_wave_order();
     }
     // The hypothesis of list l: quotients are at least 1 / 2048 off a whole number and below 32, where the product is off by 2^-18.  (Divisions of
@@ -318,12 +330,26 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamParams p) {
             const int other = __ffsll(more) - 1, l = __builtin_amdgcn_readlane(list, other);
             if (l < taken) taken = l, who = other;
         }
+        if (look && !of[owner(taken)].ended) {                // of the hypothesis' heads of this rank: the largest logit, then the lower list
+            const int begin = owner(taken) * p.parts;
+            float top = -INFINITY;
+            int pick = lists;
+            for (int l = begin + ((lane - begin) & 63); l < begin + p.parts; l += 64) {
+                if (single ? best != first : key[l] != first) continue;             // single: the lane's best is the list's
+                const float z = val[l * k + used[l]];
+                if (z > top) top = z, pick = l;
+            }
+            const float largest = ols::wave_max(top);
+            unsigned long long same = __ballot(pick < lists && top == largest);
+            for (taken = lists; same; same &= same - 1) taken = min(taken, __builtin_amdgcn_readlane(pick, __ffsll(same) - 1));
+            who = taken & 63;
+        }
         const int place = used[taken];
         if (lane == turn) from = taken, entry = place;
         if (lane == who) {
             const double rank = rank_of(taken, place + 1);
             used[taken] = (uint8_t)(place + 1);
-            if (!held) key[taken] = rank;
+            if (!single) key[taken] = rank;
 #pragma unroll
             for (int j = 0; j < kMine; ++j) mine[j] = taken == lane + 64 * j ? rank : mine[j];
         }
