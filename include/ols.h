@@ -582,8 +582,8 @@ OLS_API int64_t ols_beam_workspace_bytes(int64_t batch, int in_beams, int beams,
 /* Moves the states of hypotheses behind a step: state[b][i] = old state[b][parent[b][i]] for n tensors of any type, each of
  * [batch][in_beams] rows of row_bytes bytes, rows src_beam and requests src_batch bytes apart, to [batch][beams] rows.
  * All arrays are HOST arrays of n entries, read before the call returns.  dst[i] == src[i] moves in place (the same strides, beams ==
- * in_beams; hypotheses that stay are not touched); otherwise outputs must not lie on inputs, nor on each other in any case.  A parent outside
- * [0, in_beams) leaves its place as it was. */
+ * in_beams; hypotheses that stay are not touched); otherwise outputs must not lie on inputs, nor on each other or on `parent` in any case.  A
+ * parent outside [0, in_beams) leaves its place as it was. */
 OLS_API int ols_beam_reorder(int n, const void* const* src, void* const* dst, const int64_t* row_bytes, const int64_t* src_batch, const int64_t* src_beam,
                              const int64_t* dst_batch, const int64_t* dst_beam, int64_t batch, int in_beams, int beams, const int32_t* parent, void* stream);
 

@@ -249,6 +249,17 @@ int too_many_parts(const char* who) { return bad("%s: 2^24 parts of 32768 bf16 o
 // Rows [batch][beams] of `bytes`, as far as they reach; at least one row.
 int64_t extent(int64_t batch, int64_t batch_stride, int64_t beams, int64_t beam_stride, int64_t bytes) { return (batch - 1) * batch_stride + (beams - 1) * beam_stride + bytes; }
 
+// Whether any of these rows shares bytes with [at, at + size).
+bool rows_touch(const char* rows, int64_t batch, int64_t batch_stride, int64_t beams, int64_t beam_stride, int64_t bytes, const char* at, int64_t size) {
+    if (at + size <= rows || rows + extent(batch, batch_stride, beams, beam_stride, bytes) <= at) return false;
+    for (int64_t b = 0; b < batch; ++b)
+        for (int64_t i = 0; i < beams; ++i) {
+            const char* row = rows + b * batch_stride + i * beam_stride;
+            if (row < at + size && at < row + bytes) return true;
+        }
+    return false;
+}
+
 constexpr int64_t kMaxInt8Width = (1 << 17) - 1;      // of whole sums in 32 bits: 2^17 - 1 products of at most 2^14
 
 int check_int8_matrix(const char* who, const char* name, const void* q, int64_t row, int64_t group, int64_t rows, int64_t cols, int groups, bool written) {
@@ -555,6 +566,8 @@ int ols_beam_reorder(int n, const void* const* src, void* const* dst, const int6
             if (s < d + extent(batch, dst_batch[i], beams, dst_beam[i], bytes) && d < s + extent(batch, src_batch[i], in_beams, src_beam[i], bytes))
                 return bad("%s: output %d lies partly on its input", who, i);
         }
+        if (rows_touch((const char*)dst[i], batch, dst_batch[i], beams, dst_beam[i], bytes, (const char*)parent, 4 * batch * beams))
+            return bad("%s: output %d lies on the parents, which are read meanwhile", who, i);
     }
     BeamMove t;
     t.in_beams = in_beams, t.out_beams = beams, t.n = 0;

@@ -575,7 +575,7 @@ def beam_reorder(states, parent, out=None):
     states: tensors [batch, hypotheses, ...] of any types, what one hypothesis holds contiguous (a slice of the positions used so far is, where they
     are the first of these axes).  parent: int32 [batch, beams] (Beams.parent); one outside the hypotheses leaves its place as it was.
     Without `out` the tensors are written in place, and hypotheses that stay are not touched; `out` holds other tensors of shape
-    [batch, beams, ...], which must not overlap the states or each other."""
+    [batch, beams, ...], which must not overlap the states or each other.  Nothing that is written may be `parent` itself."""
     states = list(states)
     if not states:
         return []
