@@ -600,7 +600,10 @@ def beam_reorder(states, parent, out=None):
                 _refuse("an output is %s of shape %s, for a state of %s and shape %s", o.dtype, tuple(o.shape), s.dtype, tuple(s.shape))
         _, dst_batch, dst_beam = zip(*[_state_rows(t, batch, beams, "an output") for t in outs])
         if not set(src).isdisjoint(dst):
-            read = {p: i for i, (p, n) in enumerate(zip(src, row_bytes)) if n}
+            read = {}
+            for i, (p, n) in enumerate(zip(src, row_bytes)):
+                if n:
+                    read[p] = i if p not in read else -1       # -1: a state that is read several times
             if any(n and read.get(p, i) != i for i, (p, n) in enumerate(zip(dst, row_bytes))):
                 _refuse("an output is another state of the call")
     if not _distinct(dst, row_bytes):

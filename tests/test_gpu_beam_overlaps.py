@@ -46,3 +46,20 @@ def test_parents_that_are_copied_first_may_be_moved():
     want = parent.gather(1, parent.long())
     ops.beam_reorder([parent], parent)
     assert torch.equal(wide[:, :3], want) and bool((wide[:, 3] == 9).all())
+
+
+def test_a_state_that_is_read_twice_does_not_move_in_place():
+    """Its other copy would be taken from what has moved already, or not, as workgroups come."""
+    ops = _ops()
+    parent = torch.tensor([[1, 0, 2], [2, 2, 0]], dtype=torch.int32, device="cuda")
+    a, b, c = (torch.randn(2, 3, 5000, device="cuda") for _ in range(3))
+    start = a.clone()
+    for states, out in (([a, a], [b, a]), ([a, a], [a, b]), ([a, c, a], [b, c, a])):
+        with pytest.raises(B.OlsError, match="another state"):
+            ops.beam_reorder(states, parent, out=out)
+    assert torch.equal(a, start)
+    rows = torch.arange(2, device="cuda")[:, None]
+    ops.beam_reorder([a, a], parent, out=[b, c])
+    assert torch.equal(b, a[rows, parent.long()]) and torch.equal(c, b)
+    ops.beam_reorder([a, c], parent, out=[b, c])            # one in place, one apart
+    assert torch.equal(a, start) and torch.equal(c, b[rows, parent.long()])
