@@ -559,6 +559,8 @@ OLS_API int64_t ols_distill_workspace_bytes(int64_t rows, int64_t vocab, int dty
  *     candidate: score -inf, token -1, parent its own number (0 from in_beams on), not ended, its parent's length.
  *   - A score that is NaN or +inf, or a NaN or +inf among the logits of a hypothesis that goes on, makes all scores of its request NaN, its
  *     tokens -1 and its parents their own numbers.  Logits of ended hypotheses and of none are not read.
+ *   - new_score may lie on score, new_length on length and new_finished on finished, where beams == in_beams; results lie on nothing else that is
+ *     read, nor on each other.
  * logits: [batch][in_beams][vocab], rows beam_stride and requests batch_stride elements apart, which may be anything from 0.
  * batch < 65536; in_beams and beams in [1, OLS_MAX_TOP]; vocab <= 2^24; fewer than 2^24 parts of 32768 bf16 or 16384 fp32 logits in all. */
 typedef struct ols_beam {

@@ -249,6 +249,25 @@ int too_many_parts(const char* who) { return bad("%s: 2^24 parts of 32768 bf16 o
 // Rows [batch][beams] of `bytes`, as far as they reach; at least one row.
 int64_t extent(int64_t batch, int64_t batch_stride, int64_t beams, int64_t beam_stride, int64_t bytes) { return (batch - 1) * batch_stride + (beams - 1) * beam_stride + bytes; }
 
+// Whether a result of a choice lies on what the choice reads (what it takes the place of aside, if of one shape) or on another result.
+bool beam_overlaps(const ols_beam& b, int64_t ws_bytes) {
+    struct Span {
+        const void* at;
+        int64_t bytes;
+    };
+    const int64_t in = b.batch * b.in_beams, out = b.batch * b.beams;
+    const Span reads[4] = {{b.score, 4 * in}, {b.length, 4 * in}, {b.finished, in}, {b.ws, ws_bytes}};
+    const Span writes[5] = {{b.new_score, 4 * out}, {b.new_length, 4 * out}, {b.new_finished, out}, {b.token, 4 * out}, {b.parent, 4 * out}};
+    auto meet = [](const Span& x, const Span& y) { return x.at && y.at && (const char*)x.at < (const char*)y.at + y.bytes && (const char*)y.at < (const char*)x.at + x.bytes; };
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < 4; ++j)
+            if (meet(writes[i], reads[j]) && !(i == j && i < 3 && writes[i].at == reads[j].at && b.in_beams == b.beams)) return true;
+        for (int j = 0; j < i; ++j)
+            if (meet(writes[i], writes[j])) return true;
+    }
+    return false;
+}
+
 // Whether any of these rows shares bytes with [at, at + size).
 bool rows_touch(const char* rows, int64_t batch, int64_t batch_stride, int64_t beams, int64_t beam_stride, int64_t bytes, const char* at, int64_t size) {
     if (at + size <= rows || rows + extent(batch, batch_stride, beams, beam_stride, bytes) <= at) return false;
@@ -535,6 +554,7 @@ int ols_beam_select(const ols_beam* b, void* stream) {
     const int64_t need = beam_workspace_bytes(b->dtype, b->batch, b->in_beams, b->beams, b->vocab);
     if (need < 0) return too_many_parts(who);
     if (const int rc = check_ws(who, b->ws, b->ws_bytes, need)) return rc;
+    if (beam_overlaps(*b, need)) return bad("%s: results overlap what is read, or each other", who);
     BeamParams p = {};
     p.dtype = b->dtype, p.in_beams = b->in_beams, p.beams = b->beams, p.eos = b->eos, p.batch = b->batch, p.vocab = b->vocab;
     p.logits = b->logits, p.batch_stride = b->batch_stride, p.beam_stride = b->beam_stride, p.score = b->score, p.finished = b->finished, p.length = b->length;

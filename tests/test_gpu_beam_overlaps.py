@@ -63,3 +63,28 @@ def test_a_state_that_is_read_twice_does_not_move_in_place():
     assert torch.equal(b, a[rows, parent.long()]) and torch.equal(c, b)
     ops.beam_reorder([a, c], parent, out=[b, c])            # one in place, one apart
     assert torch.equal(a, start) and torch.equal(c, b[rows, parent.long()])
+
+
+@pytest.mark.parametrize("batch,beams,vocab", [(70, 4, 900), (3, 5, 40003), (300, 32, 77)])
+def test_a_choice_in_the_place_of_what_it_follows(batch, beams, vocab):
+    """Scores, ends and lengths are written where they were read, as a loop in C does it."""
+    ops = _ops()
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    z = torch.randn(batch, beams, vocab, generator=g, device="cuda") * 2
+    score = torch.randn(batch, beams, generator=g, device="cuda") - 9
+    finished = torch.rand(batch, beams, generator=g, device="cuda") < 0.3
+    length = torch.randint(1, 30, (batch, beams), generator=g, device="cuda", dtype=torch.int32)
+    want = ops.beam_select(z, score, finished=finished, length=length, eos=3, length_penalty=0.6)
+    token, parent = (torch.empty(batch, beams, dtype=torch.int32, device="cuda") for _ in range(2))
+    b = B.ols_beam()
+    b.dtype, b.in_beams, b.beams, b.eos, b.batch, b.vocab, b.logits, b.batch_stride, b.beam_stride = B.OLS_F32, beams, beams, 3, batch, vocab, z.data_ptr(), beams * vocab, vocab
+    b.length_penalty, b.token, b.parent = 0.6, token.data_ptr(), parent.data_ptr()
+    b.score = b.new_score = score.data_ptr()
+    b.finished = b.new_finished = finished.data_ptr()
+    b.length = b.new_length = length.data_ptr()
+    b.ws_bytes = B.ols_beam_workspace_bytes(batch, beams, beams, vocab, B.OLS_F32)
+    ws = torch.empty(b.ws_bytes, dtype=torch.uint8, device="cuda")
+    b.ws = ws.data_ptr()
+    B.ols_beam_select(b, torch.cuda.current_stream().cuda_stream)
+    for got, w in zip((score, token, parent, finished, length), want):
+        assert torch.equal(got, w)
