@@ -518,6 +518,14 @@ def distill_loss_grad(logits, top_value, top_index, result, d_loss, targets=None
 Beams = namedtuple("Beams", "score token parent finished length")
 
 
+def _int32(v, name):
+    """A whole number that the C boundary holds: ctypes would take others modulo 2^32."""
+    v = int(v)
+    if not -1 << 31 <= v < 1 << 31:
+        _refuse("%s must be in [-2^31, 2^31), got %d", name, v)
+    return v
+
+
 def beam_select(logits, score, beams=None, finished=None, length=None, eos=-1, length_penalty=0.0):
     """The best `beams` continuations (as many as there are hypotheses by default) of each request, best first.
 
@@ -532,8 +540,8 @@ def beam_select(logits, score, beams=None, finished=None, length=None, eos=-1, l
     (batch, have, vocab), stride = logits.shape, logits.stride()
     if vocab > 1 and stride[2] != 1:
         _refuse("logits: the elements of a row must be contiguous")
-    code, beams = _dtype(logits, "logits"), have if beams is None else int(beams)
-    rows = (batch, have)
+    code, beams = _dtype(logits, "logits"), have if beams is None else _int32(beams, "beams")
+    rows, eos = (batch, have), _int32(eos, "eos")
     score, finished = _per_row(score, rows, torch.float32, "score"), _per_row(finished, rows, torch.bool, "finished")
     length = _per_row(length, rows, torch.int32, "length")
     nbytes = B.ols_beam_workspace_bytes(batch, have, beams, vocab, code)
@@ -543,7 +551,7 @@ def beam_select(logits, score, beams=None, finished=None, length=None, eos=-1, l
         new_score, token, parent = parts[0].view(torch.float32), parts[1], parts[2]
         new_length = None if length is None else parts[3]
         ended = torch.empty(batch, beams, dtype=torch.bool, device=device)
-        b = B.ols_beam(code, have, beams, int(eos), batch, vocab, logits.data_ptr(), stride[0], stride[1], score.data_ptr(), _ptr(finished), _ptr(length),
+        b = B.ols_beam(code, have, beams, eos, batch, vocab, logits.data_ptr(), stride[0], stride[1], score.data_ptr(), _ptr(finished), _ptr(length),
                        float(length_penalty), new_score.data_ptr(), token.data_ptr(), parent.data_ptr(), _ptr(new_length), ended.data_ptr(), _ptr(ws), nbytes)
         B.ols_beam_select(b, _stream(device))
     return Beams(new_score, token, parent, ended, new_length)

@@ -66,3 +66,13 @@ def test_the_longer_of_two_that_are_equal():
 def test_a_length_of_none_counts_as_one():
     scores, lengths = torch.tensor([[-2.5, -1.25, -1.25]]), torch.tensor([[2, 0, 1]], dtype=torch.int32)
     assert _ended(scores, lengths, 1.0).tolist() == [[0, 1, 2]]
+
+
+@pytest.mark.parametrize("change", [dict(eos=(1 << 32) + 3), dict(eos=-(1 << 32) + 3), dict(eos=1 << 31), dict(beams=(1 << 32) + 2), dict(beams=-(1 << 32) + 2)])
+def test_numbers_that_the_boundary_does_not_hold(change):
+    """Modulo 2^32 they would be a token or a number of hypotheses."""
+    from paper_2002_09539_amd import binding as B
+    with pytest.raises(B.OlsError):
+        _ops().beam_select(torch.zeros(1, 2, 8, device="cuda"), torch.zeros(1, 2, device="cuda"), **change)
+    b = _ops().beam_select(torch.zeros(1, 2, 8, device="cuda"), torch.zeros(1, 2, device="cuda"), eos=-(1 << 31))
+    assert not bool(b.finished.any())
