@@ -526,7 +526,8 @@ OLS_API int64_t ols_clip_workspace_bytes(int n, const int64_t* numel, const int3
  * With d_logits the same call computes the gradient of sum(d_loss loss + d_logprob logprob) (each [rows]; NULL: zeros):
  *     d_logits_i = d_loss temperature (p_i (sum q + q_r) - q's of i        where i is listed
  *                                                        - q_r p_i / p_r   elsewhere) + d_logprob ([i == target] - softmax(z)_i).
- * It may lie on the logits (same pointer and row stride).  stats ([rows][8]) is what the gradient alone needs later, with the same lists,
+ * It may lie on the logits (same pointer and row stride), and shares no element with them otherwise.  A row's sums are fp32, so a loss is good to some
+ * 2^-20 temperature^2, which counts at temperatures far above ten.  stats ([rows][8]) is what the gradient alone needs later, with the same lists,
  * targets, temperature and rest.  Rows lie at least `vocab` elements apart.  vocab <= 2^24, temperature in [2^-20, 2^20]. */
 #define OLS_MAX_TEACHER 256
 typedef struct ols_distill {
@@ -594,7 +595,7 @@ OLS_API int ols_beam_reorder(int n, const void* const* src, void* const* dst, co
  * The integer sums are exact.  q_w is [out][width]: a channel's weights side by side, in int8; rows at least `width` apart.
  *   - dtype OLS_F32 or OLS_BF16: x is given in that type, and the call quantises its rows as ols_quantize_rows does; with `up` it takes
  *     act(x) up in its place, in fp32 (the hidden rows of a gated block).  OLS_I8: x and x_scale are given.  Weights are best with rows that begin on 16
- *     bytes; others are read more slowly.
+ *     bytes; others are read more slowly by up to 32 rows, and copied into the workspace first, in every call, by more.
  *   - y is of out_dtype.  It may lie on x or `up` where the call quantises them, which it does first, and on nothing else that is read.
  *     The workspace's size is that of the descriptor with its pointers.  Limits: groups <= 4096, width < 2^17, out <= 2^24, rows <= 2^24; fewer than 2^23 tiles of
  *     16 x 16 results (up to 64 rows) or 128 x 128. */
@@ -614,7 +615,8 @@ OLS_API int ols_int8_matmul(const ols_int8* f, void* stream);
 OLS_API int64_t ols_int8_workspace_bytes(const ols_int8* f);
 
 /* Rows to 8 bits: scale[r] = fp32(max |x[r]| / 127), q[r][k] = x[r][k] / scale[r] to the nearest whole number, halves to even (of the exact
- * quotient).  Rows of zeros have scale 0 and q 0, rows with a NaN or an infinity a scale of NaN and q 0.  With up.dev x is act(x) up, in fp32. */
+ * quotient), and to +-127 where that is beyond (a scale below the normal numbers, rounded down).  Rows of zeros, and those whose scale is
+ * rounded to 0, have scale 0 and q 0, rows with a NaN or an infinity a scale of NaN and q 0.  With up.dev x is act(x) up, in fp32. */
 OLS_API int ols_quantize_rows(int groups, int64_t rows, int64_t width, const ols_matrix* x, const ols_matrix* up, int act, int dtype, int8_t* q, int64_t q_row,
                               int64_t q_group, float* scale, int64_t scale_group, void* stream);
 /* Weights [width][out] to 8 bits with a scale for each column, laid out for ols_int8_matmul: q [out][width], scale [out]. */

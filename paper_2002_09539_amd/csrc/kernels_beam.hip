@@ -8,10 +8,11 @@
 // value in fp64 (a score that swallows the logits, logits that are tiny beside it).  Between hypotheses it hangs on the last bits of the
 // sums: these are added up in fp64, and candidates are compared in fp64.
 //
-// What bounds the choice is one read of the logits: a workgroup holds its part of a hypothesis' row in registers, takes the sum
+// The choice reads the logits once: a workgroup holds its part of a hypothesis' row in registers, takes the sum
 // and the part's best from there (logit_rows.h), and one wavefront for each request merges the parts' lists, each in order: a lane
 // holds the heads of its lists, and every turn takes the best head of all.  Ended hypotheses are not read.  512 hypotheses of 128 000
-// bf16 (64 requests, the best 8 of each): 33 us, 4.0 TB/s, and 10 for the merge; few requests are two launches of 6 us, latencies.
+// bf16 (64 requests, the best 8 of each; a fifth has ended, 105 MB are read): 33 us, 3.2 TB/s, since nothing of a workgroup's own is under way
+// while it looks for its best, and 10.7 for the merge; few requests are two launches of 6 to 7 us, latencies.
 //
 // Moving states is one read and one write of what moves.  A thread holds the same sixteen bytes of all hypotheses of a request: all
 // are read before one is written, so that states can be moved in place, and a hypothesis that stays where it is is not touched then.

@@ -7,7 +7,7 @@
 //
 // Few rows are bound by the weights' bytes: they go from memory straight into the registers of the matrix instruction (a row of 2048 to
 // 32 000, 65 MB: 15.4 us, 4.3 TB/s).  Many rows are bound by the matrix pipes: both operands go through tiles in LDS (8192 rows, 4096 to
-// 4096: 138 to 160 us as the clock allows, 1720 to 1990 TOP/s, where a library's product of 8192^3 reaches 2046).  Between them, some
+// 4096: 138 to 167 us as the clock allows, 1650 to 1990 TOP/s, where a library's product of 8192^3 reaches 2046).  Between them, some
 // dozens of tiles, a launch is a chain of waits.
 #include <algorithm>
 
@@ -455,7 +455,9 @@ __global__ __launch_bounds__(ffn::gemm_threads<T>(), 2) void tile_kernel(Product
     const int tile = tile_of_block(p, range);
     const Place at = place_of(p, tile, T);
     const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), wm = wave / 2, wn = wave % 2;
-    const int64_t k2 = (p.width + 15) / 16 * 8;               // a row's pairs of bytes, up to whole chunks (x holds zeros there)
+    // A row's pairs of bytes, up to whole chunks.  x holds zeros there; of w the rest of the chunk that holds the row's last weight is read, sixteen
+    // bytes on sixteen, and counts for nothing.
+    const int64_t k2 = (p.width + 15) / 16 * 8;
     const Tile ta(p.x_row / 2), tb(p.w_row / 2);
     const int slices = (int)((p.width + kSlice - 1) / kSlice);
     const int from = range < 0 ? 0 : (int)((int64_t)slices * range / p.ranges);
@@ -645,7 +647,7 @@ constexpr int64_t kMostBlocks = 1 << 21;   // of 1024 threads: a launch has fewe
 struct Plan {
     int tile;                             // 0: few rows
     int R, waves;                         // few rows: rows of a workgroup / 16, its wavefronts
-    bool fused, lay_x, lay_w;             // rows quantised where they are multiplied; operands laid out first
+    bool fused, lay_x, lay_w;             // rows quantised where they are multiplied; operands laid out first, in every call (4096 x 4096 weights: 7 us)
     int tiles_m, tiles_n, whole, rest, ranges;
     int64_t scale_at, w_at, partial_at, ws_bytes;
 };

@@ -105,8 +105,8 @@ __device__ __forceinline__ double wave_sum(double v) {
     return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
 }
 
-// log x in fp64, by log m = 2 atanh((m - 1) / (m + 1)) for m in [sqrt 1/2, sqrt 2) and its series up to the 17th power (2e-16).  Not inlined:
-// kernels of one wavefront's work wait for their instructions longer than for the arithmetic.
+// log x in fp64, by log m = 2 atanh((m - 1) / (m + 1)) for m in [sqrt 1/2, sqrt 2) and its series up to the 17th power, which is off by 9e-16
+// of the whole at the most.  Not inlined: kernels of one wavefront's work wait for their instructions longer than for the arithmetic.
 __device__ __attribute__((noinline)) double log_of(double x) {
     if (!(x > 0.0 && x < (double)INFINITY)) return x == 0.0 ? (double)-INFINITY : x > 0.0 ? x : (double)NAN;
     double m = __builtin_amdgcn_frexp_mant(x);

@@ -482,7 +482,8 @@ def distill_loss(logits, top_value, top_index, targets=None, temperature=1.0, re
     [0, vocab) is no entry.  rest=False: the teacher's distribution is that of the list alone, softmax(top_value / temperature).  rest=True:
     top_value are log probabilities at this temperature, and what they leave of one stands against what the student leaves outside the
     list.  targets (int32, optional): tokens whose log probability at temperature 1 is returned too.  Returns DistillLoss: loss and logprob of
-    shape logits.shape[:-1] (logprob None without targets), and stats for distill_loss_grad."""
+    shape logits.shape[:-1] (logprob None without targets), and stats for distill_loss_grad.  A loss is good to some 2^-20 temperature^2 (a row's sums
+    are fp32)."""
     return _distill_loss(logits, top_value, top_index, targets, None, None, temperature, rest, None)
 
 
@@ -695,7 +696,7 @@ def int8_matmul(x, weight, up=None, act="silu", out=None, dtype=None):
 
     x: fp32 or bf16 [rows, width] or [m, rows, width], quantised on the way, or what quantize_rows returned.  With `up` (of x's shape and type)
     the product is that of act(x) * up: the second one of a gated block, for a = x and b = up.  weight: Int8Weight, from quantize_weight or of any int8
-    q [out, width] or [m, out, width], whose rows are best 16 bytes apart.  y is [rows, out], with the workers' axis if anything has one, of
+    q [out, width] or [m, out, width]; rows that do not begin on 16 bytes are copied first in every call of more than 32 rows.  y is [rows, out], with the workers' axis if anything has one, of
     `dtype` (x's by default, bfloat16 for Int8Rows) or in `out`, which may lie on x or up where these are not Int8Rows.  width < 2^17."""
     given = isinstance(x, Int8Rows)
     xq, (wq, w_scale) = (x.q if given else x), weight
