@@ -182,7 +182,7 @@ __device__ __forceinline__ double wave_max(double v) {
 }
 
 // length^a, a in [0, 16], exact where it is a whole number below 2^53: equal quotients are equal numbers then.  A rounded reciprocal or a multiple
-// of a logarithm makes two numbers of most pairs of equal averages (of 6844 pairs of lengths up to 59, 4925).  So whole powers are products,
+// of a logarithm makes two numbers of two thirds of all pairs of equal averages (lengths up to 59, penalty 1).  So whole powers are products,
 // and sixteenths go by roots, which are rounded correctly; a finer fraction of a length below 2^32 is no whole number.
 __device__ __forceinline__ double power_of(double length, double a) {
     if (16.0 * a != floor(16.0 * a)) return exp(a * log_of(length));

@@ -696,8 +696,8 @@ def int8_matmul(x, weight, up=None, act="silu", out=None, dtype=None):
 
     x: fp32 or bf16 [rows, width] or [m, rows, width], quantised on the way, or what quantize_rows returned.  With `up` (of x's shape and type)
     the product is that of act(x) * up: the second one of a gated block, for a = x and b = up.  weight: Int8Weight, from quantize_weight or of any int8
-    q [out, width] or [m, out, width]; rows that do not begin on 16 bytes are copied first in every call of more than 32 rows.  y is [rows, out], with the workers' axis if anything has one, of
-    `dtype` (x's by default, bfloat16 for Int8Rows) or in `out`, which may lie on x or up where these are not Int8Rows.  width < 2^17."""
+    q [out, width] or [m, out, width]; rows that do not begin on 16 bytes are copied first in every call of more than 32 rows.  y is [rows, out],
+    with the workers' axis if anything has one, of `dtype` (x's by default, bfloat16 for Int8Rows) or in `out`, which may lie on x or up where these are not Int8Rows.  width < 2^17."""
     given = isinstance(x, Int8Rows)
     xq, (wq, w_scale) = (x.q if given else x), weight
     device = _on_gpu(xq, wq, w_scale, up, out, *((x.scale,) if given else ()))
